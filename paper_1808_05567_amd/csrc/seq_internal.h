@@ -1,0 +1,208 @@
+// Shared by the translation units of the sequence operators (include/seq_mi355x.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "seq_mi355x.h"
+
+namespace convmi {
+
+typedef unsigned seq_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned seq_u32x2 __attribute__((ext_vector_type(2)));
+typedef float seq_f32x4 __attribute__((ext_vector_type(4)));
+
+// A sequence tensor: element (n, c, l) lies n * .n + (c / V) * .c + l * .l + c % V elements behind the base.
+// 64-bit distances: a tensor may have more than 2^32 elements.
+struct SeqView {
+    long long n, c, l;
+};
+
+struct SeqConvArgs {
+    const void *x, *dy, *state_in;
+    void *y, *dx, *state_out;
+    const float *w, *bias;
+    const int *lengths, *slots;
+    float *part;  // [parts][W + 1][Cp]: partial sums of dw and dbias
+    float *dw, *dbias;
+    SeqView vx, vy, vdy, vdx;
+    int N, Cb, Cp, L, silu, n_slots;
+    int cgroups, ranges, range;  // groups of 8 blocks; runs of positions and their length
+};
+
+struct SeqScanArgs {
+    const void *x, *dt, *B, *C, *z, *dy;
+    const float *A, *D, *dt_bias, *state_in;
+    void *y, *dx, *ddt, *dB, *dC, *dz;
+    float *state_out, *dA, *dD, *ddt_bias;
+    const int *lengths, *slots;
+    SeqView vx, vdt, vB, vC, vz, vy, vdy, vdx, vddt, vdB, vdC, vdz;
+    int N, Ch, Cp, L, S, G, CG;  // Ch channels, CG of them a group
+    int softplus, n_slots;
+    int tiles;          // tiles of channels a group
+    int chunks, chunk;  // runs of positions and their length, a multiple of 8
+    float *hl;          // [N][chunks][S][Cp]: state at the end of a chunk from zeros, then at its start
+    float *gl;          // the same for the gradient, back to front
+    float *sd;          // [N][chunks][Cp]: sum of d over a chunk
+    float *vec;         // [N][chunks][2][Cp]: partial dD, ddt_bias
+    float *bc;          // [N][L][G * btiles][2][S]: partial dB, dC
+    int btiles;         // tiles of channels a group of the backward kernel
+};
+
+struct SeqNormArgs {
+    const void *x, *res, *dy, *dr;
+    const float *w;
+    void *r, *y, *dx;
+    int8_t *q;
+    float *scale, *part, *dw;
+    SeqView vx, vres, vr, vy, vq, vdy, vdr, vdx;
+    int N, C, Cb, Cp, L;
+    long long rows;  // N * L
+    float eps;
+    int parts;
+};
+
+struct SeqMv4Args {
+    const void *x, *wt;
+    const float *xscale, *scale, *bias;
+    void *y;
+    int M, C, K, Cx, Cs, Kp, Ky, group;  // Cs: runs of 128 channels
+};
+
+hipError_t launch_seq_conv_fwd(int dtype, int W, const SeqConvArgs &a, hipStream_t s);
+hipError_t launch_seq_conv_step(int dtype, int W, const SeqConvArgs &a, hipStream_t s);
+hipError_t launch_seq_conv_bwd(int dtype, int W, const SeqConvArgs &a, hipStream_t s);
+hipError_t launch_seq_scan_fwd(int dtype, const SeqScanArgs &a, hipStream_t s);
+hipError_t launch_seq_scan_step(int dtype, const SeqScanArgs &a, hipStream_t s);
+hipError_t launch_seq_scan_ends(int dtype, const SeqScanArgs &a, hipStream_t s);
+hipError_t launch_seq_scan_bwd(int dtype, const SeqScanArgs &a, hipStream_t s);
+hipError_t launch_seq_norm_fwd(int dtype, const SeqNormArgs &a, hipStream_t s);
+hipError_t launch_seq_norm_bwd(int dtype, const SeqNormArgs &a, hipStream_t s);
+hipError_t launch_seq_mv4(int dtype, const SeqMv4Args &a, hipStream_t s);
+hipError_t launch_seq_mv4_quant(const SeqMv4Args &a, const float *w, void *wt, float *scale, hipStream_t s);
+hipError_t launch_seq_mv4_unquant(const SeqMv4Args &a, float *w, hipStream_t s);
+
+// States a scan kernel is built for; channels of a tile of the backward kernel, whose threads take 4 channels x 4 states.
+constexpr int seq_scan_states(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 64; }
+constexpr int seq_scan_bwd_channels(int SP) { return 1024 / SP; }
+constexpr int kSeqBwdChunk = 64;  // positions of a run of the backward kernel
+
+#ifdef __HIPCC__
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+static __device__ __forceinline__ unsigned seq_pack_bf16(float lo, float hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 p = {(__bf16)lo, (__bf16)hi};  // to nearest even
+    return __builtin_bit_cast(unsigned, p);
+}
+
+// T: float, or unsigned short for bf16.  A block of V numbers is one 16-byte access.
+template <typename T>
+struct SeqElem;
+template <>
+struct SeqElem<float> {
+    static constexpr int V = 4;
+    static __device__ __forceinline__ float get(float x) { return x; }
+    static __device__ __forceinline__ float put(float x) { return x; }
+    static __device__ __forceinline__ void unpack(const seq_u32x4 &b, float (&f)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(b[i]);
+    }
+    static __device__ __forceinline__ seq_u32x4 pack(const float (&f)[4])
+    {
+        seq_u32x4 b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(f[i]);
+        return b;
+    }
+};
+template <>
+struct SeqElem<unsigned short> {
+    static constexpr int V = 8;
+    static __device__ __forceinline__ float get(unsigned short x) { return __uint_as_float((unsigned)x << 16); }
+    static __device__ __forceinline__ unsigned short put(float x) { return (unsigned short)seq_pack_bf16(x, x); }
+    static __device__ __forceinline__ void unpack(const seq_u32x4 &b, float (&f)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(b[i] << 16);
+            f[2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ seq_u32x4 pack(const float (&f)[8])
+    {
+        seq_u32x4 b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = seq_pack_bf16(f[2 * i], f[2 * i + 1]);
+        return b;
+    }
+};
+
+template <typename T>
+static __device__ __forceinline__ seq_u32x4 seq_load(const T *p)
+{
+    return *reinterpret_cast<const seq_u32x4 *>(p);
+}
+template <typename T>
+static __device__ __forceinline__ void seq_store(T *p, const seq_u32x4 &b)
+{
+    *reinterpret_cast<seq_u32x4 *>(p) = b;
+}
+
+// V floats of an fp32 vector from block b on.
+template <int V>
+static __device__ __forceinline__ void seq_vector(const float *p, int b, float (&f)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+        const seq_f32x4 q = *reinterpret_cast<const seq_f32x4 *>(p + (long long)b * V + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[i + j] = q[j];
+    }
+}
+
+static __device__ __forceinline__ int seq_length(const int *lengths, int n, int L)
+{
+    return lengths ? min(max(lengths[n], 0), L) : L;
+}
+
+static __device__ __forceinline__ float seq_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// 1 / (1 + exp(-x)); the hardware's exponential and reciprocal are good to an ulp
+static __device__ __forceinline__ float seq_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + seq_exp2(-kLog2e * x)); }
+
+// log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|) <= 1, by the series of the inverse hyperbolic tangent:
+// log(1 + e) = 2 (t + t^3/3 + t^5/5 + ...), t = e / (2 + e) <= 1/3: eight terms leave 3^-17 / 17 < 2^-30 of it.  (The logarithm of
+// 1 + e itself loses what e has below 2^-24: steps of 1e-3 would be good to 6e-5.)
+static __device__ __forceinline__ float seq_softplus(float x)
+{
+    const float e = seq_exp2(-kLog2e * fabsf(x));
+    const float t = e * __builtin_amdgcn_rcpf(2.0f + e), u = t * t;
+    float p = 1.0f / 15;
+    p = fmaf(p, u, 1.0f / 13);
+    p = fmaf(p, u, 1.0f / 11);
+    p = fmaf(p, u, 1.0f / 9);
+    p = fmaf(p, u, 1.0f / 7);
+    p = fmaf(p, u, 1.0f / 5);
+    p = fmaf(p, u, 1.0f / 3);
+    p = fmaf(p * u, t, t);
+    return fmaf(2.0f, p, x != x ? x : fmaxf(x, 0.0f));
+}
+
+// Lane i of every row of 16 lanes, in all lanes of that row.
+template <int I>
+static __device__ __forceinline__ float seq_row_lane(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x150 + I, 0xf, 0xf, true));
+}
+// x + x of the lane that `CTRL` names.
+template <int CTRL>
+static __device__ __forceinline__ float seq_add_lane(float x)
+{
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+#endif
+
+}  // namespace convmi

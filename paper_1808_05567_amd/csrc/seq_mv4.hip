@@ -1,0 +1,247 @@
+// Products of a few rows with weights of 4 bits and a scale for each group of channels:
+//
+//   y[m,k] = xscale[m] sum_groups scale[g][k] sum_{c in g} q[k,c] x[m,c] + bias[k]
+//
+// On the matrix instructions, weights as the rows: 16 weight rows x 16 tokens x 32 channels.  The inner sums are exact for
+// 8-bit activations (integers) and sums of exact products in fp32 for bf16 ones: a whole number from -8 to 7 is exact in both types.
+// fp32 activations go as three bf16 numbers whose sum they are.  Scales are applied to the fp32 sums.
+//
+// A lane's 16 bytes of weights are 8 channels of each of 4 runs of 32, so that one instruction takes one run of 32 whole and
+// a group of 32, 64 or 128 channels is one, two or four of them, whatever its scale.
+//
+// Bound by the weights' bytes for few rows.
+#include "seq_internal.h"
+
+namespace convmi {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Activations of one lane: 8 channels of one token.
+template <int DT>
+struct Act;
+template <>
+struct Act<SEQ_I8> {
+    typedef int8_t T;
+    typedef i32x4 Acc;
+    seq_u32x2 x;
+    __device__ __forceinline__ void load(const int8_t *p) { x = *reinterpret_cast<const seq_u32x2 *>(p); }
+    __device__ __forceinline__ void zero() { x = seq_u32x2{}; }
+    // eight weights from a word: sixteen times their values, in the upper halves of bytes (low ones of each byte first)
+    struct Wt {
+        long lo_hi;
+    };
+    static __device__ __forceinline__ Wt unpack(unsigned w)
+    {
+        const unsigned even = w << 4 & 0xF0F0F0F0u, odd = w & 0xF0F0F0F0u;
+        // bytes 0 2 4 6 and 1 3 5 7 to 0 1 2 3 4 5 6 7
+        const unsigned a = __builtin_amdgcn_perm(odd, even, 0x05010400), b = __builtin_amdgcn_perm(odd, even, 0x07030602);
+        return {(long)((unsigned long)b << 32 | a)};
+    }
+    static constexpr float unit = 1.0f / 16;
+    static __device__ __forceinline__ Acc mma(const Wt &w, const Act &a, const Acc &c)
+    {
+        return __builtin_amdgcn_mfma_i32_16x16x32_i8(w.lo_hi, (long)((unsigned long)a.x[1] << 32 | a.x[0]), c, 0, 0, 0);
+    }
+};
+struct WtBf16 {
+    seq_u32x4 b;
+    // eight weights from a word as bf16 numbers
+    __device__ __forceinline__ explicit WtBf16(unsigned w)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int lo = (int)(w << (28 - 8 * i)) >> 28, hi = (int)(w << (24 - 8 * i)) >> 28;
+            b[i] = seq_pack_bf16((float)lo, (float)hi);
+        }
+    }
+};
+template <>
+struct Act<SEQ_BF16> {
+    typedef unsigned short T;
+    typedef seq_f32x4 Acc;
+    seq_u32x4 x;
+    __device__ __forceinline__ void load(const unsigned short *p) { x = seq_load(p); }
+    __device__ __forceinline__ void zero() { x = seq_u32x4{}; }
+    typedef WtBf16 Wt;
+    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
+    static constexpr float unit = 1.0f;
+    static __device__ __forceinline__ Acc mma(const Wt &w, const Act &a, const Acc &c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.b), __builtin_bit_cast(bf16x8, a.x), c, 0, 0, 0);
+    }
+};
+template <>
+struct Act<SEQ_F32> {
+    typedef float T;
+    typedef seq_f32x4 Acc;
+    seq_u32x4 h, m, l;
+    __device__ __forceinline__ void load(const float *p)
+    {
+        alignas(16) float f[8];
+        *reinterpret_cast<seq_f32x4 *>(f) = *reinterpret_cast<const seq_f32x4 *>(p);
+        *reinterpret_cast<seq_f32x4 *>(f + 4) = *reinterpret_cast<const seq_f32x4 *>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p0 = f[2 * i], p1 = f[2 * i + 1];
+            h[i] = seq_pack_bf16(p0, p1);
+            const float r0 = p0 - __uint_as_float(h[i] << 16), r1 = p1 - __uint_as_float(h[i] & 0xFFFF0000u);
+            m[i] = seq_pack_bf16(r0, r1);
+            l[i] = seq_pack_bf16(r0 - __uint_as_float(m[i] << 16), r1 - __uint_as_float(m[i] & 0xFFFF0000u));
+        }
+    }
+    __device__ __forceinline__ void zero() { h = m = l = seq_u32x4{}; }
+    typedef WtBf16 Wt;
+    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
+    static constexpr float unit = 1.0f;
+    static __device__ __forceinline__ Acc mma(const Wt &w, const Act &a, Acc c)
+    {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.b), __builtin_bit_cast(bf16x8, a.l), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.b), __builtin_bit_cast(bf16x8, a.m), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.b), __builtin_bit_cast(bf16x8, a.h), c, 0, 0, 0);
+    }
+};
+
+// A workgroup: 16 weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.
+template <int DT, int NT>
+__global__ __launch_bounds__(512) void seq_mv4_kernel(const SeqMv4Args a)
+{
+    typedef Act<DT> A;
+    typedef typename A::T T;
+    __shared__ float lds[8 * NT * 256];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const int j = lane / 16, col = lane % 16;  // operands: row or token `col`, channels 8 j ... + 7 of a run of 32
+    const int k0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
+    const seq_u32x4 *wt = static_cast<const seq_u32x4 *>(a.wt) + (long long)(k0 + col) * 4 + j;
+    const T *x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t] = static_cast<const T *>(a.x) + (long long)min(m0 + t * 16 + col, a.M - 1) * a.Cx + 8 * j;
+    const float *scale = a.scale + k0 + 4 * j;  // results: rows 4 j ... + 3, token `col`
+    seq_f32x4 sum[NT] = {};
+    const int per = a.group / 32;  // runs of 32 a group
+    for (int c = wave; c < a.Cs; c += waves) {
+        const seq_u32x4 w = wt[(long long)c * a.Kp * 4];
+        typename A::Acc acc[NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i % per == 0)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = typename A::Acc{};
+            const typename A::Wt wi = A::unpack(w[i]);
+            const int c0 = c * 128 + i * 32, g0 = c0 - i % per * 32;  // (the group's first)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                A act;
+                // (x ends at Cx, the weights go on with zeros to the end of the run of 128)
+                if (c0 + 8 * j + 8 <= a.Cx)
+                    act.load(x[t] + c0);
+                else
+                    act.zero();
+                if constexpr (DT == SEQ_F32) {
+                    if (c0 + 8 * j + 4 == a.Cx) {  // (half of the eight)
+                        alignas(16) float f[8] = {};
+                        *reinterpret_cast<seq_f32x4 *>(f) = *reinterpret_cast<const seq_f32x4 *>(x[t] + c0);
+                        act.load(f);
+                    }
+                }
+                acc[t] = A::mma(wi, act, acc[t]);
+            }
+            if (i % per == per - 1 && g0 < a.C) {
+                const seq_f32x4 sc = *reinterpret_cast<const seq_f32x4 *>(scale + (long long)(g0 / a.group) * a.Kp);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(sc[e], (float)acc[t][e], sum[t][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds[(wave * NT + t) * 256 + col * 16 + 4 * j + e] = sum[t][e];
+    __syncthreads();
+    // one result a thread: token i / 16, row i % 16
+    for (int i = threadIdx.x; i < NT * 256; i += blockDim.x) {
+        float s = 0;
+        for (int v = 0; v < waves; ++v) s += lds[v * NT * 256 + i];
+        const int m = m0 + i / 16, k = k0 + i % 16;
+        if (m >= a.M || k >= a.Ky) continue;
+        s *= A::unit;
+        if (a.xscale) s *= a.xscale[m];
+        if (a.bias && k < a.K) s += a.bias[k];
+        if (k >= a.K) s = 0;
+        if constexpr (DT == SEQ_F32)
+            static_cast<float *>(a.y)[(long long)m * a.Ky + k] = s;
+        else
+            static_cast<unsigned short *>(a.y)[(long long)m * a.Ky + k] = SeqElem<unsigned short>::put(s);
+    }
+}
+
+// One thread a word of eight weights; the 16, 8 or 4 threads of one group's words stand side by side.
+__global__ __launch_bounds__(256) void seq_mv4_quant_kernel(const SeqMv4Args a, const float *w, unsigned *wt, float *scale)
+{
+    const long long total = (long long)a.Cs * 16 * a.Kp;
+    for (long long base = (long long)blockIdx.x * 256; base < total; base += (long long)gridDim.x * 256) {
+        // (total is a multiple of 256: Kp is one of 16)
+        const long long t = base + threadIdx.x;
+        const int u = (int)(t % 16), k = (int)(t / 16 % a.Kp), cs = (int)(t / 16 / a.Kp);
+        const int c0 = cs * 128 + u * 8;  // word i = u / 4 of the bytes j = u % 4
+        float f[8], m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f[e] = k < a.K && c0 + e < a.C ? w[(long long)k * a.C + c0 + e] : 0.0f;
+            m = fmaxf(m, fabsf(f[e]));
+        }
+        for (int d = 1; d < a.group / 8; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        const float s = m / 7.0f;
+        unsigned word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) word |= ((unsigned)(int)rintf(fminf(fmaxf(s > 0 ? f[e] / s : 0.0f, -8.0f), 7.0f)) & 15u) << 4 * e;
+        wt[(((long long)cs * a.Kp + k) * 4 + u % 4) * 4 + u / 4] = word;
+        if (c0 % a.group == 0 && c0 < a.C) scale[(long long)(c0 / a.group) * a.Kp + k] = s;
+    }
+}
+
+__global__ __launch_bounds__(256) void seq_mv4_unquant_kernel(const SeqMv4Args a, float *w)
+{
+    const long long total = (long long)a.K * a.C;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += (long long)gridDim.x * 256) {
+        const int k = (int)(t / a.C), c = (int)(t % a.C);
+        const unsigned word = static_cast<const unsigned *>(a.wt)[(((long long)(c / 128) * a.Kp + k) * 4 + c % 32 / 8) * 4 + c % 128 / 32];
+        w[t] = (float)((int)(word << (28 - 4 * (c % 8))) >> 28) * a.scale[(long long)(c / a.group) * a.Kp + k];
+    }
+}
+
+template <int DT>
+hipError_t launch(const SeqMv4Args &a, hipStream_t s)
+{
+    int waves = 1;
+    while (waves < 8 && waves < a.Cs) waves *= 2;
+    const unsigned kt = (unsigned)(a.Kp / 16);
+    if (a.M <= 16)
+        seq_mv4_kernel<DT, 1><<<dim3(kt, 1), waves * 64, 0, s>>>(a);
+    else
+        seq_mv4_kernel<DT, 2><<<dim3(kt, (a.M + 31) / 32), waves * 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_seq_mv4(int dtype, const SeqMv4Args &a, hipStream_t s)
+{
+    return dtype == SEQ_I8 ? launch<SEQ_I8>(a, s) : dtype == SEQ_BF16 ? launch<SEQ_BF16>(a, s) : launch<SEQ_F32>(a, s);
+}
+hipError_t launch_seq_mv4_quant(const SeqMv4Args &a, const float *w, void *wt, float *scale, hipStream_t s)
+{
+    const long long blocks = (long long)a.Cs * a.Kp / 16;
+    seq_mv4_quant_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(a, w, static_cast<unsigned *>(wt), scale);
+    return hipGetLastError();
+}
+hipError_t launch_seq_mv4_unquant(const SeqMv4Args &a, float *w, hipStream_t s)
+{
+    const long long blocks = ((long long)a.K * a.C + 255) / 256;
+    seq_mv4_unquant_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(a, w);
+    return hipGetLastError();
+}
+
+}  // namespace convmi

@@ -1,0 +1,352 @@
+// Selective state space scan, forward and over one new position.
+//
+//   h[s] = exp(d A[s]) h[s] + d x B[s],   y = sum_s C[s] h[s] + D x,   y *= z sigmoid(z)
+//
+// One lane a channel, its states in registers, one position after the other.  B and C are the same for all channels of a
+// group: lane i of each row of 16 holds state i, and an instruction takes it from there (row_newbcast) at no cost.
+//
+// Five operations and an exponential a state and position against 2 to 8 bytes a position: bound by the vector units.  Too few
+// channels to fill the machine are split along the positions too: a first launch takes each run of positions from a state of
+// zeros and notes the state it ends in and the sum of d, from which what the run does to any state follows:
+// exp(A sum d) h + that; a second puts these together in order; a third goes through each run from the right state.
+#include "seq_internal.h"
+
+namespace convmi {
+namespace {
+
+template <int SP>
+struct States {
+    static constexpr int R = (SP + 15) / 16;  // registers that hold SP states of B or C, 16 lanes each
+};
+
+template <int I, int SP, bool OUT>
+static __device__ __forceinline__ void seq_step(float (&h)[SP], const float (&A)[SP], float d, float dx, const float (&B)[States<SP>::R],
+                                                const float (&C)[States<SP>::R], float (&y)[4])
+{
+    if constexpr (I < SP) {
+        const float a = seq_exp2(d * A[I]);
+        h[I] = fmaf(a, h[I], seq_row_lane<I % 16>(B[I / 16]) * dx);
+        if constexpr (OUT) y[I % 4] = fmaf(seq_row_lane<I % 16>(C[I / 16]), h[I], y[I % 4]);
+        seq_step<I + 1, SP, OUT>(h, A, d, dx, B, C, y);
+    }
+}
+
+// The same for the ends of a run, in both directions: h from zeros, and the gradient g of the state before the run where none comes
+// from behind it, the sum over its positions of C dy times the product P of all decays up to there.
+template <int I, int SP>
+static __device__ __forceinline__ void seq_step_ends(float (&h)[SP], float (&g)[SP], float (&P)[SP], const float (&A)[SP], float d, float dx, float dy,
+                                                     const float (&B)[States<SP>::R], const float (&C)[States<SP>::R])
+{
+    if constexpr (I < SP) {
+        const float a = seq_exp2(d * A[I]);
+        h[I] = fmaf(a, h[I], seq_row_lane<I % 16>(B[I / 16]) * dx);
+        P[I] *= a;
+        g[I] = fmaf(P[I], seq_row_lane<I % 16>(C[I / 16]) * dy, g[I]);
+        seq_step_ends<I + 1, SP>(h, g, P, A, d, dx, dy, B, C);
+    }
+}
+
+// MODE 0: the state a run ends in from zeros; 1: results (chunks == 1: the whole sequence); 2: the ends for the gradients.
+template <typename T, int SP, int MODE>
+__global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
+{
+    constexpr int V = SeqElem<T>::V, R = States<SP>::R, CB = 64 / V, NV = CB * 8 / 64;
+    constexpr bool OUT = MODE == 1, ENDS = MODE == 2, ALL = OUT || ENDS;
+    constexpr int SG = ENDS ? SP : 1;
+    __shared__ __align__(16) T tile[ALL ? 4 : 2][8 * 64];  // x, dt, z, y (ENDS: dy) of 8 positions x 64 channels
+    const int lane = threadIdx.x;
+    int t = blockIdx.x;
+    const int chunk = t % a.chunks;
+    t /= a.chunks;
+    const int g = t % a.G, tl = t / a.G % a.tiles, n = t / a.G / a.tiles;
+    const int c0 = g * a.CG + tl * 64, c_end = min(c0 + 64, (g + 1) * a.CG);
+    const int c = c0 + lane;
+    const bool live = c < c_end;
+    const int cs = live ? c : c0;
+    const int len = seq_length(a.lengths, n, a.L);
+    const int begin = chunk * a.chunk, end = min(begin + a.chunk, a.L), stop = min(end, len);
+
+    float A[SP], h[SP], gr[SG], P[SG];
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+        A[s] = s < a.S ? a.A[(long long)s * a.Cp + cs] * kLog2e : 0.0f;
+        h[s] = 0;
+        if (ENDS) gr[s % SG] = 0, P[s % SG] = 1;
+    }
+    const float bias = a.dt_bias ? a.dt_bias[cs] : 0.0f, D = OUT && a.D ? a.D[cs] : 0.0f;
+    const int slot = a.slots ? a.slots[n] : n;
+    const bool has_slot = slot >= 0 && slot < a.n_slots;
+    const long long at = ((long long)n * a.chunks + chunk) * a.S * a.Cp + cs;
+    if (OUT) {
+        if (a.chunks > 1) {
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < a.S) h[s] = a.hl[at + (long long)s * a.Cp];
+        } else if (a.state_in && has_slot) {
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < a.S) h[s] = a.state_in[((long long)slot * a.S + s) * a.Cp + cs];
+        }
+    }
+
+    // what a lane loads and stores: block cbl of the tile's, position ll of 8
+    const T *px[NV], *pd[NV], *pz[NV];
+    const T *pg[NV];
+    T *py[NV];
+    bool in[NV];
+    int ll[NV], to[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = lane + 64 * i, cbl = e / 8;
+        ll[i] = e % 8;
+        to[i] = ll[i] * 64 + cbl * V;
+        in[i] = c0 + cbl * V < c_end;
+        const int cb = c0 / V + (in[i] ? cbl : 0);
+        px[i] = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
+        pd[i] = static_cast<const T *>(a.dt) + n * a.vdt.n + cb * a.vdt.c;
+        if (ALL) pz[i] = a.z ? static_cast<const T *>(a.z) + n * a.vz.n + cb * a.vz.c : nullptr;
+        if (ENDS) pg[i] = static_cast<const T *>(a.dy) + n * a.vdy.n + cb * a.vdy.c;
+        if (OUT) {
+            py[i] = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
+        }
+    }
+    // B and C of state lane % 16 + 16 r
+    const T *pB[R], *pC[R];
+    bool has[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = lane % 16 + 16 * r;
+        has[r] = s < a.S;
+        const int e = g * a.S + (has[r] ? s : 0);
+        pB[r] = static_cast<const T *>(a.B) + n * a.vB.n + e / V * a.vB.c + e % V;
+        if (ALL) pC[r] = static_cast<const T *>(a.C) + n * a.vC.n + e / V * a.vC.c + e % V;
+    }
+
+    seq_u32x4 nx[NV], nd[NV], nz[NV], ng[NV];
+    T nB[R][8], nC[R][8];
+    auto fetch = [&](int l0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int l = l0 + ll[i];
+            const bool ok = in[i] && l < stop;
+            nx[i] = nd[i] = nz[i] = ng[i] = seq_u32x4{};
+            if (ok) {
+                nx[i] = seq_load(px[i] + l * a.vx.l);
+                nd[i] = seq_load(pd[i] + l * a.vdt.l);
+                if (ALL && a.z) nz[i] = seq_load(pz[i] + l * a.vz.l);
+                if (ENDS) ng[i] = seq_load(pg[i] + l * a.vdy.l);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int l = l0 + j;
+                const bool ok = has[r] && l < stop;
+                nB[r][j] = ok ? pB[r][l * a.vB.l] : T(0);
+                if (ALL) nC[r][j] = ok ? pC[r][l * a.vC.l] : T(0);
+            }
+    };
+    float sum_d = 0;
+    if (begin < stop) fetch(begin);
+    for (int l0 = begin; l0 < stop; l0 += 8) {
+        T cB[R][8], cC[R][8];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                cB[r][j] = nB[r][j];
+                if (ALL) cC[r][j] = nC[r][j];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            seq_store(tile[0] + to[i], nx[i]);
+            seq_store(tile[1] + to[i], nd[i]);
+            if (ALL) seq_store(tile[ALL ? 2 : 0] + to[i], nz[i]);
+            if (ENDS) seq_store(tile[ALL ? 3 : 0] + to[i], ng[i]);
+        }
+        __syncthreads();
+        if (l0 + 8 < stop) fetch(l0 + 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = SeqElem<T>::get(tile[0][j * 64 + lane]);
+            float d = SeqElem<T>::get(tile[1][j * 64 + lane]) + bias;
+            if (a.softplus) d = seq_softplus(d);
+            if (l0 + j >= stop) d = 0;  // (what follows the end changes nothing: x, B, C and z are zero there)
+            float B[R], C[R], y[4] = {};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                B[r] = SeqElem<T>::get(cB[r][j]);
+                if (ALL) C[r] = SeqElem<T>::get(cC[r][j]);
+            }
+            const auto gate = [&] {
+                const float z = SeqElem<T>::get(tile[ALL ? 2 : 0][j * 64 + lane]);
+                return z * seq_sigmoid(z);
+            };
+            if constexpr (ENDS) {
+                float dy = SeqElem<T>::get(tile[3][j * 64 + lane]);
+                if (a.z) dy *= gate();
+                seq_step_ends<0, SP>(h, gr, P, A, d, d * x, dy, B, C);
+            } else
+                seq_step<0, SP, OUT>(h, A, d, d * x, B, C, y);
+            sum_d += d;
+            if (OUT) {
+                float o = fmaf(D, x, (y[0] + y[1]) + (y[2] + y[3]));
+                if (a.z) o *= gate();
+                tile[OUT ? 3 : 0][j * 64 + lane] = SeqElem<T>::put(live ? o : 0.0f);
+            }
+        }
+        if (OUT) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (in[i] && l0 + ll[i] < end)
+                    seq_store(py[i] + (l0 + ll[i]) * a.vy.l, l0 + ll[i] < stop ? seq_load(tile[OUT ? 3 : 0] + to[i]) : seq_u32x4{});
+        }
+    }
+    if (OUT) {
+        // zeros past the end, from where the last eight positions stopped
+        for (int l0 = begin + (max(stop - begin, 0) + 7) / 8 * 8; l0 < end; l0 += 8)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (in[i] && l0 + ll[i] < end) seq_store(py[i] + (l0 + ll[i]) * a.vy.l, seq_u32x4{});
+        // the run that the last position is in stores the state, the first one that of an empty sequence
+        const bool last = len == 0 ? chunk == 0 : begin < len && len <= begin + a.chunk;
+        if (a.state_out && has_slot && last && live)
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < a.S) a.state_out[((long long)slot * a.S + s) * a.Cp + c] = h[s];
+    } else if (live) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+            if (s < a.S) {
+                a.hl[at + (long long)s * a.Cp] = h[s];
+                if (ENDS) a.gl[at + (long long)s * a.Cp] = gr[s % SG];
+            }
+        a.sd[((long long)n * a.chunks + chunk) * a.Cp + c] = sum_d;
+    }
+}
+
+// The state at the start of each run from those the runs end in, in place; the gradient at the end of each the same way, from the back.
+__global__ __launch_bounds__(256) void seq_scan_join_kernel(const SeqScanArgs a)
+{
+    const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long state = (long long)a.S * a.Cp;
+    if (t >= a.N * state) return;
+    const int n = (int)(t / state), c = (int)(t % a.Cp);
+    const long long e = t % state;
+    if (c >= a.Ch) return;
+    const int slot = a.slots ? a.slots[n] : n;
+    const float A = a.A[e] * kLog2e;
+    float h = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f;
+    float *hl = a.hl + (long long)n * a.chunks * state + e;
+    const float *sd = a.sd + (long long)n * a.chunks * a.Cp + c;
+#pragma unroll 4
+    for (int k = 0; k < a.chunks; ++k) {
+        const float from_zero = hl[k * state];
+        hl[k * state] = h;
+        h = fmaf(seq_exp2(A * sd[(long long)k * a.Cp]), h, from_zero);
+    }
+    if (!a.gl) return;
+    float *gl = a.gl + (long long)n * a.chunks * state + e;
+    float g = 0;
+#pragma unroll 4
+    for (int k = a.chunks - 1; k >= 0; --k) {
+        const float own = gl[k * state];
+        gl[k * state] = g;
+        g = fmaf(seq_exp2(A * sd[(long long)k * a.Cp]), g, own);
+    }
+}
+
+// One new position: 64 channels a workgroup, its four waves taking every fourth state.
+template <typename T>
+__global__ __launch_bounds__(256) void seq_scan_step_kernel(const SeqScanArgs a)
+{
+    constexpr int V = SeqElem<T>::V;
+    __shared__ float lds[256];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int ct = (a.Cp + 63) / 64, n = blockIdx.x / ct, c = blockIdx.x % ct * 64 + lane;
+    const int slot = a.slots ? a.slots[n] : n;
+    const bool has_slot = slot >= 0 && slot < a.n_slots;
+    const bool live = c < a.Ch;
+    auto at = [&](const SeqView &v, int e) { return n * v.n + e / V * v.c + e % V; };
+    float x = 0, y = 0;
+    if (live && has_slot) {
+        const int g = c / a.CG;
+        x = SeqElem<T>::get(static_cast<const T *>(a.x)[at(a.vx, c)]);
+        float d = SeqElem<T>::get(static_cast<const T *>(a.dt)[at(a.vdt, c)]) + (a.dt_bias ? a.dt_bias[c] : 0.0f);
+        if (a.softplus) d = seq_softplus(d);
+        float *h = a.state_out + (long long)slot * a.S * a.Cp + c;
+#pragma unroll 4
+        for (int s = wave; s < a.S; s += 4) {
+            const float B = SeqElem<T>::get(static_cast<const T *>(a.B)[at(a.vB, g * a.S + s)]);
+            const float C = SeqElem<T>::get(static_cast<const T *>(a.C)[at(a.vC, g * a.S + s)]);
+            const float next = fmaf(seq_exp2(d * (a.A[(long long)s * a.Cp + c] * kLog2e)), h[(long long)s * a.Cp], d * x * B);
+            h[(long long)s * a.Cp] = next;
+            y = fmaf(C, next, y);
+        }
+    }
+    lds[threadIdx.x] = y;
+    __syncthreads();
+    if (wave != 0 || c >= a.Cp) return;
+    y = (lds[lane] + lds[lane + 64]) + (lds[lane + 128] + lds[lane + 192]);
+    if (live && has_slot) {
+        if (a.D) y = fmaf(a.D[c], x, y);
+        if (a.z) {
+            const float z = SeqElem<T>::get(static_cast<const T *>(a.z)[at(a.vz, c)]);
+            y *= z * seq_sigmoid(z);
+        }
+    }
+    static_cast<T *>(a.y)[at(a.vy, c)] = SeqElem<T>::put(y);
+}
+
+template <typename T, int SP>
+hipError_t launch(const SeqScanArgs &a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((long long)a.N * a.G * a.tiles * a.chunks);
+    if (a.chunks > 1) {
+        seq_scan_kernel<T, SP, 0><<<grid, 64, 0, s>>>(a);
+        seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
+    }
+    seq_scan_kernel<T, SP, 1><<<grid, 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int SP>
+hipError_t launch_ends(const SeqScanArgs &a, hipStream_t s)
+{
+    seq_scan_kernel<T, SP, 2><<<(unsigned)((long long)a.N * a.G * a.tiles * a.chunks), 64, 0, s>>>(a);
+    seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_t(bool ends, const SeqScanArgs &a, hipStream_t s)
+{
+    switch (seq_scan_states(a.S)) {
+        case 8: return ends ? launch_ends<T, 8>(a, s) : launch<T, 8>(a, s);
+        case 16: return ends ? launch_ends<T, 16>(a, s) : launch<T, 16>(a, s);
+        case 32: return ends ? launch_ends<T, 32>(a, s) : launch<T, 32>(a, s);
+    }
+    return ends ? launch_ends<T, 64>(a, s) : launch<T, 64>(a, s);
+}
+}  // namespace
+
+hipError_t launch_seq_scan_fwd(int dtype, const SeqScanArgs &a, hipStream_t s)
+{
+    return dtype == SEQ_BF16 ? launch_t<unsigned short>(false, a, s) : launch_t<float>(false, a, s);
+}
+hipError_t launch_seq_scan_ends(int dtype, const SeqScanArgs &a, hipStream_t s)
+{
+    return dtype == SEQ_BF16 ? launch_t<unsigned short>(true, a, s) : launch_t<float>(true, a, s);
+}
+hipError_t launch_seq_scan_step(int dtype, const SeqScanArgs &a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((long long)a.N * ((a.Cp + 63) / 64));
+    if (dtype == SEQ_BF16)
+        seq_scan_step_kernel<unsigned short><<<grid, 256, 0, s>>>(a);
+    else
+        seq_scan_step_kernel<float><<<grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace convmi

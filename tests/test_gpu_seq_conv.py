@@ -1,0 +1,152 @@
+"""Short causal convolution against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import seq_oracle as oracle
+from seq_util import DTYPES, LAYOUTS, Seq, close, ints, lengths_of, nans, rounded, spoil, vector, vlen
+from paper_1808_05567_amd import seq
+
+pytestmark = pytest.mark.gpu
+# Sums of at most 9 products, each product and sum rounded once, the sigmoid of the hardware's exponential and reciprocal (2 units) and
+# three operations on it: 16 units of 2^-24 of the magnitudes.  Sums over positions: one more a position.
+U = 2.0 ** -24
+
+
+def data(N, C, L, W, dtype, seed):
+    rng = np.random.default_rng(seed)
+    x, dy = rounded(rng.standard_normal((N, L, C)), dtype), rounded(rng.standard_normal((N, L, C)), dtype)
+    w = rng.standard_normal((W, C)).astype(np.float32).astype(np.float64) * 0.5
+    bias = (rng.standard_normal(C) * 0.3).astype(np.float32).astype(np.float64)
+    return rng, x, dy, w.astype(np.float32).astype(np.float64), bias
+
+
+CASES = [  # N, C, L, W, silu, lengths, state, layout
+    (1, 8, 1, 4, True, "none", True, "dense"), (2, 5, 3, 4, True, "ragged", True, "slice"), (3, 64, 33, 4, True, "ragged", True, "rows"),
+    (1, 130, 65, 2, True, "none", False, "dense"), (4, 40, 31, 3, False, "clamped", True, "slice"), (2, 72, 300, 4, True, "ragged", True, "dense"),
+    (1, 16, 7, 8, True, "none", True, "rows"), (5, 24, 2, 8, True, "ragged", True, "dense"), (2, 9, 130, 5, False, "none", False, "rows"),
+    (1, 4, 64, 6, True, "clamped", True, "dense"), (3, 12, 97, 7, True, "ragged", False, "slice"),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,C,L,W,silu,kind,with_state,layout", CASES)
+def test_forward(N, C, L, W, silu, kind, with_state, layout, dtype):
+    rng, x, _, w, bias = data(N, C, L, W, dtype, 7 * N + L + W)
+    v, lengths = vlen(dtype), lengths_of(kind, N, L, rng)
+    slots = N + 2
+    where = rng.permutation(slots)[:N]
+    old = rounded(rng.standard_normal((slots, W - 1, C)), dtype)
+    X, Y = Seq(N, C, L, dtype, layout, spoil(x, lengths)), Seq(N, C, L, dtype, layout)
+    state = Seq(slots, C, W - 1, dtype, "dense", old)
+    h = seq.seq_conv_create(N, C, L, W, dtype, silu=silu, slots=slots, views={"x": X.t, "y": Y.t})
+    st = state.t.contiguous() if with_state else None
+    seq.seq_conv_fwd(h, X.t, vector(w, v), vector(bias, v), Y.t, state_in=st, state_out=st, slots=ints(where), lengths=ints(lengths))
+    torch.cuda.synchronize()
+    args = (x, w, bias, silu, old[where] if with_state else None, lengths)
+    ref, after = oracle.conv(*args)
+    close(Y.get(), ref, 16 * U * oracle.conv(*args, mag=True)[0], dtype == seq.SEQ_BF16, "y")
+    if with_state:
+        got = st.permute(0, 2, 1, 3).reshape(slots, W - 1, -1).double().cpu().numpy()
+        want = np.zeros_like(got)
+        want[..., :C] = old
+        want[where, :, :C] = after
+        np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_slots_out_of_range_start_from_zeros_and_store_nothing(dtype):
+    N, C, L, W, slots = 4, 16, 6, 4, 3
+    rng, x, _, w, bias = data(N, C, L, W, dtype, 3)
+    v = vlen(dtype)
+    old = rounded(rng.standard_normal((slots, W - 1, C)), dtype)
+    where = np.array([1, -1, 3, 0])
+    X, Y = Seq(N, C, L, dtype, "dense", x), Seq(N, C, L, dtype)
+    state = Seq(slots, C, W - 1, dtype, "dense", old)
+    h = seq.seq_conv_create(N, C, L, W, dtype, slots=slots)
+    seq.seq_conv_fwd(h, X.t, vector(w, v), vector(bias, v), Y.t, state_in=state.t, state_out=state.t, slots=ints(where))
+    begin = np.stack([old[1], np.zeros_like(old[0]), np.zeros_like(old[0]), old[0]])
+    ref, after = oracle.conv(x, w, bias, True, begin)
+    close(Y.get(), ref, 16 * U * oracle.conv(x, w, bias, True, begin, mag=True)[0], dtype == seq.SEQ_BF16)
+    old[1], old[0] = after[0], after[3]
+    np.testing.assert_array_equal(state.get(), old)
+    # one position: rows without a state are zero
+    x1, y1 = Seq(N, C, 1, dtype, "dense", x[:, :1]), Seq(N, C, 1, dtype)
+    h = seq.seq_conv_create(N, C, 1, W, dtype, slots=slots)
+    seq.seq_conv_step(h, x1.t, vector(w, v), vector(bias, v), state.t, y1.t, slots=ints(where))
+    begin = np.stack([old[1], old[2], old[2], old[0]])
+    ref, after = oracle.conv(x[:, :1], w, bias, True, begin)
+    ref[1:3] = 0
+    close(y1.get(), ref, 16 * U * oracle.conv(x[:, :1], w, bias, True, begin, mag=True)[0], dtype == seq.SEQ_BF16)
+    old[1], old[0] = after[0], after[3]
+    np.testing.assert_array_equal(state.get(), old)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,C,W,layout", [(1, 8, 4, "dense"), (3, 21, 4, "rows"), (70, 40, 2, "slice"), (5, 136, 8, "dense")])
+def test_steps_follow_the_forward_pass(N, C, W, layout, dtype):
+    L = 5
+    rng, x, _, w, bias = data(N, C, L, W, dtype, N + W)
+    v = vlen(dtype)
+    X, Y = Seq(N, C, L, dtype, "dense", x), Seq(N, C, L, dtype)
+    h = seq.seq_conv_create(N, C, L, W, dtype)
+    seq.seq_conv_fwd(h, X.t, vector(w, v), vector(bias, v), Y.t)
+    state = Seq(N, C, W - 1, dtype, "dense", np.zeros((N, W - 1, C)))
+    x1, y1 = Seq(N, C, 1, dtype, layout, x[:, :1]), Seq(N, C, 1, dtype, layout)
+    hs = seq.seq_conv_create(N, C, 1, W, dtype, slots=N, views={"x": x1.t, "y": y1.t})
+    for l in range(L):
+        x1.t.copy_(X.t[:, :, l:l + 1])
+        seq.seq_conv_step(hs, x1.t, vector(w, v), vector(bias, v), state.t, y1.t)
+        np.testing.assert_array_equal(y1.get()[:, 0], Y.get()[:, l])  # (the same operations in the same order)
+    np.testing.assert_array_equal(state.get(), oracle.conv(x, w, bias, True)[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,C,L,W,silu,kind,_,layout", CASES + [(2, 264, 1000, 4, True, "ragged", False, "dense")])
+def test_gradients(N, C, L, W, silu, kind, _, layout, dtype):
+    rng, x, dy, w, bias = data(N, C, L, W, dtype, 11 * N + L + W)
+    v, lengths, bf16 = vlen(dtype), lengths_of(kind, N, L, rng), dtype == seq.SEQ_BF16
+    X, DY, DX = Seq(N, C, L, dtype, layout, spoil(x, lengths)), Seq(N, C, L, dtype, layout, spoil(dy, lengths)), Seq(N, C, L, dtype, layout)
+    h = seq.seq_conv_create(N, C, L, W, dtype, silu=silu, views={"x": X.t, "dy": DY.t, "dx": DX.t})
+    Cp = h.info.Cp
+    dw, db = nans(W, Cp), nans(Cp)
+    ws = seq.seq_workspace(h).fill_(0xFF)
+    seq.seq_conv_bwd(h, X.t, vector(w, v), vector(bias, v), DY.t, DX.t, dw, db, ws, lengths=ints(lengths))
+    torch.cuda.synchronize()
+    ref = oracle.conv_bwd(x, w, bias, dy, silu, lengths)
+    mag = oracle.conv_bwd(x, w, bias, dy, silu, lengths, mag=True)
+    close(DX.get(), ref[0], 24 * U * mag[0], bf16, "dx")
+    for got, r, m, name in ((dw, ref[1], mag[1], "dw"), (db, ref[2], mag[2], "dbias")):
+        got = got.double().cpu().numpy()
+        assert not got[..., C:].any()
+        close(got[..., :C], r, (24 + N * L) * U * m, False, name)
+    first = dw.clone()
+    seq.seq_conv_bwd(h, X.t, vector(w, v), vector(bias, v), DY.t, DX.t, dw, None, ws, lengths=ints(lengths))
+    assert torch.equal(first, dw)  # (and without the bias's gradient)
+
+
+@pytest.mark.parametrize("axis", ["n", "c", "l"])
+def test_distances_beyond_32_bits(axis):
+    """Each distance of a view alone takes a tensor's elements past 2^32."""
+    dtype, W, far = seq.SEQ_BF16, 4, (1 << 32) + 64
+    N, C, L = (2, 16, 12) if axis != "l" else (1, 16, 3)
+    shape = {"n": (far, 96, 8), "c": (192, far, 8), "l": (8, 8, far)}[axis]
+    rng, x, dy, w, bias = data(N, C, L, W, dtype, 5)
+    need = {"n": far + 200, "c": far + 600, "l": 2 * far + 64}[axis]
+
+    base, offsets = torch.empty(need + 16384, dtype=torch.bfloat16, device="cuda"), iter(range(0, 16384, 1024))
+
+    def tensor(data=None):
+        t = base.as_strided((N, 2, L, 8), shape + (1,), next(offsets))
+        if data is not None:
+            t.copy_(torch.from_numpy(data).view(N, L, 2, 8).permute(0, 2, 1, 3))
+        return t
+    X, Y = tensor(x), tensor()
+    h = seq.seq_conv_create(N, C, L, W, dtype, views={"x": X, "y": Y, "dy": X, "dx": Y})
+    seq.seq_conv_fwd(h, X, vector(w, 8), vector(bias, 8), Y)
+    got = Y.permute(0, 2, 1, 3).reshape(N, L, C).double().cpu().numpy()
+    close(got, oracle.conv(x, w, bias)[0], 16 * U * oracle.conv(x, w, bias, mag=True)[0], True)
+    dw, ws = nans(W, C), seq.seq_workspace(h)
+    seq.seq_conv_bwd(h, X, vector(w, 8), vector(bias, 8), X, Y, dw, None, ws)
+    got = Y.permute(0, 2, 1, 3).reshape(N, L, C).double().cpu().numpy()
+    close(got, oracle.conv_bwd(x, w, bias, x)[0], 24 * U * oracle.conv_bwd(x, w, bias, x, mag=True)[0], True)
