@@ -242,24 +242,16 @@ __global__ __launch_bounds__(256) void seq_conv_bwd_kernel(const SeqConvArgs a)
     }
 }
 
-// dw and dbias: the workgroups' sums, in order, 4 strands of them a channel.
-__global__ __launch_bounds__(256) void seq_conv_reduce_kernel(const float *part, float *dw, float *dbias, int parts, int W, int Cp)
+// dw and dbias: the workgroups' sums, in order.
+__global__ __launch_bounds__(1024) void seq_conv_reduce_kernel(const float *part, float *dw, float *dbias, int parts, int W, int Cp)
 {
-    __shared__ float lds[256];
-    const int col = blockIdx.x * 64 + threadIdx.x % 64, strand = threadIdx.x / 64;
-    const int total = (W + 1) * Cp;
-    float s = 0;
-    if (col < total)
-        for (int p = strand; p < parts; p += 4) s += part[(long long)p * total + col];
-    lds[threadIdx.x] = s;
-    __syncthreads();
-    if (strand == 0 && col < total) {
-        s = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
-        if (col < W * Cp)
-            dw[col] = s;
-        else if (dbias)
-            dbias[col - W * Cp] = s;
-    }
+    const int col = blockIdx.x * kSumColumns + threadIdx.x % kSumColumns, total = (W + 1) * Cp;
+    const float s = seq_sum_parts(part + col, total, parts, col < total);
+    if (threadIdx.x >= kSumColumns || col >= total) return;
+    if (col < W * Cp)
+        dw[col] = s;
+    else if (dbias)
+        dbias[col - W * Cp] = s;
 }
 
 template <typename T, int W>
@@ -277,7 +269,7 @@ hipError_t launch(int which, const SeqConvArgs &a, hipStream_t s)
         return hipGetLastError();
     }
     seq_conv_bwd_kernel<T, W><<<grid, 256, 0, s>>>(a);
-    seq_conv_reduce_kernel<<<((W + 1) * a.Cp + 63) / 64, 256, 0, s>>>(a.part, a.dw, a.dbias, a.N * a.ranges, W, a.Cp);
+    seq_conv_reduce_kernel<<<((W + 1) * a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, a.dbias, a.N * a.ranges, W, a.Cp);
     return hipGetLastError();
 }
 

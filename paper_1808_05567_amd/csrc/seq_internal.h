@@ -191,6 +191,35 @@ static __device__ __forceinline__ float seq_softplus(float x)
     return fmaf(2.0f, p, x != x ? x : fmaxf(x, 0.0f));
 }
 
+// Sum of parts of one column in a fixed order: 32 strands of them, each in turn, then the strands pairwise.  1024 threads a
+// workgroup, 32 columns: the result is in those of strand 0.  (512 parts of 2048 columns: 4 strands and one load at a time take 20 us.)
+constexpr int kSumColumns = 32, kSumStrands = 32;
+static __device__ __forceinline__ float seq_sum_parts(const float *p, long long pitch, int parts, bool ok)
+{
+    __shared__ float lds[kSumStrands][kSumColumns];
+    const int col = threadIdx.x % kSumColumns, strand = threadIdx.x / kSumColumns;
+    float s = 0;
+    if (ok) {
+        int k = strand;
+        for (; k + 7 * kSumStrands < parts; k += 8 * kSumStrands) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = p[(k + i * kSumStrands) * pitch];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += f[i];
+        }
+        for (; k < parts; k += kSumStrands) s += p[k * pitch];
+    }
+    lds[strand][col] = s;
+    __syncthreads();
+#pragma unroll
+    for (int d = kSumStrands / 2; d > 0; d /= 2) {
+        if (strand < d) lds[strand][col] += lds[strand + d][col];
+        __syncthreads();
+    }
+    return lds[0][col];
+}
+
 // Lane i of every row of 16 lanes, in all lanes of that row.
 template <int I>
 static __device__ __forceinline__ float seq_row_lane(float x)

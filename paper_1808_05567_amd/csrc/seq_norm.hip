@@ -10,7 +10,7 @@
 namespace convmi {
 namespace {
 
-constexpr int kMaxVectors = 16;  // blocks of one position a thread holds at most
+constexpr int kMaxThreads = 512;
 
 // Sums (or largest unsigned) of v over the threads with the same place in the tile of LT positions, in all of them.
 template <int LT, bool MAX>
@@ -32,10 +32,10 @@ static __device__ __forceinline__ float row_sum(float v, float *lds)
 // LT positions at a time, 64 / LT blocks a wave side by side: 8 x 8 where a block's positions follow one another (128 bytes),
 // 1 x 64 where a position's blocks do.  NV: blocks a thread holds; 0: more than fit, each read twice.
 template <typename T, int LT, int NV, bool Q8>
-__global__ __launch_bounds__(1024) void seq_norm_fwd_kernel(const SeqNormArgs a)
+__global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
-    __shared__ float lds[16 * LT];
+    __shared__ float lds[kMaxThreads / 64 * LT];
     const long long row = (long long)blockIdx.x * LT + threadIdx.x % LT;
     const bool live = row < a.rows;
     const int n = live ? (int)(row / a.L) : 0, l = live ? (int)(row % a.L) : 0;
@@ -163,11 +163,11 @@ __global__ __launch_bounds__(1024) void seq_norm_fwd_kernel(const SeqNormArgs a)
 }
 
 template <typename T, int LT, int NV>
-__global__ __launch_bounds__(1024) void seq_norm_bwd_kernel(const SeqNormArgs a)
+__global__ __launch_bounds__(kMaxThreads) void seq_norm_bwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
     constexpr int NK = NV ? NV : 1;
-    __shared__ float lds[16 * LT];
+    __shared__ float lds[kMaxThreads / 64 * LT];
     const int first = threadIdx.x / LT, step = blockDim.x / LT;
     float dw[NK][V] = {};
     for (long long tile = blockIdx.x; tile * LT < a.rows; tile += gridDim.x) {
@@ -263,33 +263,12 @@ __global__ __launch_bounds__(1024) void seq_norm_bwd_kernel(const SeqNormArgs a)
     }
 }
 
-// dw: the workgroups' sums in order, 4 strands of them a channel.
-__global__ __launch_bounds__(256) void seq_norm_reduce_kernel(const float *part, float *dw, int parts, int Cp)
+// dw: the workgroups' sums in order.
+__global__ __launch_bounds__(1024) void seq_norm_reduce_kernel(const float *part, float *dw, int parts, int Cp)
 {
-    __shared__ float lds[256];
-    const int c = blockIdx.x * 64 + threadIdx.x % 64, strand = threadIdx.x / 64;
-    float s = 0;
-    if (c < Cp)
-        for (int p = strand; p < parts; p += 4) s += part[(long long)p * Cp + c];
-    lds[threadIdx.x] = s;
-    __syncthreads();
-    if (strand == 0 && c < Cp) dw[c] = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
-}
-
-// Threads of a workgroup: one block each up to 256, then as many blocks a thread as that takes, then more threads.
-struct Shape {
-    int threads, nv;
-};
-Shape shape_of(int Cb, int lt)
-{
-    const long long lanes = (long long)Cb * lt;
-    int threads = 64;
-    while (threads < 256 && threads < lanes) threads *= 2;
-    while (threads < 1024 && (lanes + threads - 1) / threads > kMaxVectors / 2) threads *= 2;
-    const long long nv = (lanes + threads - 1) / threads;
-    int p = 1;
-    while (p < nv) p *= 2;
-    return {threads, p > kMaxVectors ? 0 : p};
+    const int c = blockIdx.x * kSumColumns + threadIdx.x % kSumColumns;
+    const float s = seq_sum_parts(part + c, Cp, parts, c < Cp);
+    if (threadIdx.x < kSumColumns && c < Cp) dw[c] = s;
 }
 
 template <typename T, int LT, int NV>
@@ -299,25 +278,34 @@ hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
     if (bwd) {
         const unsigned parts = grid < (unsigned)a.parts ? grid : (unsigned)a.parts;
         seq_norm_bwd_kernel<T, LT, NV><<<parts, threads, 0, s>>>(a);
-        seq_norm_reduce_kernel<<<(a.Cp + 63) / 64, 256, 0, s>>>(a.part, a.dw, (int)parts, a.Cp);
+        seq_norm_reduce_kernel<<<(a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, (int)parts, a.Cp);
     } else if (a.q)
         seq_norm_fwd_kernel<T, LT, NV, true><<<grid, threads, 0, s>>>(a);
     else
         seq_norm_fwd_kernel<T, LT, NV, false><<<grid, threads, 0, s>>>(a);
     return hipGetLastError();
 }
+
+// Threads of a workgroup and blocks that each holds: 256 threads with up to 8 blocks, then up to 512.  LT positions that do not fit
+// that go as fewer at a time, in shorter pieces; what one position does not fit is read twice.
 template <typename T, int LT>
 hipError_t launch_lt(bool bwd, const SeqNormArgs &a, hipStream_t s)
 {
-    const Shape sh = shape_of(a.Cb, LT);
-    switch (sh.nv) {
-        case 1: return launch_nv<T, LT, 1>(bwd, a, sh.threads, s);
-        case 2: return launch_nv<T, LT, 2>(bwd, a, sh.threads, s);
-        case 4: return launch_nv<T, LT, 4>(bwd, a, sh.threads, s);
-        case 8: return launch_nv<T, LT, 8>(bwd, a, sh.threads, s);
-        case 16: return launch_nv<T, LT, 16>(bwd, a, sh.threads, s);
+    const long long lanes = (long long)a.Cb * LT;
+    int threads = 64;
+    while (threads < 256 && threads < lanes) threads *= 2;
+    if (threads * 8 < lanes) threads = kMaxThreads;
+    const long long nv = (lanes + threads - 1) / threads;
+    if constexpr (LT == 8 || LT == 1) {  // (what comes to 4 and 2 has more)
+        if (nv <= 1) return launch_nv<T, LT, 1>(bwd, a, threads, s);
+        if (nv <= 2) return launch_nv<T, LT, 2>(bwd, a, threads, s);
+        if (nv <= 4) return launch_nv<T, LT, 4>(bwd, a, threads, s);
     }
-    return launch_nv<T, LT, 0>(bwd, a, sh.threads, s);
+    if (nv <= 8) return launch_nv<T, LT, 8>(bwd, a, threads, s);
+    if constexpr (LT > 1)
+        return launch_lt<T, LT / 2>(bwd, a, s);
+    else
+        return launch_nv<T, LT, 0>(bwd, a, threads, s);
 }
 template <typename T>
 hipError_t launch_t(bool bwd, const SeqNormArgs &a, hipStream_t s)

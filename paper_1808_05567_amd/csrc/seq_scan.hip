@@ -53,6 +53,8 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
     constexpr int V = SeqElem<T>::V, R = States<SP>::R, CB = 64 / V, NV = CB * 8 / 64;
     constexpr bool OUT = MODE == 1, ENDS = MODE == 2, ALL = OUT || ENDS;
     constexpr int SG = ENDS ? SP : 1;
+    constexpr int E = SP / 8, BL = SP < 16 ? SP : 16;  // elements of B of 8 positions a lane loads; lanes of a row that hold states
+    __shared__ float bc[ALL ? 2 : 1][8 * SP];
     __shared__ __align__(16) T tile[ALL ? 4 : 2][8 * 64];  // x, dt, z, y (ENDS: dy) of 8 positions x 64 channels
     const int lane = threadIdx.x;
     int t = blockIdx.x;
@@ -110,12 +112,12 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
             py[i] = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
         }
     }
-    // B and C of state lane % 16 + 16 r
-    const T *pB[R], *pC[R];
-    bool has[R];
+    // B and C: positions and states of the elements that a lane loads
+    const T *pB[E], *pC[E];
+    bool has[E];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = lane % 16 + 16 * r;
+    for (int r = 0; r < E; ++r) {
+        const int s = (lane + 64 * r) % SP;
         has[r] = s < a.S;
         const int e = g * a.S + (has[r] ? s : 0);
         pB[r] = static_cast<const T *>(a.B) + n * a.vB.n + e / V * a.vB.c + e % V;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
     }
 
     seq_u32x4 nx[NV], nd[NV], nz[NV], ng[NV];
-    T nB[R][8], nC[R][8];
+    T nB[E], nC[E];
     auto fetch = [&](int l0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -138,26 +140,16 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
             }
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int l = l0 + j;
-                const bool ok = has[r] && l < stop;
-                nB[r][j] = ok ? pB[r][l * a.vB.l] : T(0);
-                if (ALL) nC[r][j] = ok ? pC[r][l * a.vC.l] : T(0);
-            }
+        for (int r = 0; r < E; ++r) {
+            const int l = l0 + (lane + 64 * r) / SP;
+            const bool ok = has[r] && l < stop;
+            nB[r] = ok ? pB[r][l * a.vB.l] : T(0);
+            if (ALL) nC[r] = ok ? pC[r][l * a.vC.l] : T(0);
+        }
     };
     float sum_d = 0;
     if (begin < stop) fetch(begin);
     for (int l0 = begin; l0 < stop; l0 += 8) {
-        T cB[R][8], cC[R][8];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                cB[r][j] = nB[r][j];
-                if (ALL) cC[r][j] = nC[r][j];
-            }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -166,36 +158,57 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
             if (ALL) seq_store(tile[ALL ? 2 : 0] + to[i], nz[i]);
             if (ENDS) seq_store(tile[ALL ? 3 : 0] + to[i], ng[i]);
         }
+#pragma unroll
+        for (int r = 0; r < E; ++r) {
+            bc[0][lane + 64 * r] = SeqElem<T>::get(nB[r]);
+            if (ALL) bc[ALL ? 1 : 0][lane + 64 * r] = SeqElem<T>::get(nC[r]);
+        }
         __syncthreads();
         if (l0 + 8 < stop) fetch(l0 + 8);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = SeqElem<T>::get(tile[0][j * 64 + lane]);
-            float d = SeqElem<T>::get(tile[1][j * 64 + lane]) + bias;
-            if (a.softplus) d = seq_softplus(d);
-            if (l0 + j >= stop) d = 0;  // (what follows the end changes nothing: x, B, C and z are zero there)
-            float B[R], C[R], y[4] = {};
+        // one position after the other, its numbers read from LDS during the one before.  (Left to itself the compiler spreads the
+        // eight over each other, in all registers there are.)
+        struct Position {
+            T x, d, z, dy;
+            float B[R], C[R];
+        };
+        const auto read = [&](int j) {
+            Position p = {};
+            p.x = tile[0][j * 64 + lane];
+            p.d = tile[1][j * 64 + lane];
+            if (ALL) p.z = tile[ALL ? 2 : 0][j * 64 + lane];
+            if (ENDS) p.dy = tile[ALL ? 3 : 0][j * 64 + lane];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                B[r] = SeqElem<T>::get(cB[r][j]);
-                if (ALL) C[r] = SeqElem<T>::get(cC[r][j]);
+                p.B[r] = bc[0][j * SP + lane % BL + 16 * r];
+                if (ALL) p.C[r] = bc[ALL ? 1 : 0][j * SP + lane % BL + 16 * r];
             }
-            const auto gate = [&] {
-                const float z = SeqElem<T>::get(tile[ALL ? 2 : 0][j * 64 + lane]);
-                return z * seq_sigmoid(z);
-            };
-            if constexpr (ENDS) {
-                float dy = SeqElem<T>::get(tile[3][j * 64 + lane]);
-                if (a.z) dy *= gate();
-                seq_step_ends<0, SP>(h, gr, P, A, d, d * x, dy, B, C);
-            } else
-                seq_step<0, SP, OUT>(h, A, d, d * x, B, C, y);
+            return p;
+        };
+        Position now = read(0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            Position next = {};
+            if (j < 7) next = read(j + 1);
+            const float x = SeqElem<T>::get(now.x), raw = SeqElem<T>::get(now.d) + bias, soft = seq_softplus(raw);
+            float d = a.softplus ? soft : raw;
+            if (l0 + j >= stop) d = 0;  // (what follows the end changes nothing: x, B, C and z are zero there)
+            float gate = 1;
+            if (ALL) {
+                const float z = SeqElem<T>::get(now.z), of_z = z * seq_sigmoid(z);
+                gate = a.z ? of_z : 1.0f;
+            }
+            float y[4] = {};
+            if constexpr (ENDS)
+                seq_step_ends<0, SP>(h, gr, P, A, d, d * x, SeqElem<T>::get(now.dy) * gate, now.B, now.C);
+            else
+                seq_step<0, SP, OUT>(h, A, d, d * x, now.B, now.C, y);
             sum_d += d;
             if (OUT) {
-                float o = fmaf(D, x, (y[0] + y[1]) + (y[2] + y[3]));
-                if (a.z) o *= gate();
+                const float o = fmaf(D, x, (y[0] + y[1]) + (y[2] + y[3])) * gate;
                 tile[OUT ? 3 : 0][j * 64 + lane] = SeqElem<T>::put(live ? o : 0.0f);
             }
+            now = next;
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (OUT) {
             __syncthreads();
@@ -239,24 +252,30 @@ __global__ __launch_bounds__(256) void seq_scan_join_kernel(const SeqScanArgs a)
     if (c >= a.Ch) return;
     const int slot = a.slots ? a.slots[n] : n;
     const float A = a.A[e] * kLog2e;
-    float h = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f;
-    float *hl = a.hl + (long long)n * a.chunks * state + e;
+    const float first = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f;
     const float *sd = a.sd + (long long)n * a.chunks * a.Cp + c;
-#pragma unroll 4
-    for (int k = 0; k < a.chunks; ++k) {
-        const float from_zero = hl[k * state];
-        hl[k * state] = h;
-        h = fmaf(seq_exp2(A * sd[(long long)k * a.Cp]), h, from_zero);
-    }
-    if (!a.gl) return;
-    float *gl = a.gl + (long long)n * a.chunks * state + e;
-    float g = 0;
-#pragma unroll 4
-    for (int k = a.chunks - 1; k >= 0; --k) {
-        const float own = gl[k * state];
-        gl[k * state] = g;
-        g = fmaf(seq_exp2(A * sd[(long long)k * a.Cp]), g, own);
-    }
+    // what a run adds and the sum of its d come 16 runs at a time, ahead of the chain that they go into
+    const auto chain = [&](float *ends, float h, bool back) {
+        ends += (long long)n * a.chunks * state + e;
+        for (int k0 = 0; k0 < a.chunks; k0 += 16) {
+            float own[16], d[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
+                const bool ok = k0 + i < a.chunks;
+                own[i] = ok ? ends[k * state] : 0.0f;
+                d[i] = ok ? sd[(long long)k * a.Cp] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
+                if (k0 + i < a.chunks) ends[k * state] = h;
+                h = fmaf(seq_exp2(A * d[i]), h, own[i]);
+            }
+        }
+    };
+    chain(a.hl, first, false);
+    if (a.gl) chain(a.gl, 0.0f, true);
 }
 
 // One new position: 64 channels a workgroup, its four waves taking every fourth state.

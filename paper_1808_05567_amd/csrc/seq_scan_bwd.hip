@@ -343,24 +343,15 @@ __global__ __launch_bounds__(256) void seq_scan_bc_kernel(const SeqScanArgs a)
     }
 }
 
-// dA, dD, ddt_bias: the runs' parts in order, 4 strands of them a result.
-__global__ __launch_bounds__(256) void seq_scan_params_kernel(const SeqScanArgs a)
+// dA, dD, ddt_bias: the runs' parts in order.
+__global__ __launch_bounds__(1024) void seq_scan_params_kernel(const SeqScanArgs a)
 {
-    __shared__ float lds[256];
-    const long long state = (long long)a.S * a.Cp, col = (long long)blockIdx.x * 64 + threadIdx.x % 64;
-    const int strand = threadIdx.x / 64, runs = a.N * a.chunks;
+    const long long state = (long long)a.S * a.Cp, col = (long long)blockIdx.x * kSumColumns + threadIdx.x % kSumColumns;
     const bool of_A = col < state;
-    const long long e = of_A ? col : col - state;
-    const bool ok = e < (of_A ? state : 2LL * a.Cp) && e % a.Cp < a.Ch;
-    const float *p = of_A ? a.hl + e : a.vec + e;
-    const long long pitch = of_A ? state : 2LL * a.Cp;
-    float s = 0;
-    if (ok)
-        for (int k = strand; k < runs; k += 4) s += p[k * pitch];
-    lds[threadIdx.x] = s;
-    __syncthreads();
-    if (strand != 0 || e >= (of_A ? state : 2LL * a.Cp)) return;
-    s = (lds[threadIdx.x] + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
+    const long long e = of_A ? col : col - state, pitch = of_A ? state : 2LL * a.Cp;
+    // (results of channels beyond the last one are zero)
+    const float s = seq_sum_parts((of_A ? a.hl : a.vec) + e, pitch, a.N * a.chunks, e < pitch && e % a.Cp < a.Ch);
+    if (threadIdx.x >= kSumColumns || e >= pitch) return;
     float *out = of_A ? a.dA + e : e < a.Cp ? (a.dD ? a.dD + e : nullptr) : a.ddt_bias ? a.ddt_bias + (e - a.Cp) : nullptr;
     if (out) *out = s;
 }
@@ -375,7 +366,7 @@ hipError_t launch(int dtype, const SeqScanArgs &a, hipStream_t s)
     seq_scan_bwd_kernel<T, SP><<<(unsigned)((long long)a.N * a.G * a.btiles * a.chunks), 64, 0, s>>>(a);
     const long long results = ((long long)a.N * a.L * 2 * (a.G * a.S + 7) + 255) / 256;
     seq_scan_bc_kernel<T><<<(unsigned)(results < (1 << 20) ? results : 1 << 20), 256, 0, s>>>(a);
-    seq_scan_params_kernel<<<(unsigned)(((a.S + 2LL) * a.Cp + 63) / 64), 256, 0, s>>>(a);
+    seq_scan_params_kernel<<<(unsigned)(((a.S + 2LL) * a.Cp + kSumColumns - 1) / kSumColumns), 1024, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T>
