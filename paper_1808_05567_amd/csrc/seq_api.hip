@@ -248,8 +248,10 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     b = a;
     b.chunk = kSeqBwdChunk;
     b.chunks = (int)((b.L + (int64_t)b.chunk - 1) / b.chunk);
-    b.btiles = (b.CG + seq_scan_bwd_channels(seq_scan_states(b.S)) - 1) / seq_scan_bwd_channels(seq_scan_states(b.S));
-    p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
+    const int share = seq_scan_bwd_channels(seq_scan_states(b.S)) * kSeqBwdWaves;
+    b.btiles = (b.CG + share - 1) / share;
+    p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * kSeqMarks * state) +
+                up((size_t)b.N * b.chunks * kSeqMarks * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
                 up((size_t)b.N * b.L * b.G * b.btiles * 2 * b.S * 4);
     const int64_t grid = std::max(waves * std::max(a.chunks, b.chunks), (int64_t)b.N * b.G * b.btiles * b.chunks);
     const bool fits = grid <= kMaxGrid && (int64_t)a.N * a.S * a.Cp <= kMaxGrid * 256 && (int64_t)b.N * b.chunks <= kMaxGrid;
@@ -330,6 +332,8 @@ conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const 
     a.hl = take(runs * a.S * a.Cp);
     a.sd = take(runs * a.Cp);
     a.gl = take(runs * a.S * a.Cp);
+    a.marks = take(runs * kSeqMarks * a.S * a.Cp);
+    a.md = take(runs * kSeqMarks * a.Cp);
     a.vec = take(runs * 2 * a.Cp);
     a.bc = reinterpret_cast<float *>(at);
     return done(launch_seq_scan_bwd(h->dtype, a, (hipStream_t)stream));

@@ -11,6 +11,7 @@ namespace convmi {
 
 typedef unsigned seq_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned seq_u32x2 __attribute__((ext_vector_type(2)));
+typedef float seq_f32x2 __attribute__((ext_vector_type(2)));
 typedef float seq_f32x4 __attribute__((ext_vector_type(4)));
 
 // A sequence tensor: element (n, c, l) lies n * .n + (c / V) * .c + l * .l + c % V elements behind the base.
@@ -45,9 +46,11 @@ struct SeqScanArgs {
     float *hl;          // [N][chunks][S][Cp]: state at the end of a chunk from zeros, then at its start
     float *gl;          // the same for the gradient, back to front
     float *sd;          // [N][chunks][Cp]: sum of d over a chunk
+    float *marks;       // [N][chunks][7][S][Cp]: state from zeros at the start of a chunk's second to eighth eight
+    float *md;          // [N][chunks][7][Cp]: sum of d up to there
     float *vec;         // [N][chunks][2][Cp]: partial dD, ddt_bias
     float *bc;          // [N][L][G * btiles][2][S]: partial dB, dC
-    int btiles;         // tiles of channels a group of the backward kernel
+    int btiles;         // workgroups' shares of a group's channels in the backward kernel
 };
 
 struct SeqNormArgs {
@@ -83,10 +86,13 @@ hipError_t launch_seq_mv4(int dtype, const SeqMv4Args &a, hipStream_t s);
 hipError_t launch_seq_mv4_quant(const SeqMv4Args &a, const float *w, void *wt, float *scale, hipStream_t s);
 hipError_t launch_seq_mv4_unquant(const SeqMv4Args &a, float *w, hipStream_t s);
 
-// States a scan kernel is built for; channels of a tile of the backward kernel, whose threads take 4 channels x 4 states.
+// States a scan kernel is built for; channels of a wave of the backward kernel, whose lanes take 2 channels x 4 states, and its waves,
+// which take tiles side by side.
 constexpr int seq_scan_states(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 64; }
-constexpr int seq_scan_bwd_channels(int SP) { return 1024 / SP; }
+constexpr int seq_scan_bwd_channels(int SP) { return 512 / SP; }
+constexpr int kSeqBwdWaves = 4;
 constexpr int kSeqBwdChunk = 64;  // positions of a run of the backward kernel
+constexpr int kSeqMarks = kSeqBwdChunk / 8 - 1;
 
 #ifdef __HIPCC__
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -189,6 +195,14 @@ static __device__ __forceinline__ float seq_softplus(float x)
     p = fmaf(p, u, 1.0f / 3);
     p = fmaf(p * u, t, t);
     return fmaf(2.0f, p, x != x ? x : fmaxf(x, 0.0f));
+}
+
+// Between writes and reads of LDS by lanes of one wave: its LDS operations are done in order, the compiler has to keep them so.
+static __device__ __forceinline__ void seq_wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // Sum of parts of one column in a fixed order: 32 strands of them, each in turn, then the strands pairwise.  1024 threads a

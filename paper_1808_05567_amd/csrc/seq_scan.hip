@@ -14,6 +14,8 @@
 namespace convmi {
 namespace {
 
+constexpr int kWaves = 4;  // a workgroup
+
 template <int SP>
 struct States {
     static constexpr int R = (SP + 15) / 16;  // registers that hold SP states of B or C, 16 lanes each
@@ -48,19 +50,25 @@ static __device__ __forceinline__ void seq_step_ends(float (&h)[SP], float (&g)[
 
 // MODE 0: the state a run ends in from zeros; 1: results (chunks == 1: the whole sequence); 2: the ends for the gradients.
 template <typename T, int SP, int MODE>
-__global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
+__global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs a)
 {
     constexpr int V = SeqElem<T>::V, R = States<SP>::R, CB = 64 / V, NV = CB * 8 / 64;
     constexpr bool OUT = MODE == 1, ENDS = MODE == 2, ALL = OUT || ENDS;
     constexpr int SG = ENDS ? SP : 1;
     constexpr int E = SP / 8, BL = SP < 16 ? SP : 16;  // elements of B of 8 positions a lane loads; lanes of a row that hold states
-    __shared__ float bc[ALL ? 2 : 1][8 * SP];
-    __shared__ __align__(16) T tile[ALL ? 4 : 2][8 * 64];  // x, dt, z, y (ENDS: dy) of 8 positions x 64 channels
-    const int lane = threadIdx.x;
-    int t = blockIdx.x;
-    const int chunk = t % a.chunks;
-    t /= a.chunks;
-    const int g = t % a.G, tl = t / a.G % a.tiles, n = t / a.G / a.tiles;
+    __shared__ float bcs[kWaves][ALL ? 2 : 1][8 * SP];
+    __shared__ __align__(16) T tiles[kWaves][ALL ? 4 : 2][8 * 64];  // x, dt, z, y (ENDS: dy) of 8 positions x 64 channels
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    auto &tile = tiles[wave];
+    auto &bc = bcs[wave];
+    // (waves share nothing: four a workgroup are one on each SIMD)
+    long long t = (long long)blockIdx.x * kWaves + wave;
+    const int tl = (int)(t % a.tiles);
+    t /= a.tiles;
+    const int g = (int)(t % a.G);
+    t /= a.G;
+    const int chunk = (int)(t % a.chunks), n = (int)(t / a.chunks);
+    if (n >= a.N) return;
     const int c0 = g * a.CG + tl * 64, c_end = min(c0 + 64, (g + 1) * a.CG);
     const int c = c0 + lane;
     const bool live = c < c_end;
@@ -150,7 +158,7 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
     float sum_d = 0;
     if (begin < stop) fetch(begin);
     for (int l0 = begin; l0 < stop; l0 += 8) {
-        __syncthreads();
+        seq_wave_sync();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             seq_store(tile[0] + to[i], nx[i]);
@@ -163,8 +171,15 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
             bc[0][lane + 64 * r] = SeqElem<T>::get(nB[r]);
             if (ALL) bc[ALL ? 1 : 0][lane + 64 * r] = SeqElem<T>::get(nC[r]);
         }
-        __syncthreads();
+        seq_wave_sync();
         if (l0 + 8 < stop) fetch(l0 + 8);
+        if (ENDS && l0 > begin && live) {
+            const long long m = ((long long)n * a.chunks + chunk) * kSeqMarks + (l0 - begin) / 8 - 1;
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < a.S) a.marks[(m * a.S + s) * a.Cp + c] = h[s];
+            a.md[m * a.Cp + c] = sum_d;
+        }
         // one position after the other, its numbers read from LDS during the one before.  (Left to itself the compiler spreads the
         // eight over each other, in all registers there are.)
         struct Position {
@@ -211,7 +226,7 @@ __global__ __launch_bounds__(64) void seq_scan_kernel(const SeqScanArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
         if (OUT) {
-            __syncthreads();
+            seq_wave_sync();
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (in[i] && l0 + ll[i] < end)
@@ -323,19 +338,19 @@ __global__ __launch_bounds__(256) void seq_scan_step_kernel(const SeqScanArgs a)
 template <typename T, int SP>
 hipError_t launch(const SeqScanArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((long long)a.N * a.G * a.tiles * a.chunks);
+    const unsigned grid = (unsigned)(((long long)a.N * a.G * a.tiles * a.chunks + kWaves - 1) / kWaves);
     if (a.chunks > 1) {
-        seq_scan_kernel<T, SP, 0><<<grid, 64, 0, s>>>(a);
+        seq_scan_kernel<T, SP, 0><<<grid, 64 * kWaves, 0, s>>>(a);
         seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
     }
-    seq_scan_kernel<T, SP, 1><<<grid, 64, 0, s>>>(a);
+    seq_scan_kernel<T, SP, 1><<<grid, 64 * kWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int SP>
 hipError_t launch_ends(const SeqScanArgs &a, hipStream_t s)
 {
-    seq_scan_kernel<T, SP, 2><<<(unsigned)((long long)a.N * a.G * a.tiles * a.chunks), 64, 0, s>>>(a);
-    seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
+    seq_scan_kernel<T, SP, 2><<<(unsigned)(((long long)a.N * a.G * a.tiles * a.chunks + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a);
+    if (a.chunks > 1) seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T>

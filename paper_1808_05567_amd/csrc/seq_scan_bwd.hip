@@ -4,13 +4,15 @@
 //   dd = sum_s (A t + g B x),   dA = sum d t,   t = g exp(d A) h[l-1]
 //
 // (dy that of y before the gate.)  The states are formed again rather than kept: positions go in runs of 64.  A first launch finds
-// what each run does to a state and to a gradient, a second puts these together, so that a run knows the state before it and the gradient
-// behind it.  A wave then goes through its run forwards, noting the state in LDS every 8 positions, and through these
-// eights from the back: forwards again with the 8 states in registers, then backwards.
+// what each run does to a state and to a gradient and notes the state it reaches every 8 positions, all from zeros; a second puts
+// the runs together, so that a run knows the state before it and the gradient behind it, and with the sum of d the state at each note:
+// that from zeros plus exp(A sum d) times the one before the run.  A wave then goes through the eights of its run from the back,
+// forwards with the 8 states in registers, then backwards.
 //
-// A thread takes 4 channels x 4 states: half of the sums over states and over channels stay inside it; those over states end in
-// a quad of lanes, those over channels in exchanges that halve what is left each time.
-// Some 20 operations and three exponentials a state and position: bound by the vector units.
+// A lane takes 2 channels x 4 states: the sums over states end in a quad of lanes, those over channels in exchanges that halve what
+// is left each time, then over the four waves of a workgroup in LDS.  (4 x 4 need fewer exchanges but more than 256 registers, and one
+// wave a SIMD gets an operation into the vector units every 6 clocks, two in turn every 4: 2 x 2048 positions of 2048 channels 214 us.)
+// Some 20 operations and two exponentials a state and position: bound by the vector units.
 #include "seq_internal.h"
 
 namespace convmi {
@@ -18,13 +20,7 @@ namespace {
 
 constexpr int kT = 8;  // positions held at a time
 
-// Which way an eight is staged for.
-struct Forward {
-    static constexpr bool value = false;
-};
-struct Back {
-    static constexpr bool value = true;
-};
+constexpr int kWaves = kSeqBwdWaves;
 
 // Sum over the NL lanes that hold the states of the same channels.
 template <int NL>
@@ -58,267 +54,338 @@ static __device__ __forceinline__ float sum_row(float x)
     return x;
 }
 
-template <typename T, int SP>
-__global__ __launch_bounds__(64) void seq_scan_bwd_kernel(const SeqScanArgs a)
+template <typename T, int SP, bool GATE>
+__global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqScanArgs a)
 {
-    constexpr int V = SeqElem<T>::V, NL = SP / 4, WC = seq_scan_bwd_channels(SP), NSUB = kSeqBwdChunk / kT;
-    constexpr int VEC = WC / V * kT, NV = (VEC + 63) / 64;
-    __shared__ __align__(16) float marks[NSUB - 1][4][64][4];  // the states at the start of eights 1 ... 7
-    // d, x, dy of the eight; once used, what the sums over states were: A t, g B, C h
-    __shared__ __align__(16) float sd[kT][WC], sx[kT][WC], sg[kT][WC];
-    __shared__ __align__(16) float sB[kT][SP], sC[kT][SP];
-    const int lane = threadIdx.x, sl = lane % NL, cl = lane / NL;
+    constexpr int V = SeqElem<T>::V, NL = SP / 4, WC = seq_scan_bwd_channels(SP);
+    constexpr int PT = WC / V >= 8 ? 8 : 16;  // positions staged at a time: a block of one for each lane, where B and C leave room for them
+    constexpr int VEC = WC / V * PT, NV = (VEC + 63) / 64, E = PT * SP / 64;
+    struct Lds {
+        // d, x, dy before the gate, what dz and ddt are multiplied with; the sums over states: A t, g B, C h
+        float d[PT][WC], x[PT][WC], dy[PT][WC], slope[PT][WC], At[PT][WC], gB[PT][WC];
+        float dgate[GATE ? PT : 1][WC], Ch[GATE ? PT : 1][WC];
+        float B[PT][SP], C[PT][SP];  // once a position is done with: dB, dC of the wave's channels
+    };
+    __shared__ __align__(16) Lds all[kWaves];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), sl = lane % NL, cl = lane / NL;
+    Lds &my = all[wave];
     int t = blockIdx.x;
-    const int chunk = t % a.chunks;
-    t /= a.chunks;
-    const int g = t % a.G, tl = t / a.G % a.btiles, n = t / a.G / a.btiles;
-    const int c0 = g * a.CG + tl * WC, c_end = min(c0 + WC, (g + 1) * a.CG);
+    const int share = t % a.btiles;
+    t /= a.btiles;
+    const int g = t % a.G;
+    t /= a.G;
+    const int chunk = t % a.chunks, n = t / a.chunks;
+    // (the last share's waves may have no channels: they go along for the barriers)
+    const int c0 = g * a.CG + (share * kWaves + wave) * WC, c_end = min(c0 + WC, (g + 1) * a.CG);
     const int len = seq_length(a.lengths, n, a.L);
     const int begin = chunk * kSeqBwdChunk, end = min(begin + kSeqBwdChunk, a.L), stop = min(end, len);
-    const int eights = stop > begin ? (stop - begin + kT - 1) / kT : 0;
 
-    // element-wise: block cbl, position ll of an eight
-    bool in[NV];
-    int ll[NV], cb[NV], to[NV];
-    float D[NV][V], bias[NV][V], aD[NV][V] = {}, ab[NV][V] = {};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int e = lane + 64 * i, cbl = e / kT;
-        ll[i] = e % kT;
-        in[i] = e < VEC && c0 + cbl * V < c_end;
-        cb[i] = c0 / V + (in[i] ? cbl : 0);
-        to[i] = e < VEC ? cbl * V : 0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) D[i][j] = bias[i][j] = 0;
-        if (a.D) seq_vector<V>(a.D, cb[i], D[i]);
-        if (a.dt_bias) seq_vector<V>(a.dt_bias, cb[i], bias[i]);
-    }
-    auto block = [&](const void *p, const SeqView &v, int i, int l) {
-        return seq_load(static_cast<const T *>(p) + n * v.n + cb[i] * v.c + l * v.l);
+    // element-wise: a lane's block and position of what is staged.  Formed anew each time, as its addresses are: kept, they cost registers.
+    struct Place {
+        bool in;
+        int cb, to, l;
     };
-    auto put = [&](void *p, const SeqView &v, int i, int l, const float (&f)[V]) {
-        seq_store(static_cast<T *>(p) + n * v.n + cb[i] * v.c + l * v.l, SeqElem<T>::pack(f));
+    auto place = [&](int i) {
+        int e = lane + 64 * i;
+        asm volatile("" : "+v"(e));
+        const int cbl = e / PT;
+        const bool in = e < VEC && c0 + cbl * V < c_end;
+        return Place{in, in ? c0 / V + cbl : 0, e < VEC ? cbl * V : 0, e % PT};
     };
+    auto block = [&](const void *p, const SeqView &v, const Place &at, int l) {
+        return seq_load(static_cast<const T *>(p) + n * v.n + at.cb * v.c + l * v.l);
+    };
+    auto put = [&](void *p, const SeqView &v, const Place &at, int l, const float (&f)[V]) {
+        seq_store(static_cast<T *>(p) + n * v.n + at.cb * v.c + l * v.l, SeqElem<T>::pack(f));
+    };
+    auto to_lds = [&](float *p, const float (&f)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) *reinterpret_cast<seq_f32x4 *>(p + j) = seq_f32x4{f[j], f[j + 1], f[j + 2], f[j + 3]};
+    };
+    auto from_lds = [&](const float *p, float (&f)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            const seq_f32x4 q = *reinterpret_cast<const seq_f32x4 *>(p + j);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[j + k] = q[k];
+        }
+    };
+    float aD[NV], ab[NV];  // sums of dy x and ddt over the run's positions of one channel: lane ll of eight's, ll < V
+#pragma unroll
+    for (int i = 0; i < NV; ++i) aD[i] = ab[i] = 0;
 
-    // scan-wise: channels c ... + 3, states s ... + 3
-    const int c = c0 + cl * 4, s = sl * 4;
+    // scan-wise: channels c, c + 1, states s ... + 3
+    const int c = c0 + cl * 2, s = sl * 4;
     const bool live = c < c_end;
-    const long long at = ((long long)n * a.chunks + chunk) * a.S * a.Cp + (live ? c : c0);
-    float A[4][4], h[4][4], carry[4][4], dA[4][4] = {};  // [state][channel]
+    const long long run = (long long)n * a.chunks + chunk, state = (long long)a.S * a.Cp;
+    // this lane's row j of a state.  States and channels that there are not read another's: with B, C, x, dy and the gradient from behind
+    // zero they add nothing, as long as their state is a number.
+    unsigned at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at[j] = (unsigned)(min(s + j, a.S - 1) * a.Cp + (live ? c : g * a.CG));
+    const bool there[2] = {live, c + 1 < c_end};
+    auto two = [&](const float *p, int j) { return *reinterpret_cast<const seq_f32x2 *>(p + at[j]); };
+    float A[4][2], carry[4][2], dA[4][2] = {};  // [state][channel]
+    seq_f32x2 before[4];                        // the state before the run
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        seq_f32x4 q = {}, p = {}, r = {};
-        if (live && s + j < a.S) {
-            q = *reinterpret_cast<const seq_f32x4 *>(a.A + (long long)(s + j) * a.Cp + c);
-            if (a.chunks > 1) {
-                p = *reinterpret_cast<const seq_f32x4 *>(a.hl + at + (long long)(s + j) * a.Cp);
-                r = *reinterpret_cast<const seq_f32x4 *>(a.gl + at + (long long)(s + j) * a.Cp);
-            }
+        const seq_f32x2 q = two(a.A, j);
+        seq_f32x2 r = {};
+        before[j] = seq_f32x2{};
+        if (a.chunks > 1) {
+            r = two(a.gl + run * state, j);
+            before[j] = two(a.hl + run * state, j);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            // (channels beyond the last one take no part, whatever their parameters hold)
-            const bool ok = c + i < c_end;
-            A[j][i] = ok ? q[i] * kLog2e : 0.0f;
-            h[j][i] = ok ? p[i] : 0.0f;
-            carry[j][i] = ok ? r[i] : 0.0f;
+        for (int i = 0; i < 2; ++i) {
+            A[j][i] = there[i] ? q[i] * kLog2e : 0.0f;
+            carry[j][i] = there[i] && s + j < a.S ? r[i] : 0.0f;
         }
     }
 
-    float kx[NV][V], kd[NV][V], ksig[NV][V], kg[NV][V], kz[NV][V];
-    // loads the eight at l0 and puts it in LDS; BACK: with all that the way back needs
-    auto stage = [&](int l0, auto back) {
-        constexpr bool BACK = decltype(back)::value;
-        __syncthreads();
+    // what is needed next from memory, on its way meanwhile: positions to stage, the note at the start of an eight
+    seq_u32x4 nx[NV], nd[NV], ng[NV], nz[NV];
+    T nB[E], nC[E];
+    auto fetch = [&](int l0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int l = l0 + ll[i];
-#pragma unroll
-            for (int j = 0; j < V; ++j) kx[i][j] = kd[i][j] = ksig[i][j] = kg[i][j] = kz[i][j] = 0;
-            if (in[i] && l < stop) {
-                float raw[V], gate[V], z[V];
-                SeqElem<T>::unpack(block(a.x, a.vx, i, l), kx[i]);
-                SeqElem<T>::unpack(block(a.dt, a.vdt, i, l), raw);
-                if (BACK) {
-                    SeqElem<T>::unpack(block(a.dy, a.vdy, i, l), kg[i]);
-                    if (a.z) SeqElem<T>::unpack(block(a.z, a.vz, i, l), z);
-                }
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float r = raw[j] + bias[i][j];
-                    kd[i][j] = a.softplus ? seq_softplus(r) : r;
-                    if (BACK) {
-                        ksig[i][j] = a.softplus ? seq_sigmoid(r) : 1.0f;
-                        if (a.z) {
-                            const float p = seq_sigmoid(z[j]);
-                            kz[i][j] = kg[i][j] * p * (1.0f + z[j] * (1.0f - p));
-                            kg[i][j] *= z[j] * p;
-                        }
-                    }
-                    if (cb[i] * V + j >= a.Ch) kx[i][j] = kd[i][j] = kg[i][j] = kz[i][j] = 0;
-                }
+            const Place p = place(i);
+            const int l = l0 + p.l;
+            nx[i] = nd[i] = ng[i] = nz[i] = seq_u32x4{};
+            if (p.in && l < stop) {
+                nx[i] = block(a.x, a.vx, p, l);
+                nd[i] = block(a.dt, a.vdt, p, l);
+                ng[i] = block(a.dy, a.vdy, p, l);
+                if (GATE) nz[i] = block(a.z, a.vz, p, l);
             }
-            if (lane + 64 * i < VEC)
-#pragma unroll
-                for (int j = 0; j < V; j += 4) {
-                    *reinterpret_cast<seq_f32x4 *>(&sd[ll[i]][to[i] + j]) = seq_f32x4{kd[i][j], kd[i][j + 1], kd[i][j + 2], kd[i][j + 3]};
-                    *reinterpret_cast<seq_f32x4 *>(&sx[ll[i]][to[i] + j]) = seq_f32x4{kx[i][j], kx[i][j + 1], kx[i][j + 2], kx[i][j + 3]};
-                    if (BACK) *reinterpret_cast<seq_f32x4 *>(&sg[ll[i]][to[i] + j]) = seq_f32x4{kg[i][j], kg[i][j + 1], kg[i][j + 2], kg[i][j + 3]};
-                }
         }
 #pragma unroll
-        for (int i = lane; i < kT * SP; i += 64) {
-            const int l = l0 + i / SP, st = i % SP, e = g * a.S + st;
-            const bool ok = l < stop && st < a.S;
-            sB[i / SP][st] = ok ? SeqElem<T>::get(static_cast<const T *>(a.B)[n * a.vB.n + e / V * a.vB.c + l * a.vB.l + e % V]) : 0.0f;
-            if (BACK) sC[i / SP][st] = ok ? SeqElem<T>::get(static_cast<const T *>(a.C)[n * a.vC.n + e / V * a.vC.c + l * a.vC.l + e % V]) : 0.0f;
+        for (int r = 0; r < E; ++r) {
+            int q = lane + 64 * r;
+            asm volatile("" : "+v"(q));
+            const int l = l0 + q / SP, st = q % SP, e = g * a.S + st;
+            nB[r] = nC[r] = T(0);
+            if (l < stop && st < a.S) {
+                nB[r] = static_cast<const T *>(a.B)[n * a.vB.n + e / V * a.vB.c + l * a.vB.l + e % V];
+                nC[r] = static_cast<const T *>(a.C)[n * a.vC.n + e / V * a.vC.c + l * a.vC.l + e % V];
+            }
         }
-        __syncthreads();
     };
-    for (int e = 0; e + 1 < eights; ++e) {
-        stage(begin + e * kT, Forward());
+    seq_f32x2 note[4], note_d = {};
+    auto fetch_note = [&](int e) {
+        const long long m = run * kSeqMarks + e - 1;
+        note_d = *reinterpret_cast<const seq_f32x2 *>(a.md + m * a.Cp + (live ? c : g * a.CG));
 #pragma unroll
-        for (int l = 0; l < kT; ++l) {
-            const seq_f32x4 d = *reinterpret_cast<const seq_f32x4 *>(&sd[l][cl * 4]), x = *reinterpret_cast<const seq_f32x4 *>(&sx[l][cl * 4]);
-            const seq_f32x4 B = *reinterpret_cast<const seq_f32x4 *>(&sB[l][s]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float dx = d[i] * x[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j][i] = fmaf(seq_exp2(d[i] * A[j][i]), h[j][i], B[j] * dx);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<seq_f32x4 *>(marks[e][j][lane]) = seq_f32x4{h[j][0], h[j][1], h[j][2], h[j][3]};
-    }
+        for (int j = 0; j < 4; ++j) note[j] = two(a.marks + m * state, j);
+    };
+    const int eights = stop > begin ? (stop - begin + kT - 1) / kT : 0;
+    const int stages = stop > begin ? (stop - begin + PT - 1) / PT : 0;
+    if (stages > 0) fetch(begin + (stages - 1) * PT);
+    if (eights > 1) fetch_note(eights - 1);
 
-    for (int e = eights - 1; e >= 0; --e) {
-        const int l0 = begin + e * kT;
-        stage(l0, Back());
-        float hs[kT + 1][4][4], as[kT][4][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            seq_f32x4 p = {};
-            if (e > 0)
-                p = *reinterpret_cast<const seq_f32x4 *>(marks[e - 1][j][lane]);
-            else if (live && s + j < a.S && a.chunks > 1)
-                p = *reinterpret_cast<const seq_f32x4 *>(a.hl + at + (long long)(s + j) * a.Cp);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) hs[0][j][i] = c + i < c_end ? p[i] : 0.0f;
-        }
-#pragma unroll
-        for (int l = 0; l < kT; ++l) {
-            const seq_f32x4 d = *reinterpret_cast<const seq_f32x4 *>(&sd[l][cl * 4]), x = *reinterpret_cast<const seq_f32x4 *>(&sx[l][cl * 4]);
-            const seq_f32x4 B = *reinterpret_cast<const seq_f32x4 *>(&sB[l][s]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float dx = d[i] * x[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    as[l][j][i] = seq_exp2(d[i] * A[j][i]);
-                    hs[l + 1][j][i] = fmaf(as[l][j][i], hs[l][j][i], B[j] * dx);
-                }
-            }
-        }
-#pragma unroll
-        for (int l = kT - 1; l >= 0; --l) {
-            const seq_f32x4 d = *reinterpret_cast<const seq_f32x4 *>(&sd[l][cl * 4]), x = *reinterpret_cast<const seq_f32x4 *>(&sx[l][cl * 4]);
-            const seq_f32x4 dy = *reinterpret_cast<const seq_f32x4 *>(&sg[l][cl * 4]);
-            const seq_f32x4 B = *reinterpret_cast<const seq_f32x4 *>(&sB[l][s]), C = *reinterpret_cast<const seq_f32x4 *>(&sC[l][s]);
-            float bc[8] = {};  // dB, dC of the four states
-            seq_f32x4 gB = {}, At = {}, Ch = {};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float dx = d[i] * x[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float gr = fmaf(dy[i], C[j], carry[j][i]);
-                    bc[4 + j] = fmaf(dy[i], hs[l + 1][j][i], bc[4 + j]);
-                    bc[j] = fmaf(gr, dx, bc[j]);
-                    gB[i] = fmaf(gr, B[j], gB[i]);
-                    Ch[i] = fmaf(C[j], hs[l + 1][j][i], Ch[i]);
-                    carry[j][i] = gr * as[l][j][i];
-                    const float th = carry[j][i] * hs[l][j][i];
-                    dA[j][i] = fmaf(th, d[i], dA[j][i]);
-                    At[i] = fmaf(th, A[j][i], At[i]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                gB[i] = sum_states<NL>(gB[i]);
-                At[i] = sum_states<NL>(At[i]);
-                if (a.z) Ch[i] = sum_states<NL>(Ch[i]);
-            }
-            if (sl == 0) {
-                *reinterpret_cast<seq_f32x4 *>(&sd[l][cl * 4]) = At;
-                *reinterpret_cast<seq_f32x4 *>(&sx[l][cl * 4]) = gB;
-                if (a.z) *reinterpret_cast<seq_f32x4 *>(&sg[l][cl * 4]) = Ch;
-            }
-            float u[4], v[2];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = swap32(bc[j], bc[j + 4]);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) v[j] = sum_row<NL>(swap16(u[j], u[j + 2]));
-            // the lower half of the wave has dB, the upper one dC; even rows states s, s + 1, odd ones s + 2, s + 3
-            if (lane % 16 < NL && l0 + l < stop) {
-                const int st = lane % 16 * 4 + lane / 16 % 2 * 2;
-                float *bp = a.bc + (((long long)n * a.L + l0 + l) * (a.G * a.btiles) + g * a.btiles + tl) * 2 * a.S + lane / 32 * a.S + st;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (st + j < a.S) bp[j] = v[j];
-            }
-        }
-        __syncthreads();
+    for (int stage = stages - 1; stage >= 0; --stage) {
+        const int p0 = begin + stage * PT;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int l = l0 + ll[i];
-            if (!in[i] || l >= end) continue;
-            float dx[V], ddt[V], dz[V];
+            const Place p = place(i);
+            float x[V], d[V], slope[V], dy[V], dgate[V], z[V], bias[V] = {};
+            SeqElem<T>::unpack(nx[i], x);
+            SeqElem<T>::unpack(nd[i], d);
+            SeqElem<T>::unpack(ng[i], dy);
+            SeqElem<T>::unpack(nz[i], z);
+            if (a.dt_bias) seq_vector<V>(a.dt_bias, p.cb, bias);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float At = sd[ll[i]][to[i] + j], gB = sx[ll[i]][to[i] + j];
-                dx[j] = fmaf(D[i][j], kg[i][j], kd[i][j] * gB);
-                ddt[j] = fmaf(kLn2, At, kx[i][j] * gB) * ksig[i][j];
-                if (a.z) dz[j] = kz[i][j] * fmaf(D[i][j], kx[i][j], sg[ll[i]][to[i] + j]);
-                if (cb[i] * V + j >= a.Ch) ddt[j] = dx[j] = dz[j] = 0;
-                aD[i][j] = fmaf(kg[i][j], kx[i][j], aD[i][j]);
-                ab[i][j] += ddt[j];
+                const bool ok = p.in && p0 + p.l < stop && p.cb * V + j < a.Ch;
+                const float raw = d[j] + bias[j], soft = seq_softplus(raw), sig = seq_sigmoid(raw);
+                d[j] = ok ? a.softplus ? soft : raw : 0.0f;
+                slope[j] = ok ? a.softplus ? sig : 1.0f : 0.0f;
+                x[j] = ok ? x[j] : 0.0f;
+                dy[j] = ok ? dy[j] : 0.0f;
+                if (GATE) {
+                    const float q = seq_sigmoid(z[j]);
+                    dgate[j] = ok ? dy[j] * q * (1.0f + z[j] * (1.0f - q)) : 0.0f;
+                    dy[j] = ok ? dy[j] * (z[j] * q) : 0.0f;
+                }
             }
-            put(a.dx, a.vdx, i, l, dx);
-            put(a.ddt, a.vddt, i, l, ddt);
-            if (a.z) put(a.dz, a.vdz, i, l, dz);
+            if (lane + 64 * i < VEC) {
+                to_lds(&my.d[p.l][p.to], d);
+                to_lds(&my.x[p.l][p.to], x);
+                to_lds(&my.dy[p.l][p.to], dy);
+                to_lds(&my.slope[p.l][p.to], slope);
+                if (GATE) to_lds(&my.dgate[GATE ? p.l : 0][p.to], dgate);
+            }
         }
+#pragma unroll
+        for (int r = 0; r < E; ++r) {
+            (&my.B[0][0])[lane + 64 * r] = SeqElem<T>::get(nB[r]);
+            (&my.C[0][0])[lane + 64 * r] = SeqElem<T>::get(nC[r]);
+        }
+        seq_wave_sync();
+        if (stage > 0) fetch(p0 - PT);
+        auto row = [&](const float (&p)[WC]) { return *reinterpret_cast<const seq_f32x2 *>(&p[cl * 2]); };
+        auto states = [&](const float (&p)[SP]) { return *reinterpret_cast<const seq_f32x4 *>(&p[s]); };
+
+#pragma unroll 1
+        for (int first = PT - kT; first >= 0; first -= kT) {
+            if (p0 + first >= stop) continue;
+            const int e = (p0 + first - begin) / kT;
+            float hs[kT + 1][4][2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float h = e > 0 ? fmaf(seq_exp2(A[j][i] * note_d[i]), before[j][i], note[j][i]) : before[j][i];
+                    hs[0][j][i] = there[i] ? h : 0.0f;
+                }
+            if (e > 1) fetch_note(e - 1);
+#pragma unroll
+            for (int q = 0; q < kT; ++q) {
+                const int l = first + q;
+                const seq_f32x2 d = row(my.d[l]), x = row(my.x[l]);
+                const seq_f32x4 B = states(my.B[l]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float dx = d[i] * x[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) hs[q + 1][j][i] = fmaf(seq_exp2(d[i] * A[j][i]), hs[q][j][i], B[j] * dx);
+                }
+            }
+            // (else the compiler keeps the decays and the eight's numbers from the way forwards, in registers that there are not)
+            seq_wave_sync();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(A[j][i]));
+#pragma unroll
+            for (int q = kT - 1; q >= 0; --q) {
+                const int l = first + q;
+                const seq_f32x2 d = row(my.d[l]), x = row(my.x[l]), dy = row(my.dy[l]);
+                const seq_f32x4 B = states(my.B[l]), C = states(my.C[l]);
+                float bc[8] = {};  // dB, dC of the four states
+                seq_f32x2 gB = {}, At = {}, Ch = {};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float dx = d[i] * x[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float gr = fmaf(dy[i], C[j], carry[j][i]);
+                        bc[4 + j] = fmaf(dy[i], hs[q + 1][j][i], bc[4 + j]);
+                        bc[j] = fmaf(gr, dx, bc[j]);
+                        gB[i] = fmaf(gr, B[j], gB[i]);
+                        if (GATE) Ch[i] = fmaf(C[j], hs[q + 1][j][i], Ch[i]);
+                        carry[j][i] = gr * seq_exp2(d[i] * A[j][i]);
+                        const float th = carry[j][i] * hs[q][j][i];
+                        dA[j][i] = fmaf(th, d[i], dA[j][i]);
+                        At[i] = fmaf(th, A[j][i], At[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    gB[i] = sum_states<NL>(gB[i]);
+                    At[i] = sum_states<NL>(At[i]);
+                    if (GATE) Ch[i] = sum_states<NL>(Ch[i]);
+                }
+                if (sl == 0) {
+                    *reinterpret_cast<seq_f32x2 *>(&my.At[l][cl * 2]) = At;
+                    *reinterpret_cast<seq_f32x2 *>(&my.gB[l][cl * 2]) = gB;
+                    if (GATE) *reinterpret_cast<seq_f32x2 *>(&my.Ch[GATE ? l : 0][cl * 2]) = Ch;
+                }
+                float u[4], v[2];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[j] = swap32(bc[j], bc[j + 4]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) v[j] = sum_row<NL>(swap16(u[j], u[j + 2]));
+                // the lower half of the wave has dB, the upper one dC; even rows states s, s + 1, odd ones s + 2, s + 3
+                if (lane % 16 < NL) *reinterpret_cast<seq_f32x2 *>((lane < 32 ? my.B[l] : my.C[l]) + lane % 16 * 4 + lane / 16 % 2 * 2) = seq_f32x2{v[0], v[1]};
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        seq_wave_sync();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const Place p = place(i);
+            const int l = p0 + p.l;
+            const bool inside = l < stop, store = p.in && l < end;
+            float d[V], x[V], dy[V], slope[V], At[V], gB[V], dx[V], ddt[V], D[V] = {};
+            from_lds(&my.d[p.l][p.to], d);
+            from_lds(&my.x[p.l][p.to], x);
+            from_lds(&my.dy[p.l][p.to], dy);
+            from_lds(&my.slope[p.l][p.to], slope);
+            from_lds(&my.At[p.l][p.to], At);
+            from_lds(&my.gB[p.l][p.to], gB);
+            if (a.D) seq_vector<V>(a.D, p.cb, D);
+            float pD[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                // (past the end nothing has been summed; D of channels beyond the last one may be anything)
+                const bool ok = inside && p.cb * V + j < a.Ch;
+                dx[j] = ok ? fmaf(d[j], gB[j], D[j] * dy[j]) : 0.0f;
+                ddt[j] = ok ? fmaf(kLn2, At[j], x[j] * gB[j]) * slope[j] : 0.0f;
+                pD[j] = dy[j] * x[j];
+            }
+            if (store) {
+                put(a.dx, a.vdx, p, l, dx);
+                put(a.ddt, a.vddt, p, l, ddt);
+            }
+            if (GATE) {
+                float dgate[V], Ch[V];
+                from_lds(&my.dgate[GATE ? p.l : 0][p.to], dgate);
+                from_lds(&my.Ch[GATE ? p.l : 0][p.to], Ch);
+#pragma unroll
+                for (int j = 0; j < V; ++j) dgate[j] = inside && p.cb * V + j < a.Ch ? dgate[j] * fmaf(D[j], x[j], Ch[j]) : 0.0f;
+                if (store) put(a.dz, a.vdz, p, l, dgate);
+            }
+            // lane ll of eight keeps the sums of the block's channel ll
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float u = sum_states<8>(pD[j]), w = sum_states<8>(ddt[j]);
+                aD[i] += lane % 8 == j ? u : 0.0f;
+                ab[i] += lane % 8 == j ? w : 0.0f;
+            }
+        }
+        // dB and dC of the workgroup's channels
+        __syncthreads();
+        for (int i = threadIdx.x; i < PT * 2 * SP; i += 64 * kWaves) {
+            const int l = i / (2 * SP), which = i / SP % 2, st = i % SP;
+            if (p0 + l >= stop || st >= a.S) continue;
+            float sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += which ? all[w].C[l][st] : all[w].B[l][st];
+            a.bc[((((long long)n * a.L + p0 + l) * a.G + g) * a.btiles + share) * 2 * a.S + which * a.S + st] = sum;
+        }
+        __syncthreads();
     }
     // zeros past the end
     const float zero[V] = {};
-    for (int l0 = begin + eights * kT; l0 < end; l0 += kT)
+    for (int l0 = begin + stages * PT; l0 < end; l0 += PT)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (!in[i] || l0 + ll[i] >= end) continue;
-            put(a.dx, a.vdx, i, l0 + ll[i], zero);
-            put(a.ddt, a.vddt, i, l0 + ll[i], zero);
-            if (a.z) put(a.dz, a.vdz, i, l0 + ll[i], zero);
+            const Place p = place(i);
+            const int l = l0 + p.l;
+            if (!p.in || l >= end) continue;
+            put(a.dx, a.vdx, p, l, zero);
+            put(a.ddt, a.vddt, p, l, zero);
+            if (GATE) put(a.dz, a.vdz, p, l, zero);
         }
     // this run's part of the parameters' gradients; that of A where its state was
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (live && s + j < a.S) *reinterpret_cast<seq_f32x4 *>(a.hl + at + (long long)(s + j) * a.Cp) = seq_f32x4{dA[j][0], dA[j][1], dA[j][2], dA[j][3]};
+        if (live && s + j < a.S) *reinterpret_cast<seq_f32x2 *>(a.hl + run * state + at[j]) = seq_f32x2{dA[j][0], dA[j][1]};
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float p = aD[i][j], q = ab[i][j];
-#pragma unroll
-            for (int d = 1; d < kT; d *= 2) {
-                p += __shfl_xor(p, d);
-                q += __shfl_xor(q, d);
-            }
-            if (in[i] && ll[i] == 0) {
-                float *v = a.vec + ((long long)n * a.chunks + chunk) * 2 * a.Cp + cb[i] * V + j;
-                v[0] = p;
-                v[a.Cp] = q;
-            }
+    for (int i = 0; i < NV; ++i) {
+        const Place p = place(i);
+        float u = aD[i], w = ab[i];
+        if (PT == 16) {  // (the other eight of the positions)
+            u += __shfl_xor(u, 8);
+            w += __shfl_xor(w, 8);
         }
+        if (p.in && p.l < V) {
+            float *v = a.vec + run * 2 * a.Cp + p.cb * V + p.l;
+            v[0] = u;
+            v[a.Cp] = w;
+        }
+    }
 }
 
 // dB and dC: the tiles' parts of a position in order; one thread a result.
@@ -336,7 +403,15 @@ __global__ __launch_bounds__(256) void seq_scan_bc_kernel(const SeqScanArgs a)
         if (e < a.G * a.S && l < seq_length(a.lengths, n, a.L)) {
             const int g = e / a.S, s = e % a.S;
             const float *p = a.bc + ((row * a.G + g) * a.btiles * 2 + which) * a.S + s;
-            for (int k = 0; k < a.btiles; ++k) sum += p[(long long)k * 2 * a.S];
+            int k = 0;
+            for (; k + 8 <= a.btiles; k += 8) {
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = p[(long long)(k + i) * 2 * a.S];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += f[i];
+            }
+            for (; k < a.btiles; ++k) sum += p[(long long)k * 2 * a.S];
         }
         const SeqView &v = which ? a.vdC : a.vdB;
         static_cast<T *>(which ? a.dC : a.dB)[n * v.n + e / V * v.c + l * v.l + e % V] = SeqElem<T>::put(sum);
@@ -359,11 +434,15 @@ __global__ __launch_bounds__(1024) void seq_scan_params_kernel(const SeqScanArgs
 template <typename T, int SP>
 hipError_t launch(int dtype, const SeqScanArgs &a, hipStream_t s)
 {
-    if (a.chunks > 1) {
+    if (a.L > kT) {
         const hipError_t e = launch_seq_scan_ends(dtype, a, s);
         if (e != hipSuccess) return e;
     }
-    seq_scan_bwd_kernel<T, SP><<<(unsigned)((long long)a.N * a.G * a.btiles * a.chunks), 64, 0, s>>>(a);
+    const unsigned grid = (unsigned)((long long)a.N * a.G * a.btiles * a.chunks);
+    if (a.z)
+        seq_scan_bwd_kernel<T, SP, true><<<grid, 64 * kWaves, 0, s>>>(a);
+    else
+        seq_scan_bwd_kernel<T, SP, false><<<grid, 64 * kWaves, 0, s>>>(a);
     const long long results = ((long long)a.N * a.L * 2 * (a.G * a.S + 7) + 255) / 256;
     seq_scan_bc_kernel<T><<<(unsigned)(results < (1 << 20) ? results : 1 << 20), 256, 0, s>>>(a);
     seq_scan_params_kernel<<<(unsigned)(((a.S + 2LL) * a.Cp + kSumColumns - 1) / kSumColumns), 1024, 0, s>>>(a);
