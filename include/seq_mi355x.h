@@ -110,7 +110,8 @@ conv_status_t seq_conv_bwd(seq_handle_t h, const void *x, const float *w, const 
  * A: fp32 [S][Cp]; D, dt_bias: fp32 vectors or NULL (zero); B and C: sequence tensors of G*S
  * channels; z: sequence tensor or NULL; state: fp32 [slots][S][Cp].
  * Errors of create: as seq_conv_create; CONV_EINVAL where G does not divide C, CONV_EUNSUPPORTED
- * where G > 1 and C/G is no multiple of v, and for S > 64 or G*S > 2^16. */
+ * where G > 1 and C/G is no multiple of v, for S > 64 or G*S > 2^16, and for blocks or positions of
+ * a view more than 2^24 elements apart. */
 typedef struct {
     int32_t N, C, L, S, G;
     int32_t softplus, slots, dtype;

@@ -26,7 +26,7 @@ struct seq_plan {
 
 namespace {
 
-constexpr int64_t kMaxElements = 1LL << 39, kMaxGrid = (1LL << 31) - 1, kMaxStride = 1LL << 40;
+constexpr int64_t kMaxElements = 1LL << 39, kMaxGrid = (1LL << 31) - 1, kMaxStride = 1LL << 40, kMaxTileStride = 1LL << 24;
 
 bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -230,8 +230,11 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     } views[] = {{d->x, Cb, false, a.vx},   {d->dt, Cb, false, a.vdt}, {d->B, Sb, false, a.vB},    {d->C_, Sb, false, a.vC},
                  {d->z, Cb, false, a.vz},   {d->y, Cb, true, a.vy},    {d->dy, Cb, false, a.vdy},  {d->dx, Cb, true, a.vdx},
                  {d->ddt, Cb, true, a.vddt}, {d->dB, Sb, true, a.vdB},  {d->dC, Sb, true, a.vdC},   {d->dz, Cb, true, a.vdz}};
-    for (const auto &w : views)
+    for (const auto &w : views) {
         if (!view_of(w.v, a.N, w.blocks, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
+        // (a tile's elements are reached from its first one by 32 bits)
+        if (w.to.c > kMaxTileStride || w.to.l > kMaxTileStride) return finish(p, CONV_EUNSUPPORTED, out);
+    }
 
     // Forward: the sequence whole where the channels alone give every SIMD (1024) a wave, else in runs that make two.
     a.tiles = (a.CG + 63) / 64;

@@ -21,34 +21,62 @@ struct States {
     static constexpr int R = (SP + 15) / 16;  // registers that hold SP states of B or C, 16 lanes each
 };
 
-template <int I, int SP, bool OUT>
-static __device__ __forceinline__ void seq_step(float (&h)[SP], const float (&A)[SP], float d, float dx, const float (&B)[States<SP>::R],
-                                                const float (&C)[States<SP>::R], float (&y)[4])
+// One position of states 16 Q ... + 15.  In steps whose operations do not wait for each other, held apart: left to itself the compiler
+// puts each exponential right before its use, and a wave waits for every one.
+template <int I, int N>
+static __device__ __forceinline__ void seq_spread(float B, float dx, float (&to)[16])
 {
-    if constexpr (I < SP) {
-        const float a = seq_exp2(d * A[I]);
-        h[I] = fmaf(a, h[I], seq_row_lane<I % 16>(B[I / 16]) * dx);
-        if constexpr (OUT) y[I % 4] = fmaf(seq_row_lane<I % 16>(C[I / 16]), h[I], y[I % 4]);
-        seq_step<I + 1, SP, OUT>(h, A, d, dx, B, C, y);
+    if constexpr (I < N) {
+        to[I] = seq_row_lane<I>(B) * dx;
+        seq_spread<I + 1, N>(B, dx, to);
+    }
+}
+template <int I, int N>
+static __device__ __forceinline__ void seq_spread(float C, float (&to)[16])
+{
+    if constexpr (I < N) {
+        to[I] = seq_row_lane<I>(C);
+        seq_spread<I + 1, N>(C, to);
+    }
+}
+template <int Q, int SP, bool OUT, bool ENDS>
+static __device__ __forceinline__ void seq_step(float (&h)[SP], const float (&A)[SP], float (&g)[ENDS ? SP : 1], float (&P)[ENDS ? SP : 1], float d, float dx,
+                                                float dy, const float (&B)[States<SP>::R], const float (&C)[States<SP>::R], float (&y)[4])
+{
+    if constexpr (Q < States<SP>::R) {
+        constexpr int N = SP < 16 ? SP : 16, S0 = 16 * Q;
+        float a[16], b[16], c[16];
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] = d * A[S0 + i];
+        if constexpr (OUT) seq_spread<0, N>(C[Q], c);
+        if constexpr (ENDS) seq_spread<0, N>(C[Q], dy, c);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] = seq_exp2(a[i]);
+        seq_spread<0, N>(B[Q], dx, b);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[S0 + i] = fmaf(a[i], h[S0 + i], b[i]);
+        if constexpr (ENDS)
+#pragma unroll
+            for (int i = 0; i < N; ++i) P[S0 + i] *= a[i];
+        if constexpr (ENDS)
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[S0 + i] = fmaf(P[S0 + i], c[i], g[S0 + i]);
+        if constexpr (OUT)
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i % 4] = fmaf(c[i], h[S0 + i], y[i % 4]);
+        __builtin_amdgcn_sched_barrier(0);
+        seq_step<Q + 1, SP, OUT, ENDS>(h, A, g, P, d, dx, dy, B, C, y);
     }
 }
 
-// The same for the ends of a run, in both directions: h from zeros, and the gradient g of the state before the run where none comes
-// from behind it, the sum over its positions of C dy times the product P of all decays up to there.
-template <int I, int SP>
-static __device__ __forceinline__ void seq_step_ends(float (&h)[SP], float (&g)[SP], float (&P)[SP], const float (&A)[SP], float d, float dx, float dy,
-                                                     const float (&B)[States<SP>::R], const float (&C)[States<SP>::R])
-{
-    if constexpr (I < SP) {
-        const float a = seq_exp2(d * A[I]);
-        h[I] = fmaf(a, h[I], seq_row_lane<I % 16>(B[I / 16]) * dx);
-        P[I] *= a;
-        g[I] = fmaf(P[I], seq_row_lane<I % 16>(C[I / 16]) * dy, g[I]);
-        seq_step_ends<I + 1, SP>(h, g, P, A, d, dx, dy, B, C);
-    }
-}
-
-// MODE 0: the state a run ends in from zeros; 1: results (chunks == 1: the whole sequence); 2: the ends for the gradients.
+// MODE 0: the state a run ends in from zeros; 1: results (chunks == 1: the whole sequence); 2: the ends for the gradients: h from zeros,
+// noted every 8 positions, and the gradient g of the state before the run where none comes from behind it, the sum over its
+// positions of C dy times the product P of all decays up to there.
+//
+// What concerns single numbers of the tensors (the step's softplus, the gate) is done to the blocks that a lane loads, eight positions at a time;
+// LDS turns blocks into channels and back.
 template <typename T, int SP, int MODE>
 __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs a)
 {
@@ -56,11 +84,14 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     constexpr bool OUT = MODE == 1, ENDS = MODE == 2, ALL = OUT || ENDS;
     constexpr int SG = ENDS ? SP : 1;
     constexpr int E = SP / 8, BL = SP < 16 ? SP : 16;  // elements of B of 8 positions a lane loads; lanes of a row that hold states
-    __shared__ float bcs[kWaves][ALL ? 2 : 1][8 * SP];
-    __shared__ __align__(16) T tiles[kWaves][ALL ? 4 : 2][8 * 64];  // x, dt, z, y (ENDS: dy) of 8 positions x 64 channels
+    constexpr int W = 64 + 4;                          // (rows a block apart: the eight lanes with the same block write to different banks)
+    struct Lds {
+        float d[8][W], dx[8][W], dy[ENDS ? 8 : 1][W];  // d's rows take y once they are done with
+        float B[8 * SP], C[ALL ? 8 * SP : 1];
+    };
+    __shared__ __align__(16) Lds all[kWaves];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    auto &tile = tiles[wave];
-    auto &bc = bcs[wave];
+    Lds &my = all[wave];
     // (waves share nothing: four a workgroup are one on each SIMD)
     long long t = (long long)blockIdx.x * kWaves + wave;
     const int tl = (int)(t % a.tiles);
@@ -83,10 +114,9 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         h[s] = 0;
         if (ENDS) gr[s % SG] = 0, P[s % SG] = 1;
     }
-    const float bias = a.dt_bias ? a.dt_bias[cs] : 0.0f, D = OUT && a.D ? a.D[cs] : 0.0f;
     const int slot = a.slots ? a.slots[n] : n;
     const bool has_slot = slot >= 0 && slot < a.n_slots;
-    const long long at = ((long long)n * a.chunks + chunk) * a.S * a.Cp + cs;
+    const long long run = (long long)n * a.chunks + chunk, at = run * a.S * a.Cp + cs;
     if (OUT) {
         if (a.chunks > 1) {
 #pragma unroll
@@ -99,103 +129,108 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         }
     }
 
-    // what a lane loads and stores: block cbl of the tile's, position ll of 8
-    const T *px[NV], *pd[NV], *pz[NV];
-    const T *pg[NV];
-    T *py[NV];
+    // a lane's blocks: block cbl of the tile's, position ll of 8.  The distance from the tile's first one fits 32 bits.
+    const int ll = lane % 8;
     bool in[NV];
-    int ll[NV], to[NV];
+    int to[NV];
+    float bias[NV][V] = {}, D[NV][V] = {};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int e = lane + 64 * i, cbl = e / 8;
-        ll[i] = e % 8;
-        to[i] = ll[i] * 64 + cbl * V;
+        const int cbl = (lane + 64 * i) / 8;
+        to[i] = cbl * V;
         in[i] = c0 + cbl * V < c_end;
         const int cb = c0 / V + (in[i] ? cbl : 0);
-        px[i] = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
-        pd[i] = static_cast<const T *>(a.dt) + n * a.vdt.n + cb * a.vdt.c;
-        if (ALL) pz[i] = a.z ? static_cast<const T *>(a.z) + n * a.vz.n + cb * a.vz.c : nullptr;
-        if (ENDS) pg[i] = static_cast<const T *>(a.dy) + n * a.vdy.n + cb * a.vdy.c;
-        if (OUT) {
-            py[i] = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
-        }
+        if (a.dt_bias) seq_vector<V>(a.dt_bias, cb, bias[i]);
+        if (OUT && a.D) seq_vector<V>(a.D, cb, D[i]);
     }
-    // B and C: positions and states of the elements that a lane loads
-    const T *pB[E], *pC[E];
-    bool has[E];
-#pragma unroll
-    for (int r = 0; r < E; ++r) {
-        const int s = (lane + 64 * r) % SP;
-        has[r] = s < a.S;
-        const int e = g * a.S + (has[r] ? s : 0);
-        pB[r] = static_cast<const T *>(a.B) + n * a.vB.n + e / V * a.vB.c + e % V;
-        if (ALL) pC[r] = static_cast<const T *>(a.C) + n * a.vC.n + e / V * a.vC.c + e % V;
-    }
+    auto from = [&](const void *p, const SeqView &v, int i, int l0) {
+        const T *base = static_cast<const T *>(p) + n * v.n + c0 / V * v.c + l0 * v.l;
+        return base + ((unsigned)(to[i] / V) * (unsigned)v.c + (unsigned)ll * (unsigned)v.l);
+    };
+    // B and C: element r of a lane is state s of position (lane + 64 r) / SP
+    const int s_of = lane % SP < a.S ? lane % SP : 0, e_of = g * a.S + s_of;
+    auto of_states = [&](const void *p, const SeqView &v, int r, int l0) {
+        const T *base = static_cast<const T *>(p) + n * v.n + l0 * v.l;
+        return base + e_of / V * v.c + e_of % V + (lane + 64 * r) / SP * v.l;
+    };
 
     seq_u32x4 nx[NV], nd[NV], nz[NV], ng[NV];
     T nB[E], nC[E];
     auto fetch = [&](int l0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int l = l0 + ll[i];
-            const bool ok = in[i] && l < stop;
             nx[i] = nd[i] = nz[i] = ng[i] = seq_u32x4{};
-            if (ok) {
-                nx[i] = seq_load(px[i] + l * a.vx.l);
-                nd[i] = seq_load(pd[i] + l * a.vdt.l);
-                if (ALL && a.z) nz[i] = seq_load(pz[i] + l * a.vz.l);
-                if (ENDS) ng[i] = seq_load(pg[i] + l * a.vdy.l);
+            if (in[i] && l0 + ll < stop) {
+                nx[i] = seq_load(from(a.x, a.vx, i, l0));
+                nd[i] = seq_load(from(a.dt, a.vdt, i, l0));
+                if (ALL && a.z) nz[i] = seq_load(from(a.z, a.vz, i, l0));
+                if (ENDS) ng[i] = seq_load(from(a.dy, a.vdy, i, l0));
             }
         }
 #pragma unroll
         for (int r = 0; r < E; ++r) {
-            const int l = l0 + (lane + 64 * r) / SP;
-            const bool ok = has[r] && l < stop;
-            nB[r] = ok ? pB[r][l * a.vB.l] : T(0);
-            if (ALL) nC[r] = ok ? pC[r][l * a.vC.l] : T(0);
+            const bool ok = lane % SP < a.S && l0 + (lane + 64 * r) / SP < stop;
+            nB[r] = ok ? *of_states(a.B, a.vB, r, l0) : T(0);
+            if (ALL) nC[r] = ok ? *of_states(a.C, a.vC, r, l0) : T(0);
         }
     };
     float sum_d = 0;
     if (begin < stop) fetch(begin);
     for (int l0 = begin; l0 < stop; l0 += 8) {
+        float x[NV][V], gate[NV][V];
+        const bool inside = l0 + ll < stop;
         seq_wave_sync();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            seq_store(tile[0] + to[i], nx[i]);
-            seq_store(tile[1] + to[i], nd[i]);
-            if (ALL) seq_store(tile[ALL ? 2 : 0] + to[i], nz[i]);
-            if (ENDS) seq_store(tile[ALL ? 3 : 0] + to[i], ng[i]);
+            float d[V], z[V], dy[V], dx[V];
+            SeqElem<T>::unpack(nx[i], x[i]);
+            SeqElem<T>::unpack(nd[i], d);
+            SeqElem<T>::unpack(nz[i], z);
+            SeqElem<T>::unpack(ng[i], dy);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float raw = d[j] + bias[i][j], soft = seq_softplus(raw);
+                // (what follows the end changes nothing: x, B, C, dy are zero there too)
+                d[j] = !inside ? 0.0f : a.softplus ? soft : raw;
+                dx[j] = d[j] * x[i][j];
+                gate[i][j] = 1;
+                if (ALL) gate[i][j] = a.z ? z[j] * seq_sigmoid(z[j]) : 1.0f;
+                if (ENDS) dy[j] *= gate[i][j];
+            }
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                *reinterpret_cast<seq_f32x4 *>(&my.d[ll][to[i] + j]) = seq_f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
+                *reinterpret_cast<seq_f32x4 *>(&my.dx[ll][to[i] + j]) = seq_f32x4{dx[j], dx[j + 1], dx[j + 2], dx[j + 3]};
+                if (ENDS) *reinterpret_cast<seq_f32x4 *>(&my.dy[ENDS ? ll : 0][to[i] + j]) = seq_f32x4{dy[j], dy[j + 1], dy[j + 2], dy[j + 3]};
+            }
         }
 #pragma unroll
         for (int r = 0; r < E; ++r) {
-            bc[0][lane + 64 * r] = SeqElem<T>::get(nB[r]);
-            if (ALL) bc[ALL ? 1 : 0][lane + 64 * r] = SeqElem<T>::get(nC[r]);
+            my.B[lane + 64 * r] = SeqElem<T>::get(nB[r]);
+            if (ALL) my.C[ALL ? lane + 64 * r : 0] = SeqElem<T>::get(nC[r]);
         }
         seq_wave_sync();
         if (l0 + 8 < stop) fetch(l0 + 8);
         if (ENDS && l0 > begin && live) {
-            const long long m = ((long long)n * a.chunks + chunk) * kSeqMarks + (l0 - begin) / 8 - 1;
+            const long long m = run * kSeqMarks + (l0 - begin) / 8 - 1;
 #pragma unroll
             for (int s = 0; s < SP; ++s)
                 if (s < a.S) a.marks[(m * a.S + s) * a.Cp + c] = h[s];
             a.md[m * a.Cp + c] = sum_d;
         }
-        // one position after the other, its numbers read from LDS during the one before.  (Left to itself the compiler spreads the
-        // eight over each other, in all registers there are.)
+        // one position after the other, its numbers read from LDS during the one before
         struct Position {
-            T x, d, z, dy;
-            float B[R], C[R];
+            float d, dx, dy, B[R], C[R];
         };
         const auto read = [&](int j) {
             Position p = {};
-            p.x = tile[0][j * 64 + lane];
-            p.d = tile[1][j * 64 + lane];
-            if (ALL) p.z = tile[ALL ? 2 : 0][j * 64 + lane];
-            if (ENDS) p.dy = tile[ALL ? 3 : 0][j * 64 + lane];
+            p.d = my.d[j][lane];
+            p.dx = my.dx[j][lane];
+            if (ENDS) p.dy = my.dy[ENDS ? j : 0][lane];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                p.B[r] = bc[0][j * SP + lane % BL + 16 * r];
-                if (ALL) p.C[r] = bc[ALL ? 1 : 0][j * SP + lane % BL + 16 * r];
+                p.B[r] = my.B[j * SP + lane % BL + 16 * r];
+                if (ALL) p.C[r] = my.C[ALL ? j * SP + lane % BL + 16 * r : 0];
             }
             return p;
         };
@@ -204,33 +239,28 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         for (int j = 0; j < 8; ++j) {
             Position next = {};
             if (j < 7) next = read(j + 1);
-            const float x = SeqElem<T>::get(now.x), raw = SeqElem<T>::get(now.d) + bias, soft = seq_softplus(raw);
-            float d = a.softplus ? soft : raw;
-            if (l0 + j >= stop) d = 0;  // (what follows the end changes nothing: x, B, C and z are zero there)
-            float gate = 1;
-            if (ALL) {
-                const float z = SeqElem<T>::get(now.z), of_z = z * seq_sigmoid(z);
-                gate = a.z ? of_z : 1.0f;
-            }
             float y[4] = {};
-            if constexpr (ENDS)
-                seq_step_ends<0, SP>(h, gr, P, A, d, d * x, SeqElem<T>::get(now.dy) * gate, now.B, now.C);
-            else
-                seq_step<0, SP, OUT>(h, A, d, d * x, now.B, now.C, y);
-            sum_d += d;
-            if (OUT) {
-                const float o = fmaf(D, x, (y[0] + y[1]) + (y[2] + y[3])) * gate;
-                tile[OUT ? 3 : 0][j * 64 + lane] = SeqElem<T>::put(live ? o : 0.0f);
-            }
+            seq_step<0, SP, OUT, ENDS>(h, A, gr, P, now.d, now.dx, now.dy, now.B, now.C, y);
+            sum_d += now.d;
+            if (OUT) my.d[j][lane] = (y[0] + y[1]) + (y[2] + y[3]);
             now = next;
-            __builtin_amdgcn_sched_barrier(0);
         }
         if (OUT) {
             seq_wave_sync();
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (in[i] && l0 + ll[i] < end)
-                    seq_store(py[i] + (l0 + ll[i]) * a.vy.l, l0 + ll[i] < stop ? seq_load(tile[OUT ? 3 : 0] + to[i]) : seq_u32x4{});
+            for (int i = 0; i < NV; ++i) {
+                if (!in[i] || l0 + ll >= end) continue;
+                float y[V];
+#pragma unroll
+                for (int j = 0; j < V; j += 4) {
+                    const seq_f32x4 q = *reinterpret_cast<const seq_f32x4 *>(&my.d[ll][to[i] + j]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[j + k] = q[k];
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) y[j] = inside && c0 + to[i] + j < c_end ? fmaf(D[i][j], x[i][j], y[j]) * gate[i][j] : 0.0f;
+                seq_store(const_cast<T *>(from(a.y, a.vy, i, l0)), SeqElem<T>::pack(y));
+            }
         }
     }
     if (OUT) {
@@ -238,7 +268,7 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         for (int l0 = begin + (max(stop - begin, 0) + 7) / 8 * 8; l0 < end; l0 += 8)
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (in[i] && l0 + ll[i] < end) seq_store(py[i] + (l0 + ll[i]) * a.vy.l, seq_u32x4{});
+                if (in[i] && l0 + ll < end) seq_store(const_cast<T *>(from(a.y, a.vy, i, l0)), seq_u32x4{});
         // the run that the last position is in stores the state, the first one that of an empty sequence
         const bool last = len == 0 ? chunk == 0 : begin < len && len <= begin + a.chunk;
         if (a.state_out && has_slot && last && live)
@@ -252,7 +282,7 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
                 a.hl[at + (long long)s * a.Cp] = h[s];
                 if (ENDS) a.gl[at + (long long)s * a.Cp] = gr[s % SG];
             }
-        a.sd[((long long)n * a.chunks + chunk) * a.Cp + c] = sum_d;
+        a.sd[run * a.Cp + c] = sum_d;
     }
 }
 

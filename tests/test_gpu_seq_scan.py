@@ -155,31 +155,33 @@ def test_gradients(N, C, L, S, G, gate, extra, sp, kind, _, layout, dtype):
 
 @pytest.mark.parametrize("axis", ["n", "c", "l"])
 def test_distances_beyond_32_bits(axis):
-    dtype, far, S = seq.SEQ_BF16, (1 << 32) + 64, 16
-    N, C, L = (2, 16, 12) if axis != "l" else (1, 16, 3)
-    shape = {"n": (far, 96, 8), "c": (192, far, 8), "l": (8, 8, far)}[axis]
-    need = {"n": far + 200, "c": far + 600, "l": 2 * far + 64}[axis]
+    """A tensor's elements pass 2^32 by each distance of a view alone: sequences far apart, many blocks or positions as far as they may be."""
+    dtype, S, far = seq.SEQ_BF16, 5, 1 << 24
+    N, C, L = {"n": (2, 16, 12), "c": (1, 260 * 8, 2), "l": (1, 8, 260)}[axis]
+    shape = {"n": ((1 << 32) + 64, 96, 8), "c": (0, far, 8), "l": (0, 8, far)}[axis]
+    need = {"n": (1 << 32) + 512, "c": 260 * far, "l": 260 * far}[axis]
     rng, p = data(N, C, L, S, 1, dtype, 5)
-
     base, offsets = torch.empty(need + 16384, dtype=torch.bfloat16, device="cuda"), iter(range(0, 16384, 1024))
 
-    def tensor(data=None):
-        t = base.as_strided((N, 2, L, 8), shape + (1,), next(offsets))
+    def tensor(data=None, channels=C):
+        t = base.as_strided((N, channels // 8, L, 8), shape + (1,), next(offsets))
         if data is not None:
-            t.copy_(torch.from_numpy(data).view(N, L, 2, 8).permute(0, 2, 1, 3))
+            t.copy_(torch.from_numpy(data).view(N, L, channels // 8, 8).permute(0, 2, 1, 3))
         return t
-    x, dt, B, Cm, dy = (tensor(p[k]) for k in ("x", "dt", "B", "Cm", "dy"))
-    y, ddt, dB, dC = (tensor() for _ in range(4))
-    h = seq.seq_scan_create(N, C, L, S, dtype, views={"x": x, "dt": dt, "B": B, "C": Cm, "y": y, "dy": dy, "dx": y, "ddt": ddt, "dB": dB, "dC": dC})
+    x, dt, dy = (tensor(p[k]) for k in ("x", "dt", "dy"))
+    y, ddt = tensor(), tensor()
+    B, Cm = (Seq(N, S, L, dtype, "dense", p[k]).t for k in ("B", "Cm"))
+    dB, dC = Seq(N, S, L, dtype), Seq(N, S, L, dtype)
+    h = seq.seq_scan_create(N, C, L, S, dtype, views={"x": x, "dt": dt, "y": y, "dy": dy, "dx": y, "ddt": ddt})
     back = lambda t: t.permute(0, 2, 1, 3).reshape(N, L, C).double().cpu().numpy()  # noqa: E731
     ws, A = seq.seq_workspace(h), vector(p["A"], 8)
     seq.seq_scan_fwd(h, x, dt, A, B, Cm, y, ws)
     args = (p["x"], p["dt"], p["A"], p["B"], p["Cm"])
     close(back(y), oracle.scan(*args)[0], bound(L) * oracle.scan(*args, mag=True)[0], True)
-    seq.seq_scan_bwd(h, x, dt, A, B, Cm, dy, y, ddt, nans(S, C), dB, dC, ws)
+    seq.seq_scan_bwd(h, x, dt, A, B, Cm, dy, y, ddt, nans(S, C), dB.t, dC.t, ws)
     r, m = oracle.scan_bwd(*args, p["dy"]), oracle.scan_bwd(*args, p["dy"], mag=True)
-    for k, got in (("dx", y), ("ddt", ddt), ("dB", dB), ("dC", dC)):
-        close(back(got), r[k], (2 * bound(L) + C * U) * m[k], True, k)
+    for k, got in (("dx", back(y)), ("ddt", back(ddt)), ("dB", dB.get()), ("dC", dC.get())):
+        close(got, r[k], (2 * bound(L) + C * U) * m[k], True, k)
 
 
 def test_long_decays_and_large_steps():
