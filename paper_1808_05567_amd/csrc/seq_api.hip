@@ -240,7 +240,7 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     a.tiles = (a.CG + 63) / 64;
     const int64_t waves = (int64_t)a.N * a.G * a.tiles;
     const int64_t runs = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
-    a.chunk = (int)std::min<int64_t>(std::max<int64_t>((a.L + runs - 1) / runs, 32) + 7, 1 << 29) / 8 * 8;
+    a.chunk = (int)std::min<int64_t>(std::max<int64_t>((a.L + runs - 1) / runs, 16) + 7, 1 << 29) / 8 * 8;
     a.chunks = (int)((a.L + (int64_t)a.chunk - 1) / a.chunk);
     const size_t state = (size_t)a.S * a.Cp * 4;
     p->info.state_bytes = state;

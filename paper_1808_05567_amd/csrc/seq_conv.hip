@@ -20,19 +20,20 @@ __global__ __launch_bounds__(256) void seq_conv_fwd_kernel(const SeqConvArgs a)
     int t = blockIdx.x;
     const int run = t % a.ranges;
     t /= a.ranges;
-    const int cb = t % a.cgroups * 8 + cbl, n = t / a.cgroups;
-    if (cb >= a.Cb) return;
+    const int cbw = t % a.cgroups * 8 + cbl, n = t / a.cgroups, cb = min(cbw, a.Cb - 1);
+    const bool live = cbw < a.Cb;
     const int len = seq_length(a.lengths, n, a.L);
     const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
     T *y = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
     const int slot = a.slots ? a.slots[n] : n;
-    const T *state = a.state_in && slot >= 0 && slot < a.n_slots
-                         ? static_cast<const T *>(a.state_in) + ((long long)slot * a.Cb + cb) * (W - 1) * V : nullptr;
+    const bool has_slot = slot >= 0 && slot < a.n_slots;
+    const long long at = ((long long)slot * a.Cb + cb) * (W - 1) * V;
+    const T *state = a.state_in && has_slot ? static_cast<const T *>(a.state_in) + at : nullptr;
     float w[W][V], bias[V] = {};
 #pragma unroll
     for (int k = 0; k < W; ++k) seq_vector<V>(a.w + (long long)k * a.Cp, cb, w[k]);
     if (a.bias) seq_vector<V>(a.bias, cb, bias);
-    const int end = min(a.L, (run + 1) * a.range);
+    const int end = live ? min(a.L, (run + 1) * a.range) : 0;
     for (int l = run * a.range + ll; l < end; l += kPos) {
         seq_u32x4 out = {};
         if (l < len) {
@@ -58,34 +59,18 @@ __global__ __launch_bounds__(256) void seq_conv_fwd_kernel(const SeqConvArgs a)
         }
         seq_store(y + l * a.vy.l, out);
     }
-}
-
-// The last W - 1 inputs of each sequence, those before its start taken from the old state: one thread reads all that it
-// writes first, so that the state may be moved on in place.
-template <typename T, int W>
-__global__ __launch_bounds__(256) void seq_conv_state_kernel(const SeqConvArgs a)
-{
-    constexpr int V = SeqElem<T>::V;
-    const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (t >= (long long)a.N * a.Cb) return;
-    const int n = (int)(t / a.Cb), cb = (int)(t % a.Cb);
-    const int slot = a.slots ? a.slots[n] : n;
-    if (slot < 0 || slot >= a.n_slots) return;
-    const int len = seq_length(a.lengths, n, a.L);
-    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
-    const long long at = ((long long)slot * a.Cb + cb) * (W - 1) * V;
-    seq_u32x4 b[W - 1];
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-        const int l = len - (W - 1) + j;
-        b[j] = seq_u32x4{};
+    if (run != 0 || !a.state_out) return;
+    // The last W - 1 inputs.  By the workgroup that has read the old state, once all of it has: the new one may lie in its place.
+    seq_u32x4 last = {};
+    const int l = len - (W - 1) + ll;
+    if (ll < W - 1) {
         if (l >= 0)
-            b[j] = seq_load(x + l * a.vx.l);
-        else if (a.state_in)
-            b[j] = seq_load(static_cast<const T *>(a.state_in) + at + (len + j) * V);
+            last = seq_load(x + l * a.vx.l);
+        else if (state)
+            last = seq_load(state + (W - 1 + l) * V);
     }
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) seq_store(static_cast<T *>(a.state_out) + at + j * V, b[j]);
+    __syncthreads();
+    if (ll < W - 1 && live && has_slot) seq_store(static_cast<T *>(a.state_out) + at + ll * V, last);
 }
 
 template <typename T, int W>
@@ -125,100 +110,101 @@ __global__ __launch_bounds__(64) void seq_conv_step_kernel(const SeqConvArgs a)
 }
 
 //   ds = dy silu'(s),  dx[l] = sum_k w[W-1-k] ds[l+k],  dw[W-1-k] = sum_l ds[l] x[l-k],  dbias = sum_l ds[l]
-// A workgroup walks its run of positions from the back.  ds goes through LDS, so that each is formed once; the first
-// W - 1 of a tile stay there for the tile before it, those behind the run are formed here too.
+//
+// A workgroup walks along its run of positions, 32 at a time.  What its threads need of each other's numbers goes through rings in LDS of the last
+// 128 positions, so that x and dy are loaded and ds is formed once: x of a tile is written while ds of the one before is
+// formed and dx of the one before that, for positions W - 1 back, whose last ds has come by then; one barrier a tile.
+// ds of the W - 1 positions behind the run is formed here too.
+// Some 300 operations for the eight bf16 numbers of a block, two thirds of them for silu' and unpacking: the vector units need nearly as long as
+// memory does.  (Two barriers a tile, loads of x from each thread, LDS rows in the same banks: 8 x 2048 x 2048 bf16 97 us.)
 template <typename T, int W>
 __global__ __launch_bounds__(256) void seq_conv_bwd_kernel(const SeqConvArgs a)
 {
-    constexpr int V = SeqElem<T>::V;
-    __shared__ float lds[(kPos + W - 1) * 8 * V];  // [position][block][V]; at the end [wave][8][V] of one sum
+    constexpr int V = SeqElem<T>::V, Q = V / 4, RING = 128;
+    // [block][position]: eight lanes side by side take 128 bytes in a row
+    __shared__ __align__(16) seq_u32x4 rx[8][RING];
+    __shared__ __align__(16) seq_f32x4 rd[Q][8][RING];
     const int wave = threadIdx.x / 64, ll = threadIdx.x % 8 + wave * 8, cbl = threadIdx.x / 8 % 8;
     int t = blockIdx.x;
     const int run = t % a.ranges;
     t /= a.ranges;
-    const int cb = t % a.cgroups * 8 + cbl, n = t / a.cgroups;
-    const bool live = cb < a.Cb;
+    const int group = t % a.cgroups, n = t / a.cgroups;
+    const bool live = group * 8 + cbl < a.Cb;
+    const int cb = live ? group * 8 + cbl : 0;
     const int len = live ? seq_length(a.lengths, n, a.L) : 0;
-    const int cbs = live ? cb : 0;
-    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cbs * a.vx.c;
-    const T *dy = static_cast<const T *>(a.dy) + n * a.vdy.n + cbs * a.vdy.c;
-    T *dx = static_cast<T *>(a.dx) + n * a.vdx.n + cbs * a.vdx.c;
+    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
+    const T *dy = static_cast<const T *>(a.dy) + n * a.vdy.n + cb * a.vdy.c;
+    T *dx = static_cast<T *>(a.dx) + n * a.vdx.n + cb * a.vdx.c;
     float w[W][V], bias[V] = {}, dw[W + 1][V] = {};
 #pragma unroll
-    for (int k = 0; k < W; ++k) seq_vector<V>(a.w + (long long)k * a.Cp, cbs, w[k]);
-    if (a.bias) seq_vector<V>(a.bias, cbs, bias);
+    for (int k = 0; k < W; ++k) seq_vector<V>(a.w + (long long)k * a.Cp, cb, w[k]);
+    if (a.bias) seq_vector<V>(a.bias, cb, bias);
 
-    // ds at position l, and the x that it came from
-    auto form = [&](int l, float (&ds)[V], float (&f)[W][V]) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) ds[i] = 0;
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[k][i] = 0;
-        if (l >= len) return;
-        float g[V], s[V];
-        SeqElem<T>::unpack(seq_load(dy + l * a.vdy.l), g);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = bias[i];
-#pragma unroll
-        for (int k = W - 1; k >= 0; --k) {
-            if (l >= k) SeqElem<T>::unpack(seq_load(x + (l - k) * a.vx.l), f[k]);
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = fmaf(w[W - 1 - k][i], f[k][i], s[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float p = seq_sigmoid(s[i]);
-            ds[i] = a.silu ? g[i] * p * (1.0f + s[i] * (1.0f - p)) : g[i];
-        }
-    };
-    float *mine = lds + (ll * 8 + cbl) * V;
     const int begin = run * a.range, end = min(a.L, begin + a.range);
+    const int stop = min(len, end + W - 1);  // behind the last position whose ds is formed
     const int tiles = (end - begin + kPos - 1) / kPos;
-    for (int i = tiles - 1; i >= 0; --i) {
-        const int l = begin + i * kPos + ll;
-        float ds[V], f[W][V];
-        if (i == tiles - 1) {
-            if (ll < W - 1) {
-                form(l + kPos, ds, f);
+    auto load = [&](const T *p, long long stride, int l) { return l >= 0 && l < stop ? seq_load(p + l * stride) : seq_u32x4{}; };
+    if (ll < W - 1) rx[cbl][(RING - 1 - ll) % RING] = load(x, a.vx.l, begin - 1 - ll);
+    rx[cbl][ll] = load(x, a.vx.l, begin + ll);
+    seq_u32x4 nx = load(x, a.vx.l, begin + kPos + ll), ny = load(dy, a.vdy.l, begin + ll);
+    float own[V] = {};  // ds of the tile before, at this thread's place
+    __syncthreads();
+    for (int i = 0; i <= tiles + 1; ++i) {
+        const int l = begin + i * kPos + ll, at = (i * kPos + ll) % RING;
+        rx[cbl][(at + kPos) % RING] = nx;
+        const seq_u32x4 cy = ny;
+        nx = load(x, a.vx.l, l + 2 * kPos);
+        ny = load(dy, a.vdy.l, l + kPos);
+        float ds[V] = {};
+        if (l < stop) {
+            float g[V], s[V], f[W][V];
+            SeqElem<T>::unpack(cy, g);
 #pragma unroll
-                for (int j = 0; j < V; ++j) mine[kPos * 8 * V + j] = ds[j];
+            for (int j = 0; j < V; ++j) s[j] = bias[j];
+#pragma unroll
+            for (int k = W - 1; k >= 0; --k) {
+                SeqElem<T>::unpack(rx[cbl][(at + RING - k) % RING], f[k]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[j] = fmaf(w[W - 1 - k][j], f[k][j], s[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float p = seq_sigmoid(s[j]);
+                ds[j] = a.silu ? g[j] * p * fmaf(s[j], 1.0f - p, 1.0f) : g[j];
+            }
+            // (what lies behind the run counts in the next one)
+            if (l < end) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) dw[W][j] += ds[j];
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) dw[W - 1 - k][j] = fmaf(ds[j], f[k][j], dw[W - 1 - k][j]);
             }
         }
-        form(l, ds, f);
-        // (positions past the run's end belong to the next one: here they are only read)
-        if (l < end) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) dw[W][j] += ds[j];
+        for (int q = 0; q < Q; ++q) rd[q][cbl][at] = seq_f32x4{ds[4 * q], ds[4 * q + 1], ds[4 * q + 2], ds[4 * q + 3]};
+        const int back = l - kPos - (W - 1);  // where dx is complete
+        if (live && back >= begin && back < end) {
+            float d[V];
 #pragma unroll
-            for (int k = 0; k < W; ++k)
+            for (int j = 0; j < V; ++j) d[j] = w[0][j] * own[j];
 #pragma unroll
-                for (int j = 0; j < V; ++j) dw[W - 1 - k][j] = fmaf(ds[j], f[k][j], dw[W - 1 - k][j]);
+            for (int k = 1; k < W; ++k)
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const seq_f32x4 e = rd[q][cbl][(at + RING - kPos - k) % RING];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[4 * q + j] = fmaf(w[k][4 * q + j], e[j], d[4 * q + j]);
+                }
+            seq_store(dx + back * a.vdx.l, back < len ? SeqElem<T>::pack(d) : seq_u32x4{});
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) mine[j] = ds[j];
+        for (int j = 0; j < V; ++j) own[j] = ds[j];
         __syncthreads();
-        float d[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) d[j] = w[W - 1][j] * ds[j];
-#pragma unroll
-        for (int k = 1; k < W; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) d[j] = fmaf(w[W - 1 - k][j], mine[k * 8 * V + j], d[j]);
-        if (live && l < end) {
-            if (l >= len)
-#pragma unroll
-                for (int j = 0; j < V; ++j) d[j] = 0;
-            seq_store(dx + l * a.vdx.l, SeqElem<T>::pack(d));
-        }
-        __syncthreads();
-        if (ll < W - 1)
-#pragma unroll
-            for (int j = 0; j < V; ++j) mine[kPos * 8 * V + j] = ds[j];
     }
     // the workgroup's sums: over the 8 positions of a wave, then over the waves in order
-    __syncthreads();
+    float *lds = reinterpret_cast<float *>(rd);  // [wave][8][V]
 #pragma unroll
     for (int k = 0; k <= W; ++k) {
 #pragma unroll
@@ -230,13 +216,12 @@ __global__ __launch_bounds__(256) void seq_conv_bwd_kernel(const SeqConvArgs a)
             if (threadIdx.x % 8 == 0) lds[(wave * 8 + cbl) * V + j] = s;
         }
         __syncthreads();
-        if (threadIdx.x < 8 * V && blockIdx.x / a.ranges % a.cgroups * 8 + threadIdx.x / V < a.Cb) {
+        if (threadIdx.x < 8 * V && group * 8 + threadIdx.x / V < a.Cb) {
             float s = 0;
 #pragma unroll
             for (int v = 0; v < 4; ++v) s += lds[v * 8 * V + threadIdx.x];
-            const int c = blockIdx.x / a.ranges % a.cgroups * 8 * V + threadIdx.x;
             const long long part = (long long)n * a.ranges + run;
-            a.part[(part * (W + 1) + k) * a.Cp + c] = s;
+            a.part[(part * (W + 1) + k) * a.Cp + group * 8 * V + threadIdx.x] = s;
         }
         __syncthreads();
     }
@@ -265,7 +250,6 @@ hipError_t launch(int which, const SeqConvArgs &a, hipStream_t s)
     const unsigned grid = (unsigned)((long long)a.N * a.cgroups * a.ranges);
     if (which == 0) {
         seq_conv_fwd_kernel<T, W><<<grid, 256, 0, s>>>(a);
-        if (a.state_out) seq_conv_state_kernel<T, W><<<(unsigned)((vectors + 255) / 256), 256, 0, s>>>(a);
         return hipGetLastError();
     }
     seq_conv_bwd_kernel<T, W><<<grid, 256, 0, s>>>(a);

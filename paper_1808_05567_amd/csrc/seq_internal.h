@@ -182,9 +182,13 @@ static __device__ __forceinline__ float seq_sigmoid(float x) { return __builtin_
 // log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|) <= 1, and log(1 + e) = 2 atanh(t), t = e / (2 + e) <= 1/3.  atanh(t) / t is
 // 1 + t^2 times a cubic in t^2, through its values at Chebyshev's points: 1.6e-8 off at most.  (The logarithm of 1 + e itself loses what e
 // has below 2^-24: steps of 1e-3 would be good to 6e-5.  The series to the same error takes eight terms.)
-static __device__ __forceinline__ float seq_softplus(float x)
+static __device__ __forceinline__ float seq_softplus(float x, float *slope = nullptr)
 {
     const float e = seq_exp2(-kLog2e * fabsf(x));
+    if (slope) {  // its derivative, 1 / (1 + exp(-x))
+        const float r = __builtin_amdgcn_rcpf(1.0f + e);
+        *slope = x < 0 ? e * r : r;
+    }
     const float t = e * __builtin_amdgcn_rcpf(2.0f + e), u = t * t;
     float p = 0.134337744f;
     p = fmaf(p, u, 0.141169779f);

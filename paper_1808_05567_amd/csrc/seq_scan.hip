@@ -299,20 +299,20 @@ __global__ __launch_bounds__(256) void seq_scan_join_kernel(const SeqScanArgs a)
     const float A = a.A[e] * kLog2e;
     const float first = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f;
     const float *sd = a.sd + (long long)n * a.chunks * a.Cp + c;
-    // what a run adds and the sum of its d come 16 runs at a time, ahead of the chain that they go into
+    // what a run adds and the sum of its d come 32 runs at a time, ahead of the chain that they go into
     const auto chain = [&](float *ends, float h, bool back) {
         ends += (long long)n * a.chunks * state + e;
-        for (int k0 = 0; k0 < a.chunks; k0 += 16) {
-            float own[16], d[16];
+        for (int k0 = 0; k0 < a.chunks; k0 += 32) {
+            float own[32], d[32];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 32; ++i) {
                 const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
                 const bool ok = k0 + i < a.chunks;
                 own[i] = ok ? ends[k * state] : 0.0f;
                 d[i] = ok ? sd[(long long)k * a.Cp] : 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 32; ++i) {
                 const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
                 if (k0 + i < a.chunks) ends[k * state] = h;
                 h = fmaf(seq_exp2(A * d[i]), h, own[i]);

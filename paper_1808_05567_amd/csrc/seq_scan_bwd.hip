@@ -84,28 +84,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     struct Place {
         bool in;
         int cb, to, l;
+        unsigned blocks;
     };
     auto place = [&](int i) {
         int e = lane + 64 * i;
         asm volatile("" : "+v"(e));
         const int cbl = e / PT;
         const bool in = e < VEC && c0 + cbl * V < c_end;
-        return Place{in, in ? c0 / V + cbl : 0, e < VEC ? cbl * V : 0, e % PT};
+        return Place{in, in ? c0 / V + cbl : 0, e < VEC ? cbl * V : 0, e % PT, (unsigned)cbl};
     };
-    auto block = [&](const void *p, const SeqView &v, const Place &at, int l) {
-        return seq_load(static_cast<const T *>(p) + n * v.n + at.cb * v.c + l * v.l);
+    // (what lies between a tile's elements fits 32 bits)
+    auto address = [&](const void *p, const SeqView &v, const Place &at, int p0) {
+        const T *base = static_cast<const T *>(p) + n * v.n + c0 / V * v.c + p0 * v.l;
+        return base + (at.blocks * (unsigned)v.c + (unsigned)at.l * (unsigned)v.l);
     };
-    auto put = [&](void *p, const SeqView &v, const Place &at, int l, const float (&f)[V]) {
-        seq_store(static_cast<T *>(p) + n * v.n + at.cb * v.c + l * v.l, SeqElem<T>::pack(f));
+    auto put = [&](void *p, const SeqView &v, const Place &at, int p0, const float (&f)[V]) {
+        seq_store(const_cast<T *>(address(p, v, at, p0)), SeqElem<T>::pack(f));
     };
-    auto to_lds = [&](float *p, const float (&f)[V]) {
+    // Column of a row in LDS: the fours of a row change places with the row, or the rows of one block would lie in the same banks.
+    constexpr int FOURS = WC / 4 < 8 ? WC / 4 : 8;
+    auto column = [](int l, int c) { return c ^ (l % FOURS * 4); };
+    auto to_lds = [&](float (&row)[WC], const Place &at, const float (&f)[V]) {
 #pragma unroll
-        for (int j = 0; j < V; j += 4) *reinterpret_cast<seq_f32x4 *>(p + j) = seq_f32x4{f[j], f[j + 1], f[j + 2], f[j + 3]};
+        for (int j = 0; j < V; j += 4) *reinterpret_cast<seq_f32x4 *>(&row[column(at.l, at.to + j)]) = seq_f32x4{f[j], f[j + 1], f[j + 2], f[j + 3]};
     };
-    auto from_lds = [&](const float *p, float (&f)[V]) {
+    auto from_lds = [&](const float (&row)[WC], const Place &at, float (&f)[V]) {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
-            const seq_f32x4 q = *reinterpret_cast<const seq_f32x4 *>(p + j);
+            const seq_f32x4 q = *reinterpret_cast<const seq_f32x4 *>(&row[column(at.l, at.to + j)]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) f[j + k] = q[k];
         }
@@ -146,29 +152,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     // what is needed next from memory, on its way meanwhile: positions to stage, the note at the start of an eight
     seq_u32x4 nx[NV], nd[NV], ng[NV], nz[NV];
     T nB[E], nC[E];
+    // element r of a lane is state s of position (lane + 64 r) / SP
+    const int e_of = g * a.S + (lane % SP < a.S ? lane % SP : 0);
+    auto of_states = [&](const void *p, const SeqView &v, int r, int l0) {
+        const T *base = static_cast<const T *>(p) + n * v.n + l0 * v.l;
+        return base + e_of / V * v.c + e_of % V + (lane + 64 * r) / SP * v.l;
+    };
     auto fetch = [&](int l0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Place p = place(i);
-            const int l = l0 + p.l;
             nx[i] = nd[i] = ng[i] = nz[i] = seq_u32x4{};
-            if (p.in && l < stop) {
-                nx[i] = block(a.x, a.vx, p, l);
-                nd[i] = block(a.dt, a.vdt, p, l);
-                ng[i] = block(a.dy, a.vdy, p, l);
-                if (GATE) nz[i] = block(a.z, a.vz, p, l);
+            if (p.in && l0 + p.l < stop) {
+                nx[i] = seq_load(address(a.x, a.vx, p, l0));
+                nd[i] = seq_load(address(a.dt, a.vdt, p, l0));
+                ng[i] = seq_load(address(a.dy, a.vdy, p, l0));
+                if (GATE) nz[i] = seq_load(address(a.z, a.vz, p, l0));
             }
         }
 #pragma unroll
         for (int r = 0; r < E; ++r) {
-            int q = lane + 64 * r;
-            asm volatile("" : "+v"(q));
-            const int l = l0 + q / SP, st = q % SP, e = g * a.S + st;
-            nB[r] = nC[r] = T(0);
-            if (l < stop && st < a.S) {
-                nB[r] = static_cast<const T *>(a.B)[n * a.vB.n + e / V * a.vB.c + l * a.vB.l + e % V];
-                nC[r] = static_cast<const T *>(a.C)[n * a.vC.n + e / V * a.vC.c + l * a.vC.l + e % V];
-            }
+            const bool ok = lane % SP < a.S && l0 + (lane + 64 * r) / SP < stop;
+            nB[r] = ok ? *of_states(a.B, a.vB, r, l0) : T(0);
+            nC[r] = ok ? *of_states(a.C, a.vC, r, l0) : T(0);
         }
     };
     seq_f32x2 note[4], note_d = {};
@@ -197,7 +203,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const bool ok = p.in && p0 + p.l < stop && p.cb * V + j < a.Ch;
-                const float raw = d[j] + bias[j], soft = seq_softplus(raw), sig = seq_sigmoid(raw);
+                float sig;
+                const float raw = d[j] + bias[j], soft = seq_softplus(raw, &sig);
                 d[j] = ok ? a.softplus ? soft : raw : 0.0f;
                 slope[j] = ok ? a.softplus ? sig : 1.0f : 0.0f;
                 x[j] = ok ? x[j] : 0.0f;
@@ -209,11 +216,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
                 }
             }
             if (lane + 64 * i < VEC) {
-                to_lds(&my.d[p.l][p.to], d);
-                to_lds(&my.x[p.l][p.to], x);
-                to_lds(&my.dy[p.l][p.to], dy);
-                to_lds(&my.slope[p.l][p.to], slope);
-                if (GATE) to_lds(&my.dgate[GATE ? p.l : 0][p.to], dgate);
+                to_lds(my.d[p.l], p, d);
+                to_lds(my.x[p.l], p, x);
+                to_lds(my.dy[p.l], p, dy);
+                to_lds(my.slope[p.l], p, slope);
+                if (GATE) to_lds(my.dgate[GATE ? p.l : 0], p, dgate);
             }
         }
 #pragma unroll
@@ -223,7 +230,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
         }
         seq_wave_sync();
         if (stage > 0) fetch(p0 - PT);
-        auto row = [&](const float (&p)[WC]) { return *reinterpret_cast<const seq_f32x2 *>(&p[cl * 2]); };
+        auto row = [&](const float (&p)[WC], int l) { return *reinterpret_cast<const seq_f32x2 *>(&p[column(l, cl * 2)]); };
         auto states = [&](const float (&p)[SP]) { return *reinterpret_cast<const seq_f32x4 *>(&p[s]); };
 
 #pragma unroll 1
@@ -242,14 +249,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
 #pragma unroll
             for (int q = 0; q < kT; ++q) {
                 const int l = first + q;
-                const seq_f32x2 d = row(my.d[l]), x = row(my.x[l]);
+                const seq_f32x2 d = row(my.d[l], q), x = row(my.x[l], q);
                 const seq_f32x4 B = states(my.B[l]);
+                float a[4][2], b[4][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a[j][i] = d[i] * A[j][i];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const float dx = d[i] * x[i];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) hs[q + 1][j][i] = fmaf(seq_exp2(d[i] * A[j][i]), hs[q][j][i], B[j] * dx);
+                    for (int j = 0; j < 4; ++j) a[j][i] = seq_exp2(a[j][i]), b[j][i] = B[j] * dx;
                 }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) hs[q + 1][j][i] = fmaf(a[j][i], hs[q][j][i], b[j][i]);
             }
             // (else the compiler keeps the decays and the eight's numbers from the way forwards, in registers that there are not)
             seq_wave_sync();
@@ -260,26 +276,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
 #pragma unroll
             for (int q = kT - 1; q >= 0; --q) {
                 const int l = first + q;
-                const seq_f32x2 d = row(my.d[l]), x = row(my.x[l]), dy = row(my.dy[l]);
+                const seq_f32x2 d = row(my.d[l], q), x = row(my.x[l], q), dy = row(my.dy[l], q);
                 const seq_f32x4 B = states(my.B[l]), C = states(my.C[l]);
                 float bc[8] = {};  // dB, dC of the four states
                 seq_f32x2 gB = {}, At = {}, Ch = {};
+                float a[4][2], gr[4][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        a[j][i] = d[i] * A[j][i];
+                        gr[j][i] = fmaf(dy[i], C[j], carry[j][i]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const float dx = d[i] * x[i];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float gr = fmaf(dy[i], C[j], carry[j][i]);
+                        a[j][i] = seq_exp2(a[j][i]);
                         bc[4 + j] = fmaf(dy[i], hs[q + 1][j][i], bc[4 + j]);
-                        bc[j] = fmaf(gr, dx, bc[j]);
-                        gB[i] = fmaf(gr, B[j], gB[i]);
+                        bc[j] = fmaf(gr[j][i], dx, bc[j]);
+                        gB[i] = fmaf(gr[j][i], B[j], gB[i]);
                         if (GATE) Ch[i] = fmaf(C[j], hs[q + 1][j][i], Ch[i]);
-                        carry[j][i] = gr * seq_exp2(d[i] * A[j][i]);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        carry[j][i] = gr[j][i] * a[j][i];
                         const float th = carry[j][i] * hs[q][j][i];
                         dA[j][i] = fmaf(th, d[i], dA[j][i]);
                         At[i] = fmaf(th, A[j][i], At[i]);
                     }
-                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     gB[i] = sum_states<NL>(gB[i]);
@@ -287,9 +318,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
                     if (GATE) Ch[i] = sum_states<NL>(Ch[i]);
                 }
                 if (sl == 0) {
-                    *reinterpret_cast<seq_f32x2 *>(&my.At[l][cl * 2]) = At;
-                    *reinterpret_cast<seq_f32x2 *>(&my.gB[l][cl * 2]) = gB;
-                    if (GATE) *reinterpret_cast<seq_f32x2 *>(&my.Ch[GATE ? l : 0][cl * 2]) = Ch;
+                    *reinterpret_cast<seq_f32x2 *>(&my.At[l][column(q, cl * 2)]) = At;
+                    *reinterpret_cast<seq_f32x2 *>(&my.gB[l][column(q, cl * 2)]) = gB;
+                    if (GATE) *reinterpret_cast<seq_f32x2 *>(&my.Ch[GATE ? l : 0][column(q, cl * 2)]) = Ch;
                 }
                 float u[4], v[2];
 #pragma unroll
@@ -308,12 +339,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
             const int l = p0 + p.l;
             const bool inside = l < stop, store = p.in && l < end;
             float d[V], x[V], dy[V], slope[V], At[V], gB[V], dx[V], ddt[V], D[V] = {};
-            from_lds(&my.d[p.l][p.to], d);
-            from_lds(&my.x[p.l][p.to], x);
-            from_lds(&my.dy[p.l][p.to], dy);
-            from_lds(&my.slope[p.l][p.to], slope);
-            from_lds(&my.At[p.l][p.to], At);
-            from_lds(&my.gB[p.l][p.to], gB);
+            from_lds(my.d[p.l], p, d);
+            from_lds(my.x[p.l], p, x);
+            from_lds(my.dy[p.l], p, dy);
+            from_lds(my.slope[p.l], p, slope);
+            from_lds(my.At[p.l], p, At);
+            from_lds(my.gB[p.l], p, gB);
             if (a.D) seq_vector<V>(a.D, p.cb, D);
             float pD[V];
 #pragma unroll
@@ -325,16 +356,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
                 pD[j] = dy[j] * x[j];
             }
             if (store) {
-                put(a.dx, a.vdx, p, l, dx);
-                put(a.ddt, a.vddt, p, l, ddt);
+                put(a.dx, a.vdx, p, p0, dx);
+                put(a.ddt, a.vddt, p, p0, ddt);
             }
             if (GATE) {
                 float dgate[V], Ch[V];
-                from_lds(&my.dgate[GATE ? p.l : 0][p.to], dgate);
-                from_lds(&my.Ch[GATE ? p.l : 0][p.to], Ch);
+                from_lds(my.dgate[GATE ? p.l : 0], p, dgate);
+                from_lds(my.Ch[GATE ? p.l : 0], p, Ch);
 #pragma unroll
                 for (int j = 0; j < V; ++j) dgate[j] = inside && p.cb * V + j < a.Ch ? dgate[j] * fmaf(D[j], x[j], Ch[j]) : 0.0f;
-                if (store) put(a.dz, a.vdz, p, l, dgate);
+                if (store) put(a.dz, a.vdz, p, p0, dgate);
             }
             // lane ll of eight keeps the sums of the block's channel ll
 #pragma unroll
@@ -362,11 +393,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Place p = place(i);
-            const int l = l0 + p.l;
-            if (!p.in || l >= end) continue;
-            put(a.dx, a.vdx, p, l, zero);
-            put(a.ddt, a.vddt, p, l, zero);
-            if (GATE) put(a.dz, a.vdz, p, l, zero);
+            if (!p.in || l0 + p.l >= end) continue;
+            put(a.dx, a.vdx, p, l0, zero);
+            put(a.ddt, a.vddt, p, l0, zero);
+            if (GATE) put(a.dz, a.vdz, p, l0, zero);
         }
     // this run's part of the parameters' gradients; that of A where its state was
 #pragma unroll
