@@ -18,7 +18,8 @@ struct seq_plan {
     int dtype, W;
     seq_info_t info;
     size_t fwd_ws, bwd_ws;
-    SeqConvArgs conv;
+    SeqConvArgs conv;  // its runs are the forward pass's
+    int bwd_range, bwd_ranges;
     SeqScanArgs scan, scan_bwd;
     SeqNormArgs norm;
     SeqMv4Args mv4;
@@ -140,15 +141,22 @@ conv_status_t seq_conv_create(const seq_conv_desc_t *d, seq_handle_t *out)
     if (!view_of(d->x, a.N, a.Cb, a.L, v, false, a.vx) || !view_of(d->y, a.N, a.Cb, a.L, v, true, a.vy) ||
         !view_of(d->dy, a.N, a.Cb, a.L, v, false, a.vdy) || !view_of(d->dx, a.N, a.Cb, a.L, v, true, a.vdx))
         return finish(p, CONV_EINVAL, out);
-    // Runs of positions: long ones, as the weights are loaded and their gradients summed once a run, but some 2048 workgroups where the tensor has
-    // them (8 a compute unit).
+    // Runs of positions: as long as they may be, for the weights are loaded, their gradients summed and neighbours' positions read once a run,
+    // in one round of workgroups that are resident together.  That is 6 a compute unit forwards; backwards, whose registers and LDS
+    // go by the number of taps, 3 or 2 in bf16 and 5 or 3 in fp32.  (8 x 2048 x 2048 bf16, 4 taps, backwards: 768 workgroups 55 us, 1024 73,
+    // 1536 63, 2048 73.)
     a.cgroups = (a.Cb + 7) / 8;
-    const int64_t columns = (int64_t)a.N * a.cgroups, want = std::max<int64_t>(1, 2048 / columns);
-    a.range = (int)std::min<int64_t>(std::max<int64_t>((a.L / want + 31) / 32 * 32, 64), 1 << 29);
-    a.ranges = (int)((a.L + (int64_t)a.range - 1) / a.range);
+    const int64_t columns = (int64_t)a.N * a.cgroups;
+    const auto runs = [&](int64_t workgroups, int &range) {
+        const int64_t want = std::max<int64_t>(1, workgroups / columns);
+        range = (int)std::min<int64_t>(std::max<int64_t>(((a.L + want - 1) / want + 31) / 32 * 32, 64), 1 << 29);
+        return (int)((a.L + (int64_t)range - 1) / range);
+    };
+    a.ranges = runs(256 * 6, a.range);
+    p->bwd_ranges = runs(256 * (d->dtype == SEQ_BF16 ? d->W <= 4 ? 3 : 2 : d->W <= 4 ? 5 : 3), p->bwd_range);
     p->info.state_bytes = (size_t)a.Cb * (d->W - 1) * 16;
-    p->bwd_ws = up((size_t)a.N * a.ranges * (d->W + 1) * a.Cp * 4);
-    const bool fits = columns * a.ranges <= kMaxGrid && (int64_t)a.N * a.ranges <= kMaxGrid;
+    p->bwd_ws = up((size_t)a.N * p->bwd_ranges * (d->W + 1) * a.Cp * 4);
+    const bool fits = columns * std::max(a.ranges, p->bwd_ranges) <= kMaxGrid;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 
@@ -197,6 +205,8 @@ conv_status_t seq_conv_bwd(seq_handle_t h, const void *x, const float *w, const 
     a.dw = dw;
     a.dbias = dbias;
     a.lengths = lengths;
+    a.range = h->bwd_range;
+    a.ranges = h->bwd_ranges;
     a.part = static_cast<float *>(ws);
     return done(launch_seq_conv_bwd(h->dtype, h->W, a, (hipStream_t)stream));
 }
@@ -463,8 +473,8 @@ conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen)
     if (!h || !buf || buflen == 0) return CONV_EINVAL;
     switch (h->kind) {
         case kConv:
-            snprintf(buf, buflen, "seq_conv dt=%d W=%d runs=%d positions/run=%d grid=%lld", h->dtype, h->W, h->conv.ranges, h->conv.range,
-                     (long long)h->conv.N * h->conv.cgroups * h->conv.ranges);
+            snprintf(buf, buflen, "seq_conv dt=%d W=%d fwd: runs=%d positions/run=%d bwd: runs=%d positions/run=%d columns=%lld", h->dtype, h->W, h->conv.ranges,
+                     h->conv.range, h->bwd_ranges, h->bwd_range, (long long)h->conv.N * h->conv.cgroups);
             break;
         case kScan:
             snprintf(buf, buflen, "seq_scan dt=%d states=%d of %d fwd: runs=%d positions/run=%d waves=%lld bwd: runs=%d waves=%lld", h->dtype, h->scan.S,
