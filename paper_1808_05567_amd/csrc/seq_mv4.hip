@@ -15,6 +15,8 @@
 namespace convmi {
 namespace {
 
+constexpr int kMaxWaves = 16;
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
@@ -25,9 +27,11 @@ template <>
 struct Act<SEQ_I8> {
     typedef int8_t T;
     typedef i32x4 Acc;
+    typedef seq_u32x2 Raw;
     seq_u32x2 x;
-    __device__ __forceinline__ void load(const int8_t *p) { x = *reinterpret_cast<const seq_u32x2 *>(p); }
-    __device__ __forceinline__ void zero() { x = seq_u32x2{}; }
+    // eight channels, of which `left` there are
+    static __device__ __forceinline__ Raw fetch(const int8_t *p, int left) { return left >= 8 ? *reinterpret_cast<const seq_u32x2 *>(p) : seq_u32x2{}; }
+    __device__ __forceinline__ explicit Act(const Raw &r) : x(r) {}
     // eight weights from a word: sixteen times their values, in the upper halves of bytes (low ones of each byte first)
     struct Wt {
         long lo_hi;
@@ -61,9 +65,10 @@ template <>
 struct Act<SEQ_BF16> {
     typedef unsigned short T;
     typedef seq_f32x4 Acc;
+    typedef seq_u32x4 Raw;
     seq_u32x4 x;
-    __device__ __forceinline__ void load(const unsigned short *p) { x = seq_load(p); }
-    __device__ __forceinline__ void zero() { x = seq_u32x4{}; }
+    static __device__ __forceinline__ Raw fetch(const unsigned short *p, int left) { return left >= 8 ? seq_load(p) : seq_u32x4{}; }
+    __device__ __forceinline__ explicit Act(const Raw &r) : x(r) {}
     typedef WtBf16 Wt;
     static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
     static constexpr float unit = 1.0f;
@@ -76,22 +81,25 @@ template <>
 struct Act<SEQ_F32> {
     typedef float T;
     typedef seq_f32x4 Acc;
+    struct Raw {
+        seq_f32x4 lo, hi;
+    };
     seq_u32x4 h, m, l;
-    __device__ __forceinline__ void load(const float *p)
+    static __device__ __forceinline__ Raw fetch(const float *p, int left)
     {
-        alignas(16) float f[8];
-        *reinterpret_cast<seq_f32x4 *>(f) = *reinterpret_cast<const seq_f32x4 *>(p);
-        *reinterpret_cast<seq_f32x4 *>(f + 4) = *reinterpret_cast<const seq_f32x4 *>(p + 4);
+        return {left >= 4 ? *reinterpret_cast<const seq_f32x4 *>(p) : seq_f32x4{}, left >= 8 ? *reinterpret_cast<const seq_f32x4 *>(p + 4) : seq_f32x4{}};
+    }
+    __device__ __forceinline__ explicit Act(const Raw &r)
+    {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float p0 = f[2 * i], p1 = f[2 * i + 1];
+            const float p0 = i < 2 ? r.lo[2 * i] : r.hi[2 * i - 4], p1 = i < 2 ? r.lo[2 * i + 1] : r.hi[2 * i - 3];
             h[i] = seq_pack_bf16(p0, p1);
             const float r0 = p0 - __uint_as_float(h[i] << 16), r1 = p1 - __uint_as_float(h[i] & 0xFFFF0000u);
             m[i] = seq_pack_bf16(r0, r1);
             l[i] = seq_pack_bf16(r0 - __uint_as_float(m[i] << 16), r1 - __uint_as_float(m[i] & 0xFFFF0000u));
         }
     }
-    __device__ __forceinline__ void zero() { h = m = l = seq_u32x4{}; }
     typedef WtBf16 Wt;
     static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
     static constexpr float unit = 1.0f;
@@ -103,13 +111,14 @@ struct Act<SEQ_F32> {
     }
 };
 
-// A workgroup: 16 weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.
-template <int DT, int NT>
-__global__ __launch_bounds__(512) void seq_mv4_kernel(const SeqMv4Args a)
+// A workgroup: 16 weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.  A wave has the loads of U runs on
+// their way at a time: there are few, and each is a trip to memory.  (One at a time: 4096 x 8192 for one token 10.3 us.)
+template <int DT, int NT, int GROUP, int U>
+__global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Args a)
 {
     typedef Act<DT> A;
     typedef typename A::T T;
-    __shared__ float lds[8 * NT * 256];
+    __shared__ float lds[kMaxWaves * NT * 256];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int j = lane / 16, col = lane % 16;  // operands: row or token `col`, channels 8 j ... + 7 of a run of 32
     const int k0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
@@ -119,40 +128,45 @@ __global__ __launch_bounds__(512) void seq_mv4_kernel(const SeqMv4Args a)
     for (int t = 0; t < NT; ++t) x[t] = static_cast<const T *>(a.x) + (long long)min(m0 + t * 16 + col, a.M - 1) * a.Cx + 8 * j;
     const float *scale = a.scale + k0 + 4 * j;  // results: rows 4 j ... + 3, token `col`
     seq_f32x4 sum[NT] = {};
-    const int per = a.group / 32;  // runs of 32 a group
-    for (int c = wave; c < a.Cs; c += waves) {
-        const seq_u32x4 w = wt[(long long)c * a.Kp * 4];
-        typename A::Acc acc[NT];
+    constexpr int per = GROUP / 32, groups = 4 / per;  // runs of 32 a group, groups a run of 128
+    for (int first = wave; first < a.Cs; first += waves * U) {
+        seq_u32x4 w[U];
+        seq_f32x4 sc[U][groups];
+        typename A::Raw raw[U][NT][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i % per == 0)
+        for (int u = 0; u < U; ++u) {
+            const int c = first + u * waves;
+            if (c >= a.Cs) break;
+            w[u] = wt[(long long)c * a.Kp * 4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = typename A::Acc{};
-            const typename A::Wt wi = A::unpack(w[i]);
-            const int c0 = c * 128 + i * 32, g0 = c0 - i % per * 32;  // (the group's first)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                A act;
+            for (int i = 0; i < 4; ++i) {
+                const int c0 = c * 128 + i * 32;
                 // (x ends at Cx, the weights go on with zeros to the end of the run of 128)
-                if (c0 + 8 * j + 8 <= a.Cx)
-                    act.load(x[t] + c0);
-                else
-                    act.zero();
-                if constexpr (DT == SEQ_F32) {
-                    if (c0 + 8 * j + 4 == a.Cx) {  // (half of the eight)
-                        alignas(16) float f[8] = {};
-                        *reinterpret_cast<seq_f32x4 *>(f) = *reinterpret_cast<const seq_f32x4 *>(x[t] + c0);
-                        act.load(f);
-                    }
-                }
-                acc[t] = A::mma(wi, act, acc[t]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) raw[u][t][i] = A::fetch(x[t] + c0, a.Cx - c0 - 8 * j);
+                if (i < groups && c * 128 + i * GROUP < a.C) sc[u][i % groups] = *reinterpret_cast<const seq_f32x4 *>(scale + (long long)(c * groups + i) * a.Kp);
             }
-            if (i % per == per - 1 && g0 < a.C) {
-                const seq_f32x4 sc = *reinterpret_cast<const seq_f32x4 *>(scale + (long long)(g0 / a.group) * a.Kp);
+        }
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+        for (int u = 0; u < U; ++u) {
+            const int c = first + u * waves;
+            if (c >= a.Cs) break;
+            typename A::Acc acc[NT];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(sc[e], (float)acc[t][e], sum[t][e]);
+            for (int i = 0; i < 4; ++i) {
+                if (i % per == 0)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) acc[t] = typename A::Acc{};
+                const typename A::Wt wi = A::unpack(w[u][i]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = A::mma(wi, A(raw[u][t][i]), acc[t]);
+                if (i % per == per - 1 && c * 128 + i / per * GROUP < a.C) {
+                    const seq_f32x4 s = sc[u][i / per];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(s[e], (float)acc[t][e], sum[t][e]);
+                }
             }
         }
     }
@@ -213,23 +227,27 @@ __global__ __launch_bounds__(256) void seq_mv4_unquant_kernel(const SeqMv4Args a
     }
 }
 
-template <int DT>
+template <int DT, int GROUP>
 hipError_t launch(const SeqMv4Args &a, hipStream_t s)
 {
-    int waves = 1;
-    while (waves < 8 && waves < a.Cs) waves *= 2;
+    const int waves = a.Cs < kMaxWaves ? a.Cs : kMaxWaves;
     const unsigned kt = (unsigned)(a.Kp / 16);
     if (a.M <= 16)
-        seq_mv4_kernel<DT, 1><<<dim3(kt, 1), waves * 64, 0, s>>>(a);
+        seq_mv4_kernel<DT, 1, GROUP, 2><<<dim3(kt, 1), waves * 64, 0, s>>>(a);
     else
-        seq_mv4_kernel<DT, 2><<<dim3(kt, (a.M + 31) / 32), waves * 64, 0, s>>>(a);
+        seq_mv4_kernel<DT, 2, GROUP, 1><<<dim3(kt, (a.M + 31) / 32), waves * 64, 0, s>>>(a);
     return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_group(const SeqMv4Args &a, hipStream_t s)
+{
+    return a.group == 32 ? launch<DT, 32>(a, s) : a.group == 64 ? launch<DT, 64>(a, s) : launch<DT, 128>(a, s);
 }
 }  // namespace
 
 hipError_t launch_seq_mv4(int dtype, const SeqMv4Args &a, hipStream_t s)
 {
-    return dtype == SEQ_I8 ? launch<SEQ_I8>(a, s) : dtype == SEQ_BF16 ? launch<SEQ_BF16>(a, s) : launch<SEQ_F32>(a, s);
+    return dtype == SEQ_I8 ? launch_group<SEQ_I8>(a, s) : dtype == SEQ_BF16 ? launch_group<SEQ_BF16>(a, s) : launch_group<SEQ_F32>(a, s);
 }
 hipError_t launch_seq_mv4_quant(const SeqMv4Args &a, const float *w, void *wt, float *scale, hipStream_t s)
 {

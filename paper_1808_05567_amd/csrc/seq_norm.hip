@@ -5,6 +5,8 @@
 //
 // A few operations an element: bound by memory.  A workgroup holds whole positions in registers between the sums over
 // their channels and the result, so that each tensor is read once.
+#include <type_traits>
+
 #include "seq_internal.h"
 
 namespace convmi {
@@ -12,13 +14,21 @@ namespace {
 
 constexpr int kMaxThreads = 512;
 
-// Sums (or largest unsigned) of v over the threads with the same place in the tile of LT positions, in all of them.
+// Sums (or largest unsigned) of v over the threads with the same place in the tile of LT positions, in all of them: by turns of
+// rows of 16 lanes, then between rows and halves of a wave, then in LDS.
 template <int LT, bool MAX>
 static __device__ __forceinline__ float row_sum(float v, float *lds)
 {
     auto join = [](float p, float q) { return MAX ? __uint_as_float(max(__float_as_uint(p), __float_as_uint(q))) : p + q; };
-#pragma unroll
-    for (int d = LT; d < 64; d *= 2) v = join(v, __shfl_xor(v, d));
+    auto turn = [](float p, auto by) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(p), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };
+    if constexpr (LT <= 1) v = join(v, turn(v, std::integral_constant<int, 1>()));
+    if constexpr (LT <= 2) v = join(v, turn(v, std::integral_constant<int, 2>()));
+    if constexpr (LT <= 4) v = join(v, turn(v, std::integral_constant<int, 4>()));
+    v = join(v, turn(v, std::integral_constant<int, 8>()));
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = join(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = join(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
     const int waves = blockDim.x / 64;
     if (waves == 1) return v;
     if (threadIdx.x % 64 < LT) lds[threadIdx.x / 64 * LT + threadIdx.x % 64] = v;
