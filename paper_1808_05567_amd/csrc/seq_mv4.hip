@@ -15,7 +15,7 @@
 namespace convmi {
 namespace {
 
-constexpr int kMaxWaves = 16;
+constexpr int kMaxWaves = 8;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -52,13 +52,15 @@ struct Act<SEQ_I8> {
 struct WtBf16 {
     seq_u32x4 b;
     // eight weights from a word as bf16 numbers
-    __device__ __forceinline__ explicit WtBf16(unsigned w)
+    static __device__ __forceinline__ WtBf16 of(unsigned w)
     {
+        WtBf16 r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int lo = (int)(w << (28 - 8 * i)) >> 28, hi = (int)(w << (24 - 8 * i)) >> 28;
-            b[i] = seq_pack_bf16((float)lo, (float)hi);
+            r.b[i] = seq_pack_bf16((float)lo, (float)hi);
         }
+        return r;
     }
 };
 template <>
@@ -70,7 +72,7 @@ struct Act<SEQ_BF16> {
     static __device__ __forceinline__ Raw fetch(const unsigned short *p, int left) { return left >= 8 ? seq_load(p) : seq_u32x4{}; }
     __device__ __forceinline__ explicit Act(const Raw &r) : x(r) {}
     typedef WtBf16 Wt;
-    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
+    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16::of(w); }
     static constexpr float unit = 1.0f;
     static __device__ __forceinline__ Acc mma(const Wt &w, const Act &a, const Acc &c)
     {
@@ -101,7 +103,7 @@ struct Act<SEQ_F32> {
         }
     }
     typedef WtBf16 Wt;
-    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16(w); }
+    static __device__ __forceinline__ Wt unpack(unsigned w) { return WtBf16::of(w); }
     static constexpr float unit = 1.0f;
     static __device__ __forceinline__ Acc mma(const Wt &w, const Act &a, Acc c)
     {
@@ -111,75 +113,97 @@ struct Act<SEQ_F32> {
     }
 };
 
-// A workgroup: 16 weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.  A wave has the loads of U runs on
-// their way at a time: there are few, and each is a trip to memory.  (One at a time: 4096 x 8192 for one token 10.3 us.)
-template <int DT, int NT, int GROUP, int U>
+// A workgroup: 16 * KT weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.  A wave has the loads of U runs on
+// their way at a time: there are few, and each is a trip to memory.  The activations come from the caches, once for all KT tiles of weights.
+template <int DT, int KT, int NT, int GROUP, int U>
 __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Args a)
 {
     typedef Act<DT> A;
     typedef typename A::T T;
-    __shared__ float lds[kMaxWaves * NT * 256];
+    __shared__ float lds[kMaxWaves * NT * KT * 256];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int j = lane / 16, col = lane % 16;  // operands: row or token `col`, channels 8 j ... + 7 of a run of 32
-    const int k0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
-    const seq_u32x4 *wt = static_cast<const seq_u32x4 *>(a.wt) + (long long)(k0 + col) * 4 + j;
+    const int k0 = blockIdx.x * 16 * KT, m0 = blockIdx.y * 16 * NT;
+    const seq_u32x4 *wt[KT];
+    const float *scale[KT];  // results: rows 4 j ... + 3 of a tile, token `col`
+#pragma unroll
+    for (int q = 0; q < KT; ++q) {
+        const int k = min(k0 + 16 * q, a.Kp - 16);  // (a tile past the last one is the last one, and is not stored)
+        wt[q] = static_cast<const seq_u32x4 *>(a.wt) + (long long)(k + col) * 4 + j;
+        scale[q] = a.scale + k + 4 * j;
+    }
     const T *x[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) x[t] = static_cast<const T *>(a.x) + (long long)min(m0 + t * 16 + col, a.M - 1) * a.Cx + 8 * j;
-    const float *scale = a.scale + k0 + 4 * j;  // results: rows 4 j ... + 3, token `col`
-    seq_f32x4 sum[NT] = {};
+    seq_f32x4 sum[KT][NT] = {};
     constexpr int per = GROUP / 32, groups = 4 / per;  // runs of 32 a group, groups a run of 128
     for (int first = wave; first < a.Cs; first += waves * U) {
-        seq_u32x4 w[U];
-        seq_f32x4 sc[U][groups];
+        seq_u32x4 w[U][KT];
+        seq_f32x4 sc[U][KT][groups];
         typename A::Raw raw[U][NT][4];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = first + u * waves;
             if (c >= a.Cs) break;
-            w[u] = wt[(long long)c * a.Kp * 4];
+#pragma unroll
+            for (int q = 0; q < KT; ++q) {
+                w[u][q] = wt[q][(long long)c * a.Kp * 4];
+#pragma unroll
+                for (int i = 0; i < groups; ++i)
+                    if (c * 128 + i * GROUP < a.C) sc[u][q][i] = *reinterpret_cast<const seq_f32x4 *>(scale[q] + (long long)(c * groups + i) * a.Kp);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c0 = c * 128 + i * 32;
                 // (x ends at Cx, the weights go on with zeros to the end of the run of 128)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) raw[u][t][i] = A::fetch(x[t] + c0, a.Cx - c0 - 8 * j);
-                if (i < groups && c * 128 + i * GROUP < a.C) sc[u][i % groups] = *reinterpret_cast<const seq_f32x4 *>(scale + (long long)(c * groups + i) * a.Kp);
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = first + u * waves;
             if (c >= a.Cs) break;
-            typename A::Acc acc[NT];
+            typename A::Acc acc[KT][NT];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (i % per == 0)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[t] = typename A::Acc{};
-                const typename A::Wt wi = A::unpack(w[u][i]);
+                    for (int q = 0; q < KT; ++q)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = A::mma(wi, A(raw[u][t][i]), acc[t]);
+                        for (int t = 0; t < NT; ++t) acc[q][t] = typename A::Acc{};
+                typename A::Wt wi[KT];
+#pragma unroll
+                for (int q = 0; q < KT; ++q) wi[q] = A::unpack(w[u][q][i]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const A act(raw[u][t][i]);
+#pragma unroll
+                    for (int q = 0; q < KT; ++q) acc[q][t] = A::mma(wi[q], act, acc[q][t]);
+                }
                 if (i % per == per - 1 && c * 128 + i / per * GROUP < a.C) {
-                    const seq_f32x4 s = sc[u][i / per];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                    for (int q = 0; q < KT; ++q)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(s[e], (float)acc[t][e], sum[t][e]);
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum[q][t][e] = fmaf(sc[u][q][i / per][e], (float)acc[q][t][e], sum[q][t][e]);
                 }
             }
         }
     }
+    // [wave][token][row]: the waves' parts are added in order, one result a thread
+    constexpr int ROWS = 16 * KT, TILE = NT * 16 * ROWS;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int q = 0; q < KT; ++q)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) lds[(wave * NT + t) * 256 + col * 16 + 4 * j + e] = sum[t][e];
+        for (int t = 0; t < NT; ++t)
+            *reinterpret_cast<seq_f32x4 *>(&lds[wave * TILE + (t * 16 + col) * ROWS + q * 16 + 4 * j]) = sum[q][t];
     __syncthreads();
-    // one result a thread: token i / 16, row i % 16
-    for (int i = threadIdx.x; i < NT * 256; i += blockDim.x) {
+    for (int i = threadIdx.x; i < TILE; i += blockDim.x) {
         float s = 0;
-        for (int v = 0; v < waves; ++v) s += lds[v * NT * 256 + i];
-        const int m = m0 + i / 16, k = k0 + i % 16;
+        for (int v = 0; v < waves; ++v) s += lds[v * TILE + i];
+        const int m = m0 + i / ROWS, k = k0 + i % ROWS;
         if (m >= a.M || k >= a.Ky) continue;
         s *= A::unit;
         if (a.xscale) s *= a.xscale[m];
@@ -227,16 +251,26 @@ __global__ __launch_bounds__(256) void seq_mv4_unquant_kernel(const SeqMv4Args a
     }
 }
 
+template <int DT, int GROUP, int KT>
+hipError_t launch_kt(const SeqMv4Args &a, hipStream_t s)
+{
+    constexpr int U = DT == SEQ_F32 ? 2 : 4;
+    const int threads = (a.Cs < kMaxWaves ? a.Cs : kMaxWaves) * 64;
+    const unsigned kt = (unsigned)((a.Kp / 16 + KT - 1) / KT);
+    if (a.M <= 16)
+        seq_mv4_kernel<DT, KT, 1, GROUP, U><<<dim3(kt, 1), threads, 0, s>>>(a);
+    else
+        seq_mv4_kernel<DT, KT, 2, GROUP, U / 2><<<dim3(kt, (a.M + 31) / 32), threads, 0, s>>>(a);
+    return hipGetLastError();
+}
 template <int DT, int GROUP>
 hipError_t launch(const SeqMv4Args &a, hipStream_t s)
 {
-    const int waves = a.Cs < kMaxWaves ? a.Cs : kMaxWaves;
-    const unsigned kt = (unsigned)(a.Kp / 16);
-    if (a.M <= 16)
-        seq_mv4_kernel<DT, 1, GROUP, 2><<<dim3(kt, 1), waves * 64, 0, s>>>(a);
-    else
-        seq_mv4_kernel<DT, 2, GROUP, 1><<<dim3(kt, (a.M + 31) / 32), waves * 64, 0, s>>>(a);
-    return hipGetLastError();
+    // Two tiles of weights a workgroup where there are workgroups for all compute units (256) even so; for half of them already where there
+    // are two tiles of tokens, whose reads of the activations otherwise take longer than the weights.  (4096 x 8192: 32 tokens bf16
+    // 19.5 -> 14.0 us, 48 fp32 61 -> 40, one bf16 10.4 -> 8.6, one in 8 bits 7.0 both; 24 tokens 2048 x 4100 8.9 -> 8.1; 8 tokens 1024 x 1024
+    // 3.6 -> 4.1.  Four tiles: 15.6, 29, 23, 8.0, 17, 5.4.)
+    return a.Kp / 32 >= (a.M > 16 ? 128 : 256) ? launch_kt<DT, GROUP, 2>(a, s) : launch_kt<DT, GROUP, 1>(a, s);
 }
 template <int DT>
 hipError_t launch_group(const SeqMv4Args &a, hipStream_t s)
