@@ -145,6 +145,7 @@ conv_status_t seq_conv_create(const seq_conv_desc_t *d, seq_handle_t *out)
     // in one round of workgroups that are resident together.  That is 6 a compute unit forwards; backwards, whose registers and LDS
     // go by the number of taps, 3 or 2 in bf16 and 5 or 3 in fp32.  (8 x 2048 x 2048 bf16, 4 taps, backwards: 768 workgroups 55 us, 1024 73,
     // 1536 63, 2048 73.)
+    a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
     a.cgroups = (a.Cb + 7) / 8;
     const int64_t columns = (int64_t)a.N * a.cgroups;
     const auto runs = [&](int64_t workgroups, int &range) {
@@ -368,6 +369,7 @@ conv_status_t seq_norm_create(const seq_norm_desc_t *d, seq_handle_t *out)
     a.Cp = p->info.Cp;
     a.eps = d->eps;
     a.rows = (long long)d->N * d->L;
+    a.past = a.rows * a.Cb * 16 > kSeqPastBytes;
     const struct {
         const seq_view_t &v;
         bool out;

@@ -12,7 +12,7 @@ namespace {
 // follow one another.  A workgroup: 8 blocks x 32 positions at a time.
 constexpr int kPos = 32;
 
-template <typename T, int W>
+template <typename T, int W, bool PAST>
 __global__ __launch_bounds__(256) void seq_conv_fwd_kernel(const SeqConvArgs a)
 {
     constexpr int V = SeqElem<T>::V;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void seq_conv_fwd_kernel(const SeqConvArgs a)
                 for (int i = 0; i < V; ++i) s[i] *= seq_sigmoid(s[i]);
             out = SeqElem<T>::pack(s);
         }
-        seq_store(y + l * a.vy.l, out);
+        seq_store_result<PAST>(y + l * a.vy.l, out);
     }
     if (run != 0 || !a.state_out) return;
     // The last W - 1 inputs.  By the workgroup that has read the old state, once all of it has: the new one may lie in its place.
@@ -249,7 +249,10 @@ hipError_t launch(int which, const SeqConvArgs &a, hipStream_t s)
     }
     const unsigned grid = (unsigned)((long long)a.N * a.cgroups * a.ranges);
     if (which == 0) {
-        seq_conv_fwd_kernel<T, W><<<grid, 256, 0, s>>>(a);
+        if (a.past)
+            seq_conv_fwd_kernel<T, W, true><<<grid, 256, 0, s>>>(a);
+        else
+            seq_conv_fwd_kernel<T, W, false><<<grid, 256, 0, s>>>(a);
         return hipGetLastError();
     }
     seq_conv_bwd_kernel<T, W><<<grid, 256, 0, s>>>(a);

@@ -29,6 +29,7 @@ struct SeqConvArgs {
     float *dw, *dbias;
     SeqView vx, vy, vdy, vdx;
     int N, Cb, Cp, L, silu, n_slots;
+    int past;                    // results go past the caches
     int cgroups, ranges, range;  // groups of 8 blocks; runs of positions and their length
 };
 
@@ -64,6 +65,7 @@ struct SeqNormArgs {
     long long rows;  // N * L
     float eps;
     int parts;
+    int past;  // results go past the caches
 };
 
 struct SeqMv4Args {
@@ -93,6 +95,9 @@ constexpr int seq_scan_bwd_channels(int SP) { return 512 / SP; }
 constexpr int kSeqBwdWaves = 4;
 constexpr int kSeqBwdChunk = 64;  // positions of a run of the backward kernel
 constexpr int kSeqMarks = kSeqBwdChunk / 8 - 1;
+
+// Results of more bytes than this go past the caches (the L2s hold 32 MB together).
+constexpr long long kSeqPastBytes = 16LL << 20;
 
 #ifdef __HIPCC__
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -156,6 +161,16 @@ template <typename T>
 static __device__ __forceinline__ void seq_store(T *p, const seq_u32x4 &b)
 {
     *reinterpret_cast<seq_u32x4 *>(p) = b;
+}
+
+// PAST: past the caches, for results that they would not hold until someone reads them, and that push out what is read again.
+template <bool PAST, typename T>
+static __device__ __forceinline__ void seq_store_result(T *p, const seq_u32x4 &b)
+{
+    if constexpr (PAST)
+        __builtin_nontemporal_store(b, reinterpret_cast<seq_u32x4 *>(p));
+    else
+        seq_store(p, b);
 }
 
 // V floats of an fp32 vector from block b on.

@@ -24,7 +24,7 @@ static __device__ __forceinline__ float row_sum(float v, float *lds)
     if constexpr (LT <= 1) v = join(v, turn(v, std::integral_constant<int, 1>()));
     if constexpr (LT <= 2) v = join(v, turn(v, std::integral_constant<int, 2>()));
     if constexpr (LT <= 4) v = join(v, turn(v, std::integral_constant<int, 4>()));
-    v = join(v, turn(v, std::integral_constant<int, 8>()));
+    if constexpr (LT <= 8) v = join(v, turn(v, std::integral_constant<int, 8>()));
     const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = join(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
     const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -41,7 +41,7 @@ static __device__ __forceinline__ float row_sum(float v, float *lds)
 
 // LT positions at a time, 64 / LT blocks a wave side by side: 8 x 8 where a block's positions follow one another (128 bytes),
 // 1 x 64 where a position's blocks do.  NV: blocks a thread holds; 0: more than fit, each read twice.
-template <typename T, int LT, int NV, bool Q8>
+template <typename T, int LT, int NV, bool Q8, bool PAST>
 __global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNorm
             for (int i = 0; i < V; ++i) f[i] += g[i];
             p = SeqElem<T>::pack(f);
         }
-        if (r) seq_store(r + b * a.vr.c, p);
+        if (r) seq_store_result<PAST && NV != 0>(r + b * a.vr.c, p);
         return p;
     };
     auto squares = [](const seq_u32x4 &p, float s) {
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNorm
         auto put = [&](int j, int b) {
             float f[V];
             norm(again(j, b), b, f);
-            seq_store(y + b * a.vy.c, SeqElem<T>::pack(f));
+            seq_store_result<PAST>(y + b * a.vy.c, SeqElem<T>::pack(f));
         };
         if constexpr (NV > 0) {
 #pragma unroll
@@ -285,14 +285,20 @@ template <typename T, int LT, int NV>
 hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
 {
     const unsigned grid = (unsigned)((a.rows + LT - 1) / LT);
-    if (bwd) {
+    if constexpr (LT == 16) {
+        if (bwd) return hipErrorInvalidValue;  // (goes by eight)
+    } else if (bwd) {
         const unsigned parts = grid < (unsigned)a.parts ? grid : (unsigned)a.parts;
         seq_norm_bwd_kernel<T, LT, NV><<<parts, threads, 0, s>>>(a);
         seq_norm_reduce_kernel<<<(a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, (int)parts, a.Cp);
-    } else if (a.q)
-        seq_norm_fwd_kernel<T, LT, NV, true><<<grid, threads, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    if (a.q)
+        seq_norm_fwd_kernel<T, LT, NV, true, false><<<grid, threads, 0, s>>>(a);
+    else if (a.past)
+        seq_norm_fwd_kernel<T, LT, NV, false, true><<<grid, threads, 0, s>>>(a);
     else
-        seq_norm_fwd_kernel<T, LT, NV, false><<<grid, threads, 0, s>>>(a);
+        seq_norm_fwd_kernel<T, LT, NV, false, false><<<grid, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -306,7 +312,7 @@ hipError_t launch_lt(bool bwd, const SeqNormArgs &a, hipStream_t s)
     while (threads < 256 && threads < lanes) threads *= 2;
     if (threads * 8 < lanes) threads = kMaxThreads;
     const long long nv = (lanes + threads - 1) / threads;
-    if constexpr (LT == 8 || LT == 1) {  // (what comes to 4 and 2 has more)
+    if constexpr (LT >= 8 || LT == 1) {  // (what comes to 4 and 2 has more)
         if (nv <= 1) return launch_nv<T, LT, 1>(bwd, a, threads, s);
         if (nv <= 2) return launch_nv<T, LT, 2>(bwd, a, threads, s);
         if (nv <= 4) return launch_nv<T, LT, 4>(bwd, a, threads, s);
@@ -320,10 +326,12 @@ hipError_t launch_lt(bool bwd, const SeqNormArgs &a, hipStream_t s)
 template <typename T>
 hipError_t launch_t(bool bwd, const SeqNormArgs &a, hipStream_t s)
 {
-    // one position at a time where its blocks follow one another in what is read
+    // one position at a time where its blocks follow one another in what is read; else eight, forwards sixteen where that leaves two
+    // workgroups for each compute unit (8 x 2048 x 2048 bf16 61 -> 55 us; backwards, with fewer registers left, 78 -> 86)
     constexpr int V = SeqElem<T>::V;
     const SeqView &v = bwd ? a.vr : a.vx;
-    return v.c == V || a.L == 1 ? launch_lt<T, 1>(bwd, a, s) : launch_lt<T, 8>(bwd, a, s);
+    if (v.c == V || a.L == 1) return launch_lt<T, 1>(bwd, a, s);
+    return bwd || a.rows < 16 * 512 ? launch_lt<T, 8>(bwd, a, s) : launch_lt<T, 16>(bwd, a, s);
 }
 }  // namespace
 
