@@ -15,8 +15,8 @@ namespace {
 constexpr int kMaxThreads = 512;
 
 // Sums (or largest unsigned) of v over the threads with the same place in the tile of LT positions, in all of them: by turns of
-// rows of 16 lanes, then between rows and halves of a wave, then in LDS.
-template <int LT, bool MAX>
+// rows of 16 lanes, then between rows and halves of a wave, then in LDS (ALONE: each wave has a position of its own).
+template <int LT, bool MAX, bool ALONE = false>
 static __device__ __forceinline__ float row_sum(float v, float *lds)
 {
     auto join = [](float p, float q) { return MAX ? __uint_as_float(max(__float_as_uint(p), __float_as_uint(q))) : p + q; };
@@ -30,7 +30,7 @@ static __device__ __forceinline__ float row_sum(float v, float *lds)
     const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = join(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
     const int waves = blockDim.x / 64;
-    if (waves == 1) return v;
+    if (ALONE || waves == 1) return v;
     if (threadIdx.x % 64 < LT) lds[threadIdx.x / 64 * LT + threadIdx.x % 64] = v;
     __syncthreads();
     v = lds[threadIdx.x % LT];
@@ -172,16 +172,19 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNorm
     }
 }
 
-template <typename T, int LT, int NV>
+// ALONE: each wave has positions of its own, and waits for no other until their parts of dw are added.
+template <typename T, int LT, int NV, bool ALONE>
 __global__ __launch_bounds__(kMaxThreads) void seq_norm_bwd_kernel(const SeqNormArgs a)
 {
+    static_assert(!ALONE || LT == 1, "one position a wave");
     constexpr int V = SeqElem<T>::V;
     constexpr int NK = NV ? NV : 1;
     __shared__ float lds[kMaxThreads / 64 * LT];
-    const int first = threadIdx.x / LT, step = blockDim.x / LT;
+    const int first = ALONE ? threadIdx.x % 64 : threadIdx.x / LT, step = ALONE ? 64 : blockDim.x / LT;
+    const int waves = blockDim.x / 64, each = ALONE ? waves : LT;  // positions of a workgroup at a time
     float dw[NK][V] = {};
-    for (long long tile = blockIdx.x; tile * LT < a.rows; tile += gridDim.x) {
-        const long long row = tile * LT + threadIdx.x % LT;
+    for (long long tile = blockIdx.x; tile * each < a.rows; tile += gridDim.x) {
+        const long long row = tile * each + (ALONE ? threadIdx.x / 64 : threadIdx.x % LT);
         const bool live = row < a.rows;
         const int n = live ? (int)(row / a.L) : 0, l = live ? (int)(row % a.L) : 0;
         const T *r = static_cast<const T *>(a.r) + n * a.vr.n + l * a.vr.l;
@@ -216,8 +219,8 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_bwd_kernel(const SeqNorm
                 if (first + j * step < a.Cb) sums(kr[j], ky[j], first + j * step);
         } else if (live)
             for (int b = first; b < a.Cb; b += step) sums(seq_load(r + b * a.vr.c), seq_load(dy + b * a.vdy.c), b);
-        ss = row_sum<LT, false>(ss, lds);
-        dot = row_sum<LT, false>(dot, lds);
+        ss = row_sum<LT, false, ALONE>(ss, lds);
+        dot = row_sum<LT, false, ALONE>(dot, lds);
         const float rstd = 1.0f / sqrtf(ss / a.C + a.eps);
         const float mean = dot / a.C * rstd * rstd;
         auto put = [&](const seq_u32x4 &p, const seq_u32x4 &q, int j, int b) {
@@ -257,7 +260,24 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_bwd_kernel(const SeqNorm
             }
         }
     }
-    if constexpr (NV > 0) {
+    if constexpr (ALONE) {
+        // the waves' sums in order, a block a lane at a time
+        __shared__ float sums[kMaxThreads / 64][64 * V];
+        float *part = a.part + (long long)blockIdx.x * a.Cp;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[threadIdx.x / 64][i * 64 + first] = dw[j][i];
+            __syncthreads();
+            for (int e = threadIdx.x; e < 64 * V; e += blockDim.x) {
+                const int b = j * 64 + e % 64;
+                float s = 0;
+                for (int w = 0; w < waves; ++w) s += sums[w][e];
+                if (b < a.Cb) part[(long long)b * V + e / 64] = s;
+            }
+            __syncthreads();
+        }
+    } else if constexpr (NV > 0) {
         float *part = a.part + (long long)blockIdx.x * a.Cp;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -281,6 +301,12 @@ __global__ __launch_bounds__(1024) void seq_norm_reduce_kernel(const float *part
     if (threadIdx.x < kSumColumns && c < Cp) dw[c] = s;
 }
 
+hipError_t reduce(const SeqNormArgs &a, unsigned parts, hipStream_t s)
+{
+    seq_norm_reduce_kernel<<<(a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, (int)parts, a.Cp);
+    return hipGetLastError();
+}
+
 template <typename T, int LT, int NV>
 hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
 {
@@ -289,9 +315,8 @@ hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
         if (bwd) return hipErrorInvalidValue;  // (goes by eight)
     } else if (bwd) {
         const unsigned parts = grid < (unsigned)a.parts ? grid : (unsigned)a.parts;
-        seq_norm_bwd_kernel<T, LT, NV><<<parts, threads, 0, s>>>(a);
-        seq_norm_reduce_kernel<<<(a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, (int)parts, a.Cp);
-        return hipGetLastError();
+        seq_norm_bwd_kernel<T, LT, NV, false><<<parts, threads, 0, s>>>(a);
+        return reduce(a, parts, s);
     }
     if (a.q)
         seq_norm_fwd_kernel<T, LT, NV, true, false><<<grid, threads, 0, s>>>(a);
@@ -323,6 +348,12 @@ hipError_t launch_lt(bool bwd, const SeqNormArgs &a, hipStream_t s)
     else
         return launch_nv<T, LT, 0>(bwd, a, threads, s);
 }
+template <typename T, int NV>
+hipError_t launch_alone(const SeqNormArgs &a, hipStream_t s)
+{
+    seq_norm_bwd_kernel<T, 1, NV, true><<<(unsigned)a.parts, 256, 0, s>>>(a);
+    return reduce(a, (unsigned)a.parts, s);
+}
 template <typename T>
 hipError_t launch_t(bool bwd, const SeqNormArgs &a, hipStream_t s)
 {
@@ -330,7 +361,12 @@ hipError_t launch_t(bool bwd, const SeqNormArgs &a, hipStream_t s)
     // workgroups for each compute unit (8 x 2048 x 2048 bf16 61 -> 55 us; backwards, with fewer registers left, 78 -> 86)
     constexpr int V = SeqElem<T>::V;
     const SeqView &v = bwd ? a.vr : a.vx;
-    if (v.c == V || a.L == 1) return launch_lt<T, 1>(bwd, a, s);
+    if (v.c == V || a.L == 1) {
+        // a wave each where that leaves every workgroup two for each of its waves (8 x 2048 x 2048 bf16, workgroups of one position: 85 us)
+        if (bwd && a.rows >= 8LL * a.parts && a.Cb <= 8 * 64)
+            return a.Cb <= 64 ? launch_alone<T, 1>(a, s) : a.Cb <= 2 * 64 ? launch_alone<T, 2>(a, s) : a.Cb <= 4 * 64 ? launch_alone<T, 4>(a, s) : launch_alone<T, 8>(a, s);
+        return launch_lt<T, 1>(bwd, a, s);
+    }
     return bwd || a.rows < 16 * 512 ? launch_lt<T, 8>(bwd, a, s) : launch_lt<T, 16>(bwd, a, s);
 }
 }  // namespace

@@ -13,7 +13,7 @@ U, EPS = 2.0 ** -24, 1e-5
 CASES = [  # N, C, L, residual, layout.  (The last ones: more than a workgroup holds at once.)
     (1, 8, 1, True, "dense"), (2, 5, 3, False, "slice"), (3, 40, 17, True, "rows"), (1, 130, 65, True, "dense"), (16, 4096, 1, True, "dense"),
     (2, 2048, 9, True, "dense"), (1, 1000, 7, True, "slice"), (1, 8200, 3, True, "rows"), (1, 8200, 9, False, "dense"), (2, 20000, 5, True, "dense"),
-    (3, 34000, 2, True, "rows"), (700, 16, 1, True, "dense"),
+    (3, 34000, 2, True, "rows"), (700, 16, 1, True, "dense"), (3, 520, 1500, True, "rows"), (1, 40, 4200, False, "rows"), (5, 1100, 900, True, "rows"), (2, 136, 4100, True, "dense"),
 ]
 
 
