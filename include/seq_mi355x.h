@@ -80,8 +80,8 @@ conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen);
  * there is none.  w: fp32 [W][Cp]; bias: fp32 vector or NULL; state: [slots][Cb][W-1][v] of the
  * tensors' type.
  * Errors of create: CONV_EINVAL for a NULL pointer, an extent < 1, slots < 0, an unknown type, a
- * view that is not as stated; CONV_EUNSUPPORTED beyond N, C <= 2^20, L <= 2^30, 2^39 elements a
- * tensor, and for W outside 2 ... 8. */
+ * view that is not as stated; CONV_EUNSUPPORTED beyond N, C <= 2^20, L <= 2^30, 2^31 positions
+ * and 2^39 elements a tensor, problems of more than 2^32 work-items, and for W outside 2 ... 8. */
 typedef struct {
     int32_t N, C, L, W;
     int32_t silu, slots, dtype;
@@ -89,11 +89,12 @@ typedef struct {
     seq_view_t x, y, dy, dx;
 } seq_conv_desc_t;
 conv_status_t seq_conv_create(const seq_conv_desc_t *desc, seq_handle_t *out);
-/* state_in, state_out: NULL or a state tensor; the two may be the same. */
+/* state_in, state_out: NULL or a state tensor (CONV_EINVAL for a plan without slots); the two
+ * may be the same. */
 conv_status_t seq_conv_fwd(seq_handle_t h, const void *x, const float *w, const float *bias,
                            const void *state_in, void *y, void *state_out, const int32_t *slots,
                            const int32_t *lengths, void *stream);
-/* One new position of each sequence (position 0 of x and y), the state moved on in place. */
+/* One new position of each sequence, the state moved on in place: a plan of L = 1 with slots. */
 conv_status_t seq_conv_step(seq_handle_t h, const void *x, const float *w, const float *bias,
                             void *state, void *y, const int32_t *slots, void *stream);
 /* Gradients of seq_conv_fwd without states: dx, dw (fp32 [W][Cp]), dbias (fp32 vector or NULL).
@@ -125,7 +126,7 @@ conv_status_t seq_scan_fwd(seq_handle_t h, const void *x, const void *dt, const 
                            const float *dt_bias, const float *state_in, void *y, float *state_out,
                            const int32_t *slots, const int32_t *lengths, void *ws, size_t ws_bytes,
                            void *stream);
-/* One new position of each sequence (position 0 of the tensors), the state moved on in place. */
+/* One new position of each sequence, the state moved on in place: a plan of L = 1 with slots. */
 conv_status_t seq_scan_step(seq_handle_t h, const void *x, const void *dt, const float *A,
                             const void *B, const void *C, const float *D, const void *z,
                             const float *dt_bias, float *state, void *y, const int32_t *slots,
@@ -154,7 +155,7 @@ typedef struct {
 conv_status_t seq_norm_create(const seq_norm_desc_t *desc, seq_handle_t *out);
 conv_status_t seq_norm_fwd(seq_handle_t h, const void *x, const void *res, const float *w, void *r,
                            void *y, void *stream);
-/* The same with y in 8 bits: q = y / scale rounded to nearest even, scale[n][l] = max_c |y| / 127
+/* The same with y in 8 bits: q = y / scale (by its reciprocal) rounded to nearest even, scale[n][l] = max_c |y| / 127
  * (fp32, [N][L]); a position of zeros has scale and q zero.  q: int8, a sequence tensor of
  * v = 16 whatever the others are (its view is in bytes). */
 conv_status_t seq_norm_fwd_q8(seq_handle_t h, const void *x, const void *res, const float *w,
@@ -175,7 +176,9 @@ conv_status_t seq_norm_bwd(seq_handle_t h, const void *r, const float *w, const 
  * bytes j of row k holds channels 128 b + 32 i + 8 j ... + 7, the first in the lowest bits, in
  * two's complement; rows and channels beyond K and C hold zeros.
  * Errors of create: CONV_EINVAL for extents < 1, an unknown type, a group that is not 32, 64 or
- * 128; CONV_EUNSUPPORTED beyond M <= 65536, C, K <= 2^24, K*C <= 2^39. */
+ * 128; CONV_EUNSUPPORTED beyond M <= 65536, C, K <= 2^24, K*C <= 2^39, K*M <= 2^31.
+ * fp32 activations are taken as three bf16 numbers each: their products are exact to fp32 down to
+ * 2^-109, and numbers from 3.39e38 on count as infinite. */
 typedef struct {
     int32_t M, C, K, group;
     int32_t dtype; /* of x */

@@ -27,7 +27,8 @@ struct seq_plan {
 
 namespace {
 
-constexpr int64_t kMaxElements = 1LL << 39, kMaxGrid = (1LL << 31) - 1, kMaxStride = 1LL << 40, kMaxTileStride = 1LL << 24;
+// (a launch has at most 2^32 work-items)
+constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxTileStride = 1LL << 24;
 
 bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -36,14 +37,14 @@ size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 bool sizes_ok(int N, int C, int L) { return N >= 1 && C >= 1 && L >= 1; }
 bool sizes_supported(int64_t N, int64_t C, int64_t L, int v)
 {
-    return N <= 1 << 20 && C <= 1 << 20 && L <= 1 << 30 && N * L < kMaxGrid && N * L <= kMaxElements / ((C + v - 1) / v * v);
+    return N <= 1 << 20 && C <= 1 << 20 && L <= 1 << 30 && N * L < 1LL << 31 && N * L <= kMaxElements / ((C + v - 1) / v * v);
 }
 
 // A view as the kernels take it, or false where it is not as the header says.  `out`: no two elements may share a place.
 bool view_of(const seq_view_t &v, int N, int Cb, int L, int vlen, bool out, SeqView &to)
 {
     if (v.n == 0 && v.c == 0 && v.l == 0) {
-        to = {(long long)Cb * L * vlen, (long long)L * vlen, vlen};
+        to = {(long long)Cb * L * vlen, Cb > 1 ? (long long)L * vlen : 0, vlen};
         return true;
     }
     struct {
@@ -157,14 +158,15 @@ conv_status_t seq_conv_create(const seq_conv_desc_t *d, seq_handle_t *out)
     p->bwd_ranges = runs(256 * (d->dtype == SEQ_BF16 ? d->W <= 4 ? 3 : 2 : d->W <= 4 ? 5 : 3), p->bwd_range);
     p->info.state_bytes = (size_t)a.Cb * (d->W - 1) * 16;
     p->bwd_ws = up((size_t)a.N * p->bwd_ranges * (d->W + 1) * a.Cp * 4);
-    const bool fits = columns * std::max(a.ranges, p->bwd_ranges) <= kMaxGrid;
+    const bool fits = columns * std::max(a.ranges, p->bwd_ranges) * 256 <= kMaxItems;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 
 conv_status_t seq_conv_fwd(seq_handle_t h, const void *x, const float *w, const float *bias, const void *state_in, void *y,
                            void *state_out, const int32_t *slots, const int32_t *lengths, void *stream)
 {
-    if (!h || h->kind != kConv || !given(x, w, y) || !fine(bias, state_in, state_out) || !aligned(slots, 4) || !aligned(lengths, 4))
+    if (!h || h->kind != kConv || !given(x, w, y) || !fine(bias, state_in, state_out) || !aligned(slots, 4) || !aligned(lengths, 4) ||
+        ((state_in || state_out) && h->conv.n_slots == 0))
         return CONV_EINVAL;
     SeqConvArgs a = h->conv;
     a.x = x;
@@ -181,7 +183,7 @@ conv_status_t seq_conv_fwd(seq_handle_t h, const void *x, const float *w, const 
 conv_status_t seq_conv_step(seq_handle_t h, const void *x, const float *w, const float *bias, void *state, void *y,
                             const int32_t *slots, void *stream)
 {
-    if (!h || h->kind != kConv || !given(x, w, state, y) || !fine(bias) || !aligned(slots, 4)) return CONV_EINVAL;
+    if (!h || h->kind != kConv || !given(x, w, state, y) || !fine(bias) || !aligned(slots, 4) || h->conv.n_slots == 0 || h->conv.L != 1) return CONV_EINVAL;
     SeqConvArgs a = h->conv;
     a.x = x;
     a.w = w;
@@ -267,8 +269,9 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * kSeqMarks * state) +
                 up((size_t)b.N * b.chunks * kSeqMarks * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
                 up((size_t)b.N * b.L * b.G * b.btiles * 2 * b.S * 4);
-    const int64_t grid = std::max(waves * std::max(a.chunks, b.chunks), (int64_t)b.N * b.G * b.btiles * b.chunks);
-    const bool fits = grid <= kMaxGrid && (int64_t)a.N * a.S * a.Cp <= kMaxGrid * 256 && (int64_t)b.N * b.chunks <= kMaxGrid;
+    const int64_t items[] = {waves * std::max(a.chunks, b.chunks) * 64, (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves, (int64_t)a.N * a.S * a.Cp,
+                             (int64_t)a.N * ((a.Cp + 127) / 128) * 256};
+    const bool fits = *std::max_element(items, items + 4) <= kMaxItems && (int64_t)b.N * b.chunks < 1LL << 31;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 
@@ -289,7 +292,8 @@ conv_status_t seq_scan_fwd(seq_handle_t h, const void *x, const void *dt, const 
                            const float *dt_bias, const float *state_in, void *y, float *state_out, const int32_t *slots, const int32_t *lengths, void *ws,
                            size_t ws_bytes, void *stream)
 {
-    if (!h || h->kind != kScan || !given(x, dt, A, B, C, y) || !fine(D, z, dt_bias, state_in, state_out, ws) || !aligned(slots, 4) || !aligned(lengths, 4))
+    if (!h || h->kind != kScan || !given(x, dt, A, B, C, y) || !fine(D, z, dt_bias, state_in, state_out, ws) || !aligned(slots, 4) || !aligned(lengths, 4) ||
+        ((state_in || state_out) && h->scan.n_slots == 0))
         return CONV_EINVAL;
     if (h->fwd_ws && (!ws || ws_bytes < h->fwd_ws)) return CONV_EWORKSPACE;
     SeqScanArgs a = h->scan;
@@ -307,7 +311,7 @@ conv_status_t seq_scan_fwd(seq_handle_t h, const void *x, const void *dt, const 
 conv_status_t seq_scan_step(seq_handle_t h, const void *x, const void *dt, const float *A, const void *B, const void *C, const float *D, const void *z,
                             const float *dt_bias, float *state, void *y, const int32_t *slots, void *stream)
 {
-    if (!h || h->kind != kScan || !given(x, dt, A, B, C, state, y) || !fine(D, z, dt_bias) || !aligned(slots, 4)) return CONV_EINVAL;
+    if (!h || h->kind != kScan || !given(x, dt, A, B, C, state, y) || !fine(D, z, dt_bias) || !aligned(slots, 4) || h->scan.n_slots == 0 || h->scan.L != 1) return CONV_EINVAL;
     SeqScanArgs a = h->scan;
     scan_inputs(a, x, dt, A, B, C, D, z, dt_bias);
     a.state_out = state;
@@ -440,6 +444,7 @@ conv_status_t seq_mv4_create(const seq_mv4_desc_t *d, seq_handle_t *out)
     a.Kp = (d->K + 15) / 16 * 16;
     const int vy = d->dtype == SEQ_F32 ? 4 : 8;
     a.Ky = (d->K + vy - 1) / vy * vy;
+    if ((int64_t)(a.Kp / 16) * ((a.M + 15) / 16) * 512 > kMaxItems) return finish(p, CONV_EUNSUPPORTED, out);
     p->info.wt_bytes = (size_t)a.Cs * a.Kp * 64;
     p->info.scale_bytes = (size_t)((d->C + d->group - 1) / d->group) * a.Kp * 4;
     return finish(p, CONV_OK, out);

@@ -97,7 +97,10 @@ struct Act<SEQ_F32> {
         for (int i = 0; i < 4; ++i) {
             const float p0 = i < 2 ? r.lo[2 * i] : r.hi[2 * i - 4], p1 = i < 2 ? r.lo[2 * i + 1] : r.hi[2 * i - 3];
             h[i] = seq_pack_bf16(p0, p1);
-            const float r0 = p0 - __uint_as_float(h[i] << 16), r1 = p1 - __uint_as_float(h[i] & 0xFFFF0000u);
+            // (of infinities and numbers that round to them, from 3.39e38 on, nothing is left)
+            float r0 = p0 - __uint_as_float(h[i] << 16), r1 = p1 - __uint_as_float(h[i] & 0xFFFF0000u);
+            r0 = fabsf(r0) < INFINITY ? r0 : 0.0f;
+            r1 = fabsf(r1) < INFINITY ? r1 : 0.0f;
             m[i] = seq_pack_bf16(r0, r1);
             l[i] = seq_pack_bf16(r0 - __uint_as_float(m[i] << 16), r1 - __uint_as_float(m[i] & 0xFFFF0000u));
         }

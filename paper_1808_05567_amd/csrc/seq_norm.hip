@@ -46,129 +46,132 @@ __global__ __launch_bounds__(kMaxThreads) void seq_norm_fwd_kernel(const SeqNorm
 {
     constexpr int V = SeqElem<T>::V;
     __shared__ float lds[kMaxThreads / 64 * LT];
-    const long long row = (long long)blockIdx.x * LT + threadIdx.x % LT;
-    const bool live = row < a.rows;
-    const int n = live ? (int)(row / a.L) : 0, l = live ? (int)(row % a.L) : 0;
-    const int first = threadIdx.x / LT, step = blockDim.x / LT;
-    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + l * a.vx.l;
-    const T *res = a.res ? static_cast<const T *>(a.res) + n * a.vres.n + l * a.vres.l : nullptr;
-    T *r = a.r ? static_cast<T *>(a.r) + n * a.vr.n + l * a.vr.l : nullptr;
-    auto sum_of = [&](int b) {
-        seq_u32x4 p = seq_load(x + b * a.vx.c);
-        if (res) {
-            float f[V], g[V];
-            SeqElem<T>::unpack(p, f);
-            SeqElem<T>::unpack(seq_load(res + b * a.vres.c), g);
+    // (a launch has at most 2^32 work-items)
+    for (long long tile = blockIdx.x; tile * LT < a.rows; tile += gridDim.x) {
+        const long long row = tile * LT + threadIdx.x % LT;
+        const bool live = row < a.rows;
+        const int n = live ? (int)(row / a.L) : 0, l = live ? (int)(row % a.L) : 0;
+        const int first = threadIdx.x / LT, step = blockDim.x / LT;
+        const T *x = static_cast<const T *>(a.x) + n * a.vx.n + l * a.vx.l;
+        const T *res = a.res ? static_cast<const T *>(a.res) + n * a.vres.n + l * a.vres.l : nullptr;
+        T *r = a.r ? static_cast<T *>(a.r) + n * a.vr.n + l * a.vr.l : nullptr;
+        auto sum_of = [&](int b) {
+            seq_u32x4 p = seq_load(x + b * a.vx.c);
+            if (res) {
+                float f[V], g[V];
+                SeqElem<T>::unpack(p, f);
+                SeqElem<T>::unpack(seq_load(res + b * a.vres.c), g);
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] += g[i];
-            p = SeqElem<T>::pack(f);
-        }
-        if (r) seq_store_result<PAST && NV != 0>(r + b * a.vr.c, p);
-        return p;
-    };
-    auto squares = [](const seq_u32x4 &p, float s) {
-        float f[V];
-        SeqElem<T>::unpack(p, f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s = fmaf(f[i], f[i], s);
-        return s;
-    };
-    seq_u32x4 keep[NV ? NV : 1];
-    float s = 0;
-    if constexpr (NV > 0) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int b = first + j * step;
-            keep[j] = seq_u32x4{};
-            if (live && b < a.Cb) keep[j] = sum_of(b);
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) s = squares(keep[j], s);
-    } else if (live) {
-        for (int b = first; b < a.Cb; b += step) s = squares(sum_of(b), s);
-    }
-    const float rstd = 1.0f / sqrtf(row_sum<LT, false>(s, lds) / a.C + a.eps);
-    // (the second time from where the first left it: r may lie in x's or res's place)
-    auto again = [&](int j, int b) {
-        if constexpr (NV > 0) return keep[j];
-        if (r) return seq_load(r + b * a.vr.c);
-        seq_u32x4 p = seq_load(x + b * a.vx.c);
-        if (res) {
-            float f[V], g[V];
-            SeqElem<T>::unpack(p, f);
-            SeqElem<T>::unpack(seq_load(res + b * a.vres.c), g);
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] += g[i];
-            p = SeqElem<T>::pack(f);
-        }
-        return p;
-    };
-    auto norm = [&](const seq_u32x4 &p, int b, float (&f)[V]) {
-        float w[V];
-        SeqElem<T>::unpack(p, f);
-        seq_vector<V>(a.w, b, w);
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = f[i] * rstd * w[i];
-    };
-    if constexpr (!Q8) {
-        if (!live) return;
-        T *y = static_cast<T *>(a.y) + n * a.vy.n + l * a.vy.l;
-        auto put = [&](int j, int b) {
-            float f[V];
-            norm(again(j, b), b, f);
-            seq_store_result<PAST>(y + b * a.vy.c, SeqElem<T>::pack(f));
+                for (int i = 0; i < V; ++i) f[i] += g[i];
+                p = SeqElem<T>::pack(f);
+            }
+            if (r) seq_store_result<PAST && NV != 0>(r + b * a.vr.c, p);
+            return p;
         };
+        auto squares = [](const seq_u32x4 &p, float s) {
+            float f[V];
+            SeqElem<T>::unpack(p, f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s = fmaf(f[i], f[i], s);
+            return s;
+        };
+        seq_u32x4 keep[NV ? NV : 1];
+        float s = 0;
         if constexpr (NV > 0) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (first + j * step < a.Cb) put(j, first + j * step);
-        } else
-            for (int b = first; b < a.Cb; b += step) put(0, b);
-    } else {
-        // (as unsigned numbers NaN is the largest: one in a position makes its scale NaN)
-        float m = 0;
-        auto largest = [&](int j, int b) {
-            float f[V];
-            norm(again(j, b), b, f);
+            for (int j = 0; j < NV; ++j) {
+                const int b = first + j * step;
+                keep[j] = seq_u32x4{};
+                if (live && b < a.Cb) keep[j] = sum_of(b);
+            }
 #pragma unroll
-            for (int i = 0; i < V; ++i) m = __uint_as_float(max(__float_as_uint(m), __float_as_uint(fabsf(f[i]))));
+            for (int j = 0; j < NV; ++j) s = squares(keep[j], s);
+        } else if (live) {
+            for (int b = first; b < a.Cb; b += step) s = squares(sum_of(b), s);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<LT, false>(s, lds) / a.C + a.eps);
+        // (the second time from where the first left it: r may lie in x's or res's place)
+        auto again = [&](int j, int b) {
+            if constexpr (NV > 0) return keep[j];
+            if (r) return seq_load(r + b * a.vr.c);
+            seq_u32x4 p = seq_load(x + b * a.vx.c);
+            if (res) {
+                float f[V], g[V];
+                SeqElem<T>::unpack(p, f);
+                SeqElem<T>::unpack(seq_load(res + b * a.vres.c), g);
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] += g[i];
+                p = SeqElem<T>::pack(f);
+            }
+            return p;
         };
-        if constexpr (NV > 0) {
+        auto norm = [&](const seq_u32x4 &p, int b, float (&f)[V]) {
+            float w[V];
+            SeqElem<T>::unpack(p, f);
+            seq_vector<V>(a.w, b, w);
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (live && first + j * step < a.Cb) largest(j, first + j * step);
-        } else if (live)
-            for (int b = first; b < a.Cb; b += step) largest(0, b);
-        m = row_sum<LT, true>(m, lds);
-        if (!live) return;
-        float scale = m / 127.0f;
-        if (scale < 1.17549435e-38f) scale = 0;  // (its reciprocal would be infinite)
-        if (first == 0) a.scale[row] = scale;
-        const float inv = scale == 0 ? 0 : 1.0f / scale;
-        int8_t *q = a.q + n * a.vq.n + l * a.vq.l;
-        auto put = [&](int j, int b) {
-            unsigned word[V / 4] = {};
-            if (b < a.Cb) {
+            for (int i = 0; i < V; ++i) f[i] = f[i] * rstd * w[i];
+        };
+        if constexpr (!Q8) {
+            if (!live) continue;
+            T *y = static_cast<T *>(a.y) + n * a.vy.n + l * a.vy.l;
+            auto put = [&](int j, int b) {
+                float f[V];
+                norm(again(j, b), b, f);
+                seq_store_result<PAST>(y + b * a.vy.c, SeqElem<T>::pack(f));
+            };
+            if constexpr (NV > 0) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (first + j * step < a.Cb) put(j, first + j * step);
+            } else
+                for (int b = first; b < a.Cb; b += step) put(0, b);
+        } else {
+            // (as unsigned numbers NaN is the largest: one in a position makes its scale NaN)
+            float m = 0;
+            auto largest = [&](int j, int b) {
                 float f[V];
                 norm(again(j, b), b, f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int v = (int)rintf(fminf(fmaxf(f[i] * inv, -127.0f), 127.0f));
-                    word[i / 4] |= (unsigned)(v & 255) << i % 4 * 8;
+                for (int i = 0; i < V; ++i) m = __uint_as_float(max(__float_as_uint(m), __float_as_uint(fabsf(f[i]))));
+            };
+            if constexpr (NV > 0) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (live && first + j * step < a.Cb) largest(j, first + j * step);
+            } else if (live)
+                for (int b = first; b < a.Cb; b += step) largest(0, b);
+            m = row_sum<LT, true>(m, lds);
+            if (!live) continue;
+            float scale = m / 127.0f;
+            if (scale < 1.17549435e-38f) scale = 0;  // (its reciprocal would be infinite)
+            if (first == 0) a.scale[row] = scale;
+            const float inv = scale == 0 ? 0 : 1.0f / scale;
+            int8_t *q = a.q + n * a.vq.n + l * a.vq.l;
+            auto put = [&](int j, int b) {
+                unsigned word[V / 4] = {};
+                if (b < a.Cb) {
+                    float f[V];
+                    norm(again(j, b), b, f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int v = (int)rintf(fminf(fmaxf(f[i] * inv, -127.0f), 127.0f));
+                        word[i / 4] |= (unsigned)(v & 255) << i % 4 * 8;
+                    }
                 }
-            }
-            unsigned *at = reinterpret_cast<unsigned *>(q + b * V / 16 * a.vq.c + b * V % 16);
+                unsigned *at = reinterpret_cast<unsigned *>(q + b * V / 16 * a.vq.c + b * V % 16);
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) at[i] = word[i];
-        };
-        const int blocks = (a.Cb * V + 15) / 16 * (16 / V);  // (up to the end of the last 16 channels)
-        if constexpr (NV > 0) {
+                for (int i = 0; i < V / 4; ++i) at[i] = word[i];
+            };
+            const int blocks = (a.Cb * V + 15) / 16 * (16 / V);  // (up to the end of the last 16 channels)
+            if constexpr (NV > 0) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (first + j * step < a.Cb) put(j, first + j * step);
-            for (int b = a.Cb + first; b < blocks; b += step) put(0, b);
-        } else
-            for (int b = first; b < blocks; b += step) put(0, b);
+                for (int j = 0; j < NV; ++j)
+                    if (first + j * step < a.Cb) put(j, first + j * step);
+                for (int b = a.Cb + first; b < blocks; b += step) put(0, b);
+            } else
+                for (int b = first; b < blocks; b += step) put(0, b);
+        }
     }
 }
 
@@ -310,7 +313,8 @@ hipError_t reduce(const SeqNormArgs &a, unsigned parts, hipStream_t s)
 template <typename T, int LT, int NV>
 hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((a.rows + LT - 1) / LT);
+    const long long tiles = (a.rows + LT - 1) / LT;
+    const unsigned grid = (unsigned)(tiles < 1 << 22 ? tiles : 1 << 22);
     if constexpr (LT == 16) {
         if (bwd) return hipErrorInvalidValue;  // (goes by eight)
     } else if (bwd) {

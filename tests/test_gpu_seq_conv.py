@@ -125,6 +125,38 @@ def test_gradients(N, C, L, W, silu, kind, _, layout, dtype):
     assert torch.equal(first, dw)  # (and without the bias's gradient)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_without_a_bias(dtype):
+    N, C, L, W = 2, 24, 40, 4
+    rng, x, dy, w, bias = data(N, C, L, W, dtype, 4)
+    v, bf16 = vlen(dtype), dtype == seq.SEQ_BF16
+    X, DY, Y, DX = Seq(N, C, L, dtype, "dense", x), Seq(N, C, L, dtype, "dense", dy), Seq(N, C, L, dtype), Seq(N, C, L, dtype)
+    h = seq.seq_conv_create(N, C, L, W, dtype, slots=N)
+    seq.seq_conv_fwd(h, X.t, vector(w, v), None, Y.t)
+    close(Y.get(), oracle.conv(x, w, None)[0], 16 * U * oracle.conv(x, w, None, mag=True)[0], bf16)
+    dw = nans(W, h.info.Cp)
+    seq.seq_conv_bwd(h, X.t, vector(w, v), None, DY.t, DX.t, dw, None, seq.seq_workspace(h))
+    ref, mag = oracle.conv_bwd(x, w, None, dy), oracle.conv_bwd(x, w, None, dy, mag=True)
+    close(DX.get(), ref[0], 24 * U * mag[0], bf16)
+    close(dw.double().cpu().numpy()[:, :C], ref[1], (24 + N * L) * U * mag[1], False)
+    one, y1, state = Seq(N, C, 1, dtype, "dense", x[:, :1]), Seq(N, C, 1, dtype), Seq(N, C, W - 1, dtype, "dense", np.zeros((N, W - 1, C)))
+    seq.seq_conv_step(seq.seq_conv_create(N, C, 1, W, dtype, slots=N), one.t, vector(w, v), None, state.t, y1.t)
+    np.testing.assert_array_equal(y1.get()[:, 0], Y.get()[:, 0])
+
+
+def test_tensors_of_other_strides_are_refused():
+    N, C, L, W, dtype = 2, 24, 5, 4, seq.SEQ_F32
+    rng, x, _, w, bias = data(N, C, L, W, dtype, 4)
+    X, Y, Z = Seq(N, C, L, dtype, "dense", x), Seq(N, C, L, dtype), Seq(N, C, L, dtype, "slice")
+    dense, sliced = seq.seq_conv_create(N, C, L, W, dtype), seq.seq_conv_create(N, C, L, W, dtype, views={"y": Z.t})
+    for h, y in ((dense, Z.t), (sliced, Y.t), (dense, Y.t[:, :, :4]), (dense, Y.t.bfloat16())):
+        with pytest.raises(ValueError):
+            seq.seq_conv_fwd(h, X.t, vector(w, 4), None, y)
+    seq.seq_conv_fwd(dense, X.t.contiguous().view(-1), vector(w, 4), None, Y.t)  # (dense, without dimensions)
+    seq.seq_conv_fwd(sliced, X.t, vector(w, 4), None, Z.t)
+    np.testing.assert_array_equal(Y.get(), Z.get())
+
+
 @pytest.mark.parametrize("axis", ["n", "c", "l"])
 def test_distances_beyond_32_bits(axis):
     """Each distance of a view alone takes a tensor's elements past 2^32."""

@@ -12,7 +12,7 @@ U = 2.0 ** -24
 TYPES = (seq.SEQ_F32, seq.SEQ_BF16, seq.SEQ_I8)
 CASES = [  # M, C, K, group
     (1, 128, 16, 128), (1, 4, 1, 32), (2, 200, 40, 128), (3, 100, 17, 32), (16, 1000, 72, 64), (17, 260, 33, 64), (33, 384, 130, 128),
-    (5, 33, 100, 32), (70, 2100, 20, 32), (1, 4096, 300, 128),
+    (5, 33, 100, 32), (70, 2100, 20, 32), (1, 4096, 300, 128), (2, 300, 8200, 64), (20, 160, 4130, 32), (40, 1200, 4100, 128),
 ]
 
 
@@ -89,6 +89,20 @@ def test_rows_do_not_touch_each_other():
     seq.seq_mv4(h, x, pack(q, K, C), torch.ones(4, K, device="cuda"), Y)
     bad = torch.isnan(Y).any(1).cpu()
     assert bad[3] and bad.sum() == 1
+
+
+def test_infinite_and_tiny_activations():
+    """fp32 activations beyond what three bf16 numbers hold: infinities stay infinities, what is tiny is lost at 2^-133 at most."""
+    C, K = 128, 16
+    x = torch.zeros(3, C, device="cuda")
+    x[0, 5], x[1, 7], x[2, 9] = float("inf"), 1e-35, float("nan")
+    q = np.full((K, C), 3)
+    Y = torch.empty(3, K, device="cuda")
+    h = seq.seq_mv4_create(3, C, K, 128, seq.SEQ_F32)
+    seq.seq_mv4(h, x, pack(q, K, C), torch.ones(1, K, device="cuda"), Y)
+    y = Y.cpu()
+    assert torch.isinf(y[0]).all() and torch.isnan(y[2]).all()
+    assert np.abs(y[1].double().numpy() - 3 * np.float64(np.float32(1e-35))).max() <= 3 * 2.0 ** -133
 
 
 @pytest.mark.parametrize("C,K,group", [(128, 16, 128), (200, 40, 128), (100, 17, 32), (1000, 72, 64), (7, 3, 32)])

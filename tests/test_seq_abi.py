@@ -51,6 +51,10 @@ def test_refused_problems():
     for bad in (dict(M=0), dict(group=48), dict(dtype=3), dict(dtype=-1)):
         assert status(seq.seq_mv4_create, **{**dict(M=1, C=8, K=8, group=32), **bad}) == E, bad
     assert status(seq.seq_mv4_create, (1 << 16) + 1, 8, 8, 32) == U
+    # blocks or positions too far apart for the scan's tiles, and more work-items than a launch has
+    assert status(seq.seq_scan_create, 1, 16, 1 << 23, 4) == U
+    assert status(seq.seq_conv_create, 1 << 20, 1 << 12, 1, 4) == U and status(seq.seq_scan_create, 1 << 20, 1 << 13, 1, 4) == U
+    assert status(seq.seq_mv4_create, 1 << 16, 8, 1 << 20, 32) == U
 
 
 @pytest.mark.parametrize("strides,ok_in,ok_out", [
@@ -89,6 +93,13 @@ def test_pointers_are_checked_before_any_launch():
     # a gate without its gradient, and the other way round
     assert lib.seq_scan_bwd(s._h, p, p, p, p, p, no, p, no, p, p, p, p, p, p, no, no, no, no, p, 1 << 30, no) == E
     assert lib.seq_scan_bwd(s._h, p, p, p, p, p, no, no, no, p, p, p, p, p, p, no, p, no, no, p, 1 << 30, no) == E
+    # states without slots
+    none, nos = seq.seq_conv_create(1, 8, 4, 4), seq.seq_scan_create(1, 8, 4, 4)
+    assert lib.seq_conv_fwd(none._h, p, p, p, p, p, no, no, no, no) == E and lib.seq_conv_step(none._h, p, p, p, p, p, no, no) == E
+    assert lib.seq_scan_fwd(nos._h, p, p, p, p, p, no, no, no, p, p, no, no, no, no, 0, no) == E
+    assert lib.seq_scan_step(nos._h, p, p, p, p, p, no, no, no, p, p, no, no) == E
+    # single positions by a plan of more
+    assert lib.seq_conv_step(c._h, p, p, p, p, p, no, no) == E and lib.seq_scan_step(s._h, p, p, p, p, p, no, no, no, p, p, no, no) == E
     long = seq.seq_scan_create(1, 64, 4096, 16)
     assert lib.seq_scan_fwd(long._h, p, p, p, p, p, no, no, no, no, p, no, no, no, p, 16, no) == WS
     assert lib.seq_norm_fwd(n._h, p, no, no, no, p, no) == E
