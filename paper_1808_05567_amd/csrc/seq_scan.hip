@@ -93,12 +93,12 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Lds &my = all[wave];
     // (waves share nothing: four a workgroup are one on each SIMD)
-    long long t = (long long)blockIdx.x * kWaves + wave;
-    const int tl = (int)(t % a.tiles);
-    t /= a.tiles;
-    const int g = (int)(t % a.G);
-    t /= a.G;
-    const int chunk = (int)(t % a.chunks), n = (int)(t / a.chunks);
+    unsigned t = blockIdx.x * kWaves + wave;  // (of at most 2^26 waves)
+    const int tl = t % (unsigned)a.tiles;
+    t /= (unsigned)a.tiles;
+    const int g = t % (unsigned)a.G;
+    t /= (unsigned)a.G;
+    const int chunk = t % (unsigned)a.chunks, n = t / (unsigned)a.chunks;
     if (n >= a.N) return;
     const int c0 = g * a.CG + tl * 64, c_end = min(c0 + 64, (g + 1) * a.CG);
     const int c = c0 + lane;
@@ -129,11 +129,15 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         }
     }
 
-    // a lane's blocks: block cbl of the tile's, position ll of 8.  The distance from the tile's first one fits 32 bits.
+    // A lane's blocks: block cbl of the tile's, position ll of 8.  Its places in the tensors move on by eight positions at a time: formed
+    // anew, they would wait for the kernel's arguments each time.
     const int ll = lane % 8;
     bool in[NV];
     int to[NV];
     float bias[NV][V] = {}, D[NV][V] = {};
+    const T *px[NV], *pd[NV], *pz[NV], *pg[NV];
+    T *py[NV];
+    auto place = [&](const void *p, const SeqView &v, int cb) { return static_cast<const T *>(p) + n * v.n + cb * v.c + (begin + ll) * v.l; };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int cbl = (lane + 64 * i) / 8;
@@ -142,36 +146,47 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
         const int cb = c0 / V + (in[i] ? cbl : 0);
         if (a.dt_bias) seq_vector<V>(a.dt_bias, cb, bias[i]);
         if (OUT && a.D) seq_vector<V>(a.D, cb, D[i]);
+        px[i] = place(a.x, a.vx, cb);
+        pd[i] = place(a.dt, a.vdt, cb);
+        if (ALL && a.z) pz[i] = place(a.z, a.vz, cb);
+        if (ENDS) pg[i] = place(a.dy, a.vdy, cb);
+        if (OUT) py[i] = const_cast<T *>(place(a.y, a.vy, cb));
     }
-    auto from = [&](const void *p, const SeqView &v, int i, int l0) {
-        const T *base = static_cast<const T *>(p) + n * v.n + c0 / V * v.c + l0 * v.l;
-        return base + ((unsigned)(to[i] / V) * (unsigned)v.c + (unsigned)ll * (unsigned)v.l);
-    };
-    // B and C: element r of a lane is state s of position (lane + 64 r) / SP
-    const int s_of = lane % SP < a.S ? lane % SP : 0, e_of = g * a.S + s_of;
-    auto of_states = [&](const void *p, const SeqView &v, int r, int l0) {
-        const T *base = static_cast<const T *>(p) + n * v.n + l0 * v.l;
-        return base + e_of / V * v.c + e_of % V + (lane + 64 * r) / SP * v.l;
-    };
+    const long long on_x = 8 * a.vx.l, on_d = 8 * a.vdt.l, on_z = 8 * a.vz.l, on_g = 8 * a.vdy.l, on_y = 8 * a.vy.l;
+    // B and C: element r of a lane is state lane % SP of position (lane + 64 r) / SP
+    const int e_of = g * a.S + (lane % SP < a.S ? lane % SP : 0), l_of = lane / SP;
+    const bool has = lane % SP < a.S;
+    const T *pB = static_cast<const T *>(a.B) + n * a.vB.n + e_of / V * a.vB.c + e_of % V + (begin + l_of) * a.vB.l;
+    const T *pC = ALL ? static_cast<const T *>(a.C) + n * a.vC.n + e_of / V * a.vC.c + e_of % V + (begin + l_of) * a.vC.l : nullptr;
+    const long long on_B = 64 / SP * a.vB.l, on_C = 64 / SP * a.vC.l;  // (64 / SP positions an element: E elements are eight)
 
     seq_u32x4 nx[NV], nd[NV], nz[NV], ng[NV];
     T nB[E], nC[E];
+    const bool gated = ALL && a.z;
     auto fetch = [&](int l0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             nx[i] = nd[i] = nz[i] = ng[i] = seq_u32x4{};
             if (in[i] && l0 + ll < stop) {
-                nx[i] = seq_load(from(a.x, a.vx, i, l0));
-                nd[i] = seq_load(from(a.dt, a.vdt, i, l0));
-                if (ALL && a.z) nz[i] = seq_load(from(a.z, a.vz, i, l0));
-                if (ENDS) ng[i] = seq_load(from(a.dy, a.vdy, i, l0));
+                nx[i] = seq_load(px[i]);
+                nd[i] = seq_load(pd[i]);
+                if (gated) nz[i] = seq_load(pz[i]);
+                if (ENDS) ng[i] = seq_load(pg[i]);
             }
+            px[i] += on_x;
+            pd[i] += on_d;
+            if (gated) pz[i] += on_z;
+            if (ENDS) pg[i] += on_g;
         }
 #pragma unroll
         for (int r = 0; r < E; ++r) {
-            const bool ok = lane % SP < a.S && l0 + (lane + 64 * r) / SP < stop;
-            nB[r] = ok ? *of_states(a.B, a.vB, r, l0) : T(0);
-            if (ALL) nC[r] = ok ? *of_states(a.C, a.vC, r, l0) : T(0);
+            const bool ok = has && l0 + l_of + r * (64 / SP) < stop;
+            nB[r] = ok ? *pB : T(0);
+            pB += on_B;
+            if (ALL) {
+                nC[r] = ok ? *pC : T(0);
+                pC += on_C;
+            }
         }
     };
     float sum_d = 0;
@@ -194,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
                 d[j] = !inside ? 0.0f : a.softplus ? soft : raw;
                 dx[j] = d[j] * x[i][j];
                 gate[i][j] = 1;
-                if (ALL) gate[i][j] = a.z ? z[j] * seq_sigmoid(z[j]) : 1.0f;
+                if (ALL) gate[i][j] = gated ? z[j] * seq_sigmoid(z[j]) : 1.0f;
                 if (ENDS) dy[j] *= gate[i][j];
             }
 #pragma unroll
@@ -259,16 +274,20 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
                 }
 #pragma unroll
                 for (int j = 0; j < V; ++j) y[j] = inside && c0 + to[i] + j < c_end ? fmaf(D[i][j], x[i][j], y[j]) * gate[i][j] : 0.0f;
-                seq_store(const_cast<T *>(from(a.y, a.vy, i, l0)), SeqElem<T>::pack(y));
+                seq_store(py[i], SeqElem<T>::pack(y));
             }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) py[i] += on_y;
         }
     }
     if (OUT) {
         // zeros past the end, from where the last eight positions stopped
         for (int l0 = begin + (max(stop - begin, 0) + 7) / 8 * 8; l0 < end; l0 += 8)
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (in[i] && l0 + ll < end) seq_store(const_cast<T *>(from(a.y, a.vy, i, l0)), seq_u32x4{});
+            for (int i = 0; i < NV; ++i) {
+                if (in[i] && l0 + ll < end) seq_store(py[i], seq_u32x4{});
+                py[i] += on_y;
+            }
         // the run that the last position is in stores the state, the first one that of an empty sequence
         const bool last = len == 0 ? chunk == 0 : begin < len && len <= begin + a.chunk;
         if (a.state_out && has_slot && last && live)
