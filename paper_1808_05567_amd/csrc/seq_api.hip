@@ -249,11 +249,12 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
         if (w.to.c > kMaxTileStride || w.to.l > kMaxTileStride) return finish(p, CONV_EUNSUPPORTED, out);
     }
 
-    // Forward: the sequence whole where the channels alone give every SIMD (1024) a wave, else in runs that make two.
+    // Forward: the sequence whole where the channels alone give every SIMD (1024) a wave, else in runs that make two.  Up to 64 positions whole
+    // too: a wave of its own SIMD takes some 0.3 us a position, two launches more some 15.
     a.tiles = (a.CG + 63) / 64;
     const int64_t waves = (int64_t)a.N * a.G * a.tiles;
-    const int64_t runs = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
-    a.chunk = (int)std::min<int64_t>(std::max<int64_t>((a.L + runs - 1) / runs, 16) + 7, 1 << 29) / 8 * 8;
+    const int64_t runs = waves >= 1024 || a.L <= 64 ? 1 : (2048 + waves - 1) / waves;
+    a.chunk = (int)(std::min<int64_t>(std::max<int64_t>((a.L + runs - 1) / runs, 16) + 7, 1 << 29) / 8 * 8);
     a.chunks = (int)((a.L + (int64_t)a.chunk - 1) / a.chunk);
     const size_t state = (size_t)a.S * a.Cp * 4;
     p->info.state_bytes = state;
@@ -262,12 +263,15 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
 
     SeqScanArgs &b = p->scan_bwd;
     b = a;
-    b.chunk = kSeqBwdChunk;
-    b.chunks = (int)((b.L + (int64_t)b.chunk - 1) / b.chunk);
     const int share = seq_scan_bwd_channels(seq_scan_states(b.S)) * kSeqBwdWaves;
     b.btiles = (b.CG + share - 1) / share;
-    p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * kSeqMarks * state) +
-                up((size_t)b.N * b.chunks * kSeqMarks * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
+    // Backward: runs of 64 positions, of 32 or 16 where they leave a compute unit less than two workgroups.  (8 x 48 positions of 448 channels,
+    // 16 states, bf16, in runs of 64: 71 us.)
+    for (b.chunk = 64; b.chunk > 16 && (int64_t)b.N * b.G * b.btiles * ((b.L + b.chunk - 1) / b.chunk) < 512;) b.chunk /= 2;
+    b.chunks = (int)((b.L + (int64_t)b.chunk - 1) / b.chunk);
+    b.notes = b.chunk / 8 - 1;
+    p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * b.notes * state) +
+                up((size_t)b.N * b.chunks * b.notes * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
                 up((size_t)b.N * b.L * b.G * b.btiles * 2 * b.S * 4);
     const int64_t items[] = {waves * std::max(a.chunks, b.chunks) * 64, (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves, (int64_t)a.N * a.S * a.Cp,
                              (int64_t)a.N * ((a.Cp + 127) / 128) * 256};
@@ -350,8 +354,8 @@ conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const 
     a.hl = take(runs * a.S * a.Cp);
     a.sd = take(runs * a.Cp);
     a.gl = take(runs * a.S * a.Cp);
-    a.marks = take(runs * kSeqMarks * a.S * a.Cp);
-    a.md = take(runs * kSeqMarks * a.Cp);
+    a.marks = take(runs * a.notes * a.S * a.Cp);
+    a.md = take(runs * a.notes * a.Cp);
     a.vec = take(runs * 2 * a.Cp);
     a.bc = reinterpret_cast<float *>(at);
     return done(launch_seq_scan_bwd(h->dtype, a, (hipStream_t)stream));

@@ -47,8 +47,9 @@ struct SeqScanArgs {
     float *hl;          // [N][chunks][S][Cp]: state at the end of a chunk from zeros, then at its start
     float *gl;          // the same for the gradient, back to front
     float *sd;          // [N][chunks][Cp]: sum of d over a chunk
-    float *marks;       // [N][chunks][7][S][Cp]: state from zeros at the start of a chunk's second to eighth eight
-    float *md;          // [N][chunks][7][Cp]: sum of d up to there
+    int notes;          // chunk / 8 - 1
+    float *marks;       // [N][chunks][notes][S][Cp]: state from zeros at the start of a chunk's eights but the first
+    float *md;          // [N][chunks][notes][Cp]: sum of d up to there
     float *vec;         // [N][chunks][2][Cp]: partial dD, ddt_bias
     float *bc;          // [N][L][G * btiles][2][S]: partial dB, dC
     int btiles;         // workgroups' shares of a group's channels in the backward kernel
@@ -93,8 +94,6 @@ hipError_t launch_seq_mv4_unquant(const SeqMv4Args &a, float *w, hipStream_t s);
 constexpr int seq_scan_states(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 constexpr int seq_scan_bwd_channels(int SP) { return 512 / SP; }
 constexpr int kSeqBwdWaves = 4;
-constexpr int kSeqBwdChunk = 64;  // positions of a run of the backward kernel
-constexpr int kSeqMarks = kSeqBwdChunk / 8 - 1;
 
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;

@@ -3,7 +3,7 @@
 //   g[l] = C dy + exp(d+ A) g+,   dC = sum_c dy h,   dB = sum_c g d x,   dx = D dy + d sum_s g B,
 //   dd = sum_s (A t + g B x),   dA = sum d t,   t = g exp(d A) h[l-1]
 //
-// (dy that of y before the gate.)  The states are formed again rather than kept: positions go in runs of 64.  A first launch finds
+// (dy that of y before the gate.)  The states are formed again rather than kept: positions go in runs of 64 (16 or 32 of short tensors).  A first launch finds
 // what each run does to a state and to a gradient and notes the state it reaches every 8 positions, all from zeros; a second puts
 // the runs together, so that a run knows the state before it and the gradient behind it, and with the sum of d the state at each note:
 // that from zeros plus exp(A sum d) times the one before the run.  A wave then goes through the eights of its run from the back,
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     // (the last share's waves may have no channels: they go along for the barriers)
     const int c0 = g * a.CG + (share * kWaves + wave) * WC, c_end = min(c0 + WC, (g + 1) * a.CG);
     const int len = seq_length(a.lengths, n, a.L);
-    const int begin = chunk * kSeqBwdChunk, end = min(begin + kSeqBwdChunk, a.L), stop = min(end, len);
+    const int begin = chunk * a.chunk, end = min(begin + a.chunk, a.L), stop = min(end, len);
 
     // element-wise: a lane's block and position of what is staged.  Formed anew each time, as its addresses are: kept, they cost registers.
     struct Place {
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     };
     seq_f32x2 note[4], note_d = {};
     auto fetch_note = [&](int e) {
-        const long long m = run * kSeqMarks + e - 1;
+        const long long m = run * a.notes + e - 1;
         note_d = *reinterpret_cast<const seq_f32x2 *>(a.md + m * a.Cp + (live ? c : g * a.CG));
 #pragma unroll
         for (int j = 0; j < 4; ++j) note[j] = two(a.marks + m * state, j);
@@ -418,14 +418,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     }
 }
 
-// dB and dC: the tiles' parts of a position in order; one thread a result.
+// What the runs and shares left in parts, summed in order: dA, dD, ddt_bias over the runs by the first `params` workgroups, dB and dC of each
+// position over the shares of the channels by the others, one thread a result.  (A launch each: 4.6 and 6.4 us.)
 template <typename T>
-__global__ __launch_bounds__(256) void seq_scan_bc_kernel(const SeqScanArgs a)
+__global__ __launch_bounds__(1024) void seq_scan_parts_kernel(const SeqScanArgs a, unsigned params)
 {
+    if (blockIdx.x < params) {
+        const long long state = (long long)a.S * a.Cp, col = (long long)blockIdx.x * kSumColumns + threadIdx.x % kSumColumns;
+        const bool of_A = col < state;
+        const long long e = of_A ? col : col - state, pitch = of_A ? state : 2LL * a.Cp;
+        // (results of channels beyond the last one are zero)
+        const float s = seq_sum_parts((of_A ? a.hl : a.vec) + e, pitch, a.N * a.chunks, e < pitch && e % a.Cp < a.Ch);
+        if (threadIdx.x >= kSumColumns || e >= pitch) return;
+        float *out = of_A ? a.dA + e : e < a.Cp ? (a.dD ? a.dD + e : nullptr) : a.ddt_bias ? a.ddt_bias + (e - a.Cp) : nullptr;
+        if (out) *out = s;
+        return;
+    }
     constexpr int V = SeqElem<T>::V;
     const int Sp = (a.G * a.S + V - 1) / V * V;
     const long long total = (long long)a.N * a.L * 2 * Sp;
-    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += (long long)gridDim.x * 256) {
+    for (long long t = (long long)(blockIdx.x - params) * 1024 + threadIdx.x; t < total; t += (long long)(gridDim.x - params) * 1024) {
         const int e = (int)(t % Sp), which = (int)(t / Sp % 2);
         const long long row = t / Sp / 2;
         const int n = (int)(row / a.L), l = (int)(row % a.L);
@@ -448,19 +460,6 @@ __global__ __launch_bounds__(256) void seq_scan_bc_kernel(const SeqScanArgs a)
     }
 }
 
-// dA, dD, ddt_bias: the runs' parts in order.
-__global__ __launch_bounds__(1024) void seq_scan_params_kernel(const SeqScanArgs a)
-{
-    const long long state = (long long)a.S * a.Cp, col = (long long)blockIdx.x * kSumColumns + threadIdx.x % kSumColumns;
-    const bool of_A = col < state;
-    const long long e = of_A ? col : col - state, pitch = of_A ? state : 2LL * a.Cp;
-    // (results of channels beyond the last one are zero)
-    const float s = seq_sum_parts((of_A ? a.hl : a.vec) + e, pitch, a.N * a.chunks, e < pitch && e % a.Cp < a.Ch);
-    if (threadIdx.x >= kSumColumns || e >= pitch) return;
-    float *out = of_A ? a.dA + e : e < a.Cp ? (a.dD ? a.dD + e : nullptr) : a.ddt_bias ? a.ddt_bias + (e - a.Cp) : nullptr;
-    if (out) *out = s;
-}
-
 template <typename T, int SP>
 hipError_t launch(int dtype, const SeqScanArgs &a, hipStream_t s)
 {
@@ -473,9 +472,9 @@ hipError_t launch(int dtype, const SeqScanArgs &a, hipStream_t s)
         seq_scan_bwd_kernel<T, SP, true><<<grid, 64 * kWaves, 0, s>>>(a);
     else
         seq_scan_bwd_kernel<T, SP, false><<<grid, 64 * kWaves, 0, s>>>(a);
-    const long long results = ((long long)a.N * a.L * 2 * (a.G * a.S + 7) + 255) / 256;
-    seq_scan_bc_kernel<T><<<(unsigned)(results < (1 << 20) ? results : 1 << 20), 256, 0, s>>>(a);
-    seq_scan_params_kernel<<<(unsigned)(((a.S + 2LL) * a.Cp + kSumColumns - 1) / kSumColumns), 1024, 0, s>>>(a);
+    const unsigned params = (unsigned)(((a.S + 2LL) * a.Cp + kSumColumns - 1) / kSumColumns);
+    const long long results = ((long long)a.N * a.L * 2 * (a.G * a.S + 7) + 1023) / 1024;
+    seq_scan_parts_kernel<T><<<params + (unsigned)(results < 1 << 18 ? results : 1 << 18), 1024, 0, s>>>(a, params);
     return hipGetLastError();
 }
 template <typename T>
