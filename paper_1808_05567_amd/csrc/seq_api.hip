@@ -273,7 +273,7 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * b.notes * state) +
                 up((size_t)b.N * b.chunks * b.notes * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
                 up((size_t)b.N * b.L * b.G * b.btiles * 2 * b.S * 4);
-    const int64_t items[] = {waves * std::max(a.chunks, b.chunks) * 64, (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves, (int64_t)a.N * a.S * a.Cp,
+    const int64_t items[] = {waves * std::max(a.chunks, b.chunks) * 128, (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves, (int64_t)a.N * a.S * (a.Cp + 63) * 16,
                              (int64_t)a.N * ((a.Cp + 127) / 128) * 256};
     const bool fits = *std::max_element(items, items + 4) <= kMaxItems && (int64_t)b.N * b.chunks < 1LL << 31;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);

@@ -98,6 +98,9 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     Lds &my = all[wave];
     // (waves share nothing: four a workgroup are one on each SIMD)
     unsigned t = blockIdx.x * kWaves + wave;  // (of at most 2^26 waves)
+    // (more than 32 states in two waves where no sum over them is formed: one has not the registers)
+    const int parts = OUT ? 1 : (a.S + SP - 1) / SP, s0 = OUT ? 0 : t % (unsigned)parts * SP, S = min(a.S - s0, SP);
+    if (!OUT) t /= (unsigned)parts;
     const int tl = t % (unsigned)a.tiles;
     t /= (unsigned)a.tiles;
     const int g = t % (unsigned)a.G;
@@ -114,13 +117,13 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     float A[SP], h[SP], gr[SG], P[SG];
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s < a.S ? a.A[(long long)s * a.Cp + cs] * kLog2e : 0.0f;
+        A[s] = s < S ? a.A[(long long)(s0 + s) * a.Cp + cs] * kLog2e : 0.0f;
         h[s] = 0;
         if (ENDS) gr[s % SG] = 0, P[s % SG] = 1;
     }
     const int slot = a.slots ? a.slots[n] : n;
     const bool has_slot = slot >= 0 && slot < a.n_slots;
-    const long long run = (long long)n * a.chunks + chunk, at = run * a.S * a.Cp + cs;
+    const long long run = (long long)n * a.chunks + chunk, at = (run * a.S + s0) * a.Cp + cs;
     if (OUT) {
         if (a.chunks > 1) {
 #pragma unroll
@@ -158,8 +161,8 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     }
     const long long on_x = 8 * a.vx.l, on_d = 8 * a.vdt.l, on_z = 8 * a.vz.l, on_g = 8 * a.vdy.l, on_y = 8 * a.vy.l;
     // B and C: element r of a lane is state lane % SP of position (lane + 64 r) / SP
-    const int e_of = g * a.S + (lane % SP < a.S ? lane % SP : 0), l_of = lane / SP;
-    const bool has = lane % SP < a.S;
+    const int e_of = g * a.S + s0 + (lane % SP < S ? lane % SP : 0), l_of = lane / SP;
+    const bool has = lane % SP < S;
     const T *pB = static_cast<const T *>(a.B) + n * a.vB.n + e_of / V * a.vB.c + e_of % V + (begin + l_of) * a.vB.l;
     const T *pC = ALL ? static_cast<const T *>(a.C) + n * a.vC.n + e_of / V * a.vC.c + e_of % V + (begin + l_of) * a.vC.l : nullptr;
     const long long on_B = 64 / SP * a.vB.l, on_C = 64 / SP * a.vC.l;  // (64 / SP positions an element: E elements are eight)
@@ -234,8 +237,8 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
             const long long m = run * a.notes + (l0 - begin) / 8 - 1;
 #pragma unroll
             for (int s = 0; s < SP; ++s)
-                if (s < a.S) a.marks[(m * a.S + s) * a.Cp + c] = h[s];
-            a.md[m * a.Cp + c] = sum_d;
+                if (s < S) a.marks[(m * a.S + s0 + s) * a.Cp + c] = h[s];
+            if (s0 == 0) a.md[m * a.Cp + c] = sum_d;
         }
         // one position after the other, its numbers read from LDS during the one before
         struct Position {
@@ -301,48 +304,71 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     } else if (live) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
-            if (s < a.S) {
+            if (s < S) {
                 a.hl[at + (long long)s * a.Cp] = h[s];
                 if (ENDS) a.gl[at + (long long)s * a.Cp] = gr[s % SG];
             }
-        a.sd[run * a.Cp + c] = sum_d;
+        if (s0 == 0) a.sd[run * a.Cp + c] = sum_d;
     }
 }
 
-// The state at the start of each run from those the runs end in, in place; the gradient at the end of each the same way, from the back.
-__global__ __launch_bounds__(256) void seq_scan_join_kernel(const SeqScanArgs a)
+// The state at the start of each run from those the runs end in, in place; the gradient at the end of each the same way, from the back.  The
+// waves of a workgroup (one per 16 runs, up to 16) take a part each of the runs of 64 columns: what a part does to a state is put
+// together first, then it is gone through again from the right one.  (One thread for all runs: 2 x 174 of them, both ways, 256 channels, 16 states, 30 us; so 11.)
+constexpr int kJoinParts = 16;
+__global__ __launch_bounds__(64 * kJoinParts) void seq_scan_join_kernel(const SeqScanArgs a)
 {
-    const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long state = (long long)a.S * a.Cp;
-    if (t >= a.N * state) return;
-    const int n = (int)(t / state), c = (int)(t % a.Cp);
-    const long long e = t % state;
-    if (c >= a.Ch) return;
+    __shared__ float of_zero[kJoinParts][64], of_d[kJoinParts][64];
+    const int lane = threadIdx.x % 64, part = threadIdx.x / 64, parts = blockDim.x / 64;
+    const long long state = (long long)a.S * a.Cp, columns = (state + 63) / 64;
+    const int n = (int)(blockIdx.x / columns);
+    const long long e = blockIdx.x % columns * 64 + lane;
+    const int c = (int)(e % a.Cp);
+    const bool live = e < state && c < a.Ch;
     const int slot = a.slots ? a.slots[n] : n;
-    const float A = a.A[e] * kLog2e;
-    const float first = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f;
+    const float A = live ? a.A[e] * kLog2e : 0.0f;
+    const int each = (a.chunks + parts - 1) / parts, begin = min(part * each, a.chunks), end = min(begin + each, a.chunks);
     const float *sd = a.sd + (long long)n * a.chunks * a.Cp + c;
-    // what a run adds and the sum of its d come 32 runs at a time, ahead of the chain that they go into
-    const auto chain = [&](float *ends, float h, bool back) {
+    const auto chain = [&](float *ends, float first, bool back) {
         ends += (long long)n * a.chunks * state + e;
-        for (int k0 = 0; k0 < a.chunks; k0 += 32) {
-            float own[32], d[32];
+        // what a run adds and the sum of its d come 16 runs at a time, ahead of the chain that they go into
+        float own[16], d[16];
+        const auto load = [&](int k0) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16; ++i) {
                 const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
-                const bool ok = k0 + i < a.chunks;
+                const bool ok = live && k0 + i < end;
                 own[i] = ok ? ends[k * state] : 0.0f;
                 d[i] = ok ? sd[(long long)k * a.Cp] : 0.0f;
             }
+        };
+        float h = 0, sum = 0;
+        for (int k0 = begin; k0 < end; k0 += 16) {
+            load(k0);
+            if (part == parts - 1) break;  // (no part is after it; up to 16 runs are in registers now)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16; ++i) {
+                h = fmaf(seq_exp2(A * d[i]), h, own[i]);
+                sum += d[i];
+            }
+        }
+        of_zero[part][lane] = h;
+        of_d[part][lane] = sum;
+        __syncthreads();
+        h = first;
+        for (int p = 0; p < part; ++p) h = fmaf(seq_exp2(A * of_d[p][lane]), h, of_zero[p][lane]);
+        for (int k0 = begin; k0 < end; k0 += 16) {
+            if (each > 16) load(k0);  // (or still there)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
                 const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
-                if (k0 + i < a.chunks) ends[k * state] = h;
+                if (live && k0 + i < end) ends[k * state] = h;
                 h = fmaf(seq_exp2(A * d[i]), h, own[i]);
             }
         }
+        __syncthreads();
     };
-    chain(a.hl, first, false);
+    chain(a.hl, live && a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[slot * state + e] : 0.0f, false);
     if (a.gl) chain(a.gl, 0.0f, true);
 }
 
@@ -423,33 +449,38 @@ __global__ __launch_bounds__(256) void seq_scan_step_kernel(const SeqScanArgs a)
     *reinterpret_cast<Two *>(static_cast<T *>(a.y) + at(a.vy, c)) = out;
 }
 
-template <typename T, int SP>
-hipError_t launch(const SeqScanArgs &a, hipStream_t s)
+hipError_t join(const SeqScanArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(((long long)a.N * a.G * a.tiles * a.chunks + kWaves - 1) / kWaves);
-    if (a.chunks > 1) {
-        seq_scan_kernel<T, SP, 0><<<grid, 64 * kWaves, 0, s>>>(a);
-        seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
-    }
-    seq_scan_kernel<T, SP, 1><<<grid, 64 * kWaves, 0, s>>>(a);
+    const int parts = a.chunks <= 16 * kJoinParts ? (a.chunks + 15) / 16 : kJoinParts;
+    seq_scan_join_kernel<<<(unsigned)(a.N * (((long long)a.S * a.Cp + 63) / 64)), 64 * parts, 0, s>>>(a);
     return hipGetLastError();
 }
-template <typename T, int SP>
+template <typename T, int SP, int MODE>
+hipError_t launch_mode(const SeqScanArgs &a, hipStream_t s)
+{
+    const long long waves = (long long)a.N * a.G * a.tiles * a.chunks * (MODE == 1 ? 1 : (a.S + SP - 1) / SP);
+    seq_scan_kernel<T, SP, MODE><<<(unsigned)((waves + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int MODE>
 hipError_t launch_ends(const SeqScanArgs &a, hipStream_t s)
 {
-    seq_scan_kernel<T, SP, 2><<<(unsigned)(((long long)a.N * a.G * a.tiles * a.chunks + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a);
-    if (a.chunks > 1) seq_scan_join_kernel<<<(unsigned)(((long long)a.N * a.S * a.Cp + 255) / 256), 256, 0, s>>>(a);
-    return hipGetLastError();
+    return a.S <= 8 ? launch_mode<T, 8, MODE>(a, s) : a.S <= 16 ? launch_mode<T, 16, MODE>(a, s) : launch_mode<T, 32, MODE>(a, s);
 }
 template <typename T>
 hipError_t launch_t(bool ends, const SeqScanArgs &a, hipStream_t s)
 {
-    switch (seq_scan_states(a.S)) {
-        case 8: return ends ? launch_ends<T, 8>(a, s) : launch<T, 8>(a, s);
-        case 16: return ends ? launch_ends<T, 16>(a, s) : launch<T, 16>(a, s);
-        case 32: return ends ? launch_ends<T, 32>(a, s) : launch<T, 32>(a, s);
+    if (ends || a.chunks > 1) {
+        hipError_t e = ends ? launch_ends<T, 2>(a, s) : launch_ends<T, 0>(a, s);
+        if (e == hipSuccess && a.chunks > 1) e = join(a, s);
+        if (ends || e != hipSuccess) return e;
     }
-    return ends ? launch_ends<T, 64>(a, s) : launch<T, 64>(a, s);
+    switch (seq_scan_states(a.S)) {
+        case 8: return launch_mode<T, 8, 1>(a, s);
+        case 16: return launch_mode<T, 16, 1>(a, s);
+        case 32: return launch_mode<T, 32, 1>(a, s);
+    }
+    return launch_mode<T, 64, 1>(a, s);
 }
 }  // namespace
 

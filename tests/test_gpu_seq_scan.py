@@ -184,6 +184,31 @@ def test_distances_beyond_32_bits(axis):
         close(got, r[k], (2 * bound(L) + C * U) * m[k], True, k)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_runs(dtype):
+    """Sequences in more runs than 16 waves take at once, in both directions; the second one ends early."""
+    N, C, L, S = 2, 8, 20011, 3
+    rng, p = data(N, C, L, S, 1, dtype, 6)
+    p["A"] = np.float64(np.float32(-np.logspace(-4, 0, S)[:, None] * np.ones((1, C))))
+    lengths = np.array([L, L - 7000])
+    t, opt, A, ref = tensors(p, N, C, L, S, 1, True, True, lengths, "dense", dtype)
+    Y, DY = Seq(N, C, L, dtype), Seq(N, C, L, dtype, "dense", spoil(p["dy"], lengths))
+    out = {k: Seq(N, c, L, dtype) for k, c in (("dx", C), ("ddt", C), ("dz", C), ("dB", S), ("dC", S))}
+    h = seq.seq_scan_create(N, C, L, S, dtype)
+    ws = seq.seq_workspace(h).fill_(0xFF)
+    seq.seq_scan_fwd(h, t["x"].t, t["dt"].t, A, t["B"].t, t["C"].t, Y.t, ws, z=t["z"].t, lengths=ints(lengths), **opt)
+    args = (p["x"], p["dt"], p["A"], p["B"], p["Cm"])
+    close(Y.get(), oracle.scan(*args, **ref)[0], bound(L) * oracle.scan(*args, **ref, mag=True)[0], dtype == seq.SEQ_BF16, "y")
+    dA, dD, db = nans(S, h.info.Cp), nans(h.info.Cp), nans(h.info.Cp)
+    seq.seq_scan_bwd(h, t["x"].t, t["dt"].t, A, t["B"].t, t["C"].t, DY.t, out["dx"].t, out["ddt"].t, dA, out["dB"].t, out["dC"].t, ws,
+                     z=t["z"].t, dD=dD, dz=out["dz"].t, ddt_bias=db, lengths=ints(lengths), **opt)
+    r, m = oracle.scan_bwd(*args, p["dy"], **ref), oracle.scan_bwd(*args, p["dy"], **ref, mag=True)
+    for k, q in out.items():
+        close(q.get(), r[k], (2 * bound(L) + C * U) * m[k], dtype == seq.SEQ_BF16, k)
+    for k, got in (("dA", dA), ("dD", dD), ("ddt_bias", db)):
+        close(got.double().cpu().numpy()[..., :C], r[k], (2 * bound(L) + N * L * U) * m[k], False, k)
+
+
 def test_long_decays_and_large_steps():
     """States that nothing leaves and steps that leave nothing of a state: exp(d A) from 1 - 1e-6 to 0."""
     N, C, L, S, dtype = 1, 64, 700, 16, seq.SEQ_F32
