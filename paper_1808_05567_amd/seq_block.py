@@ -250,7 +250,11 @@ def main():
     print("forward and backward %.0f us" % timed(lambda: (block.forward(x, res), block.backward(dout, dr))))
     step, states = SeqBlockStep(block, M), block.states()
     x1, r1 = (torch.randn(M, C // 8, 1, 8, device="cuda").to(torch.bfloat16) for _ in range(2))
-    print("one token of %d sequences, 4-bit weights %.1f us" % (M, timed(lambda: step(x1, r1, states), 200)))
+    each = timed(lambda: step(x1, r1, states), 200)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(x1, r1, states)
+    print("one token of %d sequences, 4-bit weights %.1f us, captured %.1f us" % (M, each, timed(graph.replay, 200)))
 
 
 if __name__ == "__main__":

@@ -98,3 +98,33 @@ def test_single_tokens_continue_prompts():
         w = want[n, :, end:end + extra].float()
         got = torch.stack([t[n, :, 0] for t in tokens], 1).float()
         assert (got - w).norm() <= 0.05 * w.norm(), (n, float((got - w).norm() / w.norm()))
+
+
+def test_captured_tokens():
+    """Single tokens recorded once: every replay leaves the output and the states that a call leaves."""
+    N, C, Ci, S, W = 5, 136, 200, 16, 4
+    block = seq_block.SeqBlock(N, 8, C, Ci, S, W, seq_block.init(C, Ci, S, W, seed=4), slots=N + 2)
+    g = torch.Generator("cuda").manual_seed(5)
+    tokens = [[torch.randn(N, C // 8, 1, 8, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2)] for _ in range(4)]
+    at = torch.tensor([4, 0, 6, 1, -1], dtype=torch.int32, device="cuda")
+    step = seq_block.SeqBlockStep(block, N)
+    states, want = block.states(), []
+    for x, r in tokens:
+        out, after = step(x, r, states, at)
+        want.append([t.clone() for t in (out, after, *states)])
+    x, r, again = *(torch.empty_like(t) for t in tokens[0]), block.states()
+    x.copy_(tokens[0][0])
+    r.copy_(tokens[0][1])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out, after = step(x, r, again, at)
+    for t in again:
+        t.zero_()
+    for token, w in zip(tokens, want):
+        x.copy_(token[0])
+        r.copy_(token[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, t in zip((out, after, *again), w):
+            assert torch.equal(got, t)
