@@ -188,7 +188,8 @@ conv_status_t seq_mv4_create(const seq_mv4_desc_t *desc, seq_handle_t *out);
 conv_status_t seq_mv4(seq_handle_t h, const void *x, const float *xscale, const void *wt,
                       const float *scale, const float *bias, void *y, void *stream);
 /* Weights laid out once: q = w / scale rounded to nearest even and clamped, scale = max |w| of the
- * group / 7 (0 for a group of zeros).  w: fp32 [K][C], logical. */
+ * group / 7 (0 for a group of zeros; NaN, and q zero, for one that holds a NaN or an infinity).
+ * w: fp32 [K][C], logical. */
 conv_status_t seq_mv4_quant(seq_handle_t h, const float *w, void *wt, float *scale, void *stream);
 /* And back: w[k][c] = q * scale. */
 conv_status_t seq_mv4_unquant(seq_handle_t h, const void *wt, const float *scale, float *w,

@@ -229,14 +229,16 @@ __global__ __launch_bounds__(256) void seq_mv4_quant_kernel(const SeqMv4Args a, 
         const long long t = base + threadIdx.x;
         const int u = (int)(t % 16), k = (int)(t / 16 % a.Kp), cs = (int)(t / 16 / a.Kp);
         const int c0 = cs * 128 + u * 8;  // word i = u / 4 of the bytes j = u % 4
-        float f[8], m = 0;
+        float f[8];
+        unsigned m = 0;  // (as unsigned numbers NaN is the largest)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             f[e] = k < a.K && c0 + e < a.C ? w[(long long)k * a.C + c0 + e] : 0.0f;
-            m = fmaxf(m, fabsf(f[e]));
+            m = max(m, __float_as_uint(fabsf(f[e])));
         }
-        for (int d = 1; d < a.group / 8; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-        const float s = m / 7.0f;
+        for (int d = 1; d < a.group / 8; d *= 2) m = max(m, (unsigned)__shfl_xor((int)m, d));
+        // (no scale holds a group with an infinity: its products are no numbers, rather than wrong ones)
+        const float s = m < 0x7F800000u ? __uint_as_float(m) / 7.0f : __builtin_nanf("");
         unsigned word = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) word |= ((unsigned)(int)rintf(fminf(fmaxf(s > 0 ? f[e] / s : 0.0f, -8.0f), 7.0f)) & 15u) << 4 * e;

@@ -129,3 +129,22 @@ def test_laying_out_weights(C, K, group):
     back = nans(K, C)
     seq.seq_mv4_unquant(h, wt, sc, back)
     assert np.all(np.abs(back.cpu().numpy() - w) <= per * (0.5 + 2.0 ** -20))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_groups_without_a_scale(bad):
+    """A NaN or an infinity in a group: its scale is NaN, so that its products are, and the others stay as they are."""
+    C, K, group = 96, 20, 32
+    w = torch.linspace(-1, 1, K * C, device="cuda").reshape(K, C)
+    h = seq.seq_mv4_create(1, C, K, group, seq.SEQ_BF16)
+    out = []
+    for value in (0.0, bad):
+        w[3, 40] = value
+        wt, sc = torch.empty(h.info.wt_bytes, dtype=torch.uint8, device="cuda"), nans(h.info.scale_bytes // 4)
+        back = nans(K, C)
+        seq.seq_mv4_quant(h, w, wt, sc)
+        seq.seq_mv4_unquant(h, wt, sc, back)
+        out.append(back.cpu())
+    hit = torch.zeros(K, C, dtype=torch.bool)
+    hit[3, 32:64] = True
+    assert torch.isnan(out[1][hit]).all() and torch.equal(out[0][~hit], out[1][~hit])
