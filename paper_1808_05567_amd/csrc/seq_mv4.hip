@@ -124,7 +124,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
 {
     typedef Act<DT> A;
     typedef typename A::T T;
-    __shared__ float lds[kMaxWaves * NT * KT * 256];
+    // (a token's rows and four floats more: sixteen tokens' blocks of 16 bytes go to different banks)
+    constexpr int ROWS = 16 * KT, PITCH = ROWS + 4, TILE = NT * 16 * PITCH;
+    __shared__ __align__(16) float lds[kMaxWaves * TILE];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int j = lane / 16, col = lane % 16;  // operands: row or token `col`, channels 8 j ... + 7 of a run of 32
     const int k0 = blockIdx.x * 16 * KT, m0 = blockIdx.y * 16 * NT;
@@ -197,16 +199,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
         }
     }
     // [wave][token][row]: the waves' parts are added in order, one result a thread
-    constexpr int ROWS = 16 * KT, TILE = NT * 16 * ROWS;
 #pragma unroll
     for (int q = 0; q < KT; ++q)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            *reinterpret_cast<seq_f32x4 *>(&lds[wave * TILE + (t * 16 + col) * ROWS + q * 16 + 4 * j]) = sum[q][t];
+            *reinterpret_cast<seq_f32x4 *>(&lds[wave * TILE + (t * 16 + col) * PITCH + q * 16 + 4 * j]) = sum[q][t];
     __syncthreads();
-    for (int i = threadIdx.x; i < TILE; i += blockDim.x) {
+    for (int i = threadIdx.x; i < NT * 16 * ROWS; i += blockDim.x) {
         float s = 0;
-        for (int v = 0; v < waves; ++v) s += lds[v * TILE + i];
+        for (int v = 0; v < waves; ++v) s += lds[v * TILE + i / ROWS * PITCH + i % ROWS];
         const int m = m0 + i / ROWS, k = k0 + i % ROWS;
         if (m >= a.M || k >= a.Ky) continue;
         s *= A::unit;
