@@ -10,7 +10,7 @@
 // a group of 32, 64 or 128 channels is one, two or four of them, whatever its scale.
 //
 // Bound by the weights' bytes for few rows: 4096 x 8192 for one token in 8 bits 7.0 us (18 MB, 2.5 TB/s, of which a launch and a first trip to memory
-// are some 4 us), in bf16 8.6, for 32 tokens 14.
+// are some 4 us), in bf16 8.3; for 32 tokens 7.9 and 10.0, for 64 11.4 and 14.6, in fp32 14 for one, 20 for 32.
 #include "seq_internal.h"
 
 namespace convmi {
@@ -119,14 +119,19 @@ struct Act<SEQ_F32> {
 
 // A workgroup: 16 * KT weight rows, 16 * NT tokens, all channels, the runs of 128 dealt to its waves in turn.  A wave has the loads of U runs on
 // their way at a time: there are few, and each is a trip to memory.  The activations come from the caches, once for all KT tiles of weights.
-template <int DT, int KT, int NT, int GROUP, int U>
+//
+// STAGE: several tokens.  Loaded as the instructions want them a token's 128 channels are four loads of a quarter (8 bits) or half of each of its
+// cache lines, 16 tokens' lines at a time, and the caches take longer to look these up than to deliver them.  So a wave loads whole lines and
+// turns them in an LDS area of its own.
+template <int DT, int KT, int NT, int GROUP, int U, bool STAGE>
 __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Args a)
 {
     typedef Act<DT> A;
     typedef typename A::T T;
-    // (a token's rows and four floats more: sixteen tokens' blocks of 16 bytes go to different banks)
-    constexpr int ROWS = 16 * KT, PITCH = ROWS + 4, TILE = NT * 16 * PITCH;
-    __shared__ __align__(16) float lds[kMaxWaves * TILE];
+    // (a token's rows, or channels, and 16 bytes more: sixteen tokens' blocks of 16 bytes go to different banks)
+    constexpr int ROWS = 16 * KT, PITCH = ROWS + 4, LINE = 128 * sizeof(T) + 16, TOKEN = STAGE && LINE > PITCH * 4 ? LINE / 4 : PITCH, AREA = NT * 16 * TOKEN;
+    constexpr int PIECES = 128 * sizeof(T) / 16, PART = 16 / sizeof(T), LOADS = NT * 16 * PIECES / 64;  // of 16 bytes a token; channels of one
+    __shared__ __align__(16) float lds[kMaxWaves * AREA];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const int j = lane / 16, col = lane % 16;  // operands: row or token `col`, channels 8 j ... + 7 of a run of 32
     const int k0 = blockIdx.x * 16 * KT, m0 = blockIdx.y * 16 * NT;
@@ -141,12 +146,21 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
     const T *x[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) x[t] = static_cast<const T *>(a.x) + (long long)min(m0 + t * 16 + col, a.M - 1) * a.Cx + 8 * j;
+    // staged: load r is piece lane % PIECES of token (lane + 64 r) / PIECES
+    const int piece = lane % PIECES * PART;
+    char *const mine = reinterpret_cast<char *>(lds + wave * AREA), *const to = mine + lane / PIECES * LINE + lane % PIECES * 16;
+    const char *const from = mine + col * LINE + 8 * j * sizeof(T);
+    const T *xs[STAGE ? LOADS : 1];
+    if (STAGE)
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) xs[r] = static_cast<const T *>(a.x) + (long long)min(m0 + (lane + 64 * r) / PIECES, a.M - 1) * a.Cx + piece;
     seq_f32x4 sum[KT][NT] = {};
     constexpr int per = GROUP / 32, groups = 4 / per;  // runs of 32 a group, groups a run of 128
     for (int first = wave; first < a.Cs; first += waves * U) {
         seq_u32x4 w[U][KT];
         seq_f32x4 sc[U][KT][groups];
-        typename A::Raw raw[U][NT][4];
+        typename A::Raw raw[STAGE ? 1 : U][NT][4];
+        seq_u32x4 whole[STAGE ? U : 1][STAGE ? LOADS : 1];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = first + u * waves;
@@ -158,18 +172,30 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
                 for (int i = 0; i < groups; ++i)
                     if (c * 128 + i * GROUP < a.C) sc[u][q][i] = *reinterpret_cast<const seq_f32x4 *>(scale[q] + (long long)(c * groups + i) * a.Kp);
             }
+            // (x ends at Cx, the weights go on with zeros to the end of the run of 128)
+            if constexpr (STAGE) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c0 = c * 128 + i * 32;
-                // (x ends at Cx, the weights go on with zeros to the end of the run of 128)
+                for (int r = 0; r < LOADS; ++r) {
+                    whole[u][r] = seq_u32x4{};
+                    if (c * 128 + piece < a.Cx) whole[u][r] = seq_load(xs[r] + c * 128);
+                }
+            } else {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) raw[u][t][i] = A::fetch(x[t] + c0, a.Cx - c0 - 8 * j);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) raw[u][t][i] = A::fetch(x[t] + c * 128 + i * 32, a.Cx - c * 128 - i * 32 - 8 * j);
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = first + u * waves;
             if (c >= a.Cs) break;
+            if constexpr (STAGE) {
+                seq_wave_sync();
+#pragma unroll
+                for (int r = 0; r < LOADS; ++r) *reinterpret_cast<seq_u32x4 *>(to + r * (64 / PIECES) * LINE) = whole[u][r];
+                seq_wave_sync();
+            }
             typename A::Acc acc[KT][NT];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -183,7 +209,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
                 for (int q = 0; q < KT; ++q) wi[q] = A::unpack(w[u][q][i]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const A act(raw[u][t][i]);
+                    if constexpr (STAGE) raw[0][t][i] = A::fetch(reinterpret_cast<const T *>(from + t * 16 * LINE) + 32 * i, 8);
+                    const A act(raw[STAGE ? 0 : u][t][i]);
 #pragma unroll
                     for (int q = 0; q < KT; ++q) acc[q][t] = A::mma(wi[q], act, acc[q][t]);
                 }
@@ -199,15 +226,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void seq_mv4_kernel(const SeqMv4Arg
         }
     }
     // [wave][token][row]: the waves' parts are added in order, one result a thread
+    if (STAGE) seq_wave_sync();
 #pragma unroll
     for (int q = 0; q < KT; ++q)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            *reinterpret_cast<seq_f32x4 *>(&lds[wave * TILE + (t * 16 + col) * PITCH + q * 16 + 4 * j]) = sum[q][t];
+            *reinterpret_cast<seq_f32x4 *>(&lds[wave * AREA + (t * 16 + col) * PITCH + q * 16 + 4 * j]) = sum[q][t];
     __syncthreads();
     for (int i = threadIdx.x; i < NT * 16 * ROWS; i += blockDim.x) {
         float s = 0;
-        for (int v = 0; v < waves; ++v) s += lds[v * TILE + i / ROWS * PITCH + i % ROWS];
+        for (int v = 0; v < waves; ++v) s += lds[v * AREA + i / ROWS * PITCH + i % ROWS];
         const int m = m0 + i / ROWS, k = k0 + i % ROWS;
         if (m >= a.M || k >= a.Ky) continue;
         s *= A::unit;
@@ -258,25 +286,39 @@ __global__ __launch_bounds__(256) void seq_mv4_unquant_kernel(const SeqMv4Args a
     }
 }
 
+template <int DT, int GROUP, int KT, int NT, int U, bool STAGE>
+hipError_t launch_nt(const SeqMv4Args &a, hipStream_t s)
+{
+    const int threads = (a.Cs < kMaxWaves ? a.Cs : kMaxWaves) * 64;
+    seq_mv4_kernel<DT, KT, NT, GROUP, U, STAGE><<<dim3((a.Kp / 16 + KT - 1) / KT, (a.M + 16 * NT - 1) / (16 * NT)), threads, 0, s>>>(a);
+    return hipGetLastError();
+}
 template <int DT, int GROUP, int KT>
 hipError_t launch_kt(const SeqMv4Args &a, hipStream_t s)
 {
-    constexpr int U = DT == SEQ_F32 ? 2 : 4;
-    const int threads = (a.Cs < kMaxWaves ? a.Cs : kMaxWaves) * 64;
-    const unsigned kt = (unsigned)((a.Kp / 16 + KT - 1) / KT);
-    if (a.M <= 16)
-        seq_mv4_kernel<DT, KT, 1, GROUP, U><<<dim3(kt, 1), threads, 0, s>>>(a);
-    else
-        seq_mv4_kernel<DT, KT, 2, GROUP, U / 2><<<dim3(kt, (a.M + 31) / 32), threads, 0, s>>>(a);
-    return hipGetLastError();
+    // Staged from five tokens on; not fp32, of which a token's quarter of a run is a whole line (48 tokens of 4096 x 8192 44 us both).
+    constexpr bool STAGE = DT != SEQ_F32;
+    constexpr int U = STAGE && !(DT == SEQ_BF16 && GROUP == 32 && KT == 2) ? 4 : 2;  // (as many as the registers hold)
+    if (a.M <= 4) return launch_nt<DT, GROUP, KT, 1, U, false>(a, s);
+    if (a.M <= 16) return launch_nt<DT, GROUP, KT, 1, U, STAGE>(a, s);
+    if constexpr (KT > 1) {
+        // The tokens by up to four tiles of 16 a workgroup (fp32 three: 64 tokens 42 and 40 us), evenly: for each share the weights come again.  (48 tokens of 4096 x 8192, by
+        // twos and by threes: 8 bits 14.2 and 9.9 us, fp32 43 and 31.  Few weights want the workgroups: 1024 x 2048 in 8 bits 3.5 and 4.2.)
+        constexpr int most = STAGE ? 4 : 3;
+        const int tiles = (a.M + 15) / 16, rows = (tiles + most - 1) / most, each = (tiles + rows - 1) / rows;
+        if (each == 3) return launch_nt<DT, GROUP, KT, 3, 1, STAGE>(a, s);
+        if constexpr (STAGE)
+            if (each == 4) return launch_nt<DT, GROUP, KT, 4, 1, STAGE>(a, s);
+    }
+    return launch_nt<DT, GROUP, KT, 2, STAGE ? 2 : 1, STAGE>(a, s);
 }
 template <int DT, int GROUP>
 hipError_t launch(const SeqMv4Args &a, hipStream_t s)
 {
     // Two tiles of weights a workgroup where there are workgroups for all compute units (256) even so; for half of them already where there
-    // are two tiles of tokens, whose reads of the activations otherwise take longer than the weights.  (4096 x 8192: 32 tokens bf16
-    // 19.5 -> 14.0 us, 48 fp32 61 -> 40, one bf16 10.4 -> 8.6, one in 8 bits 7.0 both; 24 tokens 2048 x 4100 8.9 -> 8.1; 8 tokens 1024 x 1024
-    // 3.6 -> 4.1.  Four tiles: 15.6, 29, 23, 8.0, 17, 5.4.)
+    // are two tiles of tokens, whose turns through LDS otherwise take longer than the weights.  (One tile and two: 4096 x 8192, 32 tokens bf16 12.9
+    // and 10.8 us, 48 fp32 63 and 32, one 8.2 both; 24 tokens 2048 x 4100 8.4 and 6.8, 2048 x 2048 5.5 and 6.6; 16 in 8 bits 4096 x 4096
+    // 5.7 and 6.7; 8 bf16 1024 x 1024 3.6 and 4.0.  Four tiles: 24 tokens 2048 x 4100 11.6.)
     return a.Kp / 32 >= (a.M > 16 ? 128 : 256) ? launch_kt<DT, GROUP, 2>(a, s) : launch_kt<DT, GROUP, 1>(a, s);
 }
 template <int DT>

@@ -13,6 +13,7 @@ TYPES = (seq.SEQ_F32, seq.SEQ_BF16, seq.SEQ_I8)
 CASES = [  # M, C, K, group
     (1, 128, 16, 128), (1, 4, 1, 32), (2, 200, 40, 128), (3, 100, 17, 32), (16, 1000, 72, 64), (17, 260, 33, 64), (33, 384, 130, 128),
     (5, 33, 100, 32), (70, 2100, 20, 32), (1, 4096, 300, 128), (2, 300, 8200, 64), (20, 160, 4130, 32), (40, 1200, 4100, 128),
+    (48, 1300, 4100, 32), (64, 200, 4128, 64), (70, 170, 4110, 128), (130, 96, 4097, 64), (6, 2200, 8196, 32), (12, 520, 64, 64),
 ]
 
 
