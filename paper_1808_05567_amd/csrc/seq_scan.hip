@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     constexpr int SG = ENDS ? SP : 1;
     constexpr int E = SP / 8, BL = SP < 16 ? SP : 16;  // elements of B of 8 positions a lane loads; lanes of a row that hold states
     constexpr int W = 64 + 4;                          // (rows a block apart: the eight lanes with the same block write to different banks)
-    struct Lds {
+    struct __align__(16) Lds {
         float d[8][W], dx[8][W], dy[ENDS ? 8 : 1][W];  // d's rows take y once they are done with
         float B[8 * SP], C[ALL ? 8 * SP : 1];
     };

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
     constexpr int V = SeqElem<T>::V, NL = SP / 4, WC = seq_scan_bwd_channels(SP);
     constexpr int PT = WC / V >= 8 ? 8 : 16;  // positions staged at a time: a block of one for each lane, where B and C leave room for them
     constexpr int VEC = WC / V * PT, NV = (VEC + 63) / 64, E = PT * SP / 64;
-    struct Lds {
+    struct __align__(16) Lds {
         // d, x, dy before the gate, what dz and ddt are multiplied with; the sums over states: A t, g B, C h
         float d[PT][WC], x[PT][WC], dy[PT][WC], slope[PT][WC], At[PT][WC], gB[PT][WC];
         float dgate[GATE ? PT : 1][WC], Ch[GATE ? PT : 1][WC];
