@@ -77,7 +77,6 @@ class SeqBlock:
 
     def __init__(self, N, L, C, Ci, S, W, params, dtype=seq.SEQ_BF16, slots=0, eps=1e-5, device="cuda"):
         self.dims, self.dtype, self.device, self.slots = (N, L, C, Ci, S, W), dtype, torch.device(device), slots
-        self.params = params
         v = self.v = 4 if dtype == seq.SEQ_F32 else 8
         up = lambda n: -(-n // v) * v  # noqa: E731
         self.Cp, self.Cip, self.Sp = up(C), up(Ci), up(S)
@@ -114,9 +113,11 @@ class SeqBlock:
         return [t[:, a:b] for a, b in zip(at, at[1:] + [t.shape[1]])]
 
     def load(self, params):
-        """Parameters into the layouts of the operators."""
+        """Parameters (as ``init`` makes them) into the layouts of the operators.  The block keeps numbers of its own: a ``SeqBlockStep`` lays out
+        what was loaded last, whatever the tensors given here hold by then."""
         N, L, C, Ci, S, W = self.dims
-        p, Cip, Sp = params, self.Cip, self.Sp
+        p = self.params = {k: t.detach().clone() for k, t in params.items()}
+        Cip, Sp = self.Cip, self.Sp
 
         def rows(*parts):
             w = torch.zeros(sum(n for n, _ in parts), parts[0][1].shape[1], device=self.device)
