@@ -72,6 +72,16 @@ def init(C, Ci, S, W, seed=0, device="cuda"):
     return {k: t.to(device) for k, t in p.items()}
 
 
+def _rows(*parts):
+    """Matrices one below the other, each in as many rows as are given with it, the others zero."""
+    w = torch.zeros(sum(n for n, _ in parts), parts[0][1].shape[1], device=parts[0][1].device)
+    at = 0
+    for n, t in parts:
+        w[at:at + t.shape[0]] = t
+        at += n
+    return w
+
+
 class SeqBlock:
     """The block over N sequences of L positions: ``forward`` for training and prompts, ``backward`` after it."""
 
@@ -85,6 +95,11 @@ class SeqBlock:
         self.w_mid = _Projection(N, L, Ci, self.Cip + 2 * self.Sp, dtype, device)
         self.w_mid_t = _Projection(N, L, self.Cip + 2 * self.Sp, Ci, dtype, device)
         self.w_out = _Projection(N, L, Ci, C, dtype, device)
+        f = lambda *s: torch.zeros(*s, device=self.device)  # noqa: E731
+        self.params = {"norm": f(C), "w_in": f(2 * Ci, C), "taps": f(W, Ci), "bias": f(Ci), "w_dt": f(Ci, Ci), "w_B": f(S, Ci), "w_C": f(S, Ci),
+                       "A": f(S, Ci), "D": f(Ci), "dt_bias": f(Ci), "w_out": f(C, Ci)}
+        self.nw, self.taps, self.A = f(self.Cp), f(W, self.Cip), f(S, self.Cip)
+        self.bias, self.D, self.dt_bias = f(self.Cip), f(self.Cip), f(self.Cip)
         self.load(params)
 
         T = self._tensor
@@ -112,28 +127,24 @@ class SeqBlock:
             at.append(at[-1] + n // self.v)
         return [t[:, a:b] for a, b in zip(at, at[1:] + [t.shape[1]])]
 
+    @torch.no_grad()
     def load(self, params):
-        """Parameters (as ``init`` makes them) into the layouts of the operators.  The block keeps numbers of its own: a ``SeqBlockStep`` lays out
-        what was loaded last, whatever the tensors given here hold by then."""
-        N, L, C, Ci, S, W = self.dims
-        p = self.params = {k: t.detach().clone() for k, t in params.items()}
-        Cip, Sp = self.Cip, self.Sp
-
-        def rows(*parts):
-            w = torch.zeros(sum(n for n, _ in parts), parts[0][1].shape[1], device=self.device)
-            at = 0
-            for n, t in parts:
-                w[at:at + t.shape[0]] = t
-                at += n
-            return w
-        self.w_in.set(rows((Cip, p["w_in"][:Ci]), (Cip, p["w_in"][Ci:])))
-        mid = rows((Cip, p["w_dt"]), (Sp, p["w_B"]), (Sp, p["w_C"]))
+        """Parameters (as ``init`` makes them) into the layouts of the operators, each time into the same memory: a graph that was recorded before runs
+        with the new ones.  The block keeps numbers of its own: a ``SeqBlockStep`` lays out what was loaded last, whatever the tensors given
+        here hold by then."""
+        for k, t in self.params.items():
+            if params[k].shape != t.shape:
+                raise ValueError("%s: a tensor of %s is wanted, not one of %s" % (k, tuple(t.shape), tuple(params[k].shape)))
+        for k, t in self.params.items():
+            t.copy_(params[k])
+        p, Ci, Cip, Sp = self.params, self.dims[3], self.Cip, self.Sp
+        self.w_in.set(_rows((Cip, p["w_in"][:Ci]), (Cip, p["w_in"][Ci:])))
+        mid = _rows((Cip, p["w_dt"]), (Sp, p["w_B"]), (Sp, p["w_C"]))
         self.w_mid.set(mid)
         self.w_mid_t.set(mid.t())
         self.w_out.set(p["w_out"])
-        wide = lambda t, n: torch.nn.functional.pad(t, (0, n - t.shape[-1])).contiguous()  # noqa: E731
-        self.nw = wide(p["norm"], self.Cp)
-        self.taps, self.bias, self.A, self.D, self.dt_bias = (wide(p[k], Cip) for k in ("taps", "bias", "A", "D", "dt_bias"))
+        for t, k in ((self.nw, "norm"), (self.taps, "taps"), (self.bias, "bias"), (self.A, "A"), (self.D, "D"), (self.dt_bias, "dt_bias")):
+            t[..., :p[k].shape[-1]] = p[k]
 
     def forward(self, x, res, states=None, at=None, lengths=None):
         """x, res: blocked [N, Cb, L, v].  states: the pair that ``states`` makes, moved on from slots `at`; lengths: int32 [N].
@@ -204,11 +215,7 @@ class SeqBlockStep:
         self.scan = seq.seq_scan_create(M, Ci, 1, S, seq.SEQ_BF16, slots=slots, views={"x": self.c, "dt": self.dt, "B": self.B, "C": self.Cm, "z": self.pz})
 
         def quantised(dtype, *parts):
-            w = torch.zeros(sum(n for n, _ in parts), parts[0][1].shape[1], device=dev)
-            at = 0
-            for n, t in parts:
-                w[at:at + t.shape[0]] = t
-                at += n
+            w = _rows(*parts)
             h = seq.seq_mv4_create(M, w.shape[1], w.shape[0], group, dtype)
             wt = torch.empty(h.info.wt_bytes, dtype=torch.uint8, device=dev)
             sc = torch.empty(h.info.scale_bytes // 4, device=dev)

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_1808_05567_amd import seq_block
+from paper_1808_05567_amd import seq, seq_block
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,43 @@ def test_a_step_serves_what_was_laid_out_last():
         t.zero_()
     pairs = tokens(M, DIMS["C"], 3)
     same(serve(seq_block.SeqBlockStep(block, M), block.states(), pairs), serve(seq_block.SeqBlockStep(want, M), want.states(), pairs))
+
+
+@pytest.mark.parametrize("dtype", [seq.SEQ_F32, seq.SEQ_BF16])
+def test_parameters_stay_in_their_memory(dtype):
+    """A recorded forward pass runs with the parameters that were laid out since."""
+    N, L, C, Ci, S, W = 2, 20, 40, 56, 8, 4
+    make = lambda seed: seq_block.SeqBlock(N, L, C, Ci, S, W, seq_block.init(C, Ci, S, W, seed=seed), dtype)  # noqa: E731
+    block, other = make(1), make(2)
+    x, res = (torch.randn(N, C // block.v, L, block.v, device="cuda").to(block.u.dtype) for _ in range(2))
+    tensors = lambda b: [b.nw, b.taps, b.bias, b.A, b.D, b.dt_bias] + [p.wt for p in (b.w_in, b.w_mid, b.w_mid_t, b.w_out)]  # noqa: E731
+    at = [t.data_ptr() for t in tensors(block)]
+    block.forward(x, res)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, r = block.forward(x, res)
+    block.load(seq_block.init(C, Ci, S, W, seed=2))
+    assert at == [t.data_ptr() for t in tensors(block)]
+    want = other.forward(x, res)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        same((out, r), want)
+
+
+def test_parameters_that_do_not_fit_are_refused():
+    """... before any of them is laid out."""
+    block = block_of(params_of(1))
+    pairs = tokens(M, DIMS["C"], 1)
+    want = serve(seq_block.SeqBlockStep(block, M), block.states(), pairs)
+    for name, bad in (("w_in", torch.zeros(1, 1)), ("taps", torch.zeros(DIMS["Ci"], DIMS["W"])), ("w_out", None)):
+        p = params_of(2)
+        if bad is None:
+            del p[name]
+        else:
+            p[name] = bad.cuda()
+        with pytest.raises((KeyError, ValueError)):
+            block.load(p)
+    same(serve(seq_block.SeqBlockStep(block, M), block.states(), pairs), want)
