@@ -14,6 +14,8 @@ it in place, by their strides, and backwards writes them there.  All computation
 """
 from __future__ import annotations
 
+import weakref
+
 import torch
 
 from . import conv, seq
@@ -100,6 +102,7 @@ class SeqBlock:
                        "A": f(S, Ci), "D": f(Ci), "dt_bias": f(Ci), "w_out": f(C, Ci)}
         self.nw, self.taps, self.A = f(self.Cp), f(W, self.Cip), f(S, self.Cip)
         self.bias, self.D, self.dt_bias = f(self.Cip), f(self.Cip), f(self.Cip)
+        self.steps = weakref.WeakSet()  # (those that are still used)
         self.load(params)
 
         T = self._tensor
@@ -129,9 +132,9 @@ class SeqBlock:
 
     @torch.no_grad()
     def load(self, params):
-        """Parameters (as ``init`` makes them) into the layouts of the operators, each time into the same memory: a graph that was recorded before runs
-        with the new ones.  The block keeps numbers of its own: a ``SeqBlockStep`` lays out what was loaded last, whatever the tensors given
-        here hold by then."""
+        """Parameters (as ``init`` makes them) into the layouts of the operators, and of its steps, each time into the same memory: a graph
+        that was recorded before runs with the new ones.  The block keeps numbers of its own: a ``SeqBlockStep`` lays out what was loaded
+        last, whatever the tensors given here hold by then."""
         for k, t in self.params.items():
             if params[k].shape != t.shape:
                 raise ValueError("%s: a tensor of %s is wanted, not one of %s" % (k, tuple(t.shape), tuple(params[k].shape)))
@@ -145,6 +148,8 @@ class SeqBlock:
         self.w_out.set(p["w_out"])
         for t, k in ((self.nw, "norm"), (self.taps, "taps"), (self.bias, "bias"), (self.A, "A"), (self.D, "D"), (self.dt_bias, "dt_bias")):
             t[..., :p[k].shape[-1]] = p[k]
+        for step in self.steps:
+            step.load()
 
     def forward(self, x, res, states=None, at=None, lengths=None):
         """x, res: blocked [N, Cb, L, v].  states: the pair that ``states`` makes, moved on from slots `at`; lengths: int32 [N].
@@ -202,7 +207,7 @@ class SeqBlockStep:
         if block.dtype != seq.SEQ_BF16:
             raise ValueError("single tokens are served in bf16")
         self.block, dev, slots = block, block.device, block.slots
-        v, Cip, Sp, p = block.v, block.Cip, block.Sp, block.params
+        v, Cip, Sp = block.v, block.Cip, block.Sp
         T = lambda n: torch.zeros(M, n // v, 1, v, dtype=torch.bfloat16, device=dev)  # noqa: E731
         self.r, self.out = T(block.Cp), T(block.Cp)
         self.p, self.c, self.q, self.s = T(2 * Cip), T(Cip), T(Cip + 2 * Sp), T(Cip)
@@ -214,16 +219,21 @@ class SeqBlockStep:
         self.conv = seq.seq_conv_create(M, Ci, 1, W, seq.SEQ_BF16, slots=slots, views={"x": self.px})
         self.scan = seq.seq_scan_create(M, Ci, 1, S, seq.SEQ_BF16, slots=slots, views={"x": self.c, "dt": self.dt, "B": self.B, "C": self.Cm, "z": self.pz})
 
-        def quantised(dtype, *parts):
-            w = _rows(*parts)
-            h = seq.seq_mv4_create(M, w.shape[1], w.shape[0], group, dtype)
-            wt = torch.empty(h.info.wt_bytes, dtype=torch.uint8, device=dev)
-            sc = torch.empty(h.info.scale_bytes // 4, device=dev)
-            seq.seq_mv4_quant(h, w, wt, sc)
-            return h, wt, sc
-        self.w_in = quantised(seq.SEQ_I8, (Cip, p["w_in"][:Ci]), (Cip, p["w_in"][Ci:]))
-        self.w_mid = quantised(seq.SEQ_BF16, (Cip, p["w_dt"]), (Sp, p["w_B"]), (Sp, p["w_C"]))
-        self.w_out = quantised(seq.SEQ_BF16, (block.Cp, p["w_out"]))
+        def quantised(dtype, C, K):
+            h = seq.seq_mv4_create(M, C, K, group, dtype)
+            return h, torch.empty(h.info.wt_bytes, dtype=torch.uint8, device=dev), torch.empty(h.info.scale_bytes // 4, device=dev)
+        self.w_in = quantised(seq.SEQ_I8, C, 2 * Cip)
+        self.w_mid = quantised(seq.SEQ_BF16, Ci, Cip + 2 * Sp)
+        self.w_out = quantised(seq.SEQ_BF16, Ci, block.Cp)
+        self.load()
+        block.steps.add(self)
+
+    def load(self):
+        """The block's projections into 4 bits, as ``SeqBlock.load`` does with each step of the block."""
+        b, p, Ci = self.block, self.block.params, self.block.dims[3]
+        for (h, wt, scale), *parts in ((self.w_in, (b.Cip, p["w_in"][:Ci]), (b.Cip, p["w_in"][Ci:])),
+                                       (self.w_mid, (b.Cip, p["w_dt"]), (b.Sp, p["w_B"]), (b.Sp, p["w_C"])), (self.w_out, (b.Cp, p["w_out"]))):
+            seq.seq_mv4_quant(h, _rows(*parts), wt, scale)
 
     def __call__(self, x, res, states, at=None):
         """x, res: [M, Cb, 1, v]; states and slots as for ``SeqBlock.forward``."""

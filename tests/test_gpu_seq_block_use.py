@@ -86,3 +86,32 @@ def test_parameters_that_do_not_fit_are_refused():
         with pytest.raises((KeyError, ValueError)):
             block.load(p)
     same(serve(seq_block.SeqBlockStep(block, M), block.states(), pairs), want)
+
+
+def test_steps_follow_the_block():
+    """Parameters laid out again: a step that was there serves them too, called or recorded."""
+    want = block_of(params_of(2))
+    block = block_of(params_of(1))
+    step = seq_block.SeqBlockStep(block, M)
+    pairs = tokens(M, DIMS["C"], 3)
+    serve(step, block.states(), pairs)
+    x, r, states = *(torch.empty_like(t) for t in pairs[0]), block.states()
+    x.copy_(pairs[0][0])
+    r.copy_(pairs[0][1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, after = step(x, r, states)
+    block.load(params_of(2))
+    expected = serve(seq_block.SeqBlockStep(want, M), want.states(), pairs)
+    same(serve(step, block.states(), pairs), expected)
+    for t in states:
+        t.zero_()
+    got = []
+    for token in pairs:
+        x.copy_(token[0])
+        r.copy_(token[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        got += [out.clone(), after.clone()]
+    same(got + list(states), expected)
