@@ -88,7 +88,7 @@ class SeqBlock:
     """The block over N sequences of L positions: ``forward`` for training and prompts, ``backward`` after it."""
 
     def __init__(self, N, L, C, Ci, S, W, params, dtype=seq.SEQ_BF16, slots=0, eps=1e-5, device="cuda"):
-        self.dims, self.dtype, self.device, self.slots = (N, L, C, Ci, S, W), dtype, torch.device(device), slots
+        self.dims, self.dtype, self.device, self.slots, self.eps = (N, L, C, Ci, S, W), dtype, torch.device(device), slots, eps
         v = self.v = 4 if dtype == seq.SEQ_F32 else 8
         up = lambda n: -(-n // v) * v  # noqa: E731
         self.Cp, self.Cip, self.Sp = up(C), up(Ci), up(S)
@@ -200,9 +200,9 @@ class SeqBlock:
 
 
 class SeqBlockStep:
-    """The block over one new token of each of M sequences, its projections in 4 bits; the norm hands its result on in 8."""
+    """The block over one new token of each of M sequences, its projections in 4 bits; the norm hands its result on in 8.  eps: the block's where none is given."""
 
-    def __init__(self, block: SeqBlock, M, group=64, eps=1e-5):
+    def __init__(self, block: SeqBlock, M, group=64, eps=None):
         N, L, C, Ci, S, W = block.dims
         if block.dtype != seq.SEQ_BF16:
             raise ValueError("single tokens are served in bf16")
@@ -215,7 +215,7 @@ class SeqBlockStep:
         self.dt, self.B, self.Cm = block._split(self.q, Cip, Sp)
         self.u = torch.zeros(M, -(-C // 16), 1, 16, dtype=torch.int8, device=dev)
         self.scale = torch.zeros(M, 1, device=dev)
-        self.norm = seq.seq_norm_create(M, C, 1, seq.SEQ_BF16, eps)
+        self.norm = seq.seq_norm_create(M, C, 1, seq.SEQ_BF16, block.eps if eps is None else eps)
         self.conv = seq.seq_conv_create(M, Ci, 1, W, seq.SEQ_BF16, slots=slots, views={"x": self.px})
         self.scan = seq.seq_scan_create(M, Ci, 1, S, seq.SEQ_BF16, slots=slots, views={"x": self.c, "dt": self.dt, "B": self.B, "C": self.Cm, "z": self.pz})
 

@@ -115,3 +115,14 @@ def test_steps_follow_the_block():
         torch.cuda.synchronize()
         got += [out.clone(), after.clone()]
     same(got + list(states), expected)
+
+
+def test_steps_have_the_blocks_eps():
+    """The residual stream is small beside eps: 1e-1 and 1e-5 are far apart."""
+    params, eps = params_of(1), 1e-1
+    block = block_of(params, eps=eps)
+    pairs = [[0.1 * t for t in p] for p in tokens(M, DIMS["C"], 2)]
+    got = serve(seq_block.SeqBlockStep(block, M), block.states(), pairs)
+    same(got, serve(seq_block.SeqBlockStep(block, M, eps=eps), block.states(), pairs))
+    other = serve(seq_block.SeqBlockStep(block, M, eps=1e-5), block.states(), pairs)
+    assert (other[0].float() - got[0].float()).norm() > 0.1 * got[0].float().norm()
