@@ -10,7 +10,8 @@ its 1x1 convolutions, served over single tokens with 4-bit weights.
     out = W_out s        Ci -> C          conv 1x1
 
 Sp is S rounded up to the blocks' channels, so that B and C are whole blocks.  Every step reads parts of the tensors of the one before
-it in place, by their strides, and backwards writes them there.  All computation is the library's; torch holds memory.
+it in place, by their strides, and backwards writes them there.  All computation is the library's; torch holds memory, and
+clears what lies behind the ends of sequences.
 """
 from __future__ import annotations
 
@@ -116,6 +117,7 @@ class SeqBlock:
         self.scan = seq.seq_scan_create(N, Ci, L, S, dtype, slots=slots, views={
             "x": self.c, "dt": self.dt, "B": self.B, "C": self.Cm, "z": self.pz, "y": self.s,
             "dy": self.s, "dx": self.c, "ddt": self.dt, "dB": self.B, "dC": self.Cm, "dz": self.pz})
+        self.positions = torch.arange(L, dtype=torch.int32, device=self.device)
         size = max(h.info.workspace_bytes for h in (self.norm, self.conv, self.scan))
         self.ws = torch.empty(max(16, size), dtype=torch.uint8, device=self.device)
 
@@ -152,9 +154,14 @@ class SeqBlock:
             step.load()
 
     def forward(self, x, res, states=None, at=None, lengths=None):
-        """x, res: blocked [N, Cb, L, v].  states: the pair that ``states`` makes, moved on from slots `at`; lengths: int32 [N].
-        Returns the output and the residual stream."""
+        """x, res: blocked [N, Cb, L, v].  states: the pair that ``states`` makes, moved on from slots `at`; lengths: int32 [N], positions of each
+        sequence: what lies beyond may be anything and comes out as zero.  Returns the output and the residual stream."""
         seq.seq_norm_fwd(self.norm, x, res, self.nw, self.r, self.u)
+        if lengths is not None:
+            # (the norm and the projections take each position on its own, but the gradients of their weights are sums over all of them)
+            outside = self._outside(lengths)
+            self.r.masked_fill_(outside, 0)
+            self.u.masked_fill_(outside, 0)
         self.w_in.fwd(self.u, self.p)
         before, h = states if states is not None else (None, None)
         seq.seq_conv_fwd(self.conv, self.px, self.taps, self.bias, self.c, state_in=before, state_out=before, slots=at, lengths=lengths)
@@ -164,6 +171,17 @@ class SeqBlock:
         self.w_out.fwd(self.s, self.out)
         return self.out, self.r
 
+    def _outside(self, lengths):
+        """[N, 1, L, 1]: the positions that lie behind their sequence's end."""
+        N, L = self.dims[:2]
+        seq._t(lengths, torch.int32, N, "lengths")
+        return (self.positions >= lengths.flatten()[:N].view(N, 1)).view(N, 1, L, 1)
+
+    def _cleared(self, name, t, outside):
+        """A copy of a gradient with zeros outside."""
+        seq._s(self.norm, name, t, self.norm.all)
+        return t.as_strided(self.out.shape, self.out.stride()).masked_fill(outside, 0)
+
     def states(self):
         """Zero states for the block's slots: of the convolution and of the scan."""
         N, L, C, Ci, S, W = self.dims
@@ -171,8 +189,15 @@ class SeqBlock:
                 torch.zeros(self.slots, S, self.Cip, device=self.device))
 
     def backward(self, dout, dr, lengths=None):
-        """Gradients of the last ``forward`` without states: of x (and of res, which is the same), and a dict of the parameters'."""
+        """Gradients of the last ``forward`` without states: of x (and of res, which is the same), and a dict of the parameters'.
+        lengths: those of ``forward``; dout and dr beyond may be anything, and the gradient of x is zero there.  dr may be None."""
         N, L, C, Ci, S, W = self.dims
+        r = self.r
+        if lengths is not None:
+            outside = self._outside(lengths)
+            dout, dr = self._cleared("dy", dout, outside), None if dr is None else self._cleared("dr", dr, outside)
+            if self.eps == 0:
+                r = r.masked_fill(outside, 1)  # (zeros have no norm then; any number does where its gradient is zero)
         if self.grads is None:
             T = self._tensor
             self.grads = {"ds": T(self.Cip), "dq": T(self.Cip + 2 * self.Sp), "dp": T(2 * self.Cip), "dc": T(self.Cip), "du": T(self.Cp), "dx": T(self.Cp)}
@@ -193,14 +218,15 @@ class SeqBlock:
         w_in = self.w_in.upd(self.u, t["dp"])
         g["w_in"] = torch.cat((w_in[:Ci], w_in[self.Cip:self.Cip + Ci]))
         self.w_in.bwd(t["dp"], t["du"])
-        seq.seq_norm_bwd(self.norm, self.r, self.nw, t["du"], dr, t["dx"], g["norm"], self.ws)
+        seq.seq_norm_bwd(self.norm, r, self.nw, t["du"], dr, t["dx"], g["norm"], self.ws)
         for k, n in (("taps", Ci), ("bias", Ci), ("A", Ci), ("D", Ci), ("dt_bias", Ci), ("norm", C)):
             g[k] = g[k][..., :n]
         return t["dx"], g
 
 
 class SeqBlockStep:
-    """The block over one new token of each of M sequences, its projections in 4 bits; the norm hands its result on in 8.  eps: the block's where none is given."""
+    """The block over one new token of each of M sequences, its projections in 4 bits; the norm hands its result on in 8.
+    eps: the block's where none is given."""
 
     def __init__(self, block: SeqBlock, M, group=64, eps=None):
         N, L, C, Ci, S, W = block.dims

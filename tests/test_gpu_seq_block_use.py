@@ -1,8 +1,11 @@
-"""A block of sequence operators in use: parameters laid out again, its steps beside it."""
+"""A block of sequence operators in use: parameters laid out again, its steps beside it, sequences that end early."""
+import numpy as np
 import pytest
 import torch
 
 from paper_1808_05567_amd import seq, seq_block
+from seq_util import Seq, spoil
+from test_gpu_seq_block import reference, reference_bwd
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +129,41 @@ def test_steps_have_the_blocks_eps():
     same(got, serve(seq_block.SeqBlockStep(block, M, eps=eps), block.states(), pairs))
     other = serve(seq_block.SeqBlockStep(block, M, eps=1e-5), block.states(), pairs)
     assert (other[0].float() - got[0].float()).norm() > 0.1 * got[0].float().norm()
+
+
+@pytest.mark.parametrize("eps", [1e-5, 0.0])
+def test_a_training_step_of_sequences_that_end_early(eps, monkeypatch):
+    """In fp32, with NaN and infinities behind each end, against the sequences one by one; the bound is that of the whole step (seven operators, each good to
+    some 1e-6 of its magnitudes)."""
+    N, L, C, Ci, S, W, dtype = 5, 37, 24, 40, 16, 4, seq.SEQ_F32
+    ends = [L, 0, 1, 20, L + 3]
+    rng = np.random.default_rng(7)
+    params = seq_block.init(C, Ci, S, W, seed=1)
+    p = {k: t.double().cpu().numpy() for k, t in params.items()}
+    x, res, dout, dr = (np.float64(np.float32(rng.standard_normal((N, L, C)))) for _ in range(4))
+    block = seq_block.SeqBlock(N, L, C, Ci, S, W, params, dtype, eps=eps)
+    lengths = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    X, RES, DOUT, DR = (Seq(N, C, L, dtype, "dense", spoil(a, ends)).t.contiguous() for a in (x, res, dout, dr))
+    before = [t.clone() for t in (X, RES, DOUT, DR)]
+    out, r = block.forward(X, RES, lengths=lengths)
+    back = lambda t, n: t.permute(0, 2, 1, 3).reshape(N, L, -1)[..., :n].double().cpu().numpy()  # noqa: E731
+    out, r = back(out, C), back(r, C)
+    dx, g = block.backward(DOUT, DR, lengths=lengths)
+    dx = back(dx, C)
+    monkeypatch.setattr("test_gpu_seq_block.EPS", eps)
+    want, wx, wg = np.zeros_like(out), np.zeros_like(dx), None
+    for n, end in enumerate(ends):
+        end = min(end, L)
+        if end == 0:
+            continue
+        part = [a[n:n + 1, :end] for a in (x, res, dout, dr)]
+        want[n, :end] = reference(p, part[0], part[1], S)[-1]
+        wx[n, :end], one = reference_bwd(p, *part, S)
+        wg = one if wg is None else {k: wg[k] + one[k] for k in wg}
+        assert not out[n, end:].any() and not r[n, end:].any() and not dx[n, end:].any()
+    for got, ref, name in [(out, want, "out"), (dx, wx, "dx")] + [(g[k].double().cpu().numpy(), wg[k], k) for k in wg]:
+        assert np.linalg.norm(got - ref) <= 1e-4 * np.linalg.norm(ref), name
+    assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip((X, RES, DOUT, DR), before))
+    again, g2 = block.backward(DOUT.flatten(), DR.flatten(), lengths=lengths)  # (dense, without dimensions)
+    np.testing.assert_array_equal(back(again, C), dx)
+    assert all(torch.equal(g[k], g2[k]) for k in g)
