@@ -177,9 +177,8 @@ class SeqBlock:
         seq._t(lengths, torch.int32, N, "lengths")
         return (self.positions >= lengths.flatten()[:N].view(N, 1)).view(N, 1, L, 1)
 
-    def _cleared(self, name, t, outside):
+    def _cleared(self, t, outside):
         """A copy of a gradient with zeros outside."""
-        seq._s(self.norm, name, t, self.norm.all)
         return t.as_strided(self.out.shape, self.out.stride()).masked_fill(outside, 0)
 
     def states(self):
@@ -193,9 +192,12 @@ class SeqBlock:
         lengths: those of ``forward``; dout and dr beyond may be anything, and the gradient of x is zero there.  dr may be None."""
         N, L, C, Ci, S, W = self.dims
         r = self.r
+        # (the projections take pointers as they come)
+        seq._s(self.norm, "dy", dout, self.norm.all)
+        seq._so(self.norm, "dr", dr, self.norm.all)
         if lengths is not None:
             outside = self._outside(lengths)
-            dout, dr = self._cleared("dy", dout, outside), None if dr is None else self._cleared("dr", dr, outside)
+            dout, dr = self._cleared(dout, outside), None if dr is None else self._cleared(dr, outside)
             if self.eps == 0:
                 r = r.masked_fill(outside, 1)  # (zeros have no norm then; any number does where its gradient is zero)
         if self.grads is None:

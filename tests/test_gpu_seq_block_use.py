@@ -167,3 +167,16 @@ def test_a_training_step_of_sequences_that_end_early(eps, monkeypatch):
     again, g2 = block.backward(DOUT.flatten(), DR.flatten(), lengths=lengths)  # (dense, without dimensions)
     np.testing.assert_array_equal(back(again, C), dx)
     assert all(torch.equal(g[k], g2[k]) for k in g)
+
+
+def test_gradients_of_another_form_are_refused():
+    """What backward is given is as its outputs are: type, extents, strides."""
+    block = block_of(params_of(1))
+    good = torch.zeros_like(block.out)
+    block.forward(good, good)
+    turned = good.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    for bad in (good.float(), good[:1].clone(), turned, good.cpu()):
+        for args in ((bad, good), (good, bad)):
+            with pytest.raises(ValueError):
+                block.backward(*args)
+    block.backward(good, None)
