@@ -4,11 +4,12 @@ root-mean-square norm, products with 4-bit weights.
 As ``conv``: argument marshalling only, no fallback.  A handle is created once for its sizes, types and strides; a call takes
 the tensors.  Tensors of sequences are torch tensors [N, Cb, L, v], dense or not; give them (or tensors of the same strides) to
 the create functions as ``views``, keyed by the argument's name, where they are not dense.  Calls check each tensor's device, type,
-number of elements and strides against the plan's, so that a tensor of another layout is refused rather than read past its end.
+extents and strides against the plan's, so that a tensor of another layout is refused rather than read past its end.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 
 from . import conv
 from .conv import ConvError  # noqa: F401  (what the calls raise)
@@ -96,27 +97,28 @@ class SeqPlan:
             pass
 
 
-def _s(h, name, x, least):
+def _s(h, name, x):
     """Device pointer of a sequence tensor that is as the plan has it."""
-    if x.dtype is not h.dtype or x.numel() < least or not x.is_cuda or x.stride() != h.strides[name]:
-        _misfit(h, name, x, least, h.dtype)
+    if x.dtype is not h.dtype or x.shape != h.shapes[name] or not x.is_cuda or x.stride() != h.strides[name]:
+        _misfit(h, name, x, h.dtype)
     return x.data_ptr()
 
 
-def _so(h, name, x, least):
-    return None if x is None else _s(h, name, x, least)
+def _so(h, name, x):
+    return None if x is None else _s(h, name, x)
 
 
-def _misfit(h, name, x, least, dtype):
-    """What _s found may be the stride of a dimension of one place, or a dense tensor without dimensions."""
-    want = h.strides[name]
-    if x.dtype is dtype and x.numel() >= least and x.is_cuda:
-        if x.dim() == 4 and all(x.shape[i] == 1 or x.stride(i) == want[i] for i in range(4)):
+def _misfit(h, name, x, dtype):
+    """What _s found may be more places than there are, the stride of a dimension of one place, or a dense tensor of other dimensions."""
+    shape, strides = h.shapes[name], h.strides[name]
+    if x.dtype is dtype and x.is_cuda:
+        if x.dim() == 4 and all(x.shape[i] >= shape[i] and (shape[i] == 1 or x.stride(i) == strides[i]) for i in range(4)):
             return
-        if x.dim() != 4 and x.is_contiguous() and want == h.dense[name]:
+        one_after_the_other = x.dim() != 4 or all(x.shape[i] == 1 or x.stride(i) == strides[i] for i in range(4))
+        if one_after_the_other and x.is_contiguous() and strides == h.dense[name] and x.numel() >= math.prod(shape):
             return
-    raise ValueError("%s: a tensor of %s on the GPU with at least %d elements and strides %s is wanted, not one of %s with %d and %s on %s" % (
-        name, dtype, least, want, x.dtype, x.numel(), tuple(x.stride()), x.device))
+    raise ValueError("%s: a tensor %s of %s on the GPU with strides %s is wanted, not one of %s of %s with %s on %s" % (
+        name, list(shape), dtype, strides, tuple(x.shape), x.dtype, tuple(x.stride()), x.device))
 
 
 def _t(x, dtype, least, name):
@@ -137,13 +139,13 @@ def _of(h, kind):
     return h._h
 
 
-def _strides(h, names, views, C, L, wide=()):
-    """The strides of each sequence tensor of a plan, given or dense; `wide`: channels of those that have others than C."""
-    h.dense, h.strides = {}, {}
+def _strides(h, names, views, N, C, L, wide=()):
+    """The extents and strides of each sequence tensor of a plan, given or dense; `wide`: channels of those that have others than C."""
+    h.dense, h.strides, h.shapes = {}, {}, {}
     for name in names:
         v = 16 if name == "q" else h.info.vlen
         Cb = -(-dict(wide).get(name, C) // v)
-        h.dense[name] = (Cb * L * v, L * v, v, 1)
+        h.dense[name], h.shapes[name] = (Cb * L * v, L * v, v, 1), (N, Cb, L, v)
         t = (views or {}).get(name)
         h.strides[name] = h.dense[name] if t is None else tuple(t.stride())
 
@@ -195,8 +197,7 @@ def seq_conv_create(N, C, L, W, dtype=SEQ_F32, silu=True, slots=0, views=None) -
     d = SeqConvDesc(N=N, C=C, L=L, W=W, silu=1 if silu else 0, slots=slots, dtype=dtype)
     _views(views, _CONV_VIEWS, d, _vlen(dtype))
     h = SeqPlan("seq_conv_create", d, dtype, {"N": N})
-    _strides(h, _CONV_VIEWS, views, C, L)
-    h.rows, h.all = N * h.info.Cp, N * h.info.Cp * L
+    _strides(h, _CONV_VIEWS, views, N, C, L)
     h.w, h.state = W * h.info.Cp, slots * h.info.Cp * (W - 1)
     return h
 
@@ -204,22 +205,22 @@ def seq_conv_create(N, C, L, W, dtype=SEQ_F32, silu=True, slots=0, views=None) -
 def seq_conv_fwd(h, x, w, bias, y, state_in=None, state_out=None, slots=None, lengths=None, stream=None):
     T = h.dtype
     conv._check(load().seq_conv_fwd(
-        _of(h, "seq_conv"), _s(h, "x", x, h.all), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _o(state_in, T, h.state, "state_in"),
-        _s(h, "y", y, h.all), _o(state_out, T, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"),
+        _of(h, "seq_conv"), _s(h, "x", x), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _o(state_in, T, h.state, "state_in"),
+        _s(h, "y", y), _o(state_out, T, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"),
         conv._stream(stream)), "seq_conv_fwd")
 
 
 def seq_conv_step(h, x, w, bias, state, y, slots=None, stream=None):
     T = h.dtype
     conv._check(load().seq_conv_step(
-        _of(h, "seq_conv"), _s(h, "x", x, h.rows), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _t(state, T, h.state, "state"),
-        _s(h, "y", y, h.rows), _o(slots, h.i32, h.N, "slots"), conv._stream(stream)), "seq_conv_step")
+        _of(h, "seq_conv"), _s(h, "x", x), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _t(state, T, h.state, "state"),
+        _s(h, "y", y), _o(slots, h.i32, h.N, "slots"), conv._stream(stream)), "seq_conv_step")
 
 
 def seq_conv_bwd(h, x, w, bias, dy, dx, dw, dbias, ws, lengths=None, stream=None):
     conv._check(load().seq_conv_bwd(
-        _of(h, "seq_conv"), _s(h, "x", x, h.all), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _s(h, "dy", dy, h.all),
-        _s(h, "dx", dx, h.all), _t(dw, h.f32, h.w, "dw"), _o(dbias, h.f32, h.info.Cp, "dbias"), _o(lengths, h.i32, h.N, "lengths"),
+        _of(h, "seq_conv"), _s(h, "x", x), _t(w, h.f32, h.w, "w"), _o(bias, h.f32, h.info.Cp, "bias"), _s(h, "dy", dy),
+        _s(h, "dx", dx), _t(dw, h.f32, h.w, "dw"), _o(dbias, h.f32, h.info.Cp, "dbias"), _o(lengths, h.i32, h.N, "lengths"),
         *_ws(ws), conv._stream(stream)), "seq_conv_bwd")
 
 
@@ -228,40 +229,37 @@ def seq_scan_create(N, C, L, S, dtype=SEQ_F32, G=1, softplus=True, slots=0, view
     d = SeqScanDesc(N=N, Ch=C, L=L, S=S, G=G, softplus=1 if softplus else 0, slots=slots, dtype=dtype)
     _views(views, _SCAN_VIEWS, d, _vlen(dtype))
     h = SeqPlan("seq_scan_create", d, dtype, {"N": N})
-    h.rows, h.all = N * h.info.Cp, N * h.info.Cp * L
-    _strides(h, _SCAN_VIEWS, views, C, L, [(k, G * S) for k in ("B", "C", "dB", "dC")])
-    v = h.info.vlen
-    h.srows, h.A, h.state = N * -(-G * S // v) * v, S * h.info.Cp, slots * S * h.info.Cp
-    h.sall = h.srows * L
+    _strides(h, _SCAN_VIEWS, views, N, C, L, [(k, G * S) for k in ("B", "C", "dB", "dC")])
+    h.A, h.state = S * h.info.Cp, slots * S * h.info.Cp
     return h
 
 
-def _scan_inputs(h, x, dt, A, B, C, D, z, dt_bias, rows, srows):
+def _scan_inputs(h, x, dt, A, B, C, D, z, dt_bias):
     f, Cp = h.f32, h.info.Cp
-    return (_s(h, "x", x, rows), _s(h, "dt", dt, rows), _t(A, f, h.A, "A"), _s(h, "B", B, srows), _s(h, "C", C, srows), _o(D, f, Cp, "D"),
-            _so(h, "z", z, rows), _o(dt_bias, f, Cp, "dt_bias"))
+    return (_s(h, "x", x), _s(h, "dt", dt), _t(A, f, h.A, "A"), _s(h, "B", B), _s(h, "C", C), _o(D, f, Cp, "D"),
+            _so(h, "z", z), _o(dt_bias, f, Cp, "dt_bias"))
 
 
 def seq_scan_fwd(h, x, dt, A, B, C, y, ws=None, D=None, z=None, dt_bias=None, state_in=None, state_out=None, slots=None, lengths=None,
                  stream=None):
     conv._check(load().seq_scan_fwd(
-        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias, h.all, h.sall), _o(state_in, h.f32, h.state, "state_in"),
-        _s(h, "y", y, h.all), _o(state_out, h.f32, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"),
+        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias), _o(state_in, h.f32, h.state, "state_in"),
+        _s(h, "y", y), _o(state_out, h.f32, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"),
         *_ws(ws), conv._stream(stream)), "seq_scan_fwd")
 
 
 def seq_scan_step(h, x, dt, A, B, C, state, y, D=None, z=None, dt_bias=None, slots=None, stream=None):
     conv._check(load().seq_scan_step(
-        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias, h.rows, h.srows), _t(state, h.f32, h.state, "state"),
-        _s(h, "y", y, h.rows), _o(slots, h.i32, h.N, "slots"), conv._stream(stream)), "seq_scan_step")
+        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias), _t(state, h.f32, h.state, "state"),
+        _s(h, "y", y), _o(slots, h.i32, h.N, "slots"), conv._stream(stream)), "seq_scan_step")
 
 
 def seq_scan_bwd(h, x, dt, A, B, C, dy, dx, ddt, dA, dB, dC, ws, D=None, z=None, dt_bias=None, dD=None, dz=None, ddt_bias=None, lengths=None,
                  stream=None):
     f, Cp = h.f32, h.info.Cp
     conv._check(load().seq_scan_bwd(
-        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias, h.all, h.sall), _s(h, "dy", dy, h.all), _s(h, "dx", dx, h.all),
-        _s(h, "ddt", ddt, h.all), _t(dA, f, h.A, "dA"), _s(h, "dB", dB, h.sall), _s(h, "dC", dC, h.sall), _o(dD, f, Cp, "dD"), _so(h, "dz", dz, h.all),
+        _of(h, "seq_scan"), *_scan_inputs(h, x, dt, A, B, C, D, z, dt_bias), _s(h, "dy", dy), _s(h, "dx", dx),
+        _s(h, "ddt", ddt), _t(dA, f, h.A, "dA"), _s(h, "dB", dB), _s(h, "dC", dC), _o(dD, f, Cp, "dD"), _so(h, "dz", dz),
         _o(ddt_bias, f, Cp, "ddt_bias"), _o(lengths, h.i32, h.N, "lengths"), *_ws(ws), conv._stream(stream)), "seq_scan_bwd")
 
 
@@ -270,33 +268,29 @@ def seq_norm_create(N, C, L, dtype=SEQ_F32, eps=1e-5, views=None) -> SeqPlan:
     d = SeqNormDesc(N=N, C=C, L=L, dtype=dtype, eps=eps)
     _views(views, _NORM_VIEWS, d, _vlen(dtype))
     h = SeqPlan("seq_norm_create", d, dtype, {"N": N, "positions": N * L})
-    _strides(h, _NORM_VIEWS, views, C, L)
-    h.all, h.q = N * h.info.Cp * L, N * L * (-(-C // 16) * 16)
+    _strides(h, _NORM_VIEWS, views, N, C, L)
     return h
 
 
 def seq_norm_fwd(h, x, res, w, r, y, stream=None):
-    n = h.all
-    conv._check(load().seq_norm_fwd(_of(h, "seq_norm"), _s(h, "x", x, n), _so(h, "res", res, n), _t(w, h.f32, h.info.Cp, "w"), _so(h, "r", r, n),
-                                    _s(h, "y", y, n), conv._stream(stream)), "seq_norm_fwd")
+    conv._check(load().seq_norm_fwd(_of(h, "seq_norm"), _s(h, "x", x), _so(h, "res", res), _t(w, h.f32, h.info.Cp, "w"), _so(h, "r", r),
+                                    _s(h, "y", y), conv._stream(stream)), "seq_norm_fwd")
 
 
 def _q(h, q):
-    if q.dtype is not h.i8 or q.numel() < h.q or not q.is_cuda or q.stride() != h.strides["q"]:
-        _misfit(h, "q", q, h.q, h.i8)
+    if q.dtype is not h.i8 or q.shape != h.shapes["q"] or not q.is_cuda or q.stride() != h.strides["q"]:
+        _misfit(h, "q", q, h.i8)
     return q.data_ptr()
 
 
 def seq_norm_fwd_q8(h, x, res, w, r, q, scale, stream=None):
-    n = h.all
-    conv._check(load().seq_norm_fwd_q8(_of(h, "seq_norm"), _s(h, "x", x, n), _so(h, "res", res, n), _t(w, h.f32, h.info.Cp, "w"), _so(h, "r", r, n),
+    conv._check(load().seq_norm_fwd_q8(_of(h, "seq_norm"), _s(h, "x", x), _so(h, "res", res), _t(w, h.f32, h.info.Cp, "w"), _so(h, "r", r),
                                        _q(h, q), _t(scale, h.f32, h.positions, "scale"), conv._stream(stream)), "seq_norm_fwd_q8")
 
 
 def seq_norm_bwd(h, r, w, dy, dr, dx, dw, ws, stream=None):
-    n = h.all
-    conv._check(load().seq_norm_bwd(_of(h, "seq_norm"), _s(h, "r", r, n), _t(w, h.f32, h.info.Cp, "w"), _s(h, "dy", dy, n), _so(h, "dr", dr, n),
-                                    _s(h, "dx", dx, n), _t(dw, h.f32, h.info.Cp, "dw"), *_ws(ws), conv._stream(stream)), "seq_norm_bwd")
+    conv._check(load().seq_norm_bwd(_of(h, "seq_norm"), _s(h, "r", r), _t(w, h.f32, h.info.Cp, "w"), _s(h, "dy", dy), _so(h, "dr", dr),
+                                    _s(h, "dx", dx), _t(dw, h.f32, h.info.Cp, "dw"), *_ws(ws), conv._stream(stream)), "seq_norm_bwd")
 
 
 # ---------------------------------------------------------------------------- products with 4-bit weights

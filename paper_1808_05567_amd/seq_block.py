@@ -193,8 +193,8 @@ class SeqBlock:
         N, L, C, Ci, S, W = self.dims
         r = self.r
         # (the projections take pointers as they come)
-        seq._s(self.norm, "dy", dout, self.norm.all)
-        seq._so(self.norm, "dr", dr, self.norm.all)
+        seq._s(self.norm, "dy", dout)
+        seq._so(self.norm, "dr", dr)
         if lengths is not None:
             outside = self._outside(lengths)
             dout, dr = self._cleared(dout, outside), None if dr is None else self._cleared(dr, outside)

@@ -1,0 +1,80 @@
+"""What the binding of the sequence operators refuses before a call reaches the library: tensors that stand for ones on the GPU, and a library that
+only notes its calls."""
+import pytest
+import torch
+
+from paper_1808_05567_amd import seq
+
+
+class OnGpu(torch.Tensor):
+    """A tensor in host memory that says it is on the GPU."""
+    is_cuda = True
+
+
+def tensor(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the library's functions as they are called; none runs."""
+    done, real = [], seq.load()
+
+    class Noted:
+        def __getattr__(self, name):
+            if name.endswith("_create") or name in ("seq_query", "seq_destroy"):
+                return getattr(real, name)
+            return lambda *args: done.append(name) or 0
+    monkeypatch.setattr(seq, "load", Noted)
+    return done
+
+
+N, C, L, W = 2, 16, 4, 4  # (two blocks of bf16)
+
+
+def conv_fwd(views, x, y):
+    h = seq.seq_conv_create(N, C, L, W, seq.SEQ_BF16, views=views)
+    seq.seq_conv_fwd(h, x, tensor(W, C, dtype=torch.float32), None, y, stream=0)
+
+
+def test_tensors_of_fewer_places_are_refused(calls):
+    """Half of the blocks of a wider tensor: others of the same strides and as many elements, with fewer sequences, blocks or positions."""
+    half, dense = tensor(N, 4, L, 8)[:, :2], tensor(N, 2, L, 8)
+    fewer = [tensor(1, 4, L, 8), tensor(4, 4, L, 8)[:, :1], tensor(3, 4, L, 8)[:, :2, :3], tensor(N, 4, L, 8)[:, :2, :, :4]]
+    assert all(t.stride() == half.stride() for t in fewer) and all(t.numel() >= N * C * L for t in fewer[:3])
+    for bad in fewer:
+        with pytest.raises(ValueError):
+            conv_fwd({"x": half}, bad, dense)
+        with pytest.raises(ValueError):
+            conv_fwd({"y": half}, dense, bad)
+    assert not calls
+    conv_fwd({"x": half, "y": half}, half, tensor(3, 4, L, 8)[:, 1:])  # (more of them do)
+    with pytest.raises(ValueError):
+        conv_fwd(None, tensor(N, L, 2, 8), dense)  # (as many elements in another order)
+    # dense ones may have their places in any dimensions
+    for good in (dense, dense.flatten(), tensor(1, 4, L, 8), tensor(N + 1, 2, L, 8), tensor(N, 2, L, 1, 8)):
+        conv_fwd(None, good, dense)
+    assert calls == ["seq_conv_fwd"] * 6
+
+
+def test_places_of_states_and_of_eight_bits_are_counted_too(calls):
+    S, f = 16, torch.float32
+    part = tensor(N, 6, L, 8)[:, :2]
+    h = seq.seq_scan_create(N, C, L, S, seq.SEQ_BF16, views={"B": part})
+    x, A, ws = tensor(N, 2, L, 8), tensor(S, C, dtype=f), tensor(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        seq.seq_scan_fwd(h, x, x, A, tensor(1, 6, L, 8), x, x, ws, stream=0)
+    seq.seq_scan_fwd(h, x, x, A, part, x, x, ws, stream=0)
+    n = seq.seq_norm_create(N, 32, L, seq.SEQ_BF16, views={"q": tensor(N, 5, L, 16, dtype=torch.int8)[:, :2]})
+    x, w, scale = tensor(N, 4, L, 8), tensor(32, dtype=f), tensor(N, L, dtype=f)
+    with pytest.raises(ValueError):
+        seq.seq_norm_fwd_q8(n, x, None, w, None, tensor(1, 5, L, 16, dtype=torch.int8), scale, stream=0)
+    seq.seq_norm_fwd_q8(n, x, None, w, None, tensor(N, 5, L, 16, dtype=torch.int8)[:, 3:], scale, stream=0)
+    assert calls == ["seq_scan_fwd", "seq_norm_fwd_q8"]
+
+
+def test_single_places_have_any_stride(calls):
+    one = seq.seq_conv_create(1, 8, 1, W, seq.SEQ_BF16, slots=1)
+    x, w, state = tensor(64).as_strided((1, 1, 1, 8), (40, 16, 24, 1)), tensor(W, 8, dtype=torch.float32), tensor(1, 1, W - 1, 8)
+    seq.seq_conv_step(one, x, w, None, state, x, stream=0)
+    assert calls == ["seq_conv_step"]
