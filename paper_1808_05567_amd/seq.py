@@ -150,7 +150,7 @@ def _strides(h, names, views, N, C, L, wide=()):
         h.strides[name] = h.dense[name] if t is None else tuple(t.stride())
 
 
-def _views(views, names, desc, vlen):
+def _views(views, names, desc, vlen, N, C, L, wide=()):
     for name, t in (views or {}).items():
         if name not in names:
             continue
@@ -159,6 +159,9 @@ def _views(views, names, desc, vlen):
             continue
         if t.dim() != 4 or t.shape[3] != v or (t.stride(3) != 1 and v > 1):
             raise ValueError("%s: a tensor [N, Cb, L, %d] is wanted, its last dimension dense" % (name, v))
+        extents = (N, -(-dict(wide).get(name, C) // v), L)
+        if any(t.shape[i] == 1 < extents[i] for i in range(3)):
+            raise ValueError("%s: a tensor of %s does not give the strides of one of %s" % (name, tuple(t.shape), (*extents, v)))
         # (a dimension of one place has any stride)
         setattr(desc, name, SeqView(*(t.stride(i) if t.shape[i] > 1 else v for i in range(3))))
 
@@ -195,7 +198,7 @@ def _ws(ws):
 # ---------------------------------------------------------------------------- short convolution
 def seq_conv_create(N, C, L, W, dtype=SEQ_F32, silu=True, slots=0, views=None) -> SeqPlan:
     d = SeqConvDesc(N=N, C=C, L=L, W=W, silu=1 if silu else 0, slots=slots, dtype=dtype)
-    _views(views, _CONV_VIEWS, d, _vlen(dtype))
+    _views(views, _CONV_VIEWS, d, _vlen(dtype), N, C, L)
     h = SeqPlan("seq_conv_create", d, dtype, {"N": N})
     _strides(h, _CONV_VIEWS, views, N, C, L)
     h.w, h.state = W * h.info.Cp, slots * h.info.Cp * (W - 1)
@@ -227,9 +230,10 @@ def seq_conv_bwd(h, x, w, bias, dy, dx, dw, dbias, ws, lengths=None, stream=None
 # ---------------------------------------------------------------------------- selective scan
 def seq_scan_create(N, C, L, S, dtype=SEQ_F32, G=1, softplus=True, slots=0, views=None) -> SeqPlan:
     d = SeqScanDesc(N=N, Ch=C, L=L, S=S, G=G, softplus=1 if softplus else 0, slots=slots, dtype=dtype)
-    _views(views, _SCAN_VIEWS, d, _vlen(dtype))
+    wide = [(k, G * S) for k in ("B", "C", "dB", "dC")]
+    _views(views, _SCAN_VIEWS, d, _vlen(dtype), N, C, L, wide)
     h = SeqPlan("seq_scan_create", d, dtype, {"N": N})
-    _strides(h, _SCAN_VIEWS, views, N, C, L, [(k, G * S) for k in ("B", "C", "dB", "dC")])
+    _strides(h, _SCAN_VIEWS, views, N, C, L, wide)
     h.A, h.state = S * h.info.Cp, slots * S * h.info.Cp
     return h
 
@@ -266,7 +270,7 @@ def seq_scan_bwd(h, x, dt, A, B, C, dy, dx, ddt, dA, dB, dC, ws, D=None, z=None,
 # ---------------------------------------------------------------------------- norm
 def seq_norm_create(N, C, L, dtype=SEQ_F32, eps=1e-5, views=None) -> SeqPlan:
     d = SeqNormDesc(N=N, C=C, L=L, dtype=dtype, eps=eps)
-    _views(views, _NORM_VIEWS, d, _vlen(dtype))
+    _views(views, _NORM_VIEWS, d, _vlen(dtype), N, C, L)
     h = SeqPlan("seq_norm_create", d, dtype, {"N": N, "positions": N * L})
     _strides(h, _NORM_VIEWS, views, N, C, L)
     return h

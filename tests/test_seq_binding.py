@@ -78,3 +78,19 @@ def test_single_places_have_any_stride(calls):
     x, w, state = tensor(64).as_strided((1, 1, 1, 8), (40, 16, 24, 1)), tensor(W, 8, dtype=torch.float32), tensor(1, 1, W - 1, 8)
     seq.seq_conv_step(one, x, w, None, state, x, stream=0)
     assert calls == ["seq_conv_step"]
+
+
+def test_views_give_a_stride_for_every_place(calls):
+    """A view with one sequence, block or position says nothing of where the second lies."""
+    wide = tensor(N, 4, L, 8)
+    for view in (wide[:1, :2], wide[:, :1], wide[:, :2, :1]):
+        with pytest.raises(ValueError):
+            seq.seq_conv_create(N, C, L, W, seq.SEQ_BF16, views={"x": view})
+    with pytest.raises(ValueError):
+        seq.seq_scan_create(N, C, L, 16, seq.SEQ_BF16, views={"B": wide[:, :1]})
+    with pytest.raises(ValueError):
+        seq.seq_norm_create(N, 32, L, seq.SEQ_BF16, views={"q": tensor(N, 1, L, 16, dtype=torch.int8)})
+    # where the plan has one too, and for tensors of the same strides that have fewer, it may be any
+    seq.seq_conv_create(N, 8, 1, W, seq.SEQ_BF16, views={"x": wide[:, :1, :1]})
+    conv_fwd({"x": tensor(N + 2, 4, L, 8)[:2, :2, :3]}, wide[:, :2], wide.flatten())
+    assert calls == ["seq_conv_fwd"]
