@@ -163,7 +163,10 @@ def _views(views, names, desc, vlen, N, C, L, wide=()):
         if any(t.shape[i] == 1 < extents[i] for i in range(3)):
             raise ValueError("%s: a tensor of %s does not give the strides of one of %s" % (name, tuple(t.shape), (*extents, v)))
         # (a dimension of one place has any stride)
-        setattr(desc, name, SeqView(*(t.stride(i) if t.shape[i] > 1 else v for i in range(3))))
+        strides = [t.stride(i) if t.shape[i] > 1 else v for i in range(3)]
+        if not any(strides):  # (which would mean a dense tensor)
+            raise ValueError("%s: one block for all places" % name)
+        setattr(desc, name, SeqView(*strides))
 
 
 def _vlen(dtype):

@@ -94,3 +94,14 @@ def test_views_give_a_stride_for_every_place(calls):
     seq.seq_conv_create(N, 8, 1, W, seq.SEQ_BF16, views={"x": wide[:, :1, :1]})
     conv_fwd({"x": tensor(N + 2, 4, L, 8)[:2, :2, :3]}, wide[:, :2], wide.flatten())
     assert calls == ["seq_conv_fwd"]
+
+
+def test_views_of_one_block_for_all_places_are_refused(calls):
+    """Three distances of zero stand for a dense tensor, which a block that is expanded over all places is not."""
+    with pytest.raises(ValueError):
+        seq.seq_conv_create(N, C, L, W, seq.SEQ_BF16, views={"x": tensor(1, 1, 1, 8).expand(N, 2, L, 8)})
+    # over some of the dimensions it may be, and over all if there is one sequence (whose distance is not zero then)
+    for same in (tensor(N, 1, 1, 8).expand(N, 2, L, 8), tensor(1, 2, L, 8).expand(N, 2, L, 8)):
+        conv_fwd({"x": same}, same, tensor(N, 2, L, 8))
+    seq.seq_conv_create(1, C, L, W, seq.SEQ_BF16, views={"x": tensor(1, 1, 1, 8).expand(1, 2, L, 8)})
+    assert calls == ["seq_conv_fwd"] * 2
