@@ -195,7 +195,11 @@ def seq_workspace(h, device="cuda"):
 
 
 def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    if ws is None:
+        return None, 0
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("ws: a dense tensor on the GPU is wanted, not one with strides %s on %s" % (tuple(ws.stride()), ws.device))
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 # ---------------------------------------------------------------------------- short convolution

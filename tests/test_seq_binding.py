@@ -105,3 +105,14 @@ def test_views_of_one_block_for_all_places_are_refused(calls):
         conv_fwd({"x": same}, same, tensor(N, 2, L, 8))
     seq.seq_conv_create(1, C, L, W, seq.SEQ_BF16, views={"x": tensor(1, 1, 1, 8).expand(1, 2, L, 8)})
     assert calls == ["seq_conv_fwd"] * 2
+
+
+def test_workspaces_are_dense_and_on_the_gpu(calls):
+    h = seq.seq_conv_create(N, C, L, W, seq.SEQ_BF16)
+    x, w, size = tensor(N, 2, L, 8), tensor(W, C, dtype=torch.float32), h.info.workspace_bytes
+    for bad in (torch.zeros(size, dtype=torch.uint8), tensor(2 * size, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            seq.seq_conv_bwd(h, x, w, None, x, x, w, None, bad, stream=0)
+    assert not calls
+    seq.seq_conv_bwd(h, x, w, None, x, x, w, None, tensor(size // 4, dtype=torch.float32), stream=0)
+    assert calls == ["seq_conv_bwd"]
