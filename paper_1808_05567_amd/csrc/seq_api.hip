@@ -3,6 +3,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <iterator>
 #include <new>
 
 #include "seq_internal.h"
@@ -273,9 +274,16 @@ conv_status_t seq_scan_create(const seq_scan_desc_t *d, seq_handle_t *out)
     p->bwd_ws = ends(b) + up((size_t)b.N * b.chunks * state) + up((size_t)b.N * b.chunks * b.notes * state) +
                 up((size_t)b.N * b.chunks * b.notes * b.Cp * 4) + up((size_t)b.N * b.chunks * 2 * b.Cp * 4) +
                 up((size_t)b.N * b.L * b.G * b.btiles * 2 * b.S * 4);
-    const int64_t items[] = {waves * std::max(a.chunks, b.chunks) * 128, (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves, (int64_t)a.N * a.S * (a.Cp + 63) * 16,
-                             (int64_t)a.N * ((a.Cp + 127) / 128) * 256};
-    const bool fits = *std::max_element(items, items + 4) <= kMaxItems && (int64_t)b.N * b.chunks < 1LL << 31;
+    const auto over_runs = [](const SeqScanArgs &q, bool sums) { return (seq_scan_waves(q, sums) + kSeqScanWaves - 1) / kSeqScanWaves * 64 * kSeqScanWaves; };
+    const auto joined = [](const SeqScanArgs &q) { return q.chunks > 1 ? seq_join_groups(q) * 64 * seq_join_waves(q.chunks) : 0; };
+    const int64_t items[] = {over_runs(a, true),
+                             a.chunks > 1 ? over_runs(a, false) : 0,
+                             joined(a),
+                             b.L > 8 ? over_runs(b, false) : 0,
+                             joined(b),
+                             (int64_t)b.N * b.G * b.btiles * b.chunks * 64 * kSeqBwdWaves,
+                             a.L == 1 ? (int64_t)a.N * ((a.Cp + 127) / 128) * 256 : 0};
+    const bool fits = *std::max_element(std::begin(items), std::end(items)) <= kMaxItems && (int64_t)b.N * b.chunks < 1LL << 31;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 

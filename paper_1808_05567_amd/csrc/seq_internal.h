@@ -95,6 +95,13 @@ constexpr int seq_scan_states(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : S <= 3
 constexpr int seq_scan_bwd_channels(int SP) { return 512 / SP; }
 constexpr int kSeqBwdWaves = 4;
 
+// The scan's launches, as they are made and as a plan's are counted.  Those over runs: waves of 64 channels, kSeqScanWaves a workgroup, more than
+// 32 states by two waves where no sum over them is formed.  That which joins runs: workgroups of 64 columns, a wave per 16 runs, up to 16.
+constexpr int kSeqScanWaves = 4, kSeqJoinWaves = 16;
+inline int64_t seq_scan_waves(const SeqScanArgs &a, bool sums) { return (int64_t)a.N * a.G * a.tiles * a.chunks * (sums || a.S <= 32 ? 1 : 2); }
+inline int64_t seq_join_groups(const SeqScanArgs &a) { return a.N * (((int64_t)a.S * a.Cp + 63) / 64); }
+inline int seq_join_waves(int chunks) { return chunks <= 16 * kSeqJoinWaves ? (chunks + 15) / 16 : kSeqJoinWaves; }
+
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;
 

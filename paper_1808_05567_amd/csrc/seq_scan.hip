@@ -18,7 +18,7 @@
 namespace convmi {
 namespace {
 
-constexpr int kWaves = 4;  // a workgroup
+constexpr int kWaves = kSeqScanWaves;  // a workgroup
 
 template <int SP>
 struct States {
@@ -315,10 +315,9 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
 // The state at the start of each run from those the runs end in, in place; the gradient at the end of each the same way, from the back.  The
 // waves of a workgroup (one per 16 runs, up to 16) take a part each of the runs of 64 columns: what a part does to a state is put
 // together first, then it is gone through again from the right one.  (One thread for all runs: 2 x 174 of them, both ways, 256 channels, 16 states, 30 us; so 11.)
-constexpr int kJoinParts = 16;
-__global__ __launch_bounds__(64 * kJoinParts) void seq_scan_join_kernel(const SeqScanArgs a)
+__global__ __launch_bounds__(64 * kSeqJoinWaves) void seq_scan_join_kernel(const SeqScanArgs a)
 {
-    __shared__ float of_zero[kJoinParts][64], of_d[kJoinParts][64];
+    __shared__ float of_zero[kSeqJoinWaves][64], of_d[kSeqJoinWaves][64];
     const int lane = threadIdx.x % 64, part = threadIdx.x / 64, parts = blockDim.x / 64;
     const long long state = (long long)a.S * a.Cp, columns = (state + 63) / 64;
     const int n = (int)(blockIdx.x / columns);
@@ -451,14 +450,13 @@ __global__ __launch_bounds__(256) void seq_scan_step_kernel(const SeqScanArgs a)
 
 hipError_t join(const SeqScanArgs &a, hipStream_t s)
 {
-    const int parts = a.chunks <= 16 * kJoinParts ? (a.chunks + 15) / 16 : kJoinParts;
-    seq_scan_join_kernel<<<(unsigned)(a.N * (((long long)a.S * a.Cp + 63) / 64)), 64 * parts, 0, s>>>(a);
+    seq_scan_join_kernel<<<(unsigned)seq_join_groups(a), 64 * seq_join_waves(a.chunks), 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int SP, int MODE>
 hipError_t launch_mode(const SeqScanArgs &a, hipStream_t s)
 {
-    const long long waves = (long long)a.N * a.G * a.tiles * a.chunks * (MODE == 1 ? 1 : (a.S + SP - 1) / SP);
+    const int64_t waves = seq_scan_waves(a, MODE == 1);
     seq_scan_kernel<T, SP, MODE><<<(unsigned)((waves + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a);
     return hipGetLastError();
 }

@@ -116,3 +116,16 @@ def test_workspaces_are_dense_and_on_the_gpu(calls):
     assert not calls
     seq.seq_conv_bwd(h, x, w, None, x, x, w, None, tensor(size // 4, dtype=torch.float32), stream=0)
     assert calls == ["seq_conv_bwd"]
+
+
+def test_plans_are_refused_for_launches_that_they_make():
+    """States are joined in one launch where there are several runs, by a wave for 16 of them: single positions and short sequences of many states do not need
+    as many work-items as the longest."""
+    from paper_1808_05567_amd import conv
+    b16 = seq.SEQ_BF16
+    for n, c, l, s in ((512, 8192, 1, 64), (1024, 8192, 1, 32), (256, 1 << 14, 65, 64), (1 << 12, 1 << 14, 16, 64)):
+        seq.seq_scan_create(n, c, l, s, b16, slots=n)
+    for n, c, l, s in ((1 << 12, 1 << 14, 65, 64), (1 << 20, 1 << 13, 1, 4), (1 << 19, 1 << 10, 65, 8)):
+        with pytest.raises(conv.ConvError) as e:
+            seq.seq_scan_create(n, c, l, s, b16)
+        assert e.value.status == conv.CONV_EUNSUPPORTED
