@@ -51,7 +51,8 @@ typedef enum {
 } seq_dtype_t;
 
 /* Distances in elements between sequences, channel blocks and positions: multiples of v, not
- * negative; those of an output may not let two elements share a place. */
+ * negative, 2^40 at most and 2^58 over all of a dimension; those of an output may not let two
+ * elements share a place. */
 typedef struct {
     int64_t n, c, l;
 } seq_view_t;

@@ -29,7 +29,7 @@ struct seq_plan {
 namespace {
 
 // (a launch has at most 2^32 work-items)
-constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxTileStride = 1LL << 24;
+constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxSpan = 1LL << 58, kMaxTileStride = 1LL << 24;
 
 bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -53,7 +53,7 @@ bool view_of(const seq_view_t &v, int N, int Cb, int L, int vlen, bool out, SeqV
     } d[3] = {{N, v.n}, {Cb, v.c}, {L, v.l}};
     for (auto &e : d) {
         if (e.extent == 1) e.stride = 0;
-        if (e.stride < 0 || e.stride > kMaxStride || e.stride % vlen) return false;
+        if (e.stride < 0 || e.stride > kMaxStride || e.stride % vlen || (e.extent > 1 && e.stride > kMaxSpan / (e.extent - 1))) return false;
     }
     to = {d[0].stride, d[1].stride, d[2].stride};
     if (!out) return true;

@@ -129,3 +129,19 @@ def test_plans_are_refused_for_launches_that_they_make():
         with pytest.raises(conv.ConvError) as e:
             seq.seq_scan_create(n, c, l, s, b16)
         assert e.value.status == conv.CONV_EUNSUPPORTED
+
+
+def test_distances_that_64_bits_do_not_hold_are_refused():
+    """Positions 2^40 elements apart: 2^24 of them come back to the first one's place, modulo 2^64."""
+    import ctypes
+    from paper_1808_05567_amd import conv
+    far = 1 << 40
+    for name in ("x", "y"):
+        for n, l, strides, ok in ((2, (1 << 24) + 1, (far, 8, far), False), (1, (1 << 24) + 1, (8, 8, far), False), (1, 1 << 17, (8, 8, far), True)):
+            d = seq.SeqConvDesc(N=n, C=8, L=l, W=W, dtype=seq.SEQ_BF16)
+            setattr(d, name, seq.SeqView(*strides))
+            h = ctypes.c_void_p()
+            status = seq.load().seq_conv_create(ctypes.byref(d), ctypes.byref(h))
+            assert (status == conv.CONV_OK) == ok and (ok or status == conv.CONV_EINVAL), (name, n, l)
+            if ok:
+                seq.load().seq_destroy(h)
