@@ -197,6 +197,13 @@ static __device__ __forceinline__ int seq_length(const int *lengths, int n, int 
 }
 
 static __device__ __forceinline__ float seq_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// A state's A for the binary exponential.  Minus infinity goes as the lowest number: what fills up an eight of positions has steps of zero, which
+// times infinity are no numbers.
+static __device__ __forceinline__ float seq_decay(float A)
+{
+    const float a = A * kLog2e;
+    return a == -INFINITY ? -3.40282347e38f : a;
+}
 // 1 / (1 + exp(-x)); the hardware's exponential and reciprocal are good to an ulp
 static __device__ __forceinline__ float seq_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + seq_exp2(-kLog2e * x)); }
 

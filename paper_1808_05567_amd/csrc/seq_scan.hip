@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64 * kWaves) void seq_scan_kernel(const SeqScanArgs
     float A[SP], h[SP], gr[SG], P[SG];
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s < S ? a.A[(long long)(s0 + s) * a.Cp + cs] * kLog2e : 0.0f;
+        A[s] = s < S ? seq_decay(a.A[(long long)(s0 + s) * a.Cp + cs]) : 0.0f;
         h[s] = 0;
         if (ENDS) gr[s % SG] = 0, P[s % SG] = 1;
     }
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * kSeqJoinWaves) void seq_scan_join_kernel(const
     const int c = (int)(e % a.Cp);
     const bool live = e < state && c < a.Ch;
     const int slot = a.slots ? a.slots[n] : n;
-    const float A = live ? a.A[e] * kLog2e : 0.0f;
+    const float A = live ? seq_decay(a.A[e]) : 0.0f;
     const int each = (a.chunks + parts - 1) / parts, begin = min(part * each, a.chunks), end = min(begin + each, a.chunks);
     const float *sd = a.sd + (long long)n * a.chunks * a.Cp + c;
     const auto chain = [&](float *ends, float first, bool back) {

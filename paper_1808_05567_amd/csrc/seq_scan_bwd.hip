@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            A[j][i] = there[i] ? q[i] * kLog2e : 0.0f;
+            A[j][i] = there[i] ? seq_decay(q[i]) : 0.0f;
             carry[j][i] = there[i] && s + j < a.S ? r[i] : 0.0f;
         }
     }
