@@ -204,6 +204,8 @@ static __device__ __forceinline__ float seq_decay(float A)
     const float a = A * kLog2e;
     return a == -INFINITY ? -3.40282347e38f : a;
 }
+// What a run makes of the state h before it: `own` from zeros, and h times 2^e.  Zero stays zero, whatever it would grow by.
+static __device__ __forceinline__ float seq_carry(float e, float h, float own) { return h == 0 ? own : fmaf(seq_exp2(e), h, own); }
 // 1 / (1 + exp(-x)); the hardware's exponential and reciprocal are good to an ulp
 static __device__ __forceinline__ float seq_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + seq_exp2(-kLog2e * x)); }
 

@@ -347,7 +347,7 @@ __global__ __launch_bounds__(64 * kSeqJoinWaves) void seq_scan_join_kernel(const
             if (part == parts - 1) break;  // (no part is after it; up to 16 runs are in registers now)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                h = fmaf(seq_exp2(A * d[i]), h, own[i]);
+                h = seq_carry(A * d[i], h, own[i]);
                 sum += d[i];
             }
         }
@@ -355,14 +355,14 @@ __global__ __launch_bounds__(64 * kSeqJoinWaves) void seq_scan_join_kernel(const
         of_d[part][lane] = sum;
         __syncthreads();
         h = first;
-        for (int p = 0; p < part; ++p) h = fmaf(seq_exp2(A * of_d[p][lane]), h, of_zero[p][lane]);
+        for (int p = 0; p < part; ++p) h = seq_carry(A * of_d[p][lane], h, of_zero[p][lane]);
         for (int k0 = begin; k0 < end; k0 += 16) {
             if (each > 16) load(k0);  // (or still there)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int k = back ? a.chunks - 1 - k0 - i : k0 + i;
                 if (live && k0 + i < end) ends[k * state] = h;
-                h = fmaf(seq_exp2(A * d[i]), h, own[i]);
+                h = seq_carry(A * d[i], h, own[i]);
             }
         }
         __syncthreads();

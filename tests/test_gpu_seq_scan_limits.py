@@ -60,3 +60,24 @@ def test_a_step_of_states_that_keep_nothing(dtype):
     (y, after), (my, ma) = oracle.scan(*args, **ref), oracle.scan(*args, **ref, mag=True)
     close(Y.get(), y, bound(1) * my, dtype == seq.SEQ_BF16, "y")
     close(st.double().cpu().numpy()[..., :C], after, bound(1) * ma, False, "state")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_states_of_zero_that_would_grow(dtype):
+    """A above zero: what a run of positions multiplies a state with passes 2^128, and the state is zero until the last positions."""
+    N, C, L, S = 2, 72, 300, 5
+    rng, p = data(N, C, L, S, 1, dtype, 8)
+    p["A"] = np.float64(np.float32(rng.uniform(0.9, 1.1, (S, C))))
+    p["dt"] = np.full_like(p["dt"], 8.0)
+    p["x"][:, :L - 4] = 0
+    t, opt, A, ref = tensors(p, N, C, L, S, 1, True, False, None, "dense", dtype)
+    Y, DY = Seq(N, C, L, dtype), Seq(N, C, L, dtype, "dense", p["dy"])
+    h = seq.seq_scan_create(N, C, L, S, dtype, slots=N)
+    st = torch.zeros(N, S, h.info.Cp, device="cuda")
+    ws = seq.seq_workspace(h).fill_(0xFF)
+    seq.seq_scan_fwd(h, t["x"].t, t["dt"].t, A, t["B"].t, t["C"].t, Y.t, ws, z=t["z"].t, state_in=st, state_out=st, **opt)
+    args = (p["x"], p["dt"], p["A"], p["B"], p["Cm"])
+    (y, after), (my, ma) = oracle.scan(*args, **ref), oracle.scan(*args, **ref, mag=True)
+    # (an exponent of 13 binary places, off by its step's two units, its factor's and its product's: 36 units a position, of which there are three)
+    close(Y.get(), y, (bound(4) + 128 * U) * my, dtype == seq.SEQ_BF16, "y")
+    close(st.double().cpu().numpy()[..., :C], after, (bound(4) + 128 * U) * ma, False, "state")
