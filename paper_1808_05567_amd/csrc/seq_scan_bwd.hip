@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_scan_bwd_kernel(const SeqS
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float h = e > 0 ? seq_carry(A[j][i] * note_d[i], before[j][i], note[j][i]) : before[j][i];
+                    const float h = e > 0 ? fmaf(seq_exp2(A[j][i] * note_d[i]), before[j][i], note[j][i]) : before[j][i];
                     hs[0][j][i] = there[i] ? h : 0.0f;
                 }
             if (e > 1) fetch_note(e - 1);
