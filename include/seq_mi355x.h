@@ -134,7 +134,9 @@ conv_status_t seq_scan_step(seq_handle_t h, const void *x, const void *dt, const
                             void *stream);
 /* Gradients of seq_scan_fwd without states.  dx, ddt, dB, dC: sequence tensors; dz: one where
  * there is a z; dA: fp32 [S][Cp]; dD, ddt_bias: fp32 vectors or NULL.  The decays exp(d A) of up to
- * 64 positions are multiplied together: where d A > 0 their product has to stay below 2^128. */
+ * 64 positions are multiplied together: where d A > 0 their product has to stay below 2^128.
+ * The scratch holds the states in fp32 at every eighth position: for sequences of 64 positions and
+ * more some 11 bytes an element of x at 16 states, 53 at 64 (seq_query has the size). */
 conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const float *A,
                            const void *B, const void *C, const float *D, const void *z,
                            const float *dt_bias, const void *dy, void *dx, void *ddt, float *dA,

@@ -9,8 +9,9 @@
 // A lane's 16 bytes of weights are 8 channels of each of 4 runs of 32, so that one instruction takes one run of 32 whole and
 // a group of 32, 64 or 128 channels is one, two or four of them, whatever its scale.
 //
-// Bound by the weights' bytes for few rows: 4096 x 8192 for one token in 8 bits 7.0 us (18 MB, 2.5 TB/s, of which a launch and a first trip to memory
-// are some 4 us), in bf16 8.3; for 32 tokens 7.9 and 10.0, for 64 11.4 and 14.6, in fp32 14 for one, 20 for 32.
+// Bound by the weights' bytes for few rows.  The kernel under the profiler, three sets of tensors in turn: 4096 x 8192 for one token in 8 bits 6.8 us
+// (18 MB, 2.6 TB/s, of which a launch and a first trip to memory are some 4 us), in bf16 7.7, in fp32 12.6; for 32 tokens 8.1, 10.2 and 20.8; for 64
+// 11.0, 15.0 and 39.  (A call among others takes as long or up to 0.7 us less.)
 #include "seq_internal.h"
 
 namespace convmi {

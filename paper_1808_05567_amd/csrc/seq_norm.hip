@@ -5,7 +5,7 @@
 //
 // A few operations an element: bound by memory.  A workgroup holds whole positions in registers between the sums over
 // their channels and the result, so that each tensor is read once.  Measured, 8 x 2048 positions of 2048 channels in bf16, 268 MB: forward 54 us
-// (5.0 TB/s; positions side by side 48), backward 78 (65) and 5 for the sums of dw; 2 x 1024 positions in fp32, 67 MB, backward 18 and 4.
+// (5.0 TB/s; positions side by side 48), backward 78 (66) and 5 for the sums of dw; 2 x 1024 positions in fp32, 67 MB, backward 18 and 4.
 #include <type_traits>
 
 #include "seq_internal.h"
@@ -16,7 +16,8 @@ namespace {
 constexpr int kMaxThreads = 512;
 
 // Sums (or largest unsigned) of v over the threads with the same place in the tile of LT positions, in all of them: by turns of
-// rows of 16 lanes, then between rows and halves of a wave, then in LDS (ALONE: each wave has a position of its own).
+// rows of 16 lanes, then between rows and halves of a wave, then in LDS (ALONE: each wave has a position of its own).  Within rows a lane
+// starts from its own number: sums of one position may differ by a unit between its lanes, the same way on every run.
 template <int LT, bool MAX, bool ALONE = false>
 static __device__ __forceinline__ float row_sum(float v, float *lds)
 {

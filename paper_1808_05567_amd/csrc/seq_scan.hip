@@ -10,7 +10,7 @@
 // zeros and notes the state it ends in and the sum of d, from which what the run does to any state follows:
 // exp(A sum d) h + that; a second puts these together in order; a third goes through each run from the right state.
 //
-// Measured, one sequence of 4096 positions, 2048 channels, 16 states, bf16, 64 runs: 36, 8 and 48 us.  A position of 16 states takes the first launch
+// Measured, one sequence of 4096 positions, 2048 channels, 16 states, bf16, 64 runs: 35, 7 and 49 us.  A position of 16 states takes the first launch
 // some 350 clocks where its operations take 320; the step's softplus and the loads of a position another 130 each, and what is left is the
 // launches and the waves' first trips to memory.
 #include "seq_internal.h"
