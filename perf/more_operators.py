@@ -1,0 +1,616 @@
+"""Further operators of ``paper_1808_05567_amd.seq`` as cases that can be timed and checked.
+
+A case is one pass through one of them, as a program that trains or serves a language model of
+recurrent blocks calls it:
+
+  rec    a gated linear recurrence of every channel: over prompts and in training ("fwd"), its
+         gradients ("bwd"), over one new token a sequence ("step")
+  lnorm  a layer norm with the residual's addition: forward, its gradients, and with an output in
+         8 bits for the products that follow ("q8")
+  adamw  an AdamW step over all of a model's tensors, with states in 32 bits or in 8
+
+Tensors of sequences have the library's blocked form, [N][Cb][L][v] with v channels in 16 bytes,
+dense ("blocked") or with a position's channels side by side ("rows").  Sums, states, parameters
+and their gradients' sums are fp32.
+"""
+import math
+
+import torch
+import torch.nn.functional as F
+
+own = False
+
+_T = {"f32": torch.float32, "bf16": torch.bfloat16}
+EPS = 1e-5
+BETA1, BETA2, ADAM_EPS, DECAY, RATE = 0.9, 0.95, 1e-8, 0.1, 1e-3
+BLOCK = 256  # numbers of a tensor with a scale of their own, where states have 8 bits
+
+# One block of a model: its norm, the projections of its two inner inputs and of its gates, a short convolution, the recurrence's A, and the way back.
+_VECTORS = "1024,2048,2048,2048,2048"
+_MATRICES = "4096x1024,4x2048,2048x2048,32x2048,1024x2048"
+
+
+# ---------------------------------------------------------------------------- cases
+def listed():
+    return [
+        # one new token of each of 32 sequences: latency
+        {"name": "rec_step_b32_bf16", "op": "rec", "pass": "step", "dtype": "bf16", "layout": "blocked",
+         "N": 32, "C": 4096, "L": 1, "gate": True, "slots": 40},
+        # one long prompt, whose state serves its first new token
+        {"name": "rec_prompt_b1_bf16", "op": "rec", "pass": "fwd", "dtype": "bf16", "layout": "blocked",
+         "N": 1, "C": 2048, "L": 8192, "gate": True, "slots": 4, "ragged": False},
+        # prompts of different lengths, one of them none, in full precision, channels that are no whole number of waves
+        {"name": "rec_ragged_b5_f32", "op": "rec", "pass": "fwd", "dtype": "f32", "layout": "rows",
+         "N": 5, "C": 1000, "L": 777, "gate": False, "slots": 7, "ragged": True},
+        # a training step's forward pass
+        {"name": "rec_train_fwd_bf16", "op": "rec", "pass": "fwd", "dtype": "bf16", "layout": "blocked",
+         "N": 8, "C": 2048, "L": 2048, "gate": True, "slots": 8, "ragged": False},
+        # and its gradients
+        {"name": "rec_train_bwd_bf16", "op": "rec", "pass": "bwd", "dtype": "bf16", "layout": "blocked",
+         "N": 8, "C": 2048, "L": 2048, "gate": True, "ragged": False},
+        # before the projections of one new token of each of 16 sequences
+        {"name": "lnorm_q8_b16_bf16", "op": "lnorm", "pass": "q8", "dtype": "bf16", "layout": "blocked",
+         "N": 16, "C": 4096, "L": 1, "residual": True},
+        # where two blocks of a training step meet
+        {"name": "lnorm_train_fwd_bf16", "op": "lnorm", "pass": "fwd", "dtype": "bf16", "layout": "blocked",
+         "N": 8, "C": 2048, "L": 2048, "residual": True},
+        # the gradients there
+        {"name": "lnorm_train_bwd_bf16", "op": "lnorm", "pass": "bwd", "dtype": "bf16", "layout": "blocked",
+         "N": 8, "C": 2048, "L": 2048, "residual": True},
+        # gradients of a short batch in full precision, channels side by side
+        {"name": "lnorm_bwd_rows_f32", "op": "lnorm", "pass": "bwd", "dtype": "f32", "layout": "rows",
+         "N": 3, "C": 1000, "L": 333, "residual": False},
+        # the small tensors of eight blocks, many and some odd: launches and looking up count
+        {"name": "adamw_vectors_f32", "op": "adamw", "pass": "step", "dtype": "f32", "bits": 32, "copy": False, "device": False,
+         "sizes": ",".join((_VECTORS + ",1021,77,1",) * 8)},
+        # all tensors of one block
+        {"name": "adamw_block_f32", "op": "adamw", "pass": "step", "dtype": "f32", "bits": 32, "copy": True, "device": False,
+         "sizes": _VECTORS + "," + _MATRICES},
+        # those of four and of the table of a vocabulary, states in 8 bits, gradients in bf16 and clipped by a factor on the GPU
+        {"name": "adamw_8bit_bf16", "op": "adamw", "pass": "step", "dtype": "bf16", "bits": 8, "copy": True, "device": True,
+         "sizes": ",".join((_VECTORS + "," + _MATRICES,) * 4 + ("16001x1024",))},
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number between lo and hi, spread over its logarithm."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 1)))))))
+
+
+def _channels(rng, lo, hi):
+    """Mostly multiples of 64, as models have them; odd ones too."""
+    c = _log(rng, lo, hi)
+    return c if rng.random() < 0.35 else max(64, c // 64 * 64)
+
+
+def draw(rng):
+    op, what = rng.choice((("rec", "fwd"), ("rec", "fwd"), ("rec", "bwd"), ("rec", "bwd"), ("rec", "step"), ("lnorm", "fwd"), ("lnorm", "bwd"),
+                           ("lnorm", "q8"), ("adamw", "step"), ("adamw", "step")))
+    c = {"op": op, "pass": what, "dtype": rng.choice(("bf16", "bf16", "f32"))}
+    half = 2 if c["dtype"] == "f32" else 1
+    if op == "adamw":
+        c["bits"], c["copy"], c["device"] = rng.choice((32, 32, 8)), rng.random() < 0.5, rng.random() < 0.3
+        left, sizes = _log(rng, 1000, 24_000_000), []
+        for _ in range(_log(rng, 1, 96)):
+            n = min(left, _log(rng, 1, 8_000_000))
+            if n < 1:
+                break
+            left -= n
+            k = rng.choice((1, 1, 3, 16, 64))
+            sizes.append("%dx%d" % (k, n // k) if k > 1 and n >= 2 * k else str(n))
+        c["sizes"] = ",".join(sizes)
+        return c
+    c["layout"] = rng.choice(("blocked", "blocked", "rows"))
+    if op == "rec":
+        step = what == "step"
+        c["C"], c["gate"] = _channels(rng, 40, 4096), rng.random() < 0.6
+        c["N"] = _log(rng, 1, 128 if step else 16)
+        c["L"] = 1 if step else _log(rng, 1, max(1, min(16384, (1 << 25) // (c["N"] * c["C"]) // half)))
+        if what != "bwd":
+            c["slots"] = c["N"] + rng.randrange(4)
+        if not step:
+            c["ragged"] = rng.random() < 0.5
+        return c
+    c["C"], c["N"], c["residual"] = _channels(rng, 40, 8192), _log(rng, 1, 16), rng.random() < 0.8
+    most = (1 << 25) // (c["N"] * c["C"]) // half
+    c["L"] = _log(rng, 1, max(1, min(64 if what == "q8" else 8192, most)))
+    return c
+
+
+def _sizes(case):
+    """(numbers, whether its weights decay: a matrix's do) of each tensor."""
+    return [(math.prod(int(k) for k in s.split("x")), "x" in s) for s in case["sizes"].split(",")]
+
+
+def work(case):
+    e = _T[case["dtype"]].itemsize
+    if case["op"] == "adamw":
+        n = sum(s for s, _ in _sizes(case))
+        return {"bytes": n * (8 + e + (16 if case["bits"] == 32 else 4) + (2 if case["copy"] else 0)), "flops": n * 16}
+    N, C, L, what = case["N"], case["C"], case["L"], case["pass"]
+    n = N * C * L
+    if case["op"] == "rec":
+        gate = 1 if case["gate"] else 0
+        if what == "bwd":
+            return {"bytes": e * n * (7 + 2 * gate) + 24 * C, "flops": n * 60}
+        return {"bytes": e * n * (4 + gate) + 12 * C + 8 * N * C, "flops": n * 30}
+    res = 1 if case["residual"] else 0
+    if what == "q8":
+        return {"bytes": n * (e * (1 + 2 * res) + 1) + 4 * N * L + 8 * C, "flops": n * 10}
+    if what == "bwd":
+        return {"bytes": n * e * (3 + res) + 12 * C, "flops": n * 14}
+    return {"bytes": n * e * (2 + 2 * res) + 8 * C, "flops": n * 8}
+
+
+# ---------------------------------------------------------------------------- inputs
+def _vlen(case):
+    return 16 // _T[case["dtype"]].itemsize
+
+
+def _blocks(case, N, Cb, L, v=None, dtype=None, fill=None):
+    """A tensor [N][Cb][L][v] in the case's layout; `fill(shape)` gives the numbers, [N, L, Cb * v] in fp32."""
+    v, dtype = v or _vlen(case), dtype or _T[case["dtype"]]
+    shape = (N, Cb, L, v) if case["layout"] == "blocked" else (N, L, Cb, v)
+    t = torch.zeros(shape, dtype=dtype, device="cuda")
+    if case["layout"] != "blocked":
+        t = t.permute(0, 2, 1, 3)
+    if fill is not None:
+        t.copy_(fill((N, L, Cb * v)).view(N, L, Cb, v).permute(0, 2, 1, 3))
+    return t
+
+
+def _random(case, g, C, N, L, scale=1.0, count=1, shift=0.0):
+    """`count` tensors of C channels side by side in one, as one projection leaves them."""
+    v = _vlen(case)
+    Cb = -(-C // v)
+
+    def fill(shape):
+        x = torch.randn(shape, generator=g, device="cuda") * scale + shift
+        return (x.view(N, L, count, Cb * v) * (torch.arange(Cb * v, device="cuda") < C)).view(shape)
+    t = _blocks(case, N, Cb * count, L, fill=fill)
+    return [t[:, k * Cb:(k + 1) * Cb] for k in range(count)]
+
+
+def _padded(x, C, Cp):
+    return F.pad(x, (0, Cp - C)).contiguous()
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    st = {"case": case}
+    if case["op"] == "adamw":
+        _prepare_adamw(case, g, st)
+    else:
+        N, C, L, v = case["N"], case["C"], case["L"], _vlen(case)
+        Cb = -(-C // v)
+        {"rec": _prepare_rec, "lnorm": _prepare_lnorm}[case["op"]](case, g, st, N, C, L, Cb, Cb * v)
+    st["plan"], st["ws"] = _plan(case, st)
+    return st
+
+
+def _prepare_rec(case, g, st, N, C, L, Cb, Cp):
+    # (one projection's output: the inner input, both gates and what the result is multiplied by)
+    st["x"], st["f"], st["i"], st["z"] = _random(case, g, C, N, L, count=4)
+    if not case["gate"]:
+        st["z"] = None
+    # decays of 0.9 to 0.999 a position where the gate is half open
+    keep = torch.empty(C, device="cuda").uniform_(0.9, 0.999, generator=g)
+    st["A"] = _padded(2 * torch.log(keep), C, Cp)
+    st["f_bias"] = _padded(torch.randn(C, generator=g, device="cuda") * 0.5, C, Cp)
+    st["i_bias"] = _padded(torch.randn(C, generator=g, device="cuda") * 0.5, C, Cp)
+    if case["pass"] == "bwd":
+        st["dy"], = _random(case, g, C, N, L)
+        d = _blocks(case, N, 4 * Cb, L)
+        st["dx"], st["df"], st["di"], st["dz"] = (d[:, k * Cb:(k + 1) * Cb] for k in range(4))
+        if not case["gate"]:
+            st["dz"] = None
+        st["dA"], st["df_bias"], st["di_bias"] = (torch.zeros_like(st["A"]) for _ in range(3))
+    else:
+        st["y"] = _blocks(case, N, Cb, L)
+        st["state"] = _padded(torch.randn(case["slots"], C, generator=g, device="cuda") * 0.5, C, Cp)
+        st["slots"] = torch.randperm(case["slots"], generator=g, device="cuda")[:N].to(torch.int32)
+    st["lengths"] = None
+    if case.get("ragged"):
+        st["lengths"] = torch.randint(0, L + 1, (N,), generator=g, device="cuda", dtype=torch.int32)
+        st["lengths"][0] = L
+        if N > 2:
+            st["lengths"][1] = 0
+
+
+def _prepare_lnorm(case, g, st, N, C, L, Cb, Cp):
+    st["w"] = _padded(1 + 0.2 * torch.randn(C, generator=g, device="cuda"), C, Cp)
+    st["b"] = _padded(0.1 * torch.randn(C, generator=g, device="cuda"), C, Cp)
+    if case["pass"] == "bwd":
+        st["r"], = _random(case, g, C, N, L, 1.5, shift=0.5)
+        st["dy"], = _random(case, g, C, N, L)
+        st["dr"] = _random(case, g, C, N, L)[0] if case["residual"] else None
+        st["dx"] = _blocks(case, N, Cb, L)
+        st["dw"], st["db"] = torch.zeros_like(st["w"]), torch.zeros_like(st["w"])
+        return
+    st["x"], = _random(case, g, C, N, L)
+    st["res"] = _random(case, g, C, N, L, 1.2, shift=0.5)[0] if case["residual"] else None
+    st["r"] = _blocks(case, N, Cb, L) if case["residual"] else None
+    if case["pass"] == "q8":
+        st["q"] = _blocks(case, N, -(-C // 16), L, v=16, dtype=torch.int8)
+        st["scale"] = torch.zeros(N, L, device="cuda")
+        st["stands_for"] = torch.empty_like(st["q"], dtype=torch.bfloat16)
+    else:
+        st["y"] = _blocks(case, N, Cb, L)
+
+
+def _prepare_adamw(case, g, st):
+    sizes = _sizes(case)
+    st["sizes"] = [n for n, _ in sizes]
+    st["decay"] = [DECAY if matrix else 0.0 for _, matrix in sizes]
+    # every tensor at a whole number of blocks behind the one before it, zeros between
+    whole = torch.tensor([-(-n // BLOCK) * BLOCK for n in st["sizes"]])
+    total, at = int(whole.sum()), (torch.cumsum(whole, 0) - whole).tolist()
+    which = torch.repeat_interleave(torch.arange(len(sizes)), whole // BLOCK)  # tensor of each block
+    first = torch.tensor(at)[which] // BLOCK
+    left = (torch.tensor(st["sizes"])[which] - (torch.arange(len(which)) - first) * BLOCK).clamp(max=BLOCK).cuda()
+    inside = (torch.arange(BLOCK, device="cuda") < left.view(-1, 1)).view(-1)
+    st["decays"] = torch.tensor(st["decay"])[which].cuda().view(-1, 1)  # of each block
+
+    def numbers(scale, dtype=torch.float32):
+        return (torch.randn(total, generator=g, device="cuda") * scale).mul_(inside).to(dtype)
+    # gradients whose size differs from block to block
+    size = torch.exp(torch.randn(total // BLOCK, 1, generator=g, device="cuda") - 6).expand(-1, BLOCK).reshape(-1)
+    st["p"], st["g"] = numbers(0.05), numbers(size, _T[case["dtype"]])
+    m, v = numbers(0.4 * size), numbers(size).square_().mul_(0.7).add_(0.2 * size * size).mul_(inside)
+    st["scales"] = None
+    if case["bits"] == 8:
+        st["scales"] = torch.empty(2, total // BLOCK, device="cuda")
+        st["m"], st["v"] = torch.empty(total, dtype=torch.int8, device="cuda"), torch.empty(total, dtype=torch.uint8, device="cuda")
+        _to8(st, m, v)
+        st["stands_for"] = [torch.empty(total // BLOCK, BLOCK, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    else:
+        st["m"], st["v"] = m, v
+    st["copy"] = torch.zeros(total, dtype=torch.bfloat16, device="cuda") if case["copy"] else None
+    st["step"] = 100
+    st["now"] = torch.tensor([RATE, st["step"], 0.7], device="cuda") if case["device"] else None
+    for k in ("p", "g", "copy"):  # the tensors themselves
+        st[k + "s"] = None if st[k] is None else [st[k][a:a + n] for a, n in zip(at, st["sizes"])]
+
+
+def _plan(case, st):
+    """The framework's plan for these tensors, and its workspace."""
+    if not own:
+        return None, None
+    from paper_1808_05567_amd import seq
+    code = {"f32": seq.SEQ_F32, "bf16": seq.SEQ_BF16}[case["dtype"]]
+    if case["op"] == "adamw":
+        return seq.seq_adamw_create(st["sizes"], dtype=code, bits=case["bits"], betas=(BETA1, BETA2), eps=ADAM_EPS, decay=st["decay"]), None
+    views = {k: t for k, t in st.items() if isinstance(t, torch.Tensor) and t.dim() == 4 and k != "stands_for"}
+    if case["op"] == "rec":
+        h = seq.seq_rec_create(case["N"], case["C"], case["L"], code, slots=case.get("slots", 0), views=views)
+    else:
+        h = seq.seq_lnorm_create(case["N"], case["C"], case["L"], code, EPS, views=views)
+    return h, seq.seq_workspace(h)
+
+
+# ---------------------------------------------------------------------------- one pass
+def run(st):
+    case = st["case"]
+    key = (case["op"], case["pass"])
+    if key[0] == "adamw":
+        st["step"] += 1
+        if st["now"] is not None:
+            st["now"][1] += 1
+    if own:
+        _call(key, st)
+    else:
+        _PLAIN[key](st, case)
+    if key[0] == "adamw":
+        out = {k: st[k] for k in ("p", "m", "v", "scales", "copy")}
+        if case["bits"] == 8:  # (what the 8 bits stand for)
+            for k, to, scale in zip("mv", st["stands_for"], st["scales"]):
+                out[k] = torch.mul(out[k].view(-1, BLOCK), scale.view(-1, 1), out=to)
+        return out
+    out = {k: st[k] for k in _OUTPUTS[key] if st[k] is not None}
+    if key == ("lnorm", "q8"):
+        out["y"] = torch.mul(out.pop("q"), st["scale"].view(case["N"], 1, case["L"], 1), out=st["stands_for"])
+    return out
+
+
+_OUTPUTS = {("rec", "fwd"): ("y", "state"), ("rec", "step"): ("y", "state"), ("rec", "bwd"): ("dx", "df", "di", "dA", "dz", "df_bias", "di_bias"),
+            ("lnorm", "fwd"): ("r", "y"), ("lnorm", "q8"): ("r", "q", "scale"), ("lnorm", "bwd"): ("dx", "dw", "db")}
+
+
+def _call(key, s):
+    from paper_1808_05567_amd import seq
+    h = s["plan"]
+    if key == ("rec", "fwd"):
+        seq.seq_rec_fwd(h, s["x"], s["f"], s["i"], s["A"], s["y"], s["ws"], z=s["z"], f_bias=s["f_bias"], i_bias=s["i_bias"],
+                        state_in=s["state"], state_out=s["state"], slots=s["slots"], lengths=s["lengths"])
+    elif key == ("rec", "step"):
+        seq.seq_rec_step(h, s["x"], s["f"], s["i"], s["A"], s["state"], s["y"], z=s["z"], f_bias=s["f_bias"], i_bias=s["i_bias"], slots=s["slots"])
+    elif key == ("rec", "bwd"):
+        seq.seq_rec_bwd(h, s["x"], s["f"], s["i"], s["A"], s["dy"], s["dx"], s["df"], s["di"], s["dA"], s["ws"], z=s["z"], f_bias=s["f_bias"],
+                        i_bias=s["i_bias"], dz=s["dz"], df_bias=s["df_bias"], di_bias=s["di_bias"], lengths=s["lengths"])
+    elif key == ("lnorm", "fwd"):
+        seq.seq_lnorm_fwd(h, s["x"], s["res"], s["w"], s["b"], s["r"], s["y"])
+    elif key == ("lnorm", "q8"):
+        seq.seq_lnorm_fwd_q8(h, s["x"], s["res"], s["w"], s["b"], s["r"], s["q"], s["scale"])
+    elif key == ("lnorm", "bwd"):
+        seq.seq_lnorm_bwd(h, s["r"], s["w"], s["dy"], s["dr"], s["dx"], s["dw"], s["db"], s["ws"])
+    else:
+        now = s["now"] if s["now"] is not None else (RATE, s["step"])
+        seq.seq_adamw(h, s["ps"], s["gs"], s["m"], s["v"], now, scales=s["scales"], copies=s["copys"])
+
+
+# ---------------------------------------------------------------------------- plain forms, fp32
+def _rows(t, C):
+    """[N][Cb][L][v] -> [N, L, C] in fp32."""
+    N, Cb, L, v = t.shape
+    return t.permute(0, 2, 1, 3).reshape(N, L, Cb * v)[..., :C].float()
+
+
+def _store(t, x):
+    """[N, L, C] in fp32 -> the blocked tensor t, rounded once, zeros beyond C."""
+    N, Cb, L, v = t.shape
+    t.copy_(F.pad(x, (0, Cb * v - x.shape[-1])).view(N, L, Cb, v).permute(0, 2, 1, 3))
+
+
+def _sigmoid(x):
+    return 1 / (1 + torch.exp(-x))
+
+
+def _scan(a, b):
+    """h[l] = a[l] h[l-1] + b[l] along dimension 1 from h[-1] = 0, by doubling; a and b are used up."""
+    s = 1
+    while s < a.shape[1]:
+        b[:, s:] += a[:, s:] * b[:, :-s]
+        a[:, s:] = a[:, s:] * a[:, :-s]
+        s *= 2
+    return b
+
+
+def _rec_inputs(st, case):
+    N, C, L = case["N"], case["C"], case["L"]
+    x, A = _rows(st["x"], C), st["A"][:C]
+    s, g = _sigmoid(_rows(st["f"], C) + st["f_bias"][:C]), _sigmoid(_rows(st["i"], C) + st["i_bias"][:C])
+    inside = None
+    if st["lengths"] is not None:
+        inside = (torch.arange(L, device="cuda") < st["lengths"].view(N, 1)).unsqueeze(-1)
+        x, s = torch.where(inside, x, 0.0), torch.where(inside, s, 0.0)  # (the state stays as it was)
+    a, k = torch.exp(A * s), torch.sqrt(-torch.expm1(2 * A * s))
+    return x, s, g, a, k, A, inside
+
+
+def _plain_rec_fwd(st, case):
+    C = case["C"]
+    x, s, g, a, k, A, inside = _rec_inputs(st, case)
+    at, h = st["slots"].long(), k * g * x
+    h[:, 0] += a[:, 0] * st["state"][at][:, :C]
+    h = _scan(a, h)
+    st["state"][at] = F.pad(h[:, -1], (0, st["state"].shape[-1] - C))
+    if st["z"] is not None:
+        z = _rows(st["z"], C)
+        h = h * z * _sigmoid(z)
+    _store(st["y"], h if inside is None else torch.where(inside, h, 0.0))
+
+
+def _plain_rec_bwd(st, case):
+    C = case["C"]
+    x, s, g, a, k, A, inside = _rec_inputs(st, case)
+    dy = _rows(st["dy"], C)
+    if inside is not None:
+        dy = torch.where(inside, dy, 0.0)
+    h = _scan(a.clone(), k * g * x)
+    if st["z"] is not None:
+        z = _rows(st["z"], C)
+        p = _sigmoid(z)
+        dz = dy * h * p * (1 + z * (1 - p))
+        _store(st["dz"], dz if inside is None else torch.where(inside, dz, 0.0))
+        dy = dy * z * p if inside is None else torch.where(inside, dy * z * p, 0.0)
+    after = torch.cat((a[:, 1:], torch.zeros_like(a[:, :1])), 1)
+    dh = _scan(after.flip(1), dy.flip(1)).flip(1)
+    before = torch.cat((torch.zeros_like(h[:, :1]), h[:, :-1]), 1)
+    # (a pays for what k lets in: dk / da = -a / k)
+    dt = dh * a * (before - torch.where(k > 0, g * x * a / k, 0.0))
+    di = dh * k * x * g * (1 - g)
+    df = dt * A * s * (1 - s)
+    if inside is not None:
+        dt, di, df = (torch.where(inside, t, 0.0) for t in (dt, di, df))
+    _store(st["dx"], dh * k * g)
+    _store(st["df"], df)
+    _store(st["di"], di)
+    st["dA"][:C] = (dt * s).sum((0, 1))
+    st["df_bias"][:C] = df.sum((0, 1))
+    st["di_bias"][:C] = di.sum((0, 1))
+
+
+def _plain_lnorm(st, case):
+    C = case["C"]
+    r = _rows(st["x"], C)
+    if st["res"] is not None:
+        _store(st["r"], r + _rows(st["res"], C))
+        r = _rows(st["r"], C)  # (the norm is of what is stored)
+    r = r - r.mean(-1, keepdim=True)
+    return r / torch.sqrt((r * r).mean(-1, keepdim=True) + EPS) * st["w"][:C] + st["b"][:C]
+
+
+def _plain_lnorm_fwd(st, case):
+    _store(st["y"], _plain_lnorm(st, case))
+
+
+def _plain_lnorm_q8(st, case):
+    y = _plain_lnorm(st, case)
+    scale = y.abs().amax(-1) / 127
+    st["scale"].copy_(scale)
+    scale = torch.where(scale > 0, scale, 1.0)
+    _store(st["q"], torch.round(y / scale.unsqueeze(-1)))
+
+
+def _plain_lnorm_bwd(st, case):
+    C = case["C"]
+    r, dy = _rows(st["r"], C), _rows(st["dy"], C)
+    r = r - r.mean(-1, keepdim=True)
+    rstd = 1 / torch.sqrt((r * r).mean(-1, keepdim=True) + EPS)
+    unit, wdy = r * rstd, st["w"][:C] * dy
+    dx = rstd * (wdy - wdy.mean(-1, keepdim=True) - unit * (wdy * unit).mean(-1, keepdim=True))
+    _store(st["dx"], dx if st["dr"] is None else dx + _rows(st["dr"], C))
+    st["dw"][:C] = (dy * unit).sum((0, 1))
+    st["db"][:C] = dy.sum((0, 1))
+
+
+def _to8(st, m, v):
+    """The states as they are held in 8 bits: the signed square root of m and the fourth root of v, each in steps of a scale a block."""
+    a, b = torch.sqrt(m.abs()).view(-1, BLOCK), torch.sqrt(torch.sqrt(v)).view(-1, BLOCK)
+    scale = torch.stack((a.amax(-1) / 127, b.amax(-1) / 255))
+    st["scales"].copy_(scale)
+    scale = torch.where(scale > 0, scale, 1.0).unsqueeze(-1)
+    st["m"].copy_((torch.round(a / scale[0]) * torch.sign(m).view(-1, BLOCK)).view(-1))
+    q = torch.round(b / scale[1])
+    st["v"].copy_(torch.where(b > 0, q.clamp(min=1), q).view(-1))  # (what is not zero stays so: m is divided by it)
+
+
+def _plain_adamw(st, case):
+    lr, scale, t = RATE, 1.0, st["step"]
+    if st["now"] is not None:
+        lr, t, scale = st["now"][0], st["now"][1].double(), st["now"][2]
+    c1, c2 = 1 - BETA1 ** t, 1 - BETA2 ** t
+    rate, root = (lr / c1, math.sqrt(c2)) if st["now"] is None else ((lr / c1).float(), torch.sqrt(c2).float())
+    m, v = st["m"], st["v"]
+    if case["bits"] == 8:
+        a, b = (q.view(-1, BLOCK).float() * s.view(-1, 1) for q, s in zip((m, v), st["scales"]))
+        m, v = (a * a.abs()).view(-1), (b * b).square().view(-1)
+    g = st["g"].float() * scale
+    m, v = m * BETA1 + g * (1 - BETA1), v * BETA2 + g * g * (1 - BETA2)
+    p = st["p"].view(-1, BLOCK)
+    p -= p * st["decays"] * lr
+    st["p"] -= m * rate / (torch.sqrt(v) / root + ADAM_EPS)
+    if case["bits"] == 8:
+        _to8(st, m, v)
+    else:
+        st["m"].copy_(m)
+        st["v"].copy_(v)
+    if st["copy"] is not None:
+        st["copy"].copy_(st["p"])
+
+
+_PLAIN = {("rec", "fwd"): _plain_rec_fwd, ("rec", "step"): _plain_rec_fwd, ("rec", "bwd"): _plain_rec_bwd, ("lnorm", "fwd"): _plain_lnorm_fwd,
+          ("lnorm", "q8"): _plain_lnorm_q8, ("lnorm", "bwd"): _plain_lnorm_bwd, ("adamw", "step"): _plain_adamw}
+
+
+# ---------------------------------------------------------------------------- from the definitions, 64 bits
+def exact(case, seed):
+    """One position after the other, as the definitions have it."""
+    st = prepare(case, seed)
+    return {"rec": _exact_rec, "lnorm": _exact_lnorm, "adamw": _exact_adamw}[case["op"]](case, st)
+
+
+def _wide(t, C):
+    """[N][Cb][L][v] -> [N, L, C] in 64 bits."""
+    return t.double().transpose(1, 2).flatten(2)[:, :, :C]
+
+
+def _like(t, x):
+    """Back to the form of t."""
+    full = torch.zeros(t.shape[0], t.shape[2], t.shape[1] * t.shape[3], dtype=torch.float64, device="cuda")
+    full[:, :, :x.shape[2]] = x
+    return full.unflatten(2, (t.shape[1], t.shape[3])).transpose(1, 2)
+
+
+def _vector(t, x):
+    full = torch.zeros(t.shape, dtype=torch.float64, device="cuda")
+    full[..., :x.shape[-1]] = x
+    return full
+
+
+def _exact_rec(case, st):
+    N, C, L = case["N"], case["C"], case["L"]
+    ends = [L] * N if st["lengths"] is None else st["lengths"].tolist()
+    live = torch.zeros(N, L, 1, dtype=torch.bool, device="cuda")
+    for n, end in enumerate(ends):
+        live[n, :end] = True
+    x, A = _wide(st["x"], C), st["A"][:C].double()
+    s = torch.special.expit(_wide(st["f"], C) + st["f_bias"][:C].double())
+    g = torch.special.expit(_wide(st["i"], C) + st["i_bias"][:C].double())
+    a = torch.exp(A * s)
+    k = (1 - torch.exp(2 * A * s)).sqrt()
+    z = None if st["z"] is None else _wide(st["z"], C)
+    bwd = case["pass"] == "bwd"
+    h = torch.zeros(N, C, dtype=torch.float64, device="cuda") if bwd else st["state"][st["slots"].long()][:, :C].double()
+    hs = torch.empty(L + 1, N, C, dtype=torch.float64, device="cuda")
+    hs[0] = h
+    for l in range(L):
+        h = torch.where(live[:, l], a[:, l] * h + k[:, l] * g[:, l] * x[:, l], h)
+        hs[l + 1] = h
+    if not bwd:
+        y = hs[1:].transpose(0, 1)
+        y = (y if z is None else y * z * torch.special.expit(z)) * live
+        state = st["state"].double()
+        state[st["slots"].long(), :C] = h
+        return {"y": _like(st["y"], y), "state": state}
+    dy = _wide(st["dy"], C) * live
+    got = {}
+    if z is not None:
+        e = torch.special.expit(z)
+        got["dz"] = _like(st["dz"], dy * hs[1:].transpose(0, 1) * (e + z * e * (1 - e)))
+        dy = dy * z * e
+    back = torch.zeros_like(h)
+    dhs = torch.empty(L, N, C, dtype=torch.float64, device="cuda")
+    for l in reversed(range(L)):
+        dhs[l] = back + dy[:, l]
+        back = torch.where(live[:, l], dhs[l] * a[:, l], torch.zeros_like(back))
+    dh = dhs.transpose(0, 1) * live
+    da = dh * hs[:-1].transpose(0, 1) - dh * g * x * a / k
+    dt = da * a
+    df, di = dt * A * s * (1 - s), dh * k * x * g * (1 - g)
+    got.update(dx=_like(st["dx"], dh * k * g), df=_like(st["df"], df), di=_like(st["di"], di), dA=_vector(st["dA"], (dt * s).sum((0, 1))),
+               df_bias=_vector(st["df_bias"], df.sum((0, 1))), di_bias=_vector(st["di_bias"], di.sum((0, 1))))
+    return got
+
+
+def _exact_lnorm(case, st):
+    C, w, b = case["C"], st["w"][:case["C"]].double(), st["b"][:case["C"]].double()
+
+    def unit(r):
+        mean = r.sum(-1, keepdim=True) / C
+        return (r - mean) / ((r - mean).square().sum(-1, keepdim=True) / C + EPS).sqrt(), ((r - mean).square().sum(-1, keepdim=True) / C + EPS).rsqrt()
+    if case["pass"] == "bwd":
+        u, rstd = unit(_wide(st["r"], C))
+        up = _wide(st["dy"], C)
+        through = up * w
+        dx = (through - through.sum(-1, keepdim=True) / C - u * (through * u).sum(-1, keepdim=True) / C) * rstd
+        if st["dr"] is not None:
+            dx = dx + _wide(st["dr"], C)
+        return {"dx": _like(st["dx"], dx), "dw": _vector(st["dw"], (up * u).sum((0, 1))), "db": _vector(st["db"], up.sum((0, 1)))}
+    r, got = _wide(st["x"], C), {}
+    if st["res"] is not None:
+        r = r + _wide(st["res"], C)
+        got["r"] = _like(st["r"], r)
+        r = r.to(_T[case["dtype"]]).double()  # (by definition the norm of what is stored)
+    y = unit(r)[0] * w + b
+    if case["pass"] == "q8":
+        scale = y.abs().max(-1).values / 127
+        got["scale"] = scale
+        got["y"] = _like(st["q"], torch.round(y / scale.unsqueeze(-1)) * scale.unsqueeze(-1))
+    else:
+        got["y"] = _like(st["y"], y)
+    return got
+
+
+def _exact_adamw(case, st):
+    step = st["step"] + 1
+    lr, scale = (RATE, 1.0) if st["now"] is None else (float(st["now"][0]), float(st["now"][2]))
+    g = st["g"].double() * scale
+    m, v = st["m"].double(), st["v"].double()
+    if case["bits"] == 8:
+        m, v = (q.view(-1, BLOCK) * s.double().view(-1, 1) for q, s in zip((m, v), st["scales"]))
+        m, v = (m.abs() * m).view(-1), v.pow(4).view(-1)
+    m = BETA1 * m + (1 - BETA1) * g
+    v = BETA2 * v + (1 - BETA2) * g.square()
+    p = st["p"].double()
+    decay = st["decays"].double().expand(-1, BLOCK).reshape(-1)
+    p = p - lr * decay * p - lr * (m / (1 - BETA1 ** step)) / ((v / (1 - BETA2 ** step)).sqrt() + ADAM_EPS)
+    got = {"p": p, "m": m, "v": v, "scales": None, "copy": None if st["copy"] is None else p}
+    if case["bits"] == 8:
+        a, b = (m.sign() * m.abs().sqrt()).view(-1, BLOCK), v.pow(0.25).view(-1, BLOCK)
+        sa, sb = a.abs().max(-1, keepdim=True).values / 127, b.max(-1, keepdim=True).values / 255
+        got["scales"] = torch.cat((sa, sb), 1).t()
+        got["m"] = torch.nan_to_num(torch.round(a / sa)) * sa
+        got["v"] = torch.maximum(torch.round(b / sb), (b > 0).double()).nan_to_num() * sb
+    return got
