@@ -280,7 +280,9 @@ def _plan(case, st):
     from paper_1808_05567_amd import seq
     code = {"f32": seq.SEQ_F32, "bf16": seq.SEQ_BF16}[case["dtype"]]
     if case["op"] == "adamw":
-        return seq.seq_adamw_create(st["sizes"], dtype=code, bits=case["bits"], betas=(BETA1, BETA2), eps=ADAM_EPS, decay=st["decay"]), None
+        h = seq.seq_adamw_create(st["sizes"], dtype=code, bits=case["bits"], betas=(BETA1, BETA2), eps=ADAM_EPS, decay=st["decay"])
+        st["tensors"] = seq.seq_adamw_tensors(h, st["ps"], st["gs"], st["copys"])
+        return h, None
     views = {k: t for k, t in st.items() if isinstance(t, torch.Tensor) and t.dim() == 4 and k != "stands_for"}
     if case["op"] == "rec":
         h = seq.seq_rec_create(case["N"], case["C"], case["L"], code, slots=case.get("slots", 0), views=views)
@@ -336,7 +338,7 @@ def _call(key, s):
         seq.seq_lnorm_bwd(h, s["r"], s["w"], s["dy"], s["dr"], s["dx"], s["dw"], s["db"], s["ws"])
     else:
         now = s["now"] if s["now"] is not None else (RATE, s["step"])
-        seq.seq_adamw(h, s["ps"], s["gs"], s["m"], s["v"], now, scales=s["scales"], copies=s["copys"])
+        seq.seq_adamw(h, s["tensors"], s["m"], s["v"], now, scales=s["scales"])
 
 
 # ---------------------------------------------------------------------------- plain forms, fp32
