@@ -4,8 +4,11 @@
  *
  *   seq_conv   short causal convolution of every channel of a sequence, with SiLU
  *   seq_scan   selective state space scan
+ *   seq_rec    gated linear recurrence of every channel
  *   seq_norm   root-mean-square norm with the residual's addition
+ *   seq_lnorm  layer norm with the residual's addition
  *   seq_mv4    products of a few rows with weights of 4 bits and scales for groups of channels
+ *   seq_adamw  AdamW step over many tensors, its states in 32 bits or in 8
  *
  * A sequence is the blocked activation tensor of conv_mi355x.h with H = 1 and W = L, and its
  * projections are that library's 1x1 convolutions (all three passes); these operators read and
@@ -61,9 +64,9 @@ typedef struct {
     int32_t vlen, Cb, Cp;   /* v, channel blocks, C rounded up to v (seq_mv4: of x)         */
     int32_t reserved;
     size_t workspace_bytes; /* max over the passes; may be 0                                */
-    size_t state_bytes;     /* one slot of the state (seq_conv, seq_scan)                   */
+    size_t state_bytes;     /* one slot of the state (seq_conv, seq_scan, seq_rec); m, and v, of seq_adamw */
     size_t wt_bytes;        /* packed weights (seq_mv4)                                     */
-    size_t scale_bytes;     /* their scales (seq_mv4)                                       */
+    size_t scale_bytes;     /* their scales (seq_mv4); those of both states of seq_adamw    */
 } seq_info_t;
 
 typedef struct seq_plan *seq_handle_t;
@@ -143,6 +146,38 @@ conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const 
                            void *dB, void *dC, float *dD, void *dz, float *ddt_bias,
                            const int32_t *lengths, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------ gated linear recurrence
+ * For every channel c:
+ *   s    = sigmoid(f + f_bias),  g = sigmoid(i + i_bias),  a = exp(A[c] * s)
+ *   h[l] = a * h[l-1] + sqrt(1 - a^2) * g * x[l]
+ *   y[l] = h[l],   times z * sigmoid(z) where there is a z
+ * A: fp32 vector; numbers above zero count as zero, and so does 1 - a^2 below 2^-126.  f_bias, i_bias: fp32 vectors or NULL (zero);
+ * z: sequence tensor or NULL; state: fp32 [slots][Cp].  Errors of create: as seq_conv_create. */
+typedef struct {
+    int32_t N, C, L;
+    int32_t slots, dtype;
+    int32_t reserved;
+    seq_view_t x, f, i, z, y;
+    seq_view_t dy, dx, df, di, dz;
+} seq_rec_desc_t;
+conv_status_t seq_rec_create(const seq_rec_desc_t *desc, seq_handle_t *out);
+conv_status_t seq_rec_fwd(seq_handle_t h, const void *x, const void *f, const void *i,
+                          const float *A, const void *z, const float *f_bias, const float *i_bias,
+                          const float *state_in, void *y, float *state_out, const int32_t *slots,
+                          const int32_t *lengths, void *stream);
+/* One new position of each sequence, the state moved on in place: a plan of L = 1 with slots. */
+conv_status_t seq_rec_step(seq_handle_t h, const void *x, const void *f, const void *i,
+                           const float *A, const void *z, const float *f_bias, const float *i_bias,
+                           float *state, void *y, const int32_t *slots, void *stream);
+/* Gradients of seq_rec_fwd without states.  dx, df, di: sequence tensors; dz: one where there is a
+ * z; dA, df_bias, di_bias: fp32 vectors, the last two or NULL.  Where 1 - a^2 is zero, the square
+ * root's slope is left out of dA and df. */
+conv_status_t seq_rec_bwd(seq_handle_t h, const void *x, const void *f, const void *i,
+                          const float *A, const void *z, const float *f_bias, const float *i_bias,
+                          const void *dy, void *dx, void *df, void *di, float *dA, void *dz,
+                          float *df_bias, float *di_bias, const int32_t *lengths, void *ws,
+                          size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------ norm
  *   r = x + res (rounded to the tensors' type; without a residual r = x),
  *   y[c] = r[c] * w[c] / sqrt(mean_c r^2 + eps)          of every position on its own
@@ -169,6 +204,23 @@ conv_status_t seq_norm_fwd_q8(seq_handle_t h, const void *x, const void *res, co
 conv_status_t seq_norm_bwd(seq_handle_t h, const void *r, const float *w, const void *dy,
                            const void *dr, void *dx, float *dw, void *ws, size_t ws_bytes,
                            void *stream);
+
+/* ------------------------------------------------------------------ layer norm
+ *   r = x + res (rounded to the tensors' type; without a residual r = x),
+ *   y[c] = (r[c] - mean r) * w[c] / sqrt(mean_c (r - mean r)^2 + eps) + b[c]    of every position on its own
+ * w: fp32 vector; b: fp32 vector or NULL (zero); res, r and the errors of create: as seq_norm. */
+typedef seq_norm_desc_t seq_lnorm_desc_t;
+conv_status_t seq_lnorm_create(const seq_lnorm_desc_t *desc, seq_handle_t *out);
+conv_status_t seq_lnorm_fwd(seq_handle_t h, const void *x, const void *res, const float *w,
+                            const float *b, void *r, void *y, const int32_t *lengths, void *stream);
+/* The same with y in 8 bits, as seq_norm_fwd_q8. */
+conv_status_t seq_lnorm_fwd_q8(seq_handle_t h, const void *x, const void *res, const float *w,
+                               const float *b, void *r, int8_t *q, float *scale,
+                               const int32_t *lengths, void *stream);
+/* Gradients: r, dr and dx as seq_norm_bwd; dw: fp32 vector; db: one, or NULL. */
+conv_status_t seq_lnorm_bwd(seq_handle_t h, const void *r, const float *w, const void *dy,
+                            const void *dr, void *dx, float *dw, float *db, const int32_t *lengths,
+                            void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------ products with 4-bit weights
  *   y[m,k] = xscale[m] * sum_c x[m,c] * q[k,c] * scale[c / group][k] + bias[k],   q = -8 ... 7
@@ -198,6 +250,39 @@ conv_status_t seq_mv4_quant(seq_handle_t h, const float *w, void *wt, float *sca
 /* And back: w[k][c] = q * scale. */
 conv_status_t seq_mv4_unquant(seq_handle_t h, const void *wt, const float *scale, float *w,
                               void *stream);
+
+/* ------------------------------------------------------------------ AdamW
+ * Of every number p of every tensor, with its gradient g, at step t = 1, 2, ...:
+ *   m = beta1 m + (1 - beta1) factor g,   v = beta2 v + (1 - beta2) (factor g)^2
+ *   p = p - rate decay p - rate (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * p: dense fp32; g: dense, of the plan's type; copy: dense bf16, gets p rounded to it.  m and v are
+ * two dense arrays for all tensors: a tensor's numbers begin a whole number of 256 after those of
+ * the one before; what lies between is written as zero.  Zeros are a fresh state.
+ * bits = 32: m and v in fp32.  bits = 8: of m its signed square root, of v its fourth root, in int8
+ * and uint8 times a scale for each 256 numbers: scales [2][numbers / 256], m's first.  The scale is
+ * the largest's over 127 (m) and 255 (v); the others are rounded to nearest even, of v never down
+ * to zero.  p moves by m and v before that rounding.
+ * The step's rate, t and factor are doubles in host memory (now), or, so that a recorded step may run with new
+ * ones, fp32 in device memory (now_device); the other is NULL.
+ * sizes: numbers of each tensor, >= 0; decays: decay of each.  Both are copied.
+ * Errors of create: CONV_EINVAL for a NULL pointer, count < 1, a size < 0, an unknown type, bits
+ * other than 8 and 32, betas outside [0, 1), an eps or decay that is negative or not finite;
+ * CONV_EUNSUPPORTED beyond 2^20 tensors and 2^35 numbers. */
+typedef struct {
+    const int64_t *sizes;
+    const double *decays;
+    double beta1, beta2, eps;
+    int32_t count, bits;
+    int32_t dtype; /* of g */
+    int32_t reserved;
+} seq_adamw_desc_t;
+conv_status_t seq_adamw_create(const seq_adamw_desc_t *desc, seq_handle_t *out);
+/* p, g, copy: arrays of device pointers in host memory, one a tensor, read before the call returns.
+ * A tensor whose g is NULL stays as it is, its state too.  copy: NULL, or NULL for some.
+ * Tensors may not overlap.  scales: bits = 8 only. */
+conv_status_t seq_adamw(seq_handle_t h, void *const *p, const void *const *g, void *const *copy,
+                        void *m, void *v, float *scales, const double *now,
+                        const float *now_device, void *stream);
 
 #ifdef __cplusplus
 }

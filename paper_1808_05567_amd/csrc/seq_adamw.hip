@@ -1,0 +1,154 @@
+// AdamW step over many tensors, the states in fp32 or as roots in 8 bits with a scale for each 256 numbers.
+//
+//   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  p = p - rate decay p - rate (m / c1) / (sqrt(v / c2) + eps),  c = 1 - beta^t
+#include "seq_internal.h"
+
+namespace convmi {
+namespace {
+
+constexpr int kEach = 4;  // numbers of a lane side by side: a wave has a block of 256
+
+// Four numbers from element e of size on, zeros beyond.
+template <typename T>
+static __device__ __forceinline__ void load4(const T *p, int64_t e, int64_t size, float (&f)[kEach])
+{
+    if (e + kEach <= size) {
+        if constexpr (sizeof(T) == 4) {
+            const seq_f32x4 b = *reinterpret_cast<const seq_f32x4 *>(p + e);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) f[i] = b[i];
+        } else {
+            const seq_u32x2 b = *reinterpret_cast<const seq_u32x2 *>(p + e);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) f[i] = __uint_as_float(i % 2 ? b[i / 2] & 0xFFFF0000u : b[i / 2] << 16);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) f[i] = e + i < size ? SeqElem<T>::get(p[e + i]) : 0.0f;
+}
+template <typename T>
+static __device__ __forceinline__ void store4(T *p, int64_t e, int64_t size, const float (&f)[kEach])
+{
+    if (e + kEach <= size) {
+        if constexpr (sizeof(T) == 4)
+            *reinterpret_cast<seq_f32x4 *>(p + e) = seq_f32x4{f[0], f[1], f[2], f[3]};
+        else
+            *reinterpret_cast<seq_u32x2 *>(p + e) = seq_u32x2{seq_pack_bf16(f[0], f[1]), seq_pack_bf16(f[2], f[3])};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (e + i < size) p[e + i] = SeqElem<T>::put(f[i]);
+}
+
+// Largest of a wave's numbers, as unsigned ones: NaN is larger than all.
+static __device__ __forceinline__ float wave_max(float m)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = __uint_as_float(max(__float_as_uint(m), __float_as_uint(__shfl_xor(m, d))));
+    return m;
+}
+
+template <typename G, int BITS>
+__global__ __launch_bounds__(256) void seq_adamw_kernel(const SeqAdamwArgs a)
+{
+    int k = 0;  // the workgroup's tensor
+    for (int step = 64; step > 0; step /= 2)
+        if (k + step < a.count && a.first[k + step] <= blockIdx.x) k += step;
+    const SeqAdamwTensor t = a.tensor[k];
+    float lr = a.rate, by_m = a.by_m, by_v = a.by_v, factor = a.factor;
+    if (a.now) {
+        lr = a.now[0];
+        factor = a.now[2];
+        by_m = lr / -expm1f((float)(a.now[1] * a.log1));
+        by_v = 1.0f / sqrtf(-expm1f((float)(a.now[1] * a.log2)));
+    }
+    const float keep = lr * t.decay;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const int64_t begin = (int64_t)(blockIdx.x - a.first[k]) * kSeqAdamwShare;
+#pragma unroll 1
+    for (int b = wave; b < kSeqAdamwShare / kSeqAdamwBlock; b += 4) {
+        const int64_t from = begin + b * kSeqAdamwBlock;
+        if (from >= t.size) return;
+        const int64_t e = from + lane * kEach;
+        const unsigned block = t.block + (unsigned)(from / kSeqAdamwBlock);
+        const int64_t at = (int64_t)block * kSeqAdamwBlock + lane * kEach;
+        float p[kEach], g[kEach], m[kEach], v[kEach], root[kEach];
+        load4(t.p, e, t.size, p);
+        load4(static_cast<const G *>(t.g), e, t.size, g);
+        if constexpr (BITS == 32) {
+            load4(static_cast<const float *>(a.m), at, at + kEach, m);
+            load4(static_cast<const float *>(a.v), at, at + kEach, v);
+        } else {
+            const unsigned bm = *reinterpret_cast<const unsigned *>(static_cast<const char *>(a.m) + at);
+            const unsigned bv = *reinterpret_cast<const unsigned *>(static_cast<const char *>(a.v) + at);
+            const float sm = a.scales[block], sv = a.scales[a.blocks + block];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const float qm = (float)(int)(signed char)(bm >> 8 * i) * sm, qv = (float)(bv >> 8 * i & 255) * sv;
+                m[i] = qm * fabsf(qm);
+                v[i] = qv * qv * (qv * qv);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (e + i >= t.size) m[i] = v[i] = 0;
+            const float s = g[i] * factor;
+            m[i] = fmaf(a.rest1, s, a.beta1 * m[i]);
+            v[i] = fmaf(a.rest2 * s, s, a.beta2 * v[i]);
+            root[i] = sqrtf(v[i]);
+            p[i] = p[i] - keep * p[i] - by_m * m[i] / fmaf(root[i], by_v, a.eps);
+        }
+        store4(t.p, e, t.size, p);
+        if (t.copy) store4(t.copy, e, t.size, p);
+        if constexpr (BITS == 32) {
+            store4(static_cast<float *>(a.m), at, at + kEach, m);
+            store4(static_cast<float *>(a.v), at, at + kEach, v);
+        } else {
+            float xm = 0, xv = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                // (roots of m with its sign, and of v's root)
+                m[i] = copysignf(sqrtf(fabsf(m[i])), m[i]);
+                root[i] = sqrtf(root[i]);
+                xm = __uint_as_float(max(__float_as_uint(xm), __float_as_uint(fabsf(m[i]))));
+                xv = __uint_as_float(max(__float_as_uint(xv), __float_as_uint(root[i])));
+            }
+            const float sm = wave_max(xm) / 127.0f, sv = wave_max(xv) / 255.0f;
+            const float im = sm == 0 ? 0 : 1.0f / sm, iv = sv == 0 ? 0 : 1.0f / sv;
+            unsigned bm = 0, bv = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int qm = (int)rintf(fminf(fmaxf(m[i] * im, -127.0f), 127.0f));
+                const int qv = (int)rintf(fminf(root[i] * iv, 255.0f));
+                bm |= (unsigned)(qm & 255) << 8 * i;
+                bv |= (unsigned)(root[i] > 0 && qv == 0 ? 1 : qv) << 8 * i;
+            }
+            *reinterpret_cast<unsigned *>(static_cast<char *>(a.m) + at) = bm;
+            *reinterpret_cast<unsigned *>(static_cast<char *>(a.v) + at) = bv;
+            if (lane == 0) {
+                a.scales[block] = sm;
+                a.scales[a.blocks + block] = sv;
+            }
+        }
+    }
+}
+
+template <typename G>
+hipError_t launch(int bits, const SeqAdamwArgs &a, unsigned workgroups, hipStream_t s)
+{
+    if (bits == 8)
+        seq_adamw_kernel<G, 8><<<workgroups, 256, 0, s>>>(a);
+    else
+        seq_adamw_kernel<G, 32><<<workgroups, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_seq_adamw(int dtype, int bits, const SeqAdamwArgs &a, unsigned workgroups, hipStream_t s)
+{
+    return dtype == SEQ_BF16 ? launch<unsigned short>(bits, a, workgroups, s) : launch<float>(bits, a, workgroups, s);
+}
+
+}  // namespace convmi

@@ -11,7 +11,7 @@
 using namespace convmi;
 
 namespace {
-enum Kind { kConv, kScan, kNorm, kMv4 };
+enum Kind { kConv, kScan, kRec, kNorm, kLnorm, kMv4, kAdamw };
 }  // namespace
 
 struct seq_plan {
@@ -22,14 +22,20 @@ struct seq_plan {
     SeqConvArgs conv;  // its runs are the forward pass's
     int bwd_range, bwd_ranges;
     SeqScanArgs scan, scan_bwd;
+    SeqRecArgs rec, rec_bwd;
     SeqNormArgs norm;
     SeqMv4Args mv4;
+    SeqAdamwArgs adamw;        // without its tensors
+    SeqAdamwTensor *tensors;   // their sizes, places and decays
+    int count, bits;
+    double beta1, beta2;
+    ~seq_plan() { delete[] tensors; }
 };
 
 namespace {
 
 // (a launch has at most 2^32 work-items)
-constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxSpan = 1LL << 58, kMaxTileStride = 1LL << 24;
+constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxSpan = 1LL << 58, kMaxTileStride = 1LL << 24, kMaxNumbers = 1LL << 35;
 
 bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -369,13 +375,117 @@ conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const 
     return done(launch_seq_scan_bwd(h->dtype, a, (hipStream_t)stream));
 }
 
+// ------------------------------------------------------------------ gated linear recurrence
+conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
+{
+    if (!d || !out || !known(d->dtype) || !sizes_ok(d->N, d->C, d->L) || d->slots < 0) return CONV_EINVAL;
+    const int v = vlen_of(d->dtype);
+    if (!sizes_supported(d->N, d->C, d->L, v)) return CONV_EUNSUPPORTED;
+    seq_plan *p = new_plan(kRec, d->dtype, d->C);
+    if (!p) return CONV_EUNSUPPORTED;
+    SeqRecArgs &a = p->rec;
+    a.N = d->N;
+    a.L = d->L;
+    a.Cb = p->info.Cb;
+    a.Cp = p->info.Cp;
+    a.n_slots = d->slots;
+    const struct {
+        const seq_view_t &v;
+        bool out;
+        SeqView &to;
+    } views[] = {{d->x, false, a.vx},   {d->f, false, a.vf},  {d->i, false, a.vi},  {d->z, false, a.vz},  {d->y, true, a.vy},
+                 {d->dy, false, a.vdy}, {d->dx, true, a.vdx}, {d->df, true, a.vdf}, {d->di, true, a.vdi}, {d->dz, true, a.vdz}};
+    for (const auto &w : views)
+        if (!view_of(w.v, a.N, a.Cb, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
+    a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
+    a.lanes = seq_rec_lanes(a.vx, v);
+    const int64_t columns = a.N * seq_rec_groups(a.Cb, a.lanes);
+    // Workgroups of as many waves as make 4096 with the others (four a SIMD), and find positions.
+    const auto waves = [&](int lanes, int64_t most) {
+        int w = 1;
+        while (w < 16 && columns * w < most && (int64_t)w * lanes * kSeqRecPositions < a.L) w *= 2;
+        return w;
+    };
+    a.waves = waves(a.lanes, 4096);
+    p->rec_bwd = a;
+    SeqRecArgs &b = p->rec_bwd;
+    b.rounds = (int)((a.L + (int64_t)b.waves * b.lanes * kSeqRecPositions - 1) / ((int64_t)b.waves * b.lanes * kSeqRecPositions));
+    p->info.state_bytes = (size_t)a.Cp * 4;
+    p->bwd_ws = up((size_t)a.N * 3 * a.Cp * 4) + (b.rounds > 1 ? up((size_t)a.N * b.rounds * a.Cp * 4) : 0);
+    const bool fits = columns * 64 * a.waves <= kMaxItems;
+    return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
+}
+
+static void rec_inputs(SeqRecArgs &a, const void *x, const void *f, const void *i, const float *A, const void *z, const float *f_bias, const float *i_bias)
+{
+    a.x = x;
+    a.f = f;
+    a.i = i;
+    a.A = A;
+    a.z = z;
+    a.f_bias = f_bias;
+    a.i_bias = i_bias;
+}
+
+conv_status_t seq_rec_fwd(seq_handle_t h, const void *x, const void *f, const void *i, const float *A, const void *z, const float *f_bias,
+                          const float *i_bias, const float *state_in, void *y, float *state_out, const int32_t *slots, const int32_t *lengths, void *stream)
+{
+    if (!h || h->kind != kRec || !given(x, f, i, A, y) || !fine(z, f_bias, i_bias, state_in, state_out) || !aligned(slots, 4) || !aligned(lengths, 4) ||
+        ((state_in || state_out) && h->rec.n_slots == 0))
+        return CONV_EINVAL;
+    SeqRecArgs a = h->rec;
+    rec_inputs(a, x, f, i, A, z, f_bias, i_bias);
+    a.state_in = state_in;
+    a.y = y;
+    a.state_out = state_out;
+    a.slots = slots;
+    a.lengths = lengths;
+    return done(launch_seq_rec_fwd(h->dtype, a, (hipStream_t)stream));
+}
+
+conv_status_t seq_rec_step(seq_handle_t h, const void *x, const void *f, const void *i, const float *A, const void *z, const float *f_bias,
+                           const float *i_bias, float *state, void *y, const int32_t *slots, void *stream)
+{
+    if (!h || h->kind != kRec || !given(x, f, i, A, state, y) || !fine(z, f_bias, i_bias) || !aligned(slots, 4) || h->rec.n_slots == 0 || h->rec.L != 1)
+        return CONV_EINVAL;
+    SeqRecArgs a = h->rec;
+    rec_inputs(a, x, f, i, A, z, f_bias, i_bias);
+    a.state_out = state;
+    a.y = y;
+    a.slots = slots;
+    return done(launch_seq_rec_step(h->dtype, a, (hipStream_t)stream));
+}
+
+conv_status_t seq_rec_bwd(seq_handle_t h, const void *x, const void *f, const void *i, const float *A, const void *z, const float *f_bias,
+                          const float *i_bias, const void *dy, void *dx, void *df, void *di, float *dA, void *dz, float *df_bias, float *di_bias,
+                          const int32_t *lengths, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!h || h->kind != kRec || !given(x, f, i, A, dy, dx, df, di, dA) || !fine(z, f_bias, i_bias, dz, df_bias, di_bias, ws) || !aligned(lengths, 4) || !z != !dz)
+        return CONV_EINVAL;
+    if (!ws || ws_bytes < h->bwd_ws) return CONV_EWORKSPACE;
+    SeqRecArgs a = h->rec_bwd;
+    rec_inputs(a, x, f, i, A, z, f_bias, i_bias);
+    a.dy = dy;
+    a.dx = dx;
+    a.df = df;
+    a.di = di;
+    a.dA = dA;
+    a.dz = dz;
+    a.df_bias = df_bias;
+    a.di_bias = di_bias;
+    a.lengths = lengths;
+    a.part = static_cast<float *>(ws);
+    a.marks = reinterpret_cast<float *>(static_cast<char *>(ws) + up((size_t)a.N * 3 * a.Cp * 4));
+    return done(launch_seq_rec_bwd(h->dtype, a, (hipStream_t)stream));
+}
+
 // ------------------------------------------------------------------ norm
-conv_status_t seq_norm_create(const seq_norm_desc_t *d, seq_handle_t *out)
+static conv_status_t norm_create(Kind kind, const seq_norm_desc_t *d, seq_handle_t *out)
 {
     if (!d || !out || !known(d->dtype) || !sizes_ok(d->N, d->C, d->L) || !(d->eps >= 0) || isinf(d->eps)) return CONV_EINVAL;
     const int v = vlen_of(d->dtype);
     if (!sizes_supported(d->N, d->C, d->L, v)) return CONV_EUNSUPPORTED;
-    seq_plan *p = new_plan(kNorm, d->dtype, d->C);
+    seq_plan *p = new_plan(kind, d->dtype, d->C);
     if (!p) return CONV_EUNSUPPORTED;
     SeqNormArgs &a = p->norm;
     a.N = d->N;
@@ -394,11 +504,12 @@ conv_status_t seq_norm_create(const seq_norm_desc_t *d, seq_handle_t *out)
     for (const auto &w : views)
         if (!view_of(w.v, a.N, a.Cb, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
     if (!view_of(d->q, a.N, (a.C + 15) / 16, a.L, 16, true, a.vq)) return finish(p, CONV_EINVAL, out);
-    // backward: two workgroups a compute unit, each with a part of dw
+    // backward: two workgroups a compute unit, each with a part of dw (and db)
     a.parts = (int)std::min<int64_t>(512, a.rows);
-    p->bwd_ws = up((size_t)a.parts * a.Cp * 4);
+    p->bwd_ws = up((size_t)a.parts * a.Cp * 4 * (kind == kLnorm ? 2 : 1));
     return finish(p, CONV_OK, out);
 }
+conv_status_t seq_norm_create(const seq_norm_desc_t *d, seq_handle_t *out) { return norm_create(kNorm, d, out); }
 
 static conv_status_t norm_fwd(seq_handle_t h, const void *x, const void *res, const float *w, void *r, void *y, int8_t *q, float *scale, void *stream)
 {
@@ -436,6 +547,54 @@ conv_status_t seq_norm_bwd(seq_handle_t h, const void *r, const float *w, const 
     a.dw = dw;
     a.part = static_cast<float *>(ws);
     return done(launch_seq_norm_bwd(h->dtype, a, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------------ layer norm
+conv_status_t seq_lnorm_create(const seq_lnorm_desc_t *d, seq_handle_t *out) { return norm_create(kLnorm, d, out); }
+
+static conv_status_t lnorm_fwd(seq_handle_t h, const void *x, const void *res, const float *w, const float *b, void *r, void *y, int8_t *q, float *scale,
+                               const int32_t *lengths, void *stream)
+{
+    SeqNormArgs a = h->norm;
+    a.x = x;
+    a.res = res;
+    a.w = w;
+    a.b = b;
+    a.r = r;
+    a.y = y;
+    a.q = q;
+    a.scale = scale;
+    a.lengths = lengths;
+    return done(launch_seq_lnorm_fwd(h->dtype, a, (hipStream_t)stream));
+}
+conv_status_t seq_lnorm_fwd(seq_handle_t h, const void *x, const void *res, const float *w, const float *b, void *r, void *y, const int32_t *lengths,
+                            void *stream)
+{
+    if (!h || h->kind != kLnorm || !given(x, w, y) || !fine(res, b, r) || !aligned(lengths, 4)) return CONV_EINVAL;
+    return lnorm_fwd(h, x, res, w, b, r, y, nullptr, nullptr, lengths, stream);
+}
+conv_status_t seq_lnorm_fwd_q8(seq_handle_t h, const void *x, const void *res, const float *w, const float *b, void *r, int8_t *q, float *scale,
+                               const int32_t *lengths, void *stream)
+{
+    if (!h || h->kind != kLnorm || !given(x, w, q, scale) || !fine(res, b, r) || !aligned(lengths, 4)) return CONV_EINVAL;
+    return lnorm_fwd(h, x, res, w, b, r, nullptr, q, scale, lengths, stream);
+}
+conv_status_t seq_lnorm_bwd(seq_handle_t h, const void *r, const float *w, const void *dy, const void *dr, void *dx, float *dw, float *db,
+                            const int32_t *lengths, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!h || h->kind != kLnorm || !given(r, w, dy, dx, dw) || !fine(dr, db, ws) || !aligned(lengths, 4)) return CONV_EINVAL;
+    if (!ws || ws_bytes < h->bwd_ws) return CONV_EWORKSPACE;
+    SeqNormArgs a = h->norm;
+    a.r = const_cast<void *>(r);
+    a.w = w;
+    a.dy = dy;
+    a.dr = dr;
+    a.dx = dx;
+    a.dw = dw;
+    a.db = db;
+    a.lengths = lengths;
+    a.part = static_cast<float *>(ws);
+    return done(launch_seq_lnorm_bwd(h->dtype, a, (hipStream_t)stream));
 }
 
 // ------------------------------------------------------------------ products with 4-bit weights
@@ -487,6 +646,88 @@ conv_status_t seq_mv4_unquant(seq_handle_t h, const void *wt, const float *scale
     return done(launch_seq_mv4_unquant(a, w, (hipStream_t)stream));
 }
 
+// ------------------------------------------------------------------ AdamW
+conv_status_t seq_adamw_create(const seq_adamw_desc_t *d, seq_handle_t *out)
+{
+    const auto share = [](double x) { return x >= 0 && x < 1; };
+    const auto amount = [](double x) { return x >= 0 && !isinf(x); };
+    if (!d || !out || !d->sizes || !d->decays || d->count < 1 || !known(d->dtype) || (d->bits != 8 && d->bits != 32) || !share(d->beta1) || !share(d->beta2) ||
+        !amount(d->eps))
+        return CONV_EINVAL;
+    for (int k = 0; k < d->count; ++k)
+        if (d->sizes[k] < 0 || !amount(d->decays[k])) return CONV_EINVAL;
+    if (d->count > 1 << 20) return CONV_EUNSUPPORTED;
+    seq_plan *p = new_plan(kAdamw, d->dtype, 1);
+    if (!p) return CONV_EUNSUPPORTED;
+    p->tensors = new (std::nothrow) SeqAdamwTensor[d->count]();
+    if (!p->tensors) return finish(p, CONV_EUNSUPPORTED, out);
+    p->count = d->count;
+    p->bits = d->bits;
+    p->beta1 = d->beta1;
+    p->beta2 = d->beta2;
+    int64_t blocks = 0;
+    for (int k = 0; k < d->count; ++k) {
+        if (d->sizes[k] > kMaxNumbers - blocks * kSeqAdamwBlock) return finish(p, CONV_EUNSUPPORTED, out);
+        p->tensors[k].size = d->sizes[k];
+        p->tensors[k].block = (unsigned)blocks;
+        p->tensors[k].decay = (float)d->decays[k];
+        blocks += (d->sizes[k] + kSeqAdamwBlock - 1) / kSeqAdamwBlock;
+    }
+    SeqAdamwArgs &a = p->adamw;
+    a.blocks = (unsigned)blocks;
+    a.log1 = log(d->beta1);  // (minus infinity for zero: nothing is kept)
+    a.log2 = log(d->beta2);
+    a.beta1 = (float)d->beta1;
+    a.rest1 = (float)(1 - d->beta1);
+    a.beta2 = (float)d->beta2;
+    a.rest2 = (float)(1 - d->beta2);
+    a.eps = (float)d->eps;
+    p->info.state_bytes = (size_t)blocks * kSeqAdamwBlock * (d->bits / 8);
+    p->info.scale_bytes = d->bits == 8 ? (size_t)blocks * 8 : 0;
+    return finish(p, CONV_OK, out);
+}
+
+conv_status_t seq_adamw(seq_handle_t h, void *const *p, const void *const *g, void *const *copy, void *m, void *v, float *scales, const double *now,
+                        const float *now_device, void *stream)
+{
+    if (!h || h->kind != kAdamw || !p || !g || !now == !now_device || !aligned(now_device, 4) || !fine(m, v, scales)) return CONV_EINVAL;
+    if (h->adamw.blocks && (!m || !v || (h->bits == 8) != (scales != nullptr))) return CONV_EINVAL;
+    if (now && !(now[1] >= 1)) return CONV_EINVAL;
+    const auto stays = [&](int k) { return !g[k] || h->tensors[k].size == 0; };
+    for (int k = 0; k < h->count; ++k)
+        if (!stays(k) && (!given(p[k], g[k]) || (copy && !fine(copy[k])))) return CONV_EINVAL;
+    SeqAdamwArgs a = h->adamw;
+    a.m = m;
+    a.v = v;
+    a.scales = scales;
+    a.now = now_device;
+    if (now) {
+        a.rate = (float)now[0];
+        a.by_m = (float)(now[0] / -expm1(now[1] * h->adamw.log1));
+        a.by_v = (float)(1 / sqrt(-expm1(now[1] * h->adamw.log2)));
+        a.factor = (float)now[2];
+    }
+    unsigned workgroups = 0;
+    for (int k = 0; k <= h->count; ++k) {
+        if (k == h->count || a.count == kSeqAdamwTensors) {
+            if (a.count == 0) break;
+            const hipError_t e = launch_seq_adamw(h->dtype, h->bits, a, workgroups, (hipStream_t)stream);
+            if (e != hipSuccess) return CONV_ELAUNCH;
+            a.count = 0;
+            workgroups = 0;
+        }
+        if (k == h->count || stays(k)) continue;
+        SeqAdamwTensor &t = a.tensor[a.count];
+        t = h->tensors[k];
+        t.p = static_cast<float *>(p[k]);
+        t.g = g[k];
+        t.copy = copy ? static_cast<unsigned short *>(copy[k]) : nullptr;
+        a.first[a.count++] = workgroups;
+        workgroups += (unsigned)((t.size + kSeqAdamwShare - 1) / kSeqAdamwShare);
+    }
+    return CONV_OK;
+}
+
 conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen)
 {
     if (!h || !buf || buflen == 0) return CONV_EINVAL;
@@ -500,7 +741,13 @@ conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen)
                      seq_scan_states(h->scan.S), h->scan.chunks, h->scan.chunk, (long long)h->scan.N * h->scan.G * h->scan.tiles * h->scan.chunks,
                      h->scan_bwd.chunks, (long long)h->scan_bwd.N * h->scan_bwd.G * h->scan_bwd.btiles * h->scan_bwd.chunks);
             break;
+        case kRec:
+            snprintf(buf, buflen, "seq_rec dt=%d lanes=%d workgroups=%lld waves=%d bwd: rounds=%d", h->dtype, h->rec.lanes,
+                     (long long)(h->rec.N * seq_rec_groups(h->rec.Cb, h->rec.lanes)), h->rec.waves, h->rec_bwd.rounds);
+            break;
         case kNorm: snprintf(buf, buflen, "seq_norm dt=%d parts=%d", h->dtype, h->norm.parts); break;
+        case kLnorm: snprintf(buf, buflen, "seq_lnorm dt=%d parts=%d", h->dtype, h->norm.parts); break;
+        case kAdamw: snprintf(buf, buflen, "seq_adamw dt=%d bits=%d tensors=%d blocks=%u", h->dtype, h->bits, h->count, h->adamw.blocks); break;
         case kMv4: snprintf(buf, buflen, "seq_mv4 dt=%d group=%d rows=%d runs=%d", h->dtype, h->mv4.group, h->mv4.Kp, h->mv4.Cs); break;
     }
     return CONV_OK;

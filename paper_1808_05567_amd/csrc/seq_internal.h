@@ -55,6 +55,23 @@ struct SeqScanArgs {
     int btiles;         // workgroups' shares of a group's channels in the backward kernel
 };
 
+// f and i: what goes into the gates of the old state and of the input.
+struct SeqRecArgs {
+    const void *x, *f, *i, *z, *dy;
+    void *y, *dx, *df, *di, *dz;
+    const float *A, *f_bias, *i_bias, *state_in;
+    float *state_out, *dA, *df_bias, *di_bias;
+    const int *lengths, *slots;
+    SeqView vx, vf, vi, vz, vy, vdy, vdx, vdf, vdi, vdz;
+    int N, Cb, Cp, L, n_slots;
+    int past;                // results go past the caches
+    int lanes;               // seq_rec_lanes
+    int waves;               // of a workgroup
+    int rounds;              // backwards: times that a workgroup has all of its waves' positions
+    float *marks;  // [N][rounds][Cp]: states before them
+    float *part;   // [N][3][Cp]: sums of dA, df_bias and di_bias over a sequence
+};
+
 struct SeqNormArgs {
     const void *x, *res, *dy, *dr;
     const float *w;
@@ -67,6 +84,35 @@ struct SeqNormArgs {
     float eps;
     int parts;
     int past;  // results go past the caches
+    // the layer norm's
+    const float *b;
+    float *db;
+    const int *lengths;
+};
+
+constexpr int kSeqAdamwBlock = 256, kSeqAdamwTensors = 80;  // numbers with a scale of their own; tensors of a launch
+constexpr int kSeqAdamwShare = 4096;                        // numbers of a workgroup
+
+struct SeqAdamwTensor {
+    float *p;
+    const void *g;
+    unsigned short *copy;
+    int64_t size;
+    unsigned block;  // of the states, where the tensor's begin
+    float decay;
+};
+// A launch's tensors (4 KB hold the arguments of one).
+struct SeqAdamwArgs {
+    void *m, *v;
+    float *scales;  // [2][blocks]
+    const float *now;  // rate, step, factor; NULL: what follows
+    float rate, by_m, by_v, factor;  // rate / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    double log1, log2;  // of the betas
+    float beta1, rest1, beta2, rest2, eps;  // rest: 1 - beta
+    unsigned blocks;
+    int count;
+    unsigned first[kSeqAdamwTensors];  // of a tensor's workgroups
+    SeqAdamwTensor tensor[kSeqAdamwTensors];
 };
 
 struct SeqMv4Args {
@@ -83,8 +129,14 @@ hipError_t launch_seq_scan_fwd(int dtype, const SeqScanArgs &a, hipStream_t s);
 hipError_t launch_seq_scan_step(int dtype, const SeqScanArgs &a, hipStream_t s);
 hipError_t launch_seq_scan_ends(int dtype, const SeqScanArgs &a, hipStream_t s);
 hipError_t launch_seq_scan_bwd(int dtype, const SeqScanArgs &a, hipStream_t s);
+hipError_t launch_seq_rec_fwd(int dtype, const SeqRecArgs &a, hipStream_t s);
+hipError_t launch_seq_rec_step(int dtype, const SeqRecArgs &a, hipStream_t s);
+hipError_t launch_seq_rec_bwd(int dtype, const SeqRecArgs &a, hipStream_t s);
 hipError_t launch_seq_norm_fwd(int dtype, const SeqNormArgs &a, hipStream_t s);
 hipError_t launch_seq_norm_bwd(int dtype, const SeqNormArgs &a, hipStream_t s);
+hipError_t launch_seq_lnorm_fwd(int dtype, const SeqNormArgs &a, hipStream_t s);
+hipError_t launch_seq_lnorm_bwd(int dtype, const SeqNormArgs &a, hipStream_t s);
+hipError_t launch_seq_adamw(int dtype, int bits, const SeqAdamwArgs &a, unsigned workgroups, hipStream_t s);
 hipError_t launch_seq_mv4(int dtype, const SeqMv4Args &a, hipStream_t s);
 hipError_t launch_seq_mv4_quant(const SeqMv4Args &a, const float *w, void *wt, float *scale, hipStream_t s);
 hipError_t launch_seq_mv4_unquant(const SeqMv4Args &a, float *w, hipStream_t s);
@@ -101,6 +153,12 @@ constexpr int kSeqScanWaves = 4, kSeqJoinWaves = 16;
 inline int64_t seq_scan_waves(const SeqScanArgs &a, bool sums) { return (int64_t)a.N * a.G * a.tiles * a.chunks * (sums || a.S <= 32 ? 1 : 2); }
 inline int64_t seq_join_groups(const SeqScanArgs &a) { return a.N * (((int64_t)a.S * a.Cp + 63) / 64); }
 inline int seq_join_waves(int chunks) { return chunks <= 16 * kSeqJoinWaves ? (chunks + 15) / 16 : kSeqJoinWaves; }
+
+// Lanes that take positions of one block of the recurrence, the other lanes of a wave having other blocks: 16 where a block's positions
+// follow one another, 4 where a position's blocks do, so that a wave's accesses are 256 bytes side by side.
+inline int seq_rec_lanes(const SeqView &x, int vlen) { return x.c == vlen ? 4 : 16; }
+inline int64_t seq_rec_groups(int64_t Cb, int lanes) { return (Cb + 64 / lanes - 1) / (64 / lanes); }
+constexpr int kSeqRecPositions = 2;  // of a lane at a time
 
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;

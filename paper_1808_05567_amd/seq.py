@@ -1,5 +1,5 @@
-"""ctypes binding of the sequence operators (include/seq_mi355x.h): short causal convolution, selective scan,
-root-mean-square norm, products with 4-bit weights.
+"""ctypes binding of the sequence operators (include/seq_mi355x.h): short causal convolution, selective scan, gated linear recurrence,
+root-mean-square norm, layer norm, products with 4-bit weights, AdamW.
 
 As ``conv``: argument marshalling only, no fallback.  A handle is created once for its sizes, types and strides; a call takes
 the tensors.  Tensors of sequences are torch tensors [N, Cb, L, v], dense or not; give them (or tensors of the same strides) to
@@ -20,7 +20,10 @@ EXPORTS = (
     "seq_destroy", "seq_query", "seq_describe",
     "seq_conv_create", "seq_conv_fwd", "seq_conv_step", "seq_conv_bwd",
     "seq_scan_create", "seq_scan_fwd", "seq_scan_step", "seq_scan_bwd",
+    "seq_rec_create", "seq_rec_fwd", "seq_rec_step", "seq_rec_bwd",
     "seq_norm_create", "seq_norm_fwd", "seq_norm_fwd_q8", "seq_norm_bwd",
+    "seq_lnorm_create", "seq_lnorm_fwd", "seq_lnorm_fwd_q8", "seq_lnorm_bwd",
+    "seq_adamw_create", "seq_adamw",
     "seq_mv4_create", "seq_mv4", "seq_mv4_quant", "seq_mv4_unquant",
 )
 
@@ -43,12 +46,20 @@ def _desc(ints, views, floats=()):
 
 _CONV_VIEWS = ("x", "y", "dy", "dx")
 _SCAN_VIEWS = ("x", "dt", "B", "C", "z", "y", "dy", "dx", "ddt", "dB", "dC", "dz")
+_REC_VIEWS = ("x", "f", "i", "z", "y", "dy", "dx", "df", "di", "dz")
 _NORM_VIEWS = ("x", "res", "r", "y", "q", "dy", "dr", "dx")
 SeqConvDesc = _desc(("N", "C", "L", "W", "silu", "slots", "dtype"), _CONV_VIEWS)
 # (the descriptor has a number C and a view of the tensor C)
 SeqScanDesc = _desc(("N", "Ch", "L", "S", "G", "softplus", "slots", "dtype"), _SCAN_VIEWS)
+SeqRecDesc = _desc(("N", "C", "L", "slots", "dtype"), _REC_VIEWS)
 SeqNormDesc = _desc(("N", "C", "L", "dtype"), _NORM_VIEWS, ("eps",))
 SeqMv4Desc = _desc(("M", "C", "K", "group", "dtype"), ())
+
+
+class SeqAdamwDesc(ctypes.Structure):
+    _fields_ = [("sizes", ctypes.c_void_p), ("decays", ctypes.c_void_p)] + [(n, ctypes.c_double) for n in ("beta1", "beta2", "eps")] + \
+               [(n, ctypes.c_int32) for n in ("count", "bits", "dtype", "reserved")]
+
 
 _lib = None
 
@@ -61,6 +72,8 @@ def load():
         args = {"seq_destroy": [vp], "seq_query": [vp, vp], "seq_describe": [vp, ctypes.c_char_p, sz],
                 "seq_conv_fwd": [vp] * 10, "seq_conv_step": [vp] * 8, "seq_conv_bwd": [vp] * 10 + [sz, vp],
                 "seq_scan_fwd": [vp] * 15 + [sz, vp], "seq_scan_step": [vp] * 13, "seq_scan_bwd": [vp] * 20 + [sz, vp],
+                "seq_rec_fwd": [vp] * 14, "seq_rec_step": [vp] * 12, "seq_rec_bwd": [vp] * 18 + [sz, vp],
+                "seq_lnorm_fwd": [vp] * 9, "seq_lnorm_fwd_q8": [vp] * 10, "seq_lnorm_bwd": [vp] * 10 + [sz, vp], "seq_adamw": [vp] * 10,
                 "seq_norm_fwd": [vp] * 7, "seq_norm_fwd_q8": [vp] * 8, "seq_norm_bwd": [vp] * 8 + [sz, vp],
                 "seq_mv4": [vp] * 8, "seq_mv4_quant": [vp] * 5, "seq_mv4_unquant": [vp] * 5}
         for name in EXPORTS:
@@ -131,6 +144,20 @@ def _t(x, dtype, least, name):
 
 def _o(x, dtype, least, name):
     return None if x is None else _t(x, dtype, least, name)
+
+
+def _here(*tensors):
+    """Refuses tensors of different devices, or of another one than the current one, on which the library's calls run."""
+    at = None
+    for x in tensors:
+        if x is not None:
+            if at is None:
+                at = x.get_device()
+            elif x.get_device() != at:
+                raise ValueError("tensors on one device are wanted, not on %s and %s" % (at, x.device))
+    import torch
+    if at is not None and at >= 0 and at != torch.cuda.current_device():
+        raise ValueError("tensors on the current device (%d) are wanted, not on %d" % (torch.cuda.current_device(), at))
 
 
 def _of(h, kind):
@@ -274,13 +301,57 @@ def seq_scan_bwd(h, x, dt, A, B, C, dy, dx, ddt, dA, dB, dC, ws, D=None, z=None,
         _o(ddt_bias, f, Cp, "ddt_bias"), _o(lengths, h.i32, h.N, "lengths"), *_ws(ws), conv._stream(stream)), "seq_scan_bwd")
 
 
+# ---------------------------------------------------------------------------- gated linear recurrence
+def seq_rec_create(N, C, L, dtype=SEQ_F32, slots=0, views=None) -> SeqPlan:
+    d = SeqRecDesc(N=N, C=C, L=L, slots=slots, dtype=dtype)
+    _views(views, _REC_VIEWS, d, _vlen(dtype), N, C, L)
+    h = SeqPlan("seq_rec_create", d, dtype, {"N": N})
+    _strides(h, _REC_VIEWS, views, N, C, L)
+    h.state = slots * h.info.Cp
+    return h
+
+
+def _rec_inputs(h, x, f, i, A, z, f_bias, i_bias):
+    t, Cp = h.f32, h.info.Cp
+    return (_s(h, "x", x), _s(h, "f", f), _s(h, "i", i), _t(A, t, Cp, "A"), _so(h, "z", z), _o(f_bias, t, Cp, "f_bias"), _o(i_bias, t, Cp, "i_bias"))
+
+
+def seq_rec_fwd(h, x, f, i, A, y, ws=None, z=None, f_bias=None, i_bias=None, state_in=None, state_out=None, slots=None, lengths=None, stream=None):
+    """ws: not used (no pass but seq_rec_bwd has a workspace)."""
+    _here(x, f, i, A, y, z, f_bias, i_bias, state_in, state_out, slots, lengths)
+    conv._check(load().seq_rec_fwd(
+        _of(h, "seq_rec"), *_rec_inputs(h, x, f, i, A, z, f_bias, i_bias), _o(state_in, h.f32, h.state, "state_in"), _s(h, "y", y),
+        _o(state_out, h.f32, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"), conv._stream(stream)),
+        "seq_rec_fwd")
+
+
+def seq_rec_step(h, x, f, i, A, state, y, z=None, f_bias=None, i_bias=None, slots=None, stream=None):
+    _here(x, f, i, A, state, y, z, f_bias, i_bias, slots)
+    conv._check(load().seq_rec_step(
+        _of(h, "seq_rec"), *_rec_inputs(h, x, f, i, A, z, f_bias, i_bias), _t(state, h.f32, h.state, "state"), _s(h, "y", y),
+        _o(slots, h.i32, h.N, "slots"), conv._stream(stream)), "seq_rec_step")
+
+
+def seq_rec_bwd(h, x, f, i, A, dy, dx, df, di, dA, ws, z=None, f_bias=None, i_bias=None, dz=None, df_bias=None, di_bias=None, lengths=None, stream=None):
+    _here(x, f, i, A, dy, dx, df, di, dA, ws, z, f_bias, i_bias, dz, df_bias, di_bias, lengths)
+    t, Cp = h.f32, h.info.Cp
+    conv._check(load().seq_rec_bwd(
+        _of(h, "seq_rec"), *_rec_inputs(h, x, f, i, A, z, f_bias, i_bias), _s(h, "dy", dy), _s(h, "dx", dx), _s(h, "df", df), _s(h, "di", di),
+        _t(dA, t, Cp, "dA"), _so(h, "dz", dz), _o(df_bias, t, Cp, "df_bias"), _o(di_bias, t, Cp, "di_bias"), _o(lengths, h.i32, h.N, "lengths"),
+        *_ws(ws), conv._stream(stream)), "seq_rec_bwd")
+
+
 # ---------------------------------------------------------------------------- norm
-def seq_norm_create(N, C, L, dtype=SEQ_F32, eps=1e-5, views=None) -> SeqPlan:
+def _norm_create(kind, N, C, L, dtype, eps, views):
     d = SeqNormDesc(N=N, C=C, L=L, dtype=dtype, eps=eps)
     _views(views, _NORM_VIEWS, d, _vlen(dtype), N, C, L)
-    h = SeqPlan("seq_norm_create", d, dtype, {"N": N, "positions": N * L})
+    h = SeqPlan(kind, d, dtype, {"N": N, "positions": N * L})
     _strides(h, _NORM_VIEWS, views, N, C, L)
     return h
+
+
+def seq_norm_create(N, C, L, dtype=SEQ_F32, eps=1e-5, views=None) -> SeqPlan:
+    return _norm_create("seq_norm_create", N, C, L, dtype, eps, views)
 
 
 def seq_norm_fwd(h, x, res, w, r, y, stream=None):
@@ -302,6 +373,100 @@ def seq_norm_fwd_q8(h, x, res, w, r, q, scale, stream=None):
 def seq_norm_bwd(h, r, w, dy, dr, dx, dw, ws, stream=None):
     conv._check(load().seq_norm_bwd(_of(h, "seq_norm"), _s(h, "r", r), _t(w, h.f32, h.info.Cp, "w"), _s(h, "dy", dy), _so(h, "dr", dr),
                                     _s(h, "dx", dx), _t(dw, h.f32, h.info.Cp, "dw"), *_ws(ws), conv._stream(stream)), "seq_norm_bwd")
+
+
+# ---------------------------------------------------------------------------- layer norm
+def seq_lnorm_create(N, C, L, dtype=SEQ_F32, eps=1e-5, views=None) -> SeqPlan:
+    return _norm_create("seq_lnorm_create", N, C, L, dtype, eps, views)
+
+
+def _lnorm_inputs(h, x, res, w, b, r):
+    return (_s(h, "x", x), _so(h, "res", res), _t(w, h.f32, h.info.Cp, "w"), _o(b, h.f32, h.info.Cp, "b"), _so(h, "r", r))
+
+
+def seq_lnorm_fwd(h, x, res, w, b, r, y, lengths=None, stream=None):
+    _here(x, res, w, b, r, y, lengths)
+    conv._check(load().seq_lnorm_fwd(_of(h, "seq_lnorm"), *_lnorm_inputs(h, x, res, w, b, r), _s(h, "y", y), _o(lengths, h.i32, h.N, "lengths"),
+                                     conv._stream(stream)), "seq_lnorm_fwd")
+
+
+def seq_lnorm_fwd_q8(h, x, res, w, b, r, q, scale, lengths=None, stream=None):
+    _here(x, res, w, b, r, q, scale, lengths)
+    conv._check(load().seq_lnorm_fwd_q8(_of(h, "seq_lnorm"), *_lnorm_inputs(h, x, res, w, b, r), _q(h, q), _t(scale, h.f32, h.positions, "scale"),
+                                        _o(lengths, h.i32, h.N, "lengths"), conv._stream(stream)), "seq_lnorm_fwd_q8")
+
+
+def seq_lnorm_bwd(h, r, w, dy, dr, dx, dw, db, ws, lengths=None, stream=None):
+    _here(r, w, dy, dr, dx, dw, db, ws, lengths)
+    conv._check(load().seq_lnorm_bwd(_of(h, "seq_lnorm"), _s(h, "r", r), _t(w, h.f32, h.info.Cp, "w"), _s(h, "dy", dy), _so(h, "dr", dr),
+                                     _s(h, "dx", dx), _t(dw, h.f32, h.info.Cp, "dw"), _o(db, h.f32, h.info.Cp, "db"),
+                                     _o(lengths, h.i32, h.N, "lengths"), *_ws(ws), conv._stream(stream)), "seq_lnorm_bwd")
+
+
+# ---------------------------------------------------------------------------- AdamW
+def seq_adamw_create(sizes, dtype=SEQ_F32, bits=32, betas=(0.9, 0.999), eps=1e-8, decay=0.01) -> SeqPlan:
+    """sizes: numbers of each tensor; dtype: of the gradients; bits: of the states, 32 or 8; decay: one for all tensors, or one for each."""
+    import torch
+    sizes = [int(n) for n in sizes]
+    decays = [float(decay)] * len(sizes) if isinstance(decay, (int, float)) else [float(d) for d in decay]
+    if len(decays) != len(sizes):
+        raise ValueError("decay: one for each of %d tensors is wanted, not %d" % (len(sizes), len(decays)))
+    a, b = (ctypes.c_int64 * len(sizes))(*sizes), (ctypes.c_double * len(sizes))(*decays)
+    d = SeqAdamwDesc(sizes=ctypes.addressof(a), decays=ctypes.addressof(b), beta1=betas[0], beta2=betas[1], eps=eps, count=len(sizes), bits=bits, dtype=dtype)
+    h = SeqPlan("seq_adamw_create", d, dtype, {"sizes": sizes, "bits": bits})
+    h.state, h.scales = h.info.state_bytes * 8 // bits, h.info.scale_bytes // 4
+    h.mdtype, h.vdtype = (torch.float32, torch.float32) if bits == 32 else (torch.int8, torch.uint8)
+    h.bf16 = torch.bfloat16
+    return h
+
+
+def seq_adamw_states(h, device="cuda"):
+    """Fresh states for a plan: m, v and, for 8 bits, their scales."""
+    import torch
+    _of(h, "seq_adamw")
+    return (torch.zeros(h.state, dtype=h.mdtype, device=device), torch.zeros(h.state, dtype=h.vdtype, device=device),
+            torch.zeros(h.scales, device=device) if h.bits == 8 else None)
+
+
+class SeqAdamwTensors:
+    """Parameters, their gradients and copies for a plan's calls, checked once.  Holds the tensors."""
+
+    def __init__(self, h, p, g, copies=None):
+        _of(h, "seq_adamw")
+        lists = [list(p), list(g), [None] * len(h.sizes) if copies is None else list(copies)]
+        if any(len(x) != len(h.sizes) for x in lists):
+            raise ValueError("lists of %d tensors are wanted, not of %s" % (len(h.sizes), ", ".join(str(len(x)) for x in lists)))
+        tables = []
+        for name, dtype, tensors in zip(("p", "g", "copies"), (h.f32, h.dtype, h.bf16), lists):
+            if name == "p" and any(x is None for x in tensors):
+                raise ValueError("p: a tensor is missing")
+            for x, n in zip(tensors, h.sizes):
+                if x is not None and x.numel() != n:
+                    raise ValueError("%s: a tensor of %d numbers is wanted, not one of %s" % (name, n, tuple(x.shape)))
+            tables.append((ctypes.c_void_p * len(tensors))(*(None if x is None else _t(x, dtype, n, name) for x, n in zip(tensors, h.sizes))))
+        at = [x.data_ptr() for t in (lists[0], lists[2]) for x in t if x is not None and x.numel()]
+        if len(set(at)) != len(at):
+            raise ValueError("p, copies: a tensor stands there twice")
+        _here(*(x for t in lists for x in t if x is not None and x.numel()))
+        self.plan, self.lists, self.tables = h, lists, tables
+        self.first = next((x for x in lists[0] if x.numel()), None)
+
+
+def seq_adamw_tensors(h, p, g, copies=None) -> SeqAdamwTensors:
+    """p: fp32 tensors; g: gradients of the plan's type, None for tensors that stay as they are; copies: bf16 tensors that get p, or None."""
+    return SeqAdamwTensors(h, p, g, copies)
+
+
+def seq_adamw(h, tensors, m, v, now, scales=None, stream=None):
+    """now: (rate, step from 1 on[, factor of the gradients]) as numbers, or the three as an fp32 tensor on the GPU."""
+    if tensors.plan is not h:
+        raise ValueError("tensors of this plan are wanted")
+    on_gpu = hasattr(now, "data_ptr")
+    _here(tensors.first, m, v, scales, now if on_gpu else None)
+    p, g, copies = tensors.tables
+    host = None if on_gpu else (ctypes.c_double * 3)(now[0], now[1], now[2] if len(now) > 2 else 1.0)
+    conv._check(load().seq_adamw(_of(h, "seq_adamw"), p, g, copies, _t(m, h.mdtype, h.state, "m"), _t(v, h.vdtype, h.state, "v"),
+                                 _o(scales, h.f32, h.scales, "scales"), host, _t(now, h.f32, 3, "now") if on_gpu else None, conv._stream(stream)), "seq_adamw")
 
 
 # ---------------------------------------------------------------------------- products with 4-bit weights
