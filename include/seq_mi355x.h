@@ -151,8 +151,12 @@ conv_status_t seq_scan_bwd(seq_handle_t h, const void *x, const void *dt, const 
  *   s    = sigmoid(f + f_bias),  g = sigmoid(i + i_bias),  a = exp(A[c] * s)
  *   h[l] = a * h[l-1] + sqrt(1 - a^2) * g * x[l]
  *   y[l] = h[l],   times z * sigmoid(z) where there is a z
- * A: fp32 vector; numbers above zero count as zero, and so does 1 - a^2 below 2^-126.  f_bias, i_bias: fp32 vectors or NULL (zero);
- * z: sequence tensor or NULL; state: fp32 [slots][Cp].  Errors of create: as seq_conv_create. */
+ * A: fp32 vector; numbers above zero count as zero, and so does 1 - a^2 below 2^-126.
+ * f_bias, i_bias: fp32 vectors or NULL (zero);
+ * z: sequence tensor or NULL; state: fp32 [slots][Cp].
+ * Errors of create: as seq_conv_create; CONV_EUNSUPPORTED for positions of a view more than 2^20
+ * elements apart and, where x has its blocks nearer to each other than its positions, for blocks
+ * of a view more than 2^24. */
 typedef struct {
     int32_t N, C, L;
     int32_t slots, dtype;

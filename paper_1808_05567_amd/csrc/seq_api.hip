@@ -35,7 +35,7 @@ struct seq_plan {
 namespace {
 
 // (a launch has at most 2^32 work-items)
-constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxSpan = 1LL << 58, kMaxTileStride = 1LL << 24, kMaxNumbers = 1LL << 35;
+constexpr int64_t kMaxElements = 1LL << 39, kMaxItems = (1LL << 32) - 4096, kMaxStride = 1LL << 40, kMaxSpan = 1LL << 58, kMaxTileStride = 1LL << 24, kMaxNumbers = 1LL << 35, kMaxWaveStride = 1LL << 20;
 
 bool aligned(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -397,22 +397,27 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
                  {d->dy, false, a.vdy}, {d->dx, true, a.vdx}, {d->df, true, a.vdf}, {d->di, true, a.vdi}, {d->dz, true, a.vdz}};
     for (const auto &w : views)
         if (!view_of(w.v, a.N, a.Cb, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
+    a.rows = a.Cb > 1 && a.vx.c < a.vx.l;
+    // (a wave's elements are reached from its first one by 32 bits: 256 positions, 16 blocks)
+    for (const auto &w : views)
+        if (w.to.l > kMaxWaveStride || (a.rows && w.to.c > kMaxTileStride)) return finish(p, CONV_EUNSUPPORTED, out);
     a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
-    a.lanes = seq_rec_lanes(a.vx, v);
-    const int64_t columns = a.N * seq_rec_groups(a.Cb, a.lanes);
     // Workgroups of as many waves as make 4096 with the others (four a SIMD), and find positions.
-    const auto waves = [&](int lanes, int64_t most) {
+    const int64_t columns = a.N * seq_rec_groups(a.Cp, a.rows, v);
+    const auto waves = [&](int each, int most) {
         int w = 1;
-        while (w < 16 && columns * w < most && (int64_t)w * lanes * kSeqRecPositions < a.L) w *= 2;
+        while (w < most && columns * w < 4096 && (int64_t)w * each < a.L) w *= 2;
         return w;
     };
-    a.waves = waves(a.lanes, 4096);
+    a.waves = waves(seq_rec_lanes(a.rows, v) * seq_rec_positions(a.rows), kSeqRecWaves);
     p->rec_bwd = a;
     SeqRecArgs &b = p->rec_bwd;
-    b.rounds = (int)((a.L + (int64_t)b.waves * b.lanes * kSeqRecPositions - 1) / ((int64_t)b.waves * b.lanes * kSeqRecPositions));
+    const int each = seq_rec_lanes(a.rows, v) * kSeqRecBwdPositions;
+    b.waves = waves(each, kSeqRecBwdWaves);
+    b.rounds = (int)((a.L + (int64_t)b.waves * each - 1) / ((int64_t)b.waves * each));
     p->info.state_bytes = (size_t)a.Cp * 4;
     p->bwd_ws = up((size_t)a.N * 3 * a.Cp * 4) + (b.rounds > 1 ? up((size_t)a.N * b.rounds * a.Cp * 4) : 0);
-    const bool fits = columns * 64 * a.waves <= kMaxItems;
+    const bool fits = columns * 64 * std::max(a.waves, b.waves) <= kMaxItems;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 
@@ -742,8 +747,8 @@ conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen)
                      h->scan_bwd.chunks, (long long)h->scan_bwd.N * h->scan_bwd.G * h->scan_bwd.btiles * h->scan_bwd.chunks);
             break;
         case kRec:
-            snprintf(buf, buflen, "seq_rec dt=%d lanes=%d workgroups=%lld waves=%d bwd: rounds=%d", h->dtype, h->rec.lanes,
-                     (long long)(h->rec.N * seq_rec_groups(h->rec.Cb, h->rec.lanes)), h->rec.waves, h->rec_bwd.rounds);
+            snprintf(buf, buflen, "seq_rec dt=%d rows=%d workgroups=%lld waves=%d bwd: rounds=%d", h->dtype, h->rec.rows,
+                     (long long)(h->rec.N * seq_rec_groups(h->rec.Cp, h->rec.rows, h->info.vlen)), h->rec.waves, h->rec_bwd.rounds);
             break;
         case kNorm: snprintf(buf, buflen, "seq_norm dt=%d parts=%d", h->dtype, h->norm.parts); break;
         case kLnorm: snprintf(buf, buflen, "seq_lnorm dt=%d parts=%d", h->dtype, h->norm.parts); break;

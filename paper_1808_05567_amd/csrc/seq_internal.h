@@ -65,7 +65,7 @@ struct SeqRecArgs {
     SeqView vx, vf, vi, vz, vy, vdy, vdx, vdf, vdi, vdz;
     int N, Cb, Cp, L, n_slots;
     int past;                // results go past the caches
-    int lanes;               // seq_rec_lanes
+    int rows;                // a position's blocks follow one another
     int waves;               // of a workgroup
     int rounds;              // backwards: times that a workgroup has all of its waves' positions
     float *marks;  // [N][rounds][Cp]: states before them
@@ -154,11 +154,13 @@ inline int64_t seq_scan_waves(const SeqScanArgs &a, bool sums) { return (int64_t
 inline int64_t seq_join_groups(const SeqScanArgs &a) { return a.N * (((int64_t)a.S * a.Cp + 63) / 64); }
 inline int seq_join_waves(int chunks) { return chunks <= 16 * kSeqJoinWaves ? (chunks + 15) / 16 : kSeqJoinWaves; }
 
-// Lanes that take positions of one block of the recurrence, the other lanes of a wave having other blocks: 16 where a block's positions
-// follow one another, 4 where a position's blocks do, so that a wave's accesses are 256 bytes side by side.
-inline int seq_rec_lanes(const SeqView &x, int vlen) { return x.c == vlen ? 4 : 16; }
-inline int64_t seq_rec_groups(int64_t Cb, int lanes) { return (Cb + 64 / lanes - 1) / (64 / lanes); }
-constexpr int kSeqRecPositions = 2;  // of a lane at a time
+// The recurrence's waves have one block of channels where a block's positions follow one another, and 64 channels where a position's blocks do; the lanes
+// that have the same four channels take some positions side by side each at a time.
+inline int seq_rec_cols(bool rows, int vlen) { return rows ? 64 : vlen; }
+inline int64_t seq_rec_groups(int64_t Cp, bool rows, int vlen) { return (Cp + seq_rec_cols(rows, vlen) - 1) / seq_rec_cols(rows, vlen); }
+inline int seq_rec_lanes(bool rows, int vlen) { return 64 / (seq_rec_cols(rows, vlen) / 4); }
+constexpr int seq_rec_positions(bool rows) { return rows ? 4 : 2; }
+constexpr int kSeqRecBwdPositions = 4, kSeqRecWaves = 16, kSeqRecBwdWaves = 8;  // of a lane; of a workgroup at most
 
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;

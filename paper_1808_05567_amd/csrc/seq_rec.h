@@ -1,8 +1,8 @@
 // Of the gated linear recurrence, forwards and backwards: its gates, and how runs of positions are joined.
 //
 // A position takes the state h to a h + u, and a run of positions, one after the other, to A h + H, so that runs join as positions do:
-// (A, H) then (A', H') is (A A', A' H + H').  A lane goes through P positions side by side, the LANES lanes of a block of channels are joined within
-// their row of 16 by DPP, the waves of a workgroup through LDS.  All a are at most 1, so that no product leaves fp32's range upwards.
+// (A, H) then (A', H') is (A A', A' H + H').  A lane goes through P positions side by side of four channels, the lanes of a wave that have the same channels are
+// joined by moves between lanes, the waves of a workgroup through LDS.  All a are at most 1, so that no product leaves fp32's range upwards.
 #pragma once
 
 #include "seq_internal.h"
@@ -10,21 +10,95 @@
 namespace convmi {
 namespace {
 
-constexpr int kRecWaves = 16;  // of a workgroup, at most
+constexpr int kRecE = 4;  // channels of a lane
 
-// A channel's A and biases as the gates take them.
-template <int V>
+// Which channels and positions a lane has.  Where a block's positions follow one another a wave has one block, else 128 bytes (bf16) or 256 of
+// channels side by side, so that a wave's accesses are whole lines in both.
+template <typename T, bool ROWS>
+struct RecLanes {
+    static constexpr int V = SeqElem<T>::V;
+    static constexpr int UNITS = ROWS ? 16 : V / kRecE;  // fours of channels of a wave
+    static constexpr int LANES = 64 / UNITS;             // that have the same ones
+    static constexpr int COLS = UNITS * kRecE;
+    static __device__ __forceinline__ int unit(int lane) { return ROWS ? lane % 16 : lane / LANES; }
+    static __device__ __forceinline__ int at(int lane) { return ROWS ? lane / 16 : lane % LANES; }
+    static __device__ __forceinline__ int first(int lane) { return ROWS ? lane % 16 : lane / LANES * LANES; }  // of those that have its channels
+    static constexpr int STEP = ROWS ? 16 : 1;  // from one to the next
+};
+
+// Four channels.
+static __device__ __forceinline__ void rec_unpack(const seq_f32x4 &b, float (&f)[kRecE])
+{
+#pragma unroll
+    for (int k = 0; k < kRecE; ++k) f[k] = b[k];
+}
+static __device__ __forceinline__ void rec_unpack(const seq_u32x2 &b, float (&f)[kRecE])
+{
+#pragma unroll
+    for (int k = 0; k < kRecE; k += 2) {
+        f[k] = __uint_as_float(b[k / 2] << 16);
+        f[k + 1] = __uint_as_float(b[k / 2] & 0xFFFF0000u);
+    }
+}
+template <typename T>
+struct RecFour;
+template <>
+struct RecFour<float> {
+    typedef seq_f32x4 type;
+    static __device__ __forceinline__ type pack(const float (&f)[kRecE]) { return type{f[0], f[1], f[2], f[3]}; }
+};
+template <>
+struct RecFour<unsigned short> {
+    typedef seq_u32x2 type;
+    static __device__ __forceinline__ type pack(const float (&f)[kRecE]) { return type{seq_pack_bf16(f[0], f[1]), seq_pack_bf16(f[2], f[3])}; }
+};
+// What is computed from b behind this is computed again, rather than kept in registers from before.
+static __device__ __forceinline__ void rec_again(seq_u32x2 &b) { asm volatile("" : "+v"(b)); }
+static __device__ __forceinline__ void rec_again(seq_f32x4 &b) { asm volatile("" : "+v"(b)); }
+
+// A tensor as a wave takes it: where its first block and a sequence begin, the same for all lanes, and the bytes from there to a lane's channels and
+// first position, which 32 bits hold (a plan's views see to that).
+template <typename T>
+struct RecTensor {
+    typedef typename RecFour<T>::type Four;
+    char *base;
+    long long pitch;  // bytes from position to position
+    unsigned lane;
+    template <typename L, int P>
+    static __device__ __forceinline__ RecTensor of(const void *p, const SeqView &v, int n, int c0, int c, int at)
+    {
+        const int b0 = c0 / L::V;
+        RecTensor t;
+        t.base = static_cast<char *>(const_cast<void *>(p)) + (n * v.n + b0 * v.c) * (long long)sizeof(T);
+        t.pitch = v.l * (long long)sizeof(T);
+        t.lane = ((unsigned)(c / L::V - b0) * (unsigned)v.c + (unsigned)(at * P) * (unsigned)v.l + (unsigned)(c % L::V)) * (unsigned)sizeof(T);
+        return t;
+    }
+    // l: position of the wave's first lane, the same for all lanes
+    __device__ __forceinline__ Four load(long long l) const { return *reinterpret_cast<const Four *>(base + l * pitch + lane); }
+    template <bool PAST>
+    __device__ __forceinline__ void store(long long l, const Four &b) const
+    {
+        Four *to = reinterpret_cast<Four *>(base + l * pitch + lane);
+        if constexpr (PAST)
+            __builtin_nontemporal_store(b, to);
+        else
+            *to = b;
+    }
+};
+
+// A lane's A and biases as the gates take them; c: its first channel.
 struct RecParams {
-    float A[V], f[V], i[V];
-    __device__ __forceinline__ RecParams(const SeqRecArgs &a, int cb)
+    float A[kRecE], f[kRecE], i[kRecE];
+    __device__ __forceinline__ RecParams(const SeqRecArgs &a, int c)
     {
 #pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = i[k] = 0;
-        seq_vector<V>(a.A, cb, A);
-        if (a.f_bias) seq_vector<V>(a.f_bias, cb, f);
-        if (a.i_bias) seq_vector<V>(a.i_bias, cb, i);
+        for (int k = 0; k < kRecE; ++k) f[k] = i[k] = 0;
+        seq_vector<kRecE>(a.A + c, 0, A);
+        if (a.f_bias) seq_vector<kRecE>(a.f_bias + c, 0, f);
+        if (a.i_bias) seq_vector<kRecE>(a.i_bias + c, 0, i);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
+        for (int k = 0; k < kRecE; ++k) {
             A[k] = seq_decay(A[k] > 0 ? 0.0f : A[k]);
             f[k] *= -kLog2e;
             i[k] *= -kLog2e;
@@ -47,30 +121,87 @@ static __device__ __forceinline__ float rec_rest(float t, float a)
     return t > -0.36f ? t * p : fmaf(-a, a, 1.0f);
 }
 
-// x of the lane D places before (BACK: behind) in a row of 16, `none` where that lies outside.
-template <int D, bool BACK>
-static __device__ __forceinline__ float rec_near(float none, float x)
+// x of the lane that CTRL names, `none` where there is none.
+template <int CTRL>
+static __device__ __forceinline__ float rec_dpp(float none, float x)
 {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), (BACK ? 0x100 : 0x110) + D, 0xf, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, 0xf, 0xf, false));
 }
-// The same with zeros outside.
-template <int D, bool BACK>
-static __device__ __forceinline__ float rec_near0(float x)
+static __device__ __forceinline__ float rec_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_ds_bpermute(lane * 4, __float_as_int(x))); }
+
+// (A, H) after what `a, h` bring: of positions before it (BACK: behind).
+static __device__ __forceinline__ void rec_after(float &A, float &H, float a, float h)
 {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), (BACK ? 0x100 : 0x110) + D, 0xf, 0xf, true));
+    H = fmaf(A, h, H);
+    A *= a;
 }
 
-// Joins each lane's run with those of all lanes before (BACK: behind) it among LANES, `at` its place there.
-template <int LANES, int D, bool BACK>
-static __device__ __forceinline__ void rec_join(float &A, float &H, int at)
+// Joins each lane's four runs with those of the lane that `how` names.  A lane that has none, or whose row `how` leaves out, keeps its own: the instruction does not
+// write there.  (As moves, with 1 and 0 where there is no lane, a product and a sum: 5 instructions a channel for these 2.)  What a move between lanes reads has to be
+// written two instructions before: four channels in turn are that far apart, and the first and the last wait.
+#define REC_STEP(how)                                  \
+    "v_fmac_f32_dpp %4, %4, %0 " how " bank_mask:0xf\n" \
+    "v_fmac_f32_dpp %5, %5, %1 " how " bank_mask:0xf\n" \
+    "v_fmac_f32_dpp %6, %6, %2 " how " bank_mask:0xf\n" \
+    "v_fmac_f32_dpp %7, %7, %3 " how " bank_mask:0xf\n" \
+    "v_mul_f32_dpp %0, %0, %0 " how " bank_mask:0xf\n"  \
+    "v_mul_f32_dpp %1, %1, %1 " how " bank_mask:0xf\n"  \
+    "v_mul_f32_dpp %2, %2, %2 " how " bank_mask:0xf\n"  \
+    "v_mul_f32_dpp %3, %3, %3 " how " bank_mask:0xf\n"
+#define REC_STEPS(A, H, text)            \
+    asm volatile("s_nop 4\n" text "s_nop 1" \
+                 : "+v"(A[0]), "+v"(A[1]), "+v"(A[2]), "+v"(A[3]), "+v"(H[0]), "+v"(H[1]), "+v"(H[2]), "+v"(H[3]))
+
+// Joins each lane's runs with those of all lanes before (BACK: behind) it that have its channels.
+template <typename T, bool ROWS, bool BACK>
+static __device__ __forceinline__ void rec_join(float (&A)[kRecE], float (&H)[kRecE], int lane)
 {
-    if constexpr (D < LANES) {
-        float a = rec_near<D, BACK>(1.0f, A), h = rec_near0<D, BACK>(H);
-        if (LANES < 16 && (BACK ? at + D >= LANES : at < D)) a = 1, h = 0;
-        H = fmaf(A, h, H);
-        A *= a;
-        rec_join<LANES, 2 * D, BACK>(A, H, at);
+    typedef RecLanes<T, ROWS> L;
+    const auto across = [&](int from, bool ok) {
+#pragma unroll
+        for (int k = 0; k < kRecE; ++k) {
+            float a = rec_lane(A[k], from), h = rec_lane(H[k], from);
+            if (!ok) a = 1, h = 0;
+            rec_after(A[k], H[k], a, h);
+        }
+    };
+    if constexpr (ROWS) {
+#pragma unroll
+        for (int d = 1; d < L::LANES; d *= 2) {
+            const int from = BACK ? lane + d * L::STEP : lane - d * L::STEP;
+            across(from & 63, from >= 0 && from < 64);
+        }
+    } else if constexpr (!BACK) {
+        // within rows of 16, then the last lane of a row to the next row, then that of the lower half to the upper one
+        if constexpr (L::LANES == 64)
+            REC_STEPS(A, H, REC_STEP("row_shr:1 row_mask:0xf") REC_STEP("row_shr:2 row_mask:0xf") REC_STEP("row_shr:4 row_mask:0xf") REC_STEP("row_shr:8 row_mask:0xf")
+                                REC_STEP("row_bcast:15 row_mask:0xa") REC_STEP("row_bcast:31 row_mask:0xc"));
+        else
+            REC_STEPS(A, H, REC_STEP("row_shr:1 row_mask:0xf") REC_STEP("row_shr:2 row_mask:0xf") REC_STEP("row_shr:4 row_mask:0xf") REC_STEP("row_shr:8 row_mask:0xf")
+                                REC_STEP("row_bcast:15 row_mask:0xa"));
+    } else {
+        REC_STEPS(A, H, REC_STEP("row_shl:1 row_mask:0xf") REC_STEP("row_shl:2 row_mask:0xf") REC_STEP("row_shl:4 row_mask:0xf") REC_STEP("row_shl:8 row_mask:0xf"));
+        across(((lane | 15) + 1) & 63, !(lane & 16));
+        if constexpr (L::LANES == 64) across(32, !(lane & 32));
     }
+}
+// What all lanes before (BACK: behind) it make of x, from the joined runs.
+template <typename T, bool ROWS, bool BACK>
+static __device__ __forceinline__ float rec_until(float A, float H, float x, int lane)
+{
+    typedef RecLanes<T, ROWS> L;
+    float a, h;
+    if constexpr (ROWS) {
+        const int from = BACK ? lane + L::STEP : lane - L::STEP;
+        a = rec_lane(A, from & 63);
+        h = rec_lane(H, from & 63);
+    } else {
+        constexpr int SHIFT = BACK ? 0x130 : 0x138;  // by a lane, over the whole wave
+        a = rec_dpp<SHIFT>(1.0f, A);
+        h = rec_dpp<SHIFT>(0.0f, H);
+    }
+    const int at = L::at(lane);
+    return at == (BACK ? L::LANES - 1 : 0) ? x : fmaf(a, x, h);
 }
 
 }  // namespace

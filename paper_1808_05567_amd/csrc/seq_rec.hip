@@ -6,160 +6,146 @@
 namespace convmi {
 namespace {
 
-// A workgroup takes 64 / LANES blocks of channels of one sequence through all of its positions, waves * LANES * P of them at a time.
-template <typename T, int LANES, int P, bool PAST>
-__global__ __launch_bounds__(64 * kRecWaves) void seq_rec_fwd_kernel(const SeqRecArgs a)
+// A workgroup takes a wave's channels of one sequence through all of its positions, waves * LANES * P of them at a time.
+template <typename T, bool ROWS, int P, bool PAST>
+__global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const SeqRecArgs a)
 {
-    constexpr int V = SeqElem<T>::V, BLOCKS = 64 / LANES;
-    __shared__ float runs[2][kRecWaves][BLOCKS][2][V];
-    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, at = threadIdx.x % LANES, bl = threadIdx.x % 64 / LANES;
-    const int groups = (a.Cb + BLOCKS - 1) / BLOCKS, n = blockIdx.x / groups;
-    const bool live = blockIdx.x % groups * BLOCKS + bl < a.Cb;
-    const int cb = live ? blockIdx.x % groups * BLOCKS + bl : a.Cb - 1;
+    typedef RecLanes<T, ROWS> L;
+    typedef typename RecFour<T>::type Four;
+    constexpr int E = kRecE;
+    __shared__ __align__(16) float runs[2][kSeqRecWaves][L::COLS][2];
+    __shared__ __align__(16) float begin[kSeqRecWaves][L::COLS];
+    const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
+    const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
+    const bool live = c0 + unit * E < a.Cp;
+    const int c = live ? c0 + unit * E : c0;
     const int len = seq_length(a.lengths, n, a.L);
-    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
-    const T *f = static_cast<const T *>(a.f) + n * a.vf.n + cb * a.vf.c;
-    const T *i = static_cast<const T *>(a.i) + n * a.vi.n + cb * a.vi.c;
-    const T *z = a.z ? static_cast<const T *>(a.z) + n * a.vz.n + cb * a.vz.c : nullptr;
-    T *y = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
+    const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
+    const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), y = tensor(a.y, a.vy);
     const int slot = a.slots ? a.slots[n] : n;
     const bool has_slot = slot >= 0 && slot < a.n_slots;
-    const RecParams<V> par(a, cb);
-    float state[V] = {};
-    if (a.state_in && has_slot) seq_vector<V>(a.state_in + (long long)slot * a.Cp, cb, state);
-    const int each = waves * LANES * P;
+    const RecParams par(a, c);
+    // between waves each lane has one channel
+    const int col = lane % L::COLS;
+    const bool kept = has_slot && c0 + col < a.Cp;
+    float state = a.state_in && kept ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
+    const int each = waves * L::LANES * P;
     int turn = 0;
     for (long long base = 0; base < a.L; base += each, turn ^= 1) {
-        const long long l0 = base + (wave * LANES + at) * P;
-        float A[V], H[V], pa[P][V], ph[P][V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            A[k] = 1;
-            H[k] = 0;
-        }
+        const long long w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
+        Four bx[P], bf[P], bi[P], bz[P];
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const long long l = l0 + j;
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                pa[j][k] = 1;
-                ph[j][k] = 0;
-            }
-            if (l < len) {
-                float fx[V], ff[V], fi[V];
-                SeqElem<T>::unpack(seq_load(x + l * a.vx.l), fx);
-                SeqElem<T>::unpack(seq_load(f + l * a.vf.l), ff);
-                SeqElem<T>::unpack(seq_load(i + l * a.vi.l), fi);
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float t = par.A[k] * rec_gate(ff[k], par.f[k]);
-                    pa[j][k] = seq_exp2(t);
-                    ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, pa[j][k])) * rec_gate(fi[k], par.i[k]) * fx[k];
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                H[k] = fmaf(pa[j][k], H[k], ph[j][k]);
-                A[k] *= pa[j][k];
+            bx[j] = bf[j] = bi[j] = bz[j] = Four{};
+            if (l0 + j < len) {
+                bx[j] = x.load(w0 + j);
+                bf[j] = f.load(w0 + j);
+                bi[j] = i.load(w0 + j);
+                if (a.z) bz[j] = z.load(w0 + j);
             }
         }
+        float A[E], H[E], pa[P][E], ph[P][E];
 #pragma unroll
-        for (int k = 0; k < V; ++k) rec_join<LANES, 1, false>(A[k], H[k], at);
-        if (at == LANES - 1)
+        for (int j = 0; j < P; ++j) {
+            float fx[E], ff[E], fi[E];
+            rec_unpack(bx[j], fx);
+            rec_unpack(bf[j], ff);
+            rec_unpack(bi[j], fi);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                runs[turn][wave][bl][0][k] = A[k];
-                runs[turn][wave][bl][1][k] = H[k];
+            for (int k = 0; k < E; ++k) {
+                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
+                pa[j][k] = l0 + j < len ? p : 1.0f;
+                // (what is behind the end was loaded as zero)
+                ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
+                H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
+                A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
+        }
+        rec_join<T, ROWS, false>(A, H, lane);
+        if (at == L::LANES - 1)
+#pragma unroll
+            for (int k = 0; k < E; k += 2)
+                *reinterpret_cast<seq_f32x4 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x4{A[k], H[k], A[k + 1], H[k + 1]};
         __syncthreads();
-        float h[V];  // before the wave's positions
-        for (int w = 0; w < waves; ++w)
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (w == wave) h[k] = state[k];
-                state[k] = fmaf(runs[turn][w][bl][0][k], state[k], runs[turn][w][bl][1][k]);
-            }
-#pragma unroll
-        for (int k = 0; k < V; ++k) {  // before the lane's
-            float la = rec_near<1, false>(1.0f, A[k]), lh = rec_near0<1, false>(H[k]);
-            if (at == 0) la = 1, lh = 0;
-            h[k] = fmaf(la, h[k], lh);
+        float before = 0;
+        for (int w = 0; w < waves; ++w) {
+            if (w == wave) before = state;
+            state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
         }
+        begin[wave][col] = before;  // (the lanes that have a channel twice write the same)
+        seq_wave_sync();
+        float h[E];
+        rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[wave][unit * E]), h);
+#pragma unroll
+        for (int k = 0; k < E; ++k) h[k] = rec_until<T, ROWS, false>(A[k], H[k], h[k], lane);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const long long l = l0 + j;
-            seq_u32x4 out = {};
+            float o[E], fz[E];
+            rec_unpack(bz[j], fz);
 #pragma unroll
-            for (int k = 0; k < V; ++k) h[k] = fmaf(pa[j][k], h[k], ph[j][k]);
-            if (l < len) {
-                float o[V], fz[V];
-                if (z) SeqElem<T>::unpack(seq_load(z + l * a.vz.l), fz);
-#pragma unroll
-                for (int k = 0; k < V; ++k) o[k] = z ? h[k] * fz[k] * seq_sigmoid(fz[k]) : h[k];
-                out = SeqElem<T>::pack(o);
+            for (int k = 0; k < E; ++k) {
+                h[k] = fmaf(pa[j][k], h[k], ph[j][k]);
+                o[k] = a.z ? h[k] * fz[k] * seq_sigmoid(fz[k]) : h[k];
             }
-            if (live && l < a.L) seq_store_result<PAST>(y + l * a.vy.l, out);
+            if (live && l0 + j < a.L) y.template store<PAST>(w0 + j, l0 + j < len ? RecFour<T>::pack(o) : Four{});
         }
     }
-    if (a.state_out && has_slot && live && wave == 0 && at == 0) {
-        float *to = a.state_out + (long long)slot * a.Cp + (long long)cb * V;
-#pragma unroll
-        for (int k = 0; k < V; k += 4) *reinterpret_cast<seq_f32x4 *>(to + k) = seq_f32x4{state[k], state[k + 1], state[k + 2], state[k + 3]};
-    }
+    if (a.state_out && kept && threadIdx.x < L::COLS) a.state_out[(long long)slot * a.Cp + c0 + col] = state;
 }
 
 template <typename T>
 __global__ __launch_bounds__(64) void seq_rec_step_kernel(const SeqRecArgs a)
 {
-    constexpr int V = SeqElem<T>::V;
+    constexpr int V = SeqElem<T>::V, E = kRecE;
     const long long t = (long long)blockIdx.x * 64 + threadIdx.x;
-    if (t >= (long long)a.N * a.Cb) return;
-    const int n = (int)(t / a.Cb), cb = (int)(t % a.Cb);
+    if (t >= (long long)a.N * (a.Cp / E)) return;
+    const int n = (int)(t / (a.Cp / E)), c = (int)(t % (a.Cp / E)) * E, cb = c / V;
     const int slot = a.slots ? a.slots[n] : n;
-    T *y = static_cast<T *>(a.y) + n * a.vy.n + cb * a.vy.c;
+    typedef typename RecFour<T>::type Four;
+    const auto four = [&](const void *p, const SeqView &v) { return reinterpret_cast<const Four *>(static_cast<const T *>(p) + n * v.n + cb * v.c + c % V); };
+    Four *y = const_cast<Four *>(four(a.y, a.vy));
     if (slot < 0 || slot >= a.n_slots) {
-        seq_store(y, seq_u32x4{});
+        *y = Four{};
         return;
     }
-    float *to = a.state_out + (long long)slot * a.Cp + (long long)cb * V;
-    float h[V], fx[V], ff[V], fi[V], fz[V];
-    seq_vector<V>(to, 0, h);
-    SeqElem<T>::unpack(seq_load(static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c), fx);
-    SeqElem<T>::unpack(seq_load(static_cast<const T *>(a.f) + n * a.vf.n + cb * a.vf.c), ff);
-    SeqElem<T>::unpack(seq_load(static_cast<const T *>(a.i) + n * a.vi.n + cb * a.vi.c), fi);
-    if (a.z) SeqElem<T>::unpack(seq_load(static_cast<const T *>(a.z) + n * a.vz.n + cb * a.vz.c), fz);
-    const RecParams<V> par(a, cb);
-    float o[V];
+    float *to = a.state_out + (long long)slot * a.Cp + c;
+    float h[E], fx[E], ff[E], fi[E], fz[E], o[E];
+    seq_vector<E>(to, 0, h);
+    rec_unpack(*four(a.x, a.vx), fx);
+    rec_unpack(*four(a.f, a.vf), ff);
+    rec_unpack(*four(a.i, a.vi), fi);
+    if (a.z) rec_unpack(*four(a.z, a.vz), fz);
+    const RecParams par(a, c);
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
+    for (int k = 0; k < E; ++k) {
         const float e = par.A[k] * rec_gate(ff[k], par.f[k]), d = seq_exp2(e);
         h[k] = fmaf(d, h[k], __builtin_amdgcn_sqrtf(rec_rest(e, d)) * rec_gate(fi[k], par.i[k]) * fx[k]);
         o[k] = a.z ? h[k] * fz[k] * seq_sigmoid(fz[k]) : h[k];
     }
-    seq_store(y, SeqElem<T>::pack(o));
-#pragma unroll
-    for (int k = 0; k < V; k += 4) *reinterpret_cast<seq_f32x4 *>(to + k) = seq_f32x4{h[k], h[k + 1], h[k + 2], h[k + 3]};
+    *y = RecFour<T>::pack(o);
+    *reinterpret_cast<seq_f32x4 *>(to) = seq_f32x4{h[0], h[1], h[2], h[3]};
 }
 
-template <typename T, int LANES>
-hipError_t launch_lanes(const SeqRecArgs &a, hipStream_t s)
+template <typename T, bool ROWS>
+hipError_t launch_rows(const SeqRecArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((long long)a.N * seq_rec_groups(a.Cb, LANES));
+    constexpr int P = seq_rec_positions(ROWS);
+    const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.past)
-        seq_rec_fwd_kernel<T, LANES, kSeqRecPositions, true><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, true><<<grid, 64 * a.waves, 0, s>>>(a);
     else
-        seq_rec_fwd_kernel<T, LANES, kSeqRecPositions, false><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, false><<<grid, 64 * a.waves, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)
 {
-    return a.lanes == 16 ? launch_lanes<T, 16>(a, s) : launch_lanes<T, 4>(a, s);
+    return a.rows ? launch_rows<T, true>(a, s) : launch_rows<T, false>(a, s);
 }
 template <typename T>
 hipError_t launch_step(const SeqRecArgs &a, hipStream_t s)
 {
-    seq_rec_step_kernel<T><<<(unsigned)(((long long)a.N * a.Cb + 63) / 64), 64, 0, s>>>(a);
+    seq_rec_step_kernel<T><<<(unsigned)(((long long)a.N * (a.Cp / kRecE) + 63) / 64), 64, 0, s>>>(a);
     return hipGetLastError();
 }
 }  // namespace

@@ -8,236 +8,206 @@
 namespace convmi {
 namespace {
 
-// A workgroup takes 64 / LANES blocks of channels of one sequence through all of its positions, as forwards: first from the front for the states before
-// each round of its waves, where there are several, then from the back.
-template <typename T, int LANES, int P>
-__global__ __launch_bounds__(64 * kRecWaves) void seq_rec_bwd_kernel(const SeqRecArgs a)
+// A workgroup takes a wave's channels of one sequence through all of its positions, as forwards: first from the front for the states before each round of
+// its waves, where there are several, then from the back.
+template <typename T, bool ROWS, int P, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArgs a)
 {
-    constexpr int V = SeqElem<T>::V, BLOCKS = 64 / LANES;
-    __shared__ float runs[2][kRecWaves][BLOCKS][3][V];
-    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, at = threadIdx.x % LANES, bl = threadIdx.x % 64 / LANES;
-    const int groups = (a.Cb + BLOCKS - 1) / BLOCKS, n = blockIdx.x / groups;
-    const bool live = blockIdx.x % groups * BLOCKS + bl < a.Cb;
-    const int cb = live ? blockIdx.x % groups * BLOCKS + bl : a.Cb - 1;
+    typedef RecLanes<T, ROWS> L;
+    typedef typename RecFour<T>::type Four;
+    constexpr int E = kRecE;
+    __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, backwards, B
+    __shared__ __align__(16) float begin[2][WAVES][L::COLS];
+    const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
+    const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
+    const bool live = c0 + unit * E < a.Cp;
+    const int c = live ? c0 + unit * E : c0;
     const int len = seq_length(a.lengths, n, a.L);
-    const T *x = static_cast<const T *>(a.x) + n * a.vx.n + cb * a.vx.c;
-    const T *f = static_cast<const T *>(a.f) + n * a.vf.n + cb * a.vf.c;
-    const T *i = static_cast<const T *>(a.i) + n * a.vi.n + cb * a.vi.c;
-    const T *z = a.z ? static_cast<const T *>(a.z) + n * a.vz.n + cb * a.vz.c : nullptr;
-    const T *dy = static_cast<const T *>(a.dy) + n * a.vdy.n + cb * a.vdy.c;
-    T *dx = static_cast<T *>(a.dx) + n * a.vdx.n + cb * a.vdx.c;
-    T *df = static_cast<T *>(a.df) + n * a.vdf.n + cb * a.vdf.c;
-    T *di = static_cast<T *>(a.di) + n * a.vdi.n + cb * a.vdi.c;
-    T *dz = a.z ? static_cast<T *>(a.dz) + n * a.vdz.n + cb * a.vdz.c : nullptr;
-    const RecParams<V> par(a, cb);
-    const int each = waves * LANES * P;
-    float state[V] = {};
+    const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
+    const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
+    const RecTensor<T> dx = tensor(a.dx, a.vdx), df = tensor(a.df, a.vdf), di = tensor(a.di, a.vdi), dz = tensor(a.dz, a.vdz);
+    const RecParams par(a, c);
+    // between waves each lane has one channel
+    const int col = lane % L::COLS;
+    const bool kept = c0 + col < a.Cp;
+    float *marks = a.marks + (long long)n * a.rounds * a.Cp + c0 + col;
+    const int each = waves * L::LANES * P;
     int turn = 0;
-    if (a.rounds > 1) {
-        for (int round = 0; round < a.rounds; ++round, turn ^= 1) {
-            float *mark = a.marks + ((long long)n * a.rounds + round) * a.Cp + (long long)cb * V;
-            if (live && wave == 0 && at == 0)
+    float state = 0;
+    for (int round = 0; round < a.rounds - 1; ++round, turn ^= 1) {
+        if (kept && threadIdx.x < L::COLS) marks[(long long)round * a.Cp] = state;
+        const long long w0 = (long long)round * each + wave * L::LANES * P, l0 = w0 + at * P;
+        Four bx[P], bf[P], bi[P];
 #pragma unroll
-                for (int k = 0; k < V; ++k) mark[k] = state[k];
-            const long long l0 = (long long)round * each + (wave * LANES + at) * P;
-            float A[V], H[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                A[k] = 1;
-                H[k] = 0;
+        for (int j = 0; j < P; ++j) {
+            bx[j] = bf[j] = bi[j] = Four{};
+            if (l0 + j < len) {
+                bx[j] = x.load(w0 + j);
+                bf[j] = f.load(w0 + j);
+                bi[j] = i.load(w0 + j);
             }
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                const long long l = l0 + j;
-                if (l < len) {
-                    float fx[V], ff[V], fi[V];
-                    SeqElem<T>::unpack(seq_load(x + l * a.vx.l), fx);
-                    SeqElem<T>::unpack(seq_load(f + l * a.vf.l), ff);
-                    SeqElem<T>::unpack(seq_load(i + l * a.vi.l), fi);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const float t = par.A[k] * rec_gate(ff[k], par.f[k]), pa = seq_exp2(t);
-                        H[k] = fmaf(pa, H[k], __builtin_amdgcn_sqrtf(rec_rest(t, pa)) * rec_gate(fi[k], par.i[k]) * fx[k]);
-                        A[k] *= pa;
-                    }
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) rec_join<LANES, 1, false>(A[k], H[k], at);
-            if (at == LANES - 1)
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    runs[turn][wave][bl][0][k] = A[k];
-                    runs[turn][wave][bl][1][k] = H[k];
-                }
-            __syncthreads();
-            for (int w = 0; w < waves; ++w)
-#pragma unroll
-                for (int k = 0; k < V; ++k) state[k] = fmaf(runs[turn][w][bl][0][k], state[k], runs[turn][w][bl][1][k]);
         }
-        __syncthreads();  // (the states before the rounds are there for all waves)
+        float A[E], H[E];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            float fx[E], ff[E], fi[E];
+            rec_unpack(bx[j], fx);
+            rec_unpack(bf[j], ff);
+            rec_unpack(bi[j], fi);
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), e = seq_exp2(t), p = l0 + j < len ? e : 1.0f;
+                const float u = __builtin_amdgcn_sqrtf(rec_rest(t, e)) * rec_gate(fi[k], par.i[k]) * fx[k];
+                H[k] = j == 0 ? u : fmaf(p, H[k], u);
+                A[k] = j == 0 ? p : A[k] * p;
+            }
+        }
+        rec_join<T, ROWS, false>(A, H, lane);
+        if (at == L::LANES - 1)
+#pragma unroll
+            for (int k = 0; k < E; ++k) *reinterpret_cast<seq_f32x2 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x2{A[k], H[k]};
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
     }
-    float back[V] = {};  // a dh of the position behind a round
-    float sums[3][V] = {};
+    float back = 0;  // a dh of the position behind a round
+    float sums[3][E] = {};
     for (int round = a.rounds - 1; round >= 0; --round, turn ^= 1) {
-        if (a.rounds > 1) seq_vector<V>(a.marks + ((long long)n * a.rounds + round) * a.Cp, cb, state);
-        const long long l0 = (long long)round * each + (wave * LANES + at) * P;
-        seq_u32x4 bx[P], bf[P], bi[P], bz[P], bdy[P];
-        float pa[P][V], ph[P][V], up[P][V];  // a; k g x, then the state before; what reaches h from y
-        float A[V], H[V], B[V];
+        // (the lanes of each wave that a mark comes from, or the first one's, which has passed a barrier since it stored it)
+        if (round < a.rounds - 1) state = kept ? marks[(long long)round * a.Cp] : 0.0f;
+        const long long w0 = (long long)round * each + wave * L::LANES * P, l0 = w0 + at * P;
+        Four bx[P], bf[P], bi[P], bz[P], bdy[P];
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const long long l = l0 + j;
-            bx[j] = bf[j] = bi[j] = bz[j] = bdy[j] = seq_u32x4{};
-            if (l < len) {
-                bx[j] = seq_load(x + l * a.vx.l);
-                bf[j] = seq_load(f + l * a.vf.l);
-                bi[j] = seq_load(i + l * a.vi.l);
-                bdy[j] = seq_load(dy + l * a.vdy.l);
-                if (z) bz[j] = seq_load(z + l * a.vz.l);
+            bx[j] = bf[j] = bi[j] = bz[j] = bdy[j] = Four{};
+            if (l0 + j < len) {
+                bx[j] = x.load(w0 + j);
+                bf[j] = f.load(w0 + j);
+                bi[j] = i.load(w0 + j);
+                bdy[j] = dy.load(w0 + j);
+                if (a.z) bz[j] = z.load(w0 + j);
+            }
+        }
+        float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
+        float A[E], H[E], Ab[E], B[E];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            float fx[E], ff[E], fi[E], fz[E];
+            rec_unpack(bx[j], fx);
+            rec_unpack(bf[j], ff);
+            rec_unpack(bi[j], fi);
+            rec_unpack(bz[j], fz);
+            rec_unpack(bdy[j], up[j]);
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
+                pa[j][k] = l0 + j < len ? p : 1.0f;
+                ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
+                if (a.z) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
+                H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
+                A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
         }
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            float fx[V], ff[V], fi[V], fz[V];
-            SeqElem<T>::unpack(bx[j], fx);
-            SeqElem<T>::unpack(bf[j], ff);
-            SeqElem<T>::unpack(bi[j], fi);
-            SeqElem<T>::unpack(bz[j], fz);
-            SeqElem<T>::unpack(bdy[j], up[j]);
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (l0 + j < len) {
-                    const float t = par.A[k] * rec_gate(ff[k], par.f[k]);
-                    pa[j][k] = seq_exp2(t);
-                    ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, pa[j][k])) * rec_gate(fi[k], par.i[k]) * fx[k];
-                    if (z) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
-                } else {
-                    pa[j][k] = 1;
-                    ph[j][k] = up[j][k] = 0;
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            A[k] = 1;
-            H[k] = B[k] = 0;
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                H[k] = fmaf(pa[j][k], H[k], ph[j][k]);
-                A[k] *= pa[j][k];
-            }
+        for (int k = 0; k < E; ++k) {
+            B[k] = 0;
 #pragma unroll
             for (int j = P - 1; j >= 0; --j) B[k] = pa[j][k] * (up[j][k] + B[k]);
-        }
-        float Ab[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
             Ab[k] = A[k];
-            rec_join<LANES, 1, false>(A[k], H[k], at);
-            rec_join<LANES, 1, true>(Ab[k], B[k], at);
         }
-        if (at == LANES - 1)
+        rec_join<T, ROWS, false>(A, H, lane);
+        rec_join<T, ROWS, true>(Ab, B, lane);
+        if (at == L::LANES - 1)
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                runs[turn][wave][bl][0][k] = A[k];
-                runs[turn][wave][bl][1][k] = H[k];
-            }
+            for (int k = 0; k < E; ++k) *reinterpret_cast<seq_f32x2 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x2{A[k], H[k]};
         if (at == 0)
 #pragma unroll
-            for (int k = 0; k < V; ++k) runs[turn][wave][bl][2][k] = B[k];
+            for (int k = 0; k < E; ++k) runs[turn][wave][unit * E + k][2] = B[k];
         __syncthreads();
-        float h[V], d[V];  // before and behind the wave's positions
-        for (int w = 0; w < waves; ++w)
+        float before = 0, behind = 0;
+        for (int w = 0; w < wave; ++w) state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
+        before = state;
+        for (int w = waves - 1; w >= 0; --w) {
+            if (w == wave) behind = back;
+            back = fmaf(runs[turn][w][col][0], back, runs[turn][w][col][2]);
+        }
+        begin[0][wave][col] = before;  // (the lanes that have a channel twice write the same)
+        begin[1][wave][col] = behind;
+        seq_wave_sync();
+        float h[E], d[E];
+        rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[0][wave][unit * E]), h);
+        rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[1][wave][unit * E]), d);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (w == wave) h[k] = state[k];
-                state[k] = fmaf(runs[turn][w][bl][0][k], state[k], runs[turn][w][bl][1][k]);
-            }
-        for (int w = waves - 1; w >= 0; --w)
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (w == wave) d[k] = back[k];
-                back[k] = fmaf(runs[turn][w][bl][0][k], back[k], runs[turn][w][bl][2][k]);
-            }
-#pragma unroll
-        for (int k = 0; k < V; ++k) {  // the lane's
-            float la = rec_near<1, false>(1.0f, A[k]), lh = rec_near0<1, false>(H[k]);
-            if (at == 0) la = 1, lh = 0;
-            h[k] = fmaf(la, h[k], lh);
-            la = rec_near<1, true>(1.0f, Ab[k]), lh = rec_near0<1, true>(B[k]);
-            if (at == LANES - 1) la = 1, lh = 0;
-            d[k] = fmaf(la, d[k], lh);
+        for (int k = 0; k < E; ++k) {
+            h[k] = rec_until<T, ROWS, false>(A[k], H[k], h[k], lane);
+            d[k] = rec_until<T, ROWS, true>(Ab[k], B[k], d[k], lane);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const float before = h[k];
+                const float old = h[k];
                 h[k] = fmaf(pa[j][k], h[k], ph[j][k]);
-                ph[j][k] = before;
+                ph[j][k] = old;
             }
         }
 #pragma unroll
         for (int j = P - 1; j >= 0; --j) {
-            const long long l = l0 + j;
-            if (l >= a.L || !live) continue;
-            seq_u32x4 ox = {}, of = {}, oi = {}, oz = {};
-            if (l < len) {
-                float fx[V], ff[V], fi[V], fz[V], fdy[V];
-                SeqElem<T>::unpack(bx[j], fx);
-                SeqElem<T>::unpack(bf[j], ff);
-                SeqElem<T>::unpack(bi[j], fi);
-                SeqElem<T>::unpack(bz[j], fz);
-                SeqElem<T>::unpack(bdy[j], fdy);
+            float fx[E], ff[E], fi[E], fz[E], fdy[E];
+            rec_again(bx[j]);
+            rec_again(bf[j]);
+            rec_again(bi[j]);
+            rec_again(bz[j]);
+            rec_again(bdy[j]);
+            rec_unpack(bx[j], fx);
+            rec_unpack(bf[j], ff);
+            rec_unpack(bi[j], fi);
+            rec_unpack(bz[j], fz);
+            rec_unpack(bdy[j], fdy);
+            const bool inside = l0 + j < len;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float s = rec_gate(ff[k], par.f[k]), g = rec_gate(fi[k], par.i[k]), t = par.A[k] * s, rest = rec_rest(t, pa[j][k]);
-                    // (what is too small for a normal number is none: the hardware's root takes it for zero)
-                    const float inv = rest >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(rest) : 0.0f, root = rest * inv;
-                    const float dh = up[j][k] + d[k], dhg = dh * g, gx = g * fx[k];
-                    const float dt = dh * pa[j][k] * fmaf(-gx * pa[j][k], inv, ph[j][k]);
-                    if (z) {
-                        const float p = seq_sigmoid(fz[k]);
-                        fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root * gx) * p * fmaf(fz[k], 1.0f - p, 1.0f);
-                    }
-                    fi[k] = dhg * root * fx[k] * (1.0f - g);
-                    fx[k] = dhg * root;
-                    ff[k] = dt * (t * kLn2) * (1.0f - s);
+            for (int k = 0; k < E; ++k) {
+                const float s = rec_gate(ff[k], par.f[k]), g = rec_gate(fi[k], par.i[k]), t = par.A[k] * s, rest = rec_rest(t, pa[j][k]);
+                // (what is too small for a normal number is none: the hardware's root takes it for zero)
+                const float inv = rest >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(rest) : 0.0f, root = rest * inv;
+                const float dh = up[j][k] + d[k], dhg = dh * g, gx = g * fx[k];
+                const float dt = dh * pa[j][k] * fmaf(-gx * pa[j][k], inv, ph[j][k]);
+                if (a.z) {
+                    const float p = seq_sigmoid(fz[k]);
+                    fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root * gx) * p * fmaf(fz[k], 1.0f - p, 1.0f);
+                }
+                fi[k] = dhg * root * fx[k] * (1.0f - g);
+                fx[k] = dhg * root;
+                ff[k] = dt * (t * kLn2) * (1.0f - s);
+                d[k] = pa[j][k] * dh;
+                if (inside) {
                     sums[0][k] = fmaf(dt, s, sums[0][k]);
                     sums[1][k] += ff[k];
                     sums[2][k] += fi[k];
-                    d[k] = pa[j][k] * dh;
                 }
-                ox = SeqElem<T>::pack(fx);
-                of = SeqElem<T>::pack(ff);
-                oi = SeqElem<T>::pack(fi);
-                oz = SeqElem<T>::pack(fz);
             }
-            seq_store(dx + l * a.vdx.l, ox);
-            seq_store(df + l * a.vdf.l, of);
-            seq_store(di + l * a.vdi.l, oi);
-            if (z) seq_store(dz + l * a.vdz.l, oz);
+            if (!live || l0 + j >= a.L) continue;
+            dx.template store<false>(w0 + j, inside ? RecFour<T>::pack(fx) : Four{});
+            df.template store<false>(w0 + j, inside ? RecFour<T>::pack(ff) : Four{});
+            di.template store<false>(w0 + j, inside ? RecFour<T>::pack(fi) : Four{});
+            if (a.z) dz.template store<false>(w0 + j, inside ? RecFour<T>::pack(fz) : Four{});
         }
     }
-    // the sums of a sequence: over a block's lanes, then over the waves in order
+    // the sums of a sequence: over the lanes that have a channel, then over the waves in order
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 3; ++q)
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
+        for (int k = 0; k < E; ++k) {
             float s = sums[q][k];
 #pragma unroll
-            for (int d = 1; d < LANES; d *= 2) s += __shfl_xor(s, d);
-            if (at == 0) runs[0][wave][bl][q][k] = s;
+            for (int d = 1; d < L::LANES; d *= 2) s += __shfl_xor(s, d * L::STEP);
+            if (at == 0) runs[0][wave][unit * E + k][q] = s;
         }
     __syncthreads();
-    if (wave == 0 && at == 0 && live)
+    if (threadIdx.x < L::COLS && kept)
 #pragma unroll
-        for (int q = 0; q < 3; ++q)
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                float s = 0;
-                for (int w = 0; w < waves; ++w) s += runs[0][w][bl][q][k];
-                a.part[((long long)n * 3 + q) * a.Cp + (long long)cb * V + k] = s;
-            }
+        for (int q = 0; q < 3; ++q) {
+            float s = 0;
+            for (int w = 0; w < waves; ++w) s += runs[0][w][col][q];
+            a.part[((long long)n * 3 + q) * a.Cp + c0 + col] = s;
+        }
 }
 
 // dA, df_bias and di_bias: the sequences' sums in order.
@@ -249,14 +219,19 @@ __global__ __launch_bounds__(1024) void seq_rec_reduce_kernel(const float *part,
     if (threadIdx.x < kSumColumns && col < Cp && to) to[col] = s;
 }
 
+template <typename T, bool ROWS>
+void launch_rows(const SeqRecArgs &a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+}
 template <typename T>
 hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((long long)a.N * seq_rec_groups(a.Cb, a.lanes));
-    if (a.lanes == 16)
-        seq_rec_bwd_kernel<T, 16, kSeqRecPositions><<<grid, 64 * a.waves, 0, s>>>(a);
+    if (a.rows)
+        launch_rows<T, true>(a, s);
     else
-        seq_rec_bwd_kernel<T, 4, kSeqRecPositions><<<grid, 64 * a.waves, 0, s>>>(a);
+        launch_rows<T, false>(a, s);
     seq_rec_reduce_kernel<<<dim3((a.Cp + kSumColumns - 1) / kSumColumns, 3), 1024, 0, s>>>(a.part, a.dA, a.df_bias, a.di_bias, a.N, a.Cp);
     return hipGetLastError();
 }
