@@ -5,6 +5,7 @@
 //
 // As the root-mean-square norm: a workgroup holds whole positions in registers between the sums over their channels and the result.  The squares are
 // of the differences from the mean, formed after it is known: a mean far from zero costs nothing of the variance.
+#include <algorithm>
 #include <type_traits>
 
 #include "seq_internal.h"
@@ -12,10 +13,10 @@
 namespace convmi {
 namespace {
 
-constexpr int kMaxThreads = 512;
+constexpr int kMaxThreads = 1024, kAloneWaves = 4;
 
 // Sums (MAX: largest unsigned) of K numbers over the threads with the same place in a tile of LT positions, in all of them, in an order that goes by
-// the threads' places alone.  ALONE: each wave has positions of its own.
+// the threads' places alone.  ALONE: each wave has positions of its own.  lds: not that of the sums before, which some wave may still read.
 template <int LT, bool MAX, bool ALONE, int K>
 static __device__ __forceinline__ void row_sums(float (&v)[K], float *lds)
 {
@@ -43,8 +44,10 @@ static __device__ __forceinline__ void row_sums(float (&v)[K], float *lds)
         v[k] = lds[k * LT + at];
         for (int w = 1; w < waves; ++w) v[k] = join(v[k], lds[(w * K + k) * LT + at]);
     }
-    __syncthreads();
 }
+
+// What is unpacked from b behind this is unpacked again, rather than kept in registers from before, where it takes twice as many.
+static __device__ __forceinline__ void again_from(seq_u32x4 &b) { asm volatile("" : "+v"(b)); }
 
 // Where a position lies, and whether it is inside its sequence; what is behind its end comes out as zero.
 template <typename T>
@@ -53,9 +56,9 @@ struct Place {
     int n, l;
     __device__ __forceinline__ Place(const SeqNormArgs &a, long long row)
     {
-        live = row < a.rows;
-        n = live ? (int)(row / a.L) : 0;
-        l = live ? (int)(row % a.L) : 0;
+        live = row < a.rows;  // (which 31 bits hold)
+        n = live ? (int)((unsigned)row / (unsigned)a.L) : 0;
+        l = live ? (int)((unsigned)row - (unsigned)n * (unsigned)a.L) : 0;
         inside = live && (!a.lengths || l < seq_length(a.lengths, n, a.L));
     }
 };
@@ -75,7 +78,7 @@ template <typename T, int LT, int NV, bool Q8, bool PAST>
 __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
-    __shared__ float lds[kMaxThreads / 64 * LT];
+    __shared__ float lds[3][kMaxThreads / 64 * LT];
     for (long long tile = blockIdx.x; tile * LT < a.rows; tile += gridDim.x) {
         const long long row = tile * LT + threadIdx.x % LT;
         const Place<T> at(a, row);
@@ -127,10 +130,11 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] += f[i];
         });
-        row_sums<LT, false, false>(s, lds);
+        row_sums<LT, false, false>(s, lds[0]);
         const float mean = s[0] / a.C;
         s[0] = 0;
         auto difference = [&](int j, int b, float (&f)[V]) {
+            if constexpr (NV > 0) again_from(keep[j]);
             SeqElem<T>::unpack(again(j, b), f);
 #pragma unroll
             for (int i = 0; i < V; ++i) f[i] -= mean;
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] = fmaf(f[i], f[i], s[0]);
         });
-        row_sums<LT, false, false>(s, lds);
+        row_sums<LT, false, false>(s, lds[1]);
         const float rstd = 1.0f / sqrtf(s[0] / a.C + a.eps);
         auto norm = [&](int j, int b, float (&f)[V]) {
             float w[V], c[V] = {};
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 #pragma unroll
                 for (int i = 0; i < V; ++i) m[0] = __uint_as_float(max(__float_as_uint(m[0]), __float_as_uint(fabsf(f[i]))));
             });
-            row_sums<LT, true, false>(m, lds);
+            row_sums<LT, true, false>(m, lds[2]);
             if (!at.live) continue;
             float scale = m[0] / 127.0f;
             if (scale < 1.17549435e-38f) scale = 0;  // (its reciprocal would be infinite)
@@ -200,30 +204,41 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 }
 
 // ALONE: each wave has positions of its own, and waits for no other until their parts of dw and db are added.
-template <typename T, int LT, int NV, bool ALONE>
-__global__ __launch_bounds__(kMaxThreads) void seq_lnorm_bwd_kernel(const SeqNormArgs a)
+// What the next positions need is asked for before these are worked on: a compute unit holds one workgroup of 16 waves.
+template <typename T, int LT, int NV, bool ALONE, bool PAST>
+__global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_lnorm_bwd_kernel(const SeqNormArgs a)
 {
     static_assert(!ALONE || LT == 1, "one position a wave");
     constexpr int V = SeqElem<T>::V, NK = NV ? NV : 1;
-    __shared__ float lds[kMaxThreads / 64 * LT * 2];
+    __shared__ float lds[2][kMaxThreads / 64 * LT * 2];
     const int first = ALONE ? threadIdx.x % 64 : threadIdx.x / LT, step = ALONE ? 64 : blockDim.x / LT;
     const int waves = blockDim.x / 64, each = ALONE ? waves : LT;  // positions of a workgroup at a time
     float *part = a.part + (long long)blockIdx.x * 2 * a.Cp;
-    float dw[NK][V] = {}, db[NK][V] = {};
+    float dw[NK][V] = {}, db[NK][V] = {}, kw[NK][V];
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (first + j * step < a.Cb) seq_vector<V>(a.w, first + j * step, kw[j]);
+    }
+    struct Blocks {
+        seq_u32x4 r[NK], dy[NK], dr[NK];
+    } now, next;
+    auto place = [&](long long tile) { return Place<T>(a, tile * each + (ALONE ? threadIdx.x / 64 : threadIdx.x % LT)); };
+    auto load = [&](const Place<T> &at, Blocks &k, int j, int b) {
+        k.r[j] = k.dy[j] = k.dr[j] = seq_u32x4{};
+        if (!at.inside) return;
+        k.r[j] = seq_load(static_cast<const T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l + b * a.vr.c);
+        k.dy[j] = seq_load(static_cast<const T *>(a.dy) + at.n * a.vdy.n + at.l * a.vdy.l + b * a.vdy.c);
+        if (a.dr) k.dr[j] = seq_load(static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l + b * a.vdr.c);
+    };
+    auto load_all = [&](const Place<T> &at, Blocks &k) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (first + j * step < a.Cb) load(at, k, j, first + j * step);
+    };
+    if constexpr (NV > 0) load_all(place(blockIdx.x), next);
     for (long long tile = blockIdx.x; tile * each < a.rows; tile += gridDim.x) {
-        const Place<T> at(a, tile * each + (ALONE ? threadIdx.x / 64 : threadIdx.x % LT));
-        const T *r = static_cast<const T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l;
-        const T *dy = static_cast<const T *>(a.dy) + at.n * a.vdy.n + at.l * a.vdy.l;
-        const T *dr = a.dr ? static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l : nullptr;
-        T *dx = static_cast<T *>(a.dx) + at.n * a.vdx.n + at.l * a.vdx.l;
-        seq_u32x4 kr[NK], ky[NK];
-        auto load = [&](int j, int b) {
-            kr[j] = ky[j] = seq_u32x4{};
-            if (at.inside) {
-                kr[j] = seq_load(r + b * a.vr.c);
-                ky[j] = seq_load(dy + b * a.vdy.c);
-            }
-        };
+        const Place<T> at = place(tile);
         auto over = [&](auto &&body) {
             if constexpr (NV > 0) {
 #pragma unroll
@@ -231,51 +246,55 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_bwd_kernel(const SeqNor
                     if (at.live && first + j * step < a.Cb) body(j, first + j * step);
             } else if (at.live)
                 for (int b = first; b < a.Cb; b += step) {
-                    load(0, b);
+                    load(at, now, 0, b);
+                    seq_vector<V>(a.w, b, kw[0]);
                     body(0, b);
                 }
         };
-        if constexpr (NV > 0) over(load);
+        if constexpr (NV > 0) {
+            now = next;
+            load_all(place(tile + gridDim.x), next);
+        }
         float s[2] = {};
         over([&](int j, int b) {
-            float f[V], g[V], w[V];
-            SeqElem<T>::unpack(kr[j], f);
-            SeqElem<T>::unpack(ky[j], g);
-            seq_vector<V>(a.w, b, w);
+            float f[V], g[V];
+            SeqElem<T>::unpack(now.r[j], f);
+            SeqElem<T>::unpack(now.dy[j], g);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 s[0] += f[i];
-                s[1] = fmaf(g[i], w[i], s[1]);
+                s[1] = fmaf(g[i], kw[j][i], s[1]);
             }
         });
-        row_sums<LT, false, ALONE>(s, lds);
+        row_sums<LT, false, ALONE>(s, lds[0]);
         const float mean = s[0] / a.C, through = s[1] / a.C;
         s[0] = s[1] = 0;
         auto difference = [&](int j, int b, float (&f)[V], float (&g)[V]) {
-            SeqElem<T>::unpack(kr[j], f);
-            SeqElem<T>::unpack(ky[j], g);
+            again_from(now.r[j]);
+            again_from(now.dy[j]);
+            SeqElem<T>::unpack(now.r[j], f);
+            SeqElem<T>::unpack(now.dy[j], g);
 #pragma unroll
             for (int i = 0; i < V; ++i) f[i] -= mean;
             clear_beyond<V>(a, b, f);
         };
         over([&](int j, int b) {
-            float f[V], g[V], w[V];
+            float f[V], g[V];
             difference(j, b, f, g);
-            seq_vector<V>(a.w, b, w);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 s[0] = fmaf(f[i], f[i], s[0]);
-                s[1] = fmaf(f[i], g[i] * w[i], s[1]);
+                s[1] = fmaf(f[i], g[i] * kw[j][i], s[1]);
             }
         });
-        row_sums<LT, false, ALONE>(s, lds);
+        row_sums<LT, false, ALONE>(s, lds[1]);
         const float rstd = 1.0f / sqrtf(s[0] / a.C + a.eps);
         const float along = s[1] / a.C * rstd * rstd;
+        T *dx = static_cast<T *>(a.dx) + at.n * a.vdx.n + at.l * a.vdx.l;
         over([&](int j, int b) {
-            float f[V], g[V], w[V], d[V] = {};
+            float f[V], g[V], d[V];
             difference(j, b, f, g);
-            seq_vector<V>(a.w, b, w);
-            if (dr && at.inside) SeqElem<T>::unpack(seq_load(dr + b * a.vdr.c), d);
+            SeqElem<T>::unpack(now.dr[j], d);
             if constexpr (NV == 0) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) dw[0][i] = db[0][i] = 0;
@@ -283,13 +302,13 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_bwd_kernel(const SeqNor
             if (at.inside) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    d[i] = fmaf(rstd, fmaf(-along, f[i], fmaf(g[i], w[i], -through)), d[i]);
+                    d[i] = fmaf(rstd, fmaf(-along, f[i], fmaf(g[i], kw[j][i], -through)), d[i]);
                     dw[j][i] = fmaf(g[i], f[i] * rstd, dw[j][i]);
                     db[j][i] += g[i];
                 }
                 clear_beyond<V>(a, b, d);
             }
-            seq_store(dx + b * a.vdx.c, SeqElem<T>::pack(d));
+            seq_store_result<PAST>(dx + b * a.vdx.c, SeqElem<T>::pack(d));
             if constexpr (NV == 0) {
                 // (the positions of one workgroup in turn, one at a time: its part is summed where it is stored)
 #pragma unroll
@@ -304,7 +323,7 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_bwd_kernel(const SeqNor
     }
     if constexpr (ALONE) {
         // the waves' sums in order, a block a lane at a time
-        __shared__ float sums[kMaxThreads / 64][64 * V];
+        __shared__ float sums[kAloneWaves][64 * V];
 #pragma unroll
         for (int j = 0; j < 2 * NV; ++j) {
 #pragma unroll
@@ -351,24 +370,11 @@ __global__ __launch_bounds__(1024) void seq_lnorm_reduce_kernel(const float *par
         db[c - Cp] = s;
 }
 
-hipError_t reduce(const SeqNormArgs &a, unsigned parts, hipStream_t s)
-{
-    seq_lnorm_reduce_kernel<<<(2 * a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, a.db, (int)parts, a.Cp);
-    return hipGetLastError();
-}
-
 template <typename T, int LT, int NV>
-hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
+hipError_t launch_fwd(const SeqNormArgs &a, int threads, hipStream_t s)
 {
     const long long tiles = (a.rows + LT - 1) / LT;
     const unsigned grid = (unsigned)(tiles < 1 << 22 ? tiles : 1 << 22);
-    if constexpr (LT == 16) {
-        if (bwd) return hipErrorInvalidValue;  // (goes by eight)
-    } else if (bwd) {
-        const unsigned parts = grid < (unsigned)a.parts ? grid : (unsigned)a.parts;
-        seq_lnorm_bwd_kernel<T, LT, NV, false><<<parts, threads, 0, s>>>(a);
-        return reduce(a, parts, s);
-    }
     if (a.q)
         seq_lnorm_fwd_kernel<T, LT, NV, true, false><<<grid, threads, 0, s>>>(a);
     else if (a.past)
@@ -377,55 +383,76 @@ hipError_t launch_nv(bool bwd, const SeqNormArgs &a, int threads, hipStream_t s)
         seq_lnorm_fwd_kernel<T, LT, NV, false, false><<<grid, threads, 0, s>>>(a);
     return hipGetLastError();
 }
-
-// Threads of a workgroup and blocks that each holds: 256 threads with up to 8 blocks, then up to 512.  LT positions that do not fit
-// that go as fewer at a time; what one position does not fit is read again.
-template <typename T, int LT>
-hipError_t launch_lt(bool bwd, const SeqNormArgs &a, hipStream_t s)
+template <typename T, int LT, int NV, bool ALONE>
+hipError_t launch_bwd(const SeqNormArgs &a, int threads, hipStream_t s)
 {
+    // parts of dw and db: as many as there are workgroups at a time
+    const long long tiles = (a.rows + LT - 1) / LT, most = threads > 512 ? 256 : 512;
+    const unsigned parts = (unsigned)std::min<long long>(std::min<long long>(most, a.parts), tiles);
+    if (a.past)
+        seq_lnorm_bwd_kernel<T, LT, NV, ALONE, true><<<parts, threads, 0, s>>>(a);
+    else
+        seq_lnorm_bwd_kernel<T, LT, NV, ALONE, false><<<parts, threads, 0, s>>>(a);
+    seq_lnorm_reduce_kernel<<<(2 * a.Cp + kSumColumns - 1) / kSumColumns, 1024, 0, s>>>(a.part, a.dw, a.db, (int)parts, a.Cp);
+    return hipGetLastError();
+}
+
+// Threads of a workgroup and blocks that each holds: up to 4 forwards, 2 backwards, whose sums of dw and db take 16 registers a bf16 block, so that
+// four waves a SIMD have their registers; from 256 threads on if that takes fewer blocks.  LT positions that do not fit 1024 threads go as fewer at a time; what one
+// position does not fit is read again.
+template <typename T, int LT, bool BWD>
+hipError_t launch_lt(const SeqNormArgs &a, hipStream_t s)
+{
+    constexpr int MOST = BWD ? 2 : 4;
     const long long lanes = (long long)a.Cb * LT;
     int threads = 64;
     while (threads < 256 && threads < lanes) threads *= 2;
-    if (threads * 8 < lanes) threads = kMaxThreads;
+    while (threads < kMaxThreads && threads * MOST < lanes) threads *= 2;
     const long long nv = (lanes + threads - 1) / threads;
-    if constexpr (LT >= 8 || LT == 1) {  // (what comes to 4 and 2 has more)
-        if (nv <= 1) return launch_nv<T, LT, 1>(bwd, a, threads, s);
-        if (nv <= 2) return launch_nv<T, LT, 2>(bwd, a, threads, s);
-        if (nv <= 4) return launch_nv<T, LT, 4>(bwd, a, threads, s);
+    if constexpr (BWD) {
+        if (nv <= 1) return launch_bwd<T, LT, 1, false>(a, threads, s);
+        if (nv <= 2) return launch_bwd<T, LT, 2, false>(a, threads, s);
+    } else {
+        if (nv <= 1) return launch_fwd<T, LT, 1>(a, threads, s);
+        if (nv <= 2) return launch_fwd<T, LT, 2>(a, threads, s);
+        if (nv <= 4) return launch_fwd<T, LT, 4>(a, threads, s);
     }
-    if (nv <= 8) return launch_nv<T, LT, 8>(bwd, a, threads, s);
     if constexpr (LT > 1)
-        return launch_lt<T, LT / 2>(bwd, a, s);
+        return launch_lt<T, LT / 2, BWD>(a, s);
+    else if constexpr (BWD)
+        return launch_bwd<T, 1, 0, false>(a, threads, s);
     else
-        return launch_nv<T, LT, 0>(bwd, a, threads, s);
+        return launch_fwd<T, 1, 0>(a, threads, s);
 }
-template <typename T, int NV>
-hipError_t launch_alone(const SeqNormArgs &a, hipStream_t s)
+template <typename T, bool BWD>
+hipError_t launch_t(const SeqNormArgs &a, hipStream_t s)
 {
-    seq_lnorm_bwd_kernel<T, 1, NV, true><<<(unsigned)a.parts, 256, 0, s>>>(a);
-    return reduce(a, (unsigned)a.parts, s);
-}
-template <typename T>
-hipError_t launch_t(bool bwd, const SeqNormArgs &a, hipStream_t s)
-{
+    // one position at a time where its blocks follow one another in what is read; else eight, forwards sixteen where that leaves two
+    // workgroups for each compute unit
     constexpr int V = SeqElem<T>::V;
-    const SeqView &v = bwd ? a.vr : a.vx;
+    const SeqView &v = BWD ? a.vr : a.vx;
     if (v.c == V || a.L == 1) {
-        if (bwd && a.rows >= 8LL * a.parts && a.Cb <= 8 * 64)
-            return a.Cb <= 64 ? launch_alone<T, 1>(a, s) : a.Cb <= 2 * 64 ? launch_alone<T, 2>(a, s) : a.Cb <= 4 * 64 ? launch_alone<T, 4>(a, s) : launch_alone<T, 8>(a, s);
-        return launch_lt<T, 1>(bwd, a, s);
+        // a wave each where that leaves every workgroup two for each of its waves
+        if constexpr (BWD) {
+            if (a.rows >= 2LL * kAloneWaves * a.parts && a.Cb <= 2 * 64)
+                return a.Cb <= 64 ? launch_bwd<T, 1, 1, true>(a, 64 * kAloneWaves, s) : launch_bwd<T, 1, 2, true>(a, 64 * kAloneWaves, s);
+        }
+        return launch_lt<T, 1, BWD>(a, s);
     }
-    return bwd || a.rows < 16 * 512 ? launch_lt<T, 8>(bwd, a, s) : launch_lt<T, 16>(bwd, a, s);
+    if constexpr (!BWD) {
+        if (a.rows >= 16 * 512) return launch_lt<T, 16, false>(a, s);
+    }
+    return launch_lt<T, 8, BWD>(a, s);
 }
 }  // namespace
 
 hipError_t launch_seq_lnorm_fwd(int dtype, const SeqNormArgs &a, hipStream_t s)
 {
-    return dtype == SEQ_BF16 ? launch_t<unsigned short>(false, a, s) : launch_t<float>(false, a, s);
+    return dtype == SEQ_BF16 ? launch_t<unsigned short, false>(a, s) : launch_t<float, false>(a, s);
 }
 hipError_t launch_seq_lnorm_bwd(int dtype, const SeqNormArgs &a, hipStream_t s)
 {
-    return dtype == SEQ_BF16 ? launch_t<unsigned short>(true, a, s) : launch_t<float>(true, a, s);
+    return dtype == SEQ_BF16 ? launch_t<unsigned short, true>(a, s) : launch_t<float, true>(a, s);
 }
 
 }  // namespace convmi
