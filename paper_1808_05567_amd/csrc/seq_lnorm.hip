@@ -3,8 +3,11 @@
 //   r = x + res,   u = (r - mean r) rstd,   y = u w + b,   rstd = 1 / sqrt(mean (r - mean r)^2 + eps)
 //   dx = dr + rstd (w dy - mean(w dy) - u mean(w dy u)),   dw = sum dy u,   db = sum dy
 //
-// As the root-mean-square norm: a workgroup holds whole positions in registers between the sums over their channels and the result.  The squares are
-// of the differences from the mean, formed after it is known: a mean far from zero costs nothing of the variance.
+// As the root-mean-square norm: a workgroup holds whole positions in registers between the sums over their channels and the result.  Squares are of
+// differences from a mean, so that one far from zero costs nothing of the variance: each wave has the mean m_w of its own n_w channels and sums about that,
+//   q_w = sum (r - m_w)^2,  and backwards  G_w = sum w dy,  p_w = sum w dy (r - m_w),
+// which the workgroup joins in one exchange:  mean = sum n_w m_w / C,  sum (r - mean)^2 = sum q_w + n_w (m_w - mean)^2,
+//   sum w dy (r - mean) = sum p_w + G_w (m_w - mean).
 #include <algorithm>
 #include <type_traits>
 
@@ -15,14 +18,12 @@ namespace {
 
 constexpr int kMaxThreads = 1024, kAloneWaves = 4;
 
-// Sums (MAX: largest unsigned) of K numbers over the threads with the same place in a tile of LT positions, in all of them, in an order that goes by
-// the threads' places alone.  ALONE: each wave has positions of its own.  lds: not that of the sums before, which some wave may still read.
-template <int LT, bool MAX, bool ALONE, int K>
-static __device__ __forceinline__ void row_sums(float (&v)[K], float *lds)
+// Sums (MAX: largest unsigned) of K numbers over the lanes of a wave with the same place in a tile of LT positions, in all of them.
+template <int LT, bool MAX, int K>
+static __device__ __forceinline__ void wave_sums(float (&v)[K])
 {
     auto join = [](float p, float q) { return MAX ? __uint_as_float(max(__float_as_uint(p), __float_as_uint(q))) : p + q; };
     auto turn = [](float p, auto by) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(p), 0x120 + decltype(by)::value, 0xf, 0xf, true)); };
-    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, at = threadIdx.x % LT;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if constexpr (LT <= 1) v[k] = join(v[k], turn(v[k], std::integral_constant<int, 1>()));
@@ -34,16 +35,50 @@ static __device__ __forceinline__ void row_sums(float (&v)[K], float *lds)
         const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[k]), __float_as_uint(v[k]), false, false);
         v[k] = join(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
     }
-    if (ALONE || waves == 1) return;
-    if (threadIdx.x % 64 < LT)
-#pragma unroll
-        for (int k = 0; k < K; ++k) lds[(wave * K + k) * LT + at] = v[k];
+}
+
+// Channels of a position that wave w has: of blocks w * 64 / LT ... and of those `step` blocks on, and so forth.
+template <int LT, int V>
+static __device__ __forceinline__ float channels_of(const SeqNormArgs &a, int w, int step)
+{
+    int n = 0;
+    for (int b = w * (64 / LT); b < a.Cb; b += step) n += min(max(a.C - b * V, 0), 64 / LT * V);
+    return (float)n;
+}
+
+// A position's sums from those of its waves, all four of them in each wave's lanes in the same order.  lds: not that of the exchange before, which some wave may
+// still read.  in: mean, q and, backwards, G, p; out: mean, sum of squares and, backwards, sum of w dy, sum of w dy (r - mean).
+template <int LT, bool BWD, int V>
+static __device__ __forceinline__ void join_waves(const SeqNormArgs &a, seq_f32x4 &sums, seq_f32x4 *lds)
+{
+    constexpr int EACH = (kMaxThreads / 64 + 64 / LT - 1) / (64 / LT), K = BWD ? 2 : 1;
+    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, at = threadIdx.x % LT, bl = threadIdx.x % 64 / LT, step = blockDim.x / LT;
+    if (threadIdx.x % 64 < LT) lds[wave * LT + at] = sums;
     __syncthreads();
+    seq_f32x4 e[EACH];
+    float n[EACH], t[K] = {}, u[K] = {};
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        v[k] = lds[k * LT + at];
-        for (int w = 1; w < waves; ++w) v[k] = join(v[k], lds[(w * K + k) * LT + at]);
+    for (int i = 0; i < EACH; ++i) {
+        const int w = bl + i * (64 / LT);
+        e[i] = seq_f32x4{};
+        n[i] = 0;
+        if (w < waves) {
+            e[i] = lds[w * LT + at];
+            n[i] = channels_of<LT, V>(a, w, step);
+        }
+        t[0] = fmaf(n[i], e[i][0], t[0]);
+        if constexpr (BWD) t[1] += e[i][2];
     }
+    wave_sums<LT, false>(t);
+    const float mean = t[0] / a.C;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const float d = e[i][0] - mean;
+        u[0] += n[i] == 0 ? 0.0f : fmaf(n[i] * d, d, e[i][1]);
+        if constexpr (BWD) u[1] += n[i] == 0 ? 0.0f : fmaf(e[i][2], d, e[i][3]);
+    }
+    wave_sums<LT, false>(u);
+    sums = seq_f32x4{mean, u[0], BWD ? t[1] : 0.0f, BWD ? u[1] : 0.0f};
 }
 
 // What is unpacked from b behind this is unpacked again, rather than kept in registers from before, where it takes twice as many.
@@ -78,7 +113,10 @@ template <typename T, int LT, int NV, bool Q8, bool PAST>
 __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
-    __shared__ float lds[3][kMaxThreads / 64 * LT];
+    __shared__ seq_f32x4 lds[2][kMaxThreads / 64 * LT];
+    __shared__ float largest_of[Q8 ? kMaxThreads / 64 * LT : 1];
+    const float channels = channels_of<LT, V>(a, threadIdx.x / 64, blockDim.x / LT);
+    int turn = 0;
     for (long long tile = blockIdx.x; tile * LT < a.rows; tile += gridDim.x) {
         const long long row = tile * LT + threadIdx.x % LT;
         const Place<T> at(a, row);
@@ -130,10 +168,10 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] += f[i];
         });
-        row_sums<LT, false, false>(s, lds[0]);
-        const float mean = s[0] / a.C;
+        wave_sums<LT, false>(s);
+        const float own = s[0] / fmaxf(channels, 1.0f);
         s[0] = 0;
-        auto difference = [&](int j, int b, float (&f)[V]) {
+        auto difference = [&](int j, int b, float mean, float (&f)[V]) {
             if constexpr (NV > 0) again_from(keep[j]);
             SeqElem<T>::unpack(again(j, b), f);
 #pragma unroll
@@ -142,15 +180,18 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
         };
         over([&](int j, int b) {
             float f[V];
-            difference(j, b, f);
+            difference(j, b, own, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] = fmaf(f[i], f[i], s[0]);
         });
-        row_sums<LT, false, false>(s, lds[1]);
-        const float rstd = 1.0f / sqrtf(s[0] / a.C + a.eps);
+        wave_sums<LT, false>(s);
+        seq_f32x4 sums = {own, s[0], 0, 0};
+        if (blockDim.x > 64) join_waves<LT, false, V>(a, sums, lds[turn]);
+        turn ^= 1;
+        const float mean = sums[0], rstd = 1.0f / sqrtf(sums[1] / a.C + a.eps);
         auto norm = [&](int j, int b, float (&f)[V]) {
             float w[V], c[V] = {};
-            difference(j, b, f);
+            difference(j, b, mean, f);
             seq_vector<V>(a.w, b, w);
             if (a.b) seq_vector<V>(a.b, b, c);
 #pragma unroll
@@ -173,7 +214,13 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
 #pragma unroll
                 for (int i = 0; i < V; ++i) m[0] = __uint_as_float(max(__float_as_uint(m[0]), __float_as_uint(fabsf(f[i]))));
             });
-            row_sums<LT, true, false>(m, lds[2]);
+            wave_sums<LT, true>(m);
+            if (blockDim.x > 64) {
+                // (between two of these lies the exchange of the sums)
+                if (threadIdx.x % 64 < LT) largest_of[threadIdx.x / 64 * LT + threadIdx.x % LT] = m[0];
+                __syncthreads();
+                for (int w = 0; w < (int)blockDim.x / 64; ++w) m[0] = __uint_as_float(max(__float_as_uint(m[0]), __float_as_uint(largest_of[w * LT + threadIdx.x % LT])));
+            }
             if (!at.live) continue;
             float scale = m[0] / 127.0f;
             if (scale < 1.17549435e-38f) scale = 0;  // (its reciprocal would be infinite)
@@ -210,31 +257,46 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
 {
     static_assert(!ALONE || LT == 1, "one position a wave");
     constexpr int V = SeqElem<T>::V, NK = NV ? NV : 1;
-    __shared__ float lds[2][kMaxThreads / 64 * LT * 2];
+    __shared__ seq_f32x4 lds[2][kMaxThreads / 64 * LT];
+    constexpr bool SHARED = LT > 1 && NV > 0;  // w lies in LDS, where lanes share it
+    __shared__ __align__(16) float lw[SHARED ? kMaxThreads / LT * NV * V : 4];
     const int first = ALONE ? threadIdx.x % 64 : threadIdx.x / LT, step = ALONE ? 64 : blockDim.x / LT;
     const int waves = blockDim.x / 64, each = ALONE ? waves : LT;  // positions of a workgroup at a time
     float *part = a.part + (long long)blockIdx.x * 2 * a.Cp;
-    float dw[NK][V] = {}, db[NK][V] = {}, kw[NK][V];
-    if constexpr (NV > 0) {
+    float dw[NK][V] = {}, db[NK][V] = {}, kw[SHARED ? 1 : NK][V];
+    if constexpr (SHARED) {
+        for (int c = threadIdx.x; c < a.Cp; c += blockDim.x) lw[c] = a.w[c];
+        __syncthreads();
+    } else if constexpr (NV > 0) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (first + j * step < a.Cb) seq_vector<V>(a.w, first + j * step, kw[j]);
     }
+    auto weights = [&](int j, int b, float (&w)[V]) {
+        if constexpr (SHARED)
+            seq_vector<V>(lw, b, w);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = kw[j][i];
+    };
+    const float channels = channels_of<LT, V>(a, ALONE ? 0 : threadIdx.x / 64, step);
+    int turn = 0;
     struct Blocks {
         seq_u32x4 r[NK], dy[NK], dr[NK];
     } now, next;
     auto place = [&](long long tile) { return Place<T>(a, tile * each + (ALONE ? threadIdx.x / 64 : threadIdx.x % LT)); };
-    auto load = [&](const Place<T> &at, Blocks &k, int j, int b) {
-        k.r[j] = k.dy[j] = k.dr[j] = seq_u32x4{};
-        if (!at.inside) return;
-        k.r[j] = seq_load(static_cast<const T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l + b * a.vr.c);
-        k.dy[j] = seq_load(static_cast<const T *>(a.dy) + at.n * a.vdy.n + at.l * a.vdy.l + b * a.vdy.c);
-        if (a.dr) k.dr[j] = seq_load(static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l + b * a.vdr.c);
-    };
+    // where a position's first block of a thread lies; the others are the same distances on for all threads
+    auto where = [&](const void *p, const SeqView &v, const Place<T> &at) { return static_cast<const T *>(p) + at.n * v.n + at.l * v.l + first * v.c; };
     auto load_all = [&](const Place<T> &at, Blocks &k) {
+        const T *r = where(a.r, a.vr, at), *dy = where(a.dy, a.vdy, at), *dr = a.dr ? where(a.dr, a.vdr, at) : nullptr;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (first + j * step < a.Cb) load(at, k, j, first + j * step);
+        for (int j = 0; j < NV; ++j) {
+            k.r[j] = k.dy[j] = k.dr[j] = seq_u32x4{};
+            if (!at.inside || first + j * step >= a.Cb) continue;
+            k.r[j] = seq_load(r + j * (step * a.vr.c));
+            k.dy[j] = seq_load(dy + j * (step * a.vdy.c));
+            if (dr) k.dr[j] = seq_load(dr + j * (step * a.vdr.c));
+        }
     };
     if constexpr (NV > 0) load_all(place(blockIdx.x), next);
     for (long long tile = blockIdx.x; tile * each < a.rows; tile += gridDim.x) {
@@ -246,7 +308,12 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
                     if (at.live && first + j * step < a.Cb) body(j, first + j * step);
             } else if (at.live)
                 for (int b = first; b < a.Cb; b += step) {
-                    load(at, now, 0, b);
+                    now.r[0] = now.dy[0] = now.dr[0] = seq_u32x4{};
+                    if (at.inside) {
+                        now.r[0] = seq_load(static_cast<const T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l + b * a.vr.c);
+                        now.dy[0] = seq_load(static_cast<const T *>(a.dy) + at.n * a.vdy.n + at.l * a.vdy.l + b * a.vdy.c);
+                        if (a.dr) now.dr[0] = seq_load(static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l + b * a.vdr.c);
+                    }
                     seq_vector<V>(a.w, b, kw[0]);
                     body(0, b);
                 }
@@ -257,19 +324,20 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
         }
         float s[2] = {};
         over([&](int j, int b) {
-            float f[V], g[V];
+            float f[V], g[V], w[V];
             SeqElem<T>::unpack(now.r[j], f);
             SeqElem<T>::unpack(now.dy[j], g);
+            weights(j, b, w);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 s[0] += f[i];
-                s[1] = fmaf(g[i], kw[j][i], s[1]);
+                s[1] = fmaf(g[i], w[i], s[1]);
             }
         });
-        row_sums<LT, false, ALONE>(s, lds[0]);
-        const float mean = s[0] / a.C, through = s[1] / a.C;
+        wave_sums<LT, false>(s);
+        const float own = s[0] / fmaxf(channels, 1.0f), own_dy = s[1];
         s[0] = s[1] = 0;
-        auto difference = [&](int j, int b, float (&f)[V], float (&g)[V]) {
+        auto difference = [&](int j, int b, float mean, float (&f)[V], float (&g)[V]) {
             again_from(now.r[j]);
             again_from(now.dy[j]);
             SeqElem<T>::unpack(now.r[j], f);
@@ -279,22 +347,26 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
             clear_beyond<V>(a, b, f);
         };
         over([&](int j, int b) {
-            float f[V], g[V];
-            difference(j, b, f, g);
+            float f[V], g[V], w[V];
+            difference(j, b, own, f, g);
+            weights(j, b, w);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 s[0] = fmaf(f[i], f[i], s[0]);
-                s[1] = fmaf(f[i], g[i] * kw[j][i], s[1]);
+                s[1] = fmaf(f[i], g[i] * w[i], s[1]);
             }
         });
-        row_sums<LT, false, ALONE>(s, lds[1]);
-        const float rstd = 1.0f / sqrtf(s[0] / a.C + a.eps);
-        const float along = s[1] / a.C * rstd * rstd;
-        T *dx = static_cast<T *>(a.dx) + at.n * a.vdx.n + at.l * a.vdx.l;
+        wave_sums<LT, false>(s);
+        seq_f32x4 sums = {own, s[0], own_dy, s[1]};
+        if (!ALONE && blockDim.x > 64) join_waves<LT, true, V>(a, sums, lds[turn]);
+        turn ^= 1;
+        const float mean = sums[0], rstd = 1.0f / sqrtf(sums[1] / a.C + a.eps), through = sums[2] / a.C, along = sums[3] / a.C * rstd * rstd;
+        T *dx = const_cast<T *>(where(a.dx, a.vdx, at));
         over([&](int j, int b) {
-            float f[V], g[V], d[V];
-            difference(j, b, f, g);
+            float f[V], g[V], d[V], w[V];
+            difference(j, b, mean, f, g);
             SeqElem<T>::unpack(now.dr[j], d);
+            weights(j, b, w);
             if constexpr (NV == 0) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) dw[0][i] = db[0][i] = 0;
@@ -302,13 +374,13 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
             if (at.inside) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    d[i] = fmaf(rstd, fmaf(-along, f[i], fmaf(g[i], kw[j][i], -through)), d[i]);
+                    d[i] = fmaf(rstd, fmaf(-along, f[i], fmaf(g[i], w[i], -through)), d[i]);
                     dw[j][i] = fmaf(g[i], f[i] * rstd, dw[j][i]);
                     db[j][i] += g[i];
                 }
                 clear_beyond<V>(a, b, d);
             }
-            seq_store_result<PAST>(dx + b * a.vdx.c, SeqElem<T>::pack(d));
+            seq_store_result<PAST>(NV > 0 ? dx + j * (step * a.vdx.c) : dx + (b - first) * a.vdx.c, SeqElem<T>::pack(d));
             if constexpr (NV == 0) {
                 // (the positions of one workgroup in turn, one at a time: its part is summed where it is stored)
 #pragma unroll
