@@ -282,20 +282,29 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
     const float channels = channels_of<LT, V>(a, ALONE ? 0 : threadIdx.x / 64, step);
     int turn = 0;
     struct Blocks {
-        seq_u32x4 r[NK], dy[NK], dr[NK];
+        seq_u32x4 r[NK], dy[NK];
     } now, next;
+    seq_u32x4 now_dr[NK];
     auto place = [&](long long tile) { return Place<T>(a, tile * each + (ALONE ? threadIdx.x / 64 : threadIdx.x % LT)); };
     // where a position's first block of a thread lies; the others are the same distances on for all threads
     auto where = [&](const void *p, const SeqView &v, const Place<T> &at) { return static_cast<const T *>(p) + at.n * v.n + at.l * v.l + first * v.c; };
     auto load_all = [&](const Place<T> &at, Blocks &k) {
-        const T *r = where(a.r, a.vr, at), *dy = where(a.dy, a.vdy, at), *dr = a.dr ? where(a.dr, a.vdr, at) : nullptr;
+        const T *r = where(a.r, a.vr, at), *dy = where(a.dy, a.vdy, at);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            k.r[j] = k.dy[j] = k.dr[j] = seq_u32x4{};
+            k.r[j] = k.dy[j] = seq_u32x4{};
             if (!at.inside || first + j * step >= a.Cb) continue;
             k.r[j] = seq_load(r + j * (step * a.vr.c));
             k.dy[j] = seq_load(dy + j * (step * a.vdy.c));
-            if (dr) k.dr[j] = seq_load(dr + j * (step * a.vdr.c));
+        }
+    };
+    // (dr is needed last: it is asked for when these positions' sums begin)
+    auto load_dr = [&](const Place<T> &at) {
+        const T *dr = a.dr ? where(a.dr, a.vdr, at) : nullptr;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            now_dr[j] = seq_u32x4{};
+            if (dr && at.inside && first + j * step < a.Cb) now_dr[j] = seq_load(dr + j * (step * a.vdr.c));
         }
     };
     if constexpr (NV > 0) load_all(place(blockIdx.x), next);
@@ -308,11 +317,11 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
                     if (at.live && first + j * step < a.Cb) body(j, first + j * step);
             } else if (at.live)
                 for (int b = first; b < a.Cb; b += step) {
-                    now.r[0] = now.dy[0] = now.dr[0] = seq_u32x4{};
+                    now.r[0] = now.dy[0] = now_dr[0] = seq_u32x4{};
                     if (at.inside) {
                         now.r[0] = seq_load(static_cast<const T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l + b * a.vr.c);
                         now.dy[0] = seq_load(static_cast<const T *>(a.dy) + at.n * a.vdy.n + at.l * a.vdy.l + b * a.vdy.c);
-                        if (a.dr) now.dr[0] = seq_load(static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l + b * a.vdr.c);
+                        if (a.dr) now_dr[0] = seq_load(static_cast<const T *>(a.dr) + at.n * a.vdr.n + at.l * a.vdr.l + b * a.vdr.c);
                     }
                     seq_vector<V>(a.w, b, kw[0]);
                     body(0, b);
@@ -320,6 +329,7 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
         };
         if constexpr (NV > 0) {
             now = next;
+            load_dr(at);
             load_all(place(tile + gridDim.x), next);
         }
         float s[2] = {};
@@ -365,7 +375,7 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
         over([&](int j, int b) {
             float f[V], g[V], d[V], w[V];
             difference(j, b, mean, f, g);
-            SeqElem<T>::unpack(now.dr[j], d);
+            SeqElem<T>::unpack(now_dr[j], d);
             weights(j, b, w);
             if constexpr (NV == 0) {
 #pragma unroll
