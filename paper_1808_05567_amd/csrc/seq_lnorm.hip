@@ -124,23 +124,23 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
         const T *x = static_cast<const T *>(a.x) + at.n * a.vx.n + at.l * a.vx.l;
         const T *res = a.res ? static_cast<const T *>(a.res) + at.n * a.vres.n + at.l * a.vres.l : nullptr;
         T *r = a.r ? static_cast<T *>(a.r) + at.n * a.vr.n + at.l * a.vr.l : nullptr;
+        auto added = [](const seq_u32x4 &p, const seq_u32x4 &q) {
+            float f[V], g[V];
+            SeqElem<T>::unpack(p, f);
+            SeqElem<T>::unpack(q, g);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] += g[i];
+            return SeqElem<T>::pack(f);
+        };
         // (a position behind its sequence's end: zeros, whatever x and res hold)
         auto sum_of = [&](int b) {
             if (!at.inside) return seq_u32x4{};
-            seq_u32x4 p = seq_load(x + b * a.vx.c);
-            if (res) {
-                float f[V], g[V];
-                SeqElem<T>::unpack(p, f);
-                SeqElem<T>::unpack(seq_load(res + b * a.vres.c), g);
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[i] += g[i];
-                p = SeqElem<T>::pack(f);
-            }
-            return p;
+            const seq_u32x4 p = seq_load(x + b * a.vx.c);
+            return res ? added(p, seq_load(res + b * a.vres.c)) : p;
         };
         auto first_time = [&](int b) {
             const seq_u32x4 p = sum_of(b);
-            if (r) seq_store_result<PAST && NV != 0>(r + b * a.vr.c, p);
+            if (r) seq_store(r + b * a.vr.c, p);
             return p;
         };
         seq_u32x4 keep[NV ? NV : 1];
@@ -158,7 +158,20 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
                 for (int b = first; b < a.Cb; b += step) each(0, b);
         };
         float s[1] = {};
-        if constexpr (NV > 0) over([&](int j, int b) { keep[j] = first_time(b); });
+        if constexpr (NV > 0) {
+            // all of it is asked for before any r is stored, which may lie in x's or res's place
+            seq_u32x4 more[NV];
+            over([&](int j, int b) {
+                keep[j] = more[j] = seq_u32x4{};
+                if (!at.inside) return;
+                keep[j] = seq_load(x + b * a.vx.c);
+                if (res) more[j] = seq_load(res + b * a.vres.c);
+            });
+            over([&](int j, int b) {
+                if (res) keep[j] = added(keep[j], more[j]);
+                if (r) seq_store_result<PAST>(r + b * a.vr.c, keep[j]);
+            });
+        }
         over([&](int j, int b) {
             float f[V];
             if constexpr (NV > 0)
