@@ -74,16 +74,56 @@ struct RecTensor {
         t.lane = ((unsigned)(c / L::V - b0) * (unsigned)v.c + (unsigned)(at * P) * (unsigned)v.l + (unsigned)(c % L::V)) * (unsigned)sizeof(T);
         return t;
     }
-    // l: position of the wave's first lane, the same for all lanes
-    __device__ __forceinline__ Four load(long long l) const { return *reinterpret_cast<const Four *>(base + l * pitch + lane); }
-    template <bool PAST>
-    __device__ __forceinline__ void store(long long l, const Four &b) const
+    // l: position of the wave's first lane, the same for all lanes.  (An address in scalar registers and a lane's distance are one instruction; the compiler,
+    // left alone, adds the distance to `base` once and to that, in vector registers, the rest.)
+    template <typename B>
+    __device__ __forceinline__ __attribute__((address_space(1))) B *at(long long l, unsigned distance) const
     {
-        Four *to = reinterpret_cast<Four *>(base + l * pitch + lane);
+        auto *p = (__attribute__((address_space(1))) char *)(base + l * pitch);
+        asm("" : "+s"(p), "+v"(distance));
+        return (__attribute__((address_space(1))) B *)(p + distance);
+    }
+    __device__ __forceinline__ Four load(long long l) const { return *at<Four>(l, lane); }
+    template <bool PAST, typename B>
+    __device__ __forceinline__ void store(long long l, unsigned distance, const B &b) const
+    {
         if constexpr (PAST)
-            __builtin_nontemporal_store(b, to);
+            __builtin_nontemporal_store(b, at<B>(l, distance));
         else
-            *to = b;
+            *at<B>(l, distance) = b;
+    }
+};
+
+// A wave's results on their way out.  Where the wave has one block, a lane's P positions are 16 P bytes, of which it may have 8, and stores of them would touch
+// every line 2 P times (P = 4, forwards: 155 us where whole lines take 80): they go through LDS, in 16 bytes a position, and out by 64 positions an instruction.
+// Position P at + j lies at P at + (j + at / (16 / P)) % P, so that neither way lanes are in each other's banks more than twice.
+template <typename T, bool ROWS, int P, bool PAST>
+struct RecOut {
+    typedef RecLanes<T, ROWS> L;
+    typedef typename RecFour<T>::type Four;
+    static constexpr int SLOTS = ROWS ? 1 : L::LANES * P;
+    seq_u32x4 *lds;  // of the wave
+    RecTensor<T> to;
+    __device__ __forceinline__ void put(long long w0, int j, bool ok, int lane, const Four &b) const
+    {
+        const int at = L::at(lane);
+        if constexpr (ROWS) {
+            if (ok) to.template store<PAST>(w0 + j, to.lane, b);
+        } else {
+            const int slot = P * at + (j + at / (16 / P)) % P;
+            *reinterpret_cast<Four *>(reinterpret_cast<T *>(lds + slot) + L::unit(lane) * kRecE) = b;
+        }
+    }
+    // ends: behind the last position that there is
+    __device__ __forceinline__ void out(long long w0, long long ends, int lane) const
+    {
+        if constexpr (!ROWS) {
+            const int at = lane / P, j = (lane % P + P - at / (16 / P) % P) % P, p = P * at + j;
+            const unsigned distance = (unsigned)p * (unsigned)to.pitch;
+#pragma unroll
+            for (int q = 0; q < SLOTS / 64; ++q)
+                if (w0 + 64 * q + p < ends) to.template store<PAST>(w0 + 64 * q, distance, lds[64 * q + lane]);
+        }
     }
 };
 

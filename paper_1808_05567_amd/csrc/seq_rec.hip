@@ -7,7 +7,8 @@ namespace convmi {
 namespace {
 
 // A workgroup takes a wave's channels of one sequence through all of its positions, waves * LANES * P of them at a time.
-template <typename T, bool ROWS, int P, bool PAST>
+// GATE: there is a z.
+template <typename T, bool ROWS, int P, bool GATE, bool PAST>
 __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const SeqRecArgs a)
 {
     typedef RecLanes<T, ROWS> L;
@@ -15,13 +16,16 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     constexpr int E = kRecE;
     __shared__ __align__(16) float runs[2][kSeqRecWaves][L::COLS][2];
     __shared__ __align__(16) float begin[kSeqRecWaves][L::COLS];
+    typedef RecOut<T, ROWS, P, PAST> Out;
+    __shared__ seq_u32x4 results[kSeqRecWaves][Out::SLOTS];
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
     const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
     const int c = live ? c0 + unit * E : c0;
     const int len = seq_length(a.lengths, n, a.L);
     const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
-    const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), y = tensor(a.y, a.vy);
+    const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz);
+    const Out y = {results[wave], tensor(a.y, a.vy)};
     const int slot = a.slots ? a.slots[n] : n;
     const bool has_slot = slot >= 0 && slot < a.n_slots;
     const RecParams par(a, c);
@@ -41,7 +45,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
                 bx[j] = x.load(w0 + j);
                 bf[j] = f.load(w0 + j);
                 bi[j] = i.load(w0 + j);
-                if (a.z) bz[j] = z.load(w0 + j);
+                if (GATE) bz[j] = z.load(w0 + j);
             }
         }
         float A[E], H[E], pa[P][E], ph[P][E];
@@ -85,10 +89,13 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
 #pragma unroll
             for (int k = 0; k < E; ++k) {
                 h[k] = fmaf(pa[j][k], h[k], ph[j][k]);
-                o[k] = a.z ? h[k] * fz[k] * seq_sigmoid(fz[k]) : h[k];
+                o[k] = GATE ? h[k] * fz[k] * seq_sigmoid(fz[k]) : h[k];
             }
-            if (live && l0 + j < a.L) y.template store<PAST>(w0 + j, l0 + j < len ? RecFour<T>::pack(o) : Four{});
+            y.put(w0, j, live && l0 + j < a.L, lane, l0 + j < len ? RecFour<T>::pack(o) : Four{});
         }
+        seq_wave_sync();
+        y.out(w0, a.L, lane);
+        seq_wave_sync();
     }
     if (a.state_out && kept && threadIdx.x < L::COLS) a.state_out[(long long)slot * a.Cp + c0 + col] = state;
 }
@@ -126,16 +133,21 @@ __global__ __launch_bounds__(64) void seq_rec_step_kernel(const SeqRecArgs a)
     *reinterpret_cast<seq_f32x4 *>(to) = seq_f32x4{h[0], h[1], h[2], h[3]};
 }
 
-template <typename T, bool ROWS>
-hipError_t launch_rows(const SeqRecArgs &a, hipStream_t s)
+template <typename T, bool ROWS, bool GATE>
+hipError_t launch_gate(const SeqRecArgs &a, hipStream_t s)
 {
     constexpr int P = seq_rec_positions(ROWS);
     const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.past)
-        seq_rec_fwd_kernel<T, ROWS, P, true><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, GATE, true><<<grid, 64 * a.waves, 0, s>>>(a);
     else
-        seq_rec_fwd_kernel<T, ROWS, P, false><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, GATE, false><<<grid, 64 * a.waves, 0, s>>>(a);
     return hipGetLastError();
+}
+template <typename T, bool ROWS>
+hipError_t launch_rows(const SeqRecArgs &a, hipStream_t s)
+{
+    return a.z ? launch_gate<T, ROWS, true>(a, s) : launch_gate<T, ROWS, false>(a, s);
 }
 template <typename T>
 hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)

@@ -10,7 +10,7 @@ namespace {
 
 // A workgroup takes a wave's channels of one sequence through all of its positions, as forwards: first from the front for the states before each round of
 // its waves, where there are several, then from the back.
-template <typename T, bool ROWS, int P, int WAVES>
+template <typename T, bool ROWS, int P, bool GATE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArgs a)
 {
     typedef RecLanes<T, ROWS> L;
@@ -18,6 +18,8 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
     constexpr int E = kRecE;
     __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, backwards, B
     __shared__ __align__(16) float begin[2][WAVES][L::COLS];
+    typedef RecOut<T, ROWS, P, false> Out;
+    __shared__ seq_u32x4 results[WAVES][4][Out::SLOTS];
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
     const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
@@ -25,12 +27,13 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
     const int len = seq_length(a.lengths, n, a.L);
     const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
     const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
-    const RecTensor<T> dx = tensor(a.dx, a.vdx), df = tensor(a.df, a.vdf), di = tensor(a.di, a.vdi), dz = tensor(a.dz, a.vdz);
+    const Out dx = {results[wave][0], tensor(a.dx, a.vdx)}, df = {results[wave][1], tensor(a.df, a.vdf)}, di = {results[wave][2], tensor(a.di, a.vdi)},
+              dz = {results[wave][3], tensor(a.dz, a.vdz)};
     const RecParams par(a, c);
     // between waves each lane has one channel
     const int col = lane % L::COLS;
     const bool kept = c0 + col < a.Cp;
-    float *marks = a.marks + (long long)n * a.rounds * a.Cp + c0 + col;
+    float *marks = a.marks + (long long)n * a.rounds * a.Cp + (kept ? c0 + col : 0);
     const int each = waves * L::LANES * P;
     int turn = 0;
     float state = 0;
@@ -73,7 +76,7 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
     float sums[3][E] = {};
     for (int round = a.rounds - 1; round >= 0; --round, turn ^= 1) {
         // (the lanes of each wave that a mark comes from, or the first one's, which has passed a barrier since it stored it)
-        if (round < a.rounds - 1) state = kept ? marks[(long long)round * a.Cp] : 0.0f;
+        if (round < a.rounds - 1) state = marks[(long long)round * a.Cp];
         const long long w0 = (long long)round * each + wave * L::LANES * P, l0 = w0 + at * P;
         Four bx[P], bf[P], bi[P], bz[P], bdy[P];
 #pragma unroll
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
                 bf[j] = f.load(w0 + j);
                 bi[j] = i.load(w0 + j);
                 bdy[j] = dy.load(w0 + j);
-                if (a.z) bz[j] = z.load(w0 + j);
+                if (GATE) bz[j] = z.load(w0 + j);
             }
         }
         float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
@@ -102,7 +105,7 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
                 const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
                 pa[j][k] = l0 + j < len ? p : 1.0f;
                 ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
-                if (a.z) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
+                if (GATE) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
                 H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
@@ -168,7 +171,7 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
                 const float inv = rest >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(rest) : 0.0f, root = rest * inv;
                 const float dh = up[j][k] + d[k], dhg = dh * g, gx = g * fx[k];
                 const float dt = dh * pa[j][k] * fmaf(-gx * pa[j][k], inv, ph[j][k]);
-                if (a.z) {
+                if (GATE) {
                     const float p = seq_sigmoid(fz[k]);
                     fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root * gx) * p * fmaf(fz[k], 1.0f - p, 1.0f);
                 }
@@ -182,12 +185,18 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
                     sums[2][k] += fi[k];
                 }
             }
-            if (!live || l0 + j >= a.L) continue;
-            dx.template store<false>(w0 + j, inside ? RecFour<T>::pack(fx) : Four{});
-            df.template store<false>(w0 + j, inside ? RecFour<T>::pack(ff) : Four{});
-            di.template store<false>(w0 + j, inside ? RecFour<T>::pack(fi) : Four{});
-            if (a.z) dz.template store<false>(w0 + j, inside ? RecFour<T>::pack(fz) : Four{});
+            const bool ok = live && l0 + j < a.L;
+            dx.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fx) : Four{});
+            df.put(w0, j, ok, lane, inside ? RecFour<T>::pack(ff) : Four{});
+            di.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fi) : Four{});
+            if (GATE) dz.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fz) : Four{});
         }
+        seq_wave_sync();
+        dx.out(w0, a.L, lane);
+        df.out(w0, a.L, lane);
+        di.out(w0, a.L, lane);
+        if (GATE) dz.out(w0, a.L, lane);
+        seq_wave_sync();
     }
     // the sums of a sequence: over the lanes that have a channel, then over the waves in order
     __syncthreads();
@@ -223,7 +232,10 @@ template <typename T, bool ROWS>
 void launch_rows(const SeqRecArgs &a, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
-    seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+    if (a.z)
+        seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, true, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+    else
+        seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, false, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
 }
 template <typename T>
 hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)
