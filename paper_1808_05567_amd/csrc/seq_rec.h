@@ -97,17 +97,17 @@ struct RecTensor {
 // A wave's results on their way out.  Where the wave has one block, a lane's P positions are 16 P bytes, of which it may have 8, and stores of them would touch
 // every line 2 P times (P = 4, forwards: 155 us where whole lines take 80): they go through LDS, in 16 bytes a position, and out by 64 positions an instruction.
 // Position P at + j lies at P at + (j + at / (16 / P)) % P, so that neither way lanes are in each other's banks more than twice.
-template <typename T, bool ROWS, int P, bool PAST>
+template <typename T, bool ROWS, int P, bool PAST, bool STAGE = !ROWS>
 struct RecOut {
     typedef RecLanes<T, ROWS> L;
     typedef typename RecFour<T>::type Four;
-    static constexpr int SLOTS = ROWS ? 1 : L::LANES * P;
+    static constexpr int SLOTS = STAGE ? L::LANES * P : 1;
     seq_u32x4 *lds;  // of the wave
     RecTensor<T> to;
     __device__ __forceinline__ void put(long long w0, int j, bool ok, int lane, const Four &b) const
     {
         const int at = L::at(lane);
-        if constexpr (ROWS) {
+        if constexpr (!STAGE) {
             if (ok) to.template store<PAST>(w0 + j, to.lane, b);
         } else {
             const int slot = P * at + (j + at / (16 / P)) % P;
@@ -117,7 +117,7 @@ struct RecOut {
     // ends: behind the last position that there is
     __device__ __forceinline__ void out(long long w0, long long ends, int lane) const
     {
-        if constexpr (!ROWS) {
+        if constexpr (STAGE) {
             const int at = lane / P, j = (lane % P + P - at / (16 / P) % P) % P, p = P * at + j;
             const unsigned distance = (unsigned)p * (unsigned)to.pitch;
 #pragma unroll

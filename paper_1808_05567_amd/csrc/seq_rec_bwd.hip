@@ -8,18 +8,21 @@
 namespace convmi {
 namespace {
 
-// A workgroup takes a wave's channels of one sequence through all of its positions, as forwards: first from the front for the states before each round of
-// its waves, where there are several, then from the back.
+// A workgroup takes a wave's channels of one sequence through all of its positions: where they are more than its waves have at a time, first from the back for what
+// reaches the last position of each round from behind it (which takes f, dy and z; the states before the rounds would take x, f and i and half as much again), then from
+// the front.
 template <typename T, bool ROWS, int P, bool GATE, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArgs a)
+__global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRecArgs a)
 {
     typedef RecLanes<T, ROWS> L;
     typedef typename RecFour<T>::type Four;
     constexpr int E = kRecE;
-    __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, backwards, B
+    __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, from the back, B
     __shared__ __align__(16) float begin[2][WAVES][L::COLS];
-    typedef RecOut<T, ROWS, P, false> Out;
-    __shared__ seq_u32x4 results[WAVES][4][Out::SLOTS];
+    // of each lane, from the gates to the gradients: s, g, k and sigmoid(z), in LDS rather than computed again (20 operations of some 110) or in registers, of which four waves
+    // a SIMD have 128
+    __shared__ seq_f32x4 kept[WAVES][GATE ? 4 : 3][P][64];
+    typedef RecOut<T, ROWS, P, false, false> Out;
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
     const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
@@ -27,94 +30,122 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
     const int len = seq_length(a.lengths, n, a.L);
     const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
     const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
-    const Out dx = {results[wave][0], tensor(a.dx, a.vdx)}, df = {results[wave][1], tensor(a.df, a.vdf)}, di = {results[wave][2], tensor(a.di, a.vdi)},
-              dz = {results[wave][3], tensor(a.dz, a.vdz)};
+    const Out dx = {nullptr, tensor(a.dx, a.vdx)}, df = {nullptr, tensor(a.df, a.vdf)}, di = {nullptr, tensor(a.di, a.vdi)}, dz = {nullptr, tensor(a.dz, a.vdz)};
     const RecParams par(a, c);
     // between waves each lane has one channel
     const int col = lane % L::COLS;
-    const bool kept = c0 + col < a.Cp;
-    float *marks = a.marks + (long long)n * a.rounds * a.Cp + (kept ? c0 + col : 0);
+    const bool mine = c0 + col < a.Cp;
+    float *marks = a.marks + (long long)n * a.rounds * a.Cp + (mine ? c0 + col : 0);
     const int each = waves * L::LANES * P;
-    int turn = 0;
-    float state = 0;
-    for (int round = 0; round < a.rounds - 1; ++round, turn ^= 1) {
-        if (kept && threadIdx.x < L::COLS) marks[(long long)round * a.Cp] = state;
-        const long long w0 = (long long)round * each + wave * L::LANES * P, l0 = w0 + at * P;
-        Four bx[P], bf[P], bi[P];
+    // What is behind a sequence's end is loaded as zeros: nothing comes from there.
+    const auto load = [&](const RecTensor<T> &t, long long w0, Four (&b)[P]) {
+        const long long l0 = w0 + at * P;
+        if (w0 + L::LANES * P <= len) {
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            bx[j] = bf[j] = bi[j] = Four{};
-            if (l0 + j < len) {
-                bx[j] = x.load(w0 + j);
-                bf[j] = f.load(w0 + j);
-                bi[j] = i.load(w0 + j);
+            for (int j = 0; j < P; ++j) b[j] = t.load(w0 + j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                b[j] = Four{};
+                if (l0 + j < len) b[j] = t.load(w0 + j);
             }
         }
-        float A[E], H[E];
+    };
+    const long long first = wave * L::LANES * P;
+    int turn = 0;
+    float back = 0;  // a dh of the position behind a round
+    // (what the next round needs is asked for when this one's has come)
+    Four bx[P], bf[P], bi[P], bz[P], bdy[P];
+    const auto load_back = [&](int round) {
+        const long long w0 = (long long)round * each + first;
+        load(f, w0, bf);
+        load(dy, w0, bdy);
+        if constexpr (GATE) load(z, w0, bz);
+    };
+    if (a.rounds > 1) load_back(a.rounds - 1);
+    for (int round = a.rounds - 1; round > 0; --round, turn ^= 1) {
+        float A[E], B[E];
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            float fx[E], ff[E], fi[E];
-            rec_unpack(bx[j], fx);
+        for (int j = P - 1; j >= 0; --j) {
+            float ff[E], fz[E], up[E];
             rec_unpack(bf[j], ff);
-            rec_unpack(bi[j], fi);
+            rec_unpack(bdy[j], up);
+            if constexpr (GATE) rec_unpack(bz[j], fz);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), e = seq_exp2(t), p = l0 + j < len ? e : 1.0f;
-                const float u = __builtin_amdgcn_sqrtf(rec_rest(t, e)) * rec_gate(fi[k], par.i[k]) * fx[k];
-                H[k] = j == 0 ? u : fmaf(p, H[k], u);
-                A[k] = j == 0 ? p : A[k] * p;
+                const float p = seq_exp2(par.A[k] * rec_gate(ff[k], par.f[k]));
+                if constexpr (GATE) up[k] *= fz[k] * seq_sigmoid(fz[k]);
+                B[k] = p * (j == P - 1 ? up[k] : up[k] + B[k]);
+                A[k] = j == P - 1 ? p : A[k] * p;
             }
         }
-        rec_join<T, ROWS, false>(A, H, lane);
-        if (at == L::LANES - 1)
+        if (round > 1) load_back(round - 1);
+        rec_join<T, ROWS, true>(A, B, lane);
+        if (at == 0)
 #pragma unroll
-            for (int k = 0; k < E; ++k) *reinterpret_cast<seq_f32x2 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x2{A[k], H[k]};
+            for (int k = 0; k < E; ++k) *reinterpret_cast<seq_f32x2 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x2{A[k], B[k]};
         __syncthreads();
-        for (int w = 0; w < waves; ++w) state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
+        for (int w = waves - 1; w >= 0; --w) back = fmaf(runs[turn][w][col][0], back, runs[turn][w][col][1]);
+        if (mine && threadIdx.x < L::COLS) marks[(long long)(round - 1) * a.Cp] = back;
     }
-    float back = 0;  // a dh of the position behind a round
+    if (a.rounds > 1) __syncthreads();  // (the marks are there for all waves)
+    float state = 0;
     float sums[3][E] = {};
-    for (int round = a.rounds - 1; round >= 0; --round, turn ^= 1) {
-        // (the lanes of each wave that a mark comes from, or the first one's, which has passed a barrier since it stored it)
-        if (round < a.rounds - 1) state = marks[(long long)round * a.Cp];
-        const long long w0 = (long long)round * each + wave * L::LANES * P, l0 = w0 + at * P;
-        Four bx[P], bf[P], bi[P], bz[P], bdy[P];
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-            bx[j] = bf[j] = bi[j] = bz[j] = bdy[j] = Four{};
-            if (l0 + j < len) {
-                bx[j] = x.load(w0 + j);
-                bf[j] = f.load(w0 + j);
-                bi[j] = i.load(w0 + j);
-                bdy[j] = dy.load(w0 + j);
-                if (GATE) bz[j] = z.load(w0 + j);
-            }
-        }
+    const auto load_all = [&](int round) {
+        const long long w0 = (long long)round * each + first;
+        load(f, w0, bf);
+        load(i, w0, bi);
+        load(x, w0, bx);
+        load(dy, w0, bdy);
+        if constexpr (GATE) load(z, w0, bz);
+    };
+    load_all(0);
+    for (int round = 0; round < a.rounds; ++round, turn ^= 1) {
+        back = round < a.rounds - 1 ? marks[(long long)round * a.Cp] : 0.0f;
+        const long long w0 = (long long)round * each + first, l0 = w0 + at * P;
+        Four kx[P], kz[P], kdy[P];
         float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
         float A[E], H[E], Ab[E], B[E];
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            float fx[E], ff[E], fi[E], fz[E];
+            float fx[E], ff[E], fi[E], fz[E], root[E];
             rec_unpack(bx[j], fx);
             rec_unpack(bf[j], ff);
             rec_unpack(bi[j], fi);
-            rec_unpack(bz[j], fz);
             rec_unpack(bdy[j], up[j]);
+            if constexpr (GATE) rec_unpack(bz[j], fz);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
-                pa[j][k] = l0 + j < len ? p : 1.0f;
-                ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
-                if (GATE) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
+                ff[k] = rec_gate(ff[k], par.f[k]);
+                fi[k] = rec_gate(fi[k], par.i[k]);
+                const float t = par.A[k] * ff[k];
+                pa[j][k] = seq_exp2(t);
+                root[k] = __builtin_amdgcn_sqrtf(rec_rest(t, pa[j][k]));
+                ph[j][k] = root[k] * fi[k] * fx[k];
+                if constexpr (GATE) {
+                    const float p = seq_sigmoid(fz[k]);
+                    up[j][k] *= fz[k] * p;
+                    fz[k] = p;
+                }
                 H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
+            kept[wave][0][j][lane] = seq_f32x4{ff[0], ff[1], ff[2], ff[3]};
+            kept[wave][1][j][lane] = seq_f32x4{fi[0], fi[1], fi[2], fi[3]};
+            kept[wave][2][j][lane] = seq_f32x4{root[0], root[1], root[2], root[3]};
+            if constexpr (GATE) kept[wave][3][j][lane] = seq_f32x4{fz[0], fz[1], fz[2], fz[3]};
         }
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            B[k] = 0;
+        for (int j = 0; j < P; ++j) {
+            kx[j] = bx[j];
+            kz[j] = bz[j];
+            kdy[j] = bdy[j];
+        }
+        if (round < a.rounds - 1) load_all(round + 1);
 #pragma unroll
-            for (int j = P - 1; j >= 0; --j) B[k] = pa[j][k] * (up[j][k] + B[k]);
+        for (int k = 0; k < E; ++k) {
+#pragma unroll
+            for (int j = P - 1; j >= 0; --j) B[k] = pa[j][k] * (j == P - 1 ? up[j][k] : up[j][k] + B[k]);
             Ab[k] = A[k];
         }
         rec_join<T, ROWS, false>(A, H, lane);
@@ -126,15 +157,14 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
 #pragma unroll
             for (int k = 0; k < E; ++k) runs[turn][wave][unit * E + k][2] = B[k];
         __syncthreads();
-        float before = 0, behind = 0;
-        for (int w = 0; w < wave; ++w) state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
-        before = state;
-        for (int w = waves - 1; w >= 0; --w) {
-            if (w == wave) behind = back;
-            back = fmaf(runs[turn][w][col][0], back, runs[turn][w][col][2]);
+        float before = 0;
+        for (int w = 0; w < waves; ++w) {
+            if (w == wave) before = state;
+            state = fmaf(runs[turn][w][col][0], state, runs[turn][w][col][1]);
         }
+        for (int w = waves - 1; w > wave; --w) back = fmaf(runs[turn][w][col][0], back, runs[turn][w][col][2]);
         begin[0][wave][col] = before;  // (the lanes that have a channel twice write the same)
-        begin[1][wave][col] = behind;
+        begin[1][wave][col] = back;
         seq_wave_sync();
         float h[E], d[E];
         rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[0][wave][unit * E]), h);
@@ -152,51 +182,39 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
         }
 #pragma unroll
         for (int j = P - 1; j >= 0; --j) {
-            float fx[E], ff[E], fi[E], fz[E], fdy[E];
-            rec_again(bx[j]);
-            rec_again(bf[j]);
-            rec_again(bi[j]);
-            rec_again(bz[j]);
-            rec_again(bdy[j]);
-            rec_unpack(bx[j], fx);
-            rec_unpack(bf[j], ff);
-            rec_unpack(bi[j], fi);
-            rec_unpack(bz[j], fz);
-            rec_unpack(bdy[j], fdy);
+            float fx[E], ff[E], fi[E], fz[E], fdy[E], s[E], g[E], root[E], p[E];
+            rec_unpack(kx[j], fx);
+            rec_unpack(kept[wave][0][j][lane], s);
+            rec_unpack(kept[wave][1][j][lane], g);
+            rec_unpack(kept[wave][2][j][lane], root);
+            if constexpr (GATE) {
+                rec_unpack(kz[j], fz);
+                rec_unpack(kdy[j], fdy);
+                rec_unpack(kept[wave][3][j][lane], p);
+            }
             const bool inside = l0 + j < len;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float s = rec_gate(ff[k], par.f[k]), g = rec_gate(fi[k], par.i[k]), t = par.A[k] * s, rest = rec_rest(t, pa[j][k]);
-                // (what is too small for a normal number is none: the hardware's root takes it for zero)
-                const float inv = rest >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(rest) : 0.0f, root = rest * inv;
-                const float dh = up[j][k] + d[k], dhg = dh * g, gx = g * fx[k];
-                const float dt = dh * pa[j][k] * fmaf(-gx * pa[j][k], inv, ph[j][k]);
-                if (GATE) {
-                    const float p = seq_sigmoid(fz[k]);
-                    fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root * gx) * p * fmaf(fz[k], 1.0f - p, 1.0f);
-                }
-                fi[k] = dhg * root * fx[k] * (1.0f - g);
-                fx[k] = dhg * root;
-                ff[k] = dt * (t * kLn2) * (1.0f - s);
-                d[k] = pa[j][k] * dh;
-                if (inside) {
-                    sums[0][k] = fmaf(dt, s, sums[0][k]);
-                    sums[1][k] += ff[k];
-                    sums[2][k] += fi[k];
-                }
+                const float dh = up[j][k] + d[k], dhk = dh * root[k], gx = g[k] * fx[k], back = pa[j][k] * dh;
+                // (a pays for what k lets in; k of zero lets nothing in)
+                const float inv = root[k] > 0 ? __builtin_amdgcn_rcpf(root[k]) : 0.0f;
+                const float dt = back * fmaf(-gx * pa[j][k], inv, ph[j][k]);
+                if constexpr (GATE) fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root[k] * gx) * p[k] * fmaf(fz[k], 1.0f - p[k], 1.0f);
+                fi[k] = dhk * gx * (1.0f - g[k]);
+                fx[k] = dhk * g[k];
+                const float dts = dt * s[k];
+                ff[k] = dts * (par.A[k] * kLn2) * (1.0f - s[k]);
+                d[k] = back;
+                sums[0][k] += dts;
+                sums[1][k] += ff[k];
+                sums[2][k] += fi[k];
             }
             const bool ok = live && l0 + j < a.L;
             dx.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fx) : Four{});
             df.put(w0, j, ok, lane, inside ? RecFour<T>::pack(ff) : Four{});
             di.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fi) : Four{});
-            if (GATE) dz.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fz) : Four{});
+            if constexpr (GATE) dz.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fz) : Four{});
         }
-        seq_wave_sync();
-        dx.out(w0, a.L, lane);
-        df.out(w0, a.L, lane);
-        di.out(w0, a.L, lane);
-        if (GATE) dz.out(w0, a.L, lane);
-        seq_wave_sync();
     }
     // the sums of a sequence: over the lanes that have a channel, then over the waves in order
     __syncthreads();
@@ -210,7 +228,7 @@ __global__ __launch_bounds__(64 * WAVES) void seq_rec_bwd_kernel(const SeqRecArg
             if (at == 0) runs[0][wave][unit * E + k][q] = s;
         }
     __syncthreads();
-    if (threadIdx.x < L::COLS && kept)
+    if (threadIdx.x < L::COLS && mine)
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             float s = 0;
