@@ -21,8 +21,12 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     __shared__ __align__(16) float begin[2][WAVES][L::COLS];
     // of each lane, from the gates to the gradients: s, g, k and sigmoid(z), in LDS rather than computed again (20 operations of some 110) or in registers, of which four waves
     // a SIMD have 128
-    __shared__ seq_f32x4 kept[WAVES][GATE ? 4 : 3][P][64];
-    typedef RecOut<T, ROWS, P, false, false> Out;
+    constexpr int KEPT = GATE ? 4 : 3;
+    __shared__ seq_u32x4 kept[WAVES][KEPT][P * 64];
+    typedef RecOut<T, ROWS, P, false> Out;
+    // (the results go out through the place of the last position's, or of the same lane's, which have been read by then)
+    static_assert(ROWS || Out::SLOTS == 64 * P || (Out::SLOTS <= 64 && P > 1), "results in the place of what was kept");
+    constexpr int RESULTS = ROWS || Out::SLOTS == 64 * P ? 0 : 64 * (P - 1);
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
     const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
@@ -30,7 +34,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     const int len = seq_length(a.lengths, n, a.L);
     const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
     const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
-    const Out dx = {nullptr, tensor(a.dx, a.vdx)}, df = {nullptr, tensor(a.df, a.vdf)}, di = {nullptr, tensor(a.di, a.vdi)}, dz = {nullptr, tensor(a.dz, a.vdz)};
+    const Out dx = {kept[wave][0] + RESULTS, tensor(a.dx, a.vdx)}, df = {kept[wave][1] + RESULTS, tensor(a.df, a.vdf)},
+              di = {kept[wave][2] + RESULTS, tensor(a.di, a.vdi)}, dz = {kept[wave][KEPT - 1] + RESULTS, tensor(a.dz, a.vdz)};
     const RecParams par(a, c);
     // between waves each lane has one channel
     const int col = lane % L::COLS;
@@ -130,10 +135,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
                 H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
-            kept[wave][0][j][lane] = seq_f32x4{ff[0], ff[1], ff[2], ff[3]};
-            kept[wave][1][j][lane] = seq_f32x4{fi[0], fi[1], fi[2], fi[3]};
-            kept[wave][2][j][lane] = seq_f32x4{root[0], root[1], root[2], root[3]};
-            if constexpr (GATE) kept[wave][3][j][lane] = seq_f32x4{fz[0], fz[1], fz[2], fz[3]};
+            kept[wave][0][j * 64 + lane] = SeqElem<float>::pack(ff);
+            kept[wave][1][j * 64 + lane] = SeqElem<float>::pack(fi);
+            kept[wave][2][j * 64 + lane] = SeqElem<float>::pack(root);
+            if constexpr (GATE) kept[wave][3][j * 64 + lane] = SeqElem<float>::pack(fz);
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) {
@@ -184,14 +189,15 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         for (int j = P - 1; j >= 0; --j) {
             float fx[E], ff[E], fi[E], fz[E], fdy[E], s[E], g[E], root[E], p[E];
             rec_unpack(kx[j], fx);
-            rec_unpack(kept[wave][0][j][lane], s);
-            rec_unpack(kept[wave][1][j][lane], g);
-            rec_unpack(kept[wave][2][j][lane], root);
+            SeqElem<float>::unpack(kept[wave][0][j * 64 + lane], s);
+            SeqElem<float>::unpack(kept[wave][1][j * 64 + lane], g);
+            SeqElem<float>::unpack(kept[wave][2][j * 64 + lane], root);
             if constexpr (GATE) {
                 rec_unpack(kz[j], fz);
                 rec_unpack(kdy[j], fdy);
-                rec_unpack(kept[wave][3][j][lane], p);
+                SeqElem<float>::unpack(kept[wave][3][j * 64 + lane], p);
             }
+            seq_wave_sync();
             const bool inside = l0 + j < len;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
@@ -215,6 +221,12 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             di.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fi) : Four{});
             if constexpr (GATE) dz.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fz) : Four{});
         }
+        seq_wave_sync();
+        dx.out(w0, a.L, lane);
+        df.out(w0, a.L, lane);
+        di.out(w0, a.L, lane);
+        if constexpr (GATE) dz.out(w0, a.L, lane);
+        seq_wave_sync();
     }
     // the sums of a sequence: over the lanes that have a channel, then over the waves in order
     __syncthreads();
