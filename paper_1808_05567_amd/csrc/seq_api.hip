@@ -402,15 +402,16 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
     for (const auto &w : views)
         if (w.to.l > kMaxWaveStride || (a.rows && w.to.c > kMaxTileStride)) return finish(p, CONV_EUNSUPPORTED, out);
     a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
-    // Waves of a workgroup: as many as find positions.  Forwards up to 8 where workgroups are four or more a compute unit (8 x 2048 x 2048 bf16: 73 us, with 4 of them 77,
+    // Waves of a workgroup: as many as find positions.  Forwards up to 8 where workgroups are two or more a compute unit (8 x 2048 x 2048 bf16: 73 us, with 4 of them 77,
     // with 16 95), else up to 16 (1 x 8192 x 2048: 46 and 51); backwards 4, whose registers and LDS are three workgroups' a compute unit (2: 227 us, 4: 177).
     const int64_t columns = a.N * seq_rec_groups(a.Cp, a.rows, v);
+    a.few = columns < 512;
     const auto waves = [&](int each, int most) {
         int w = 1;
         while (w < most && (int64_t)w * each < a.L) w *= 2;
         return w;
     };
-    a.waves = waves(seq_rec_lanes(a.rows, v) * seq_rec_positions(a.rows), columns >= 1024 ? kSeqRecWaves / 2 : kSeqRecWaves);
+    a.waves = waves(seq_rec_lanes(a.rows, v) * seq_rec_positions(a.rows), a.few ? kSeqRecWaves : kSeqRecWaves / 2);
     p->rec_bwd = a;
     SeqRecArgs &b = p->rec_bwd;
     const int each = seq_rec_lanes(a.rows, v) * kSeqRecBwdPositions;

@@ -66,6 +66,7 @@ struct SeqRecArgs {
     int N, Cb, Cp, L, n_slots;
     int past;                // results go past the caches
     int rows;                // a position's blocks follow one another
+    int few;                 // workgroups: fewer than two a compute unit
     int waves;               // of a workgroup
     int rounds;              // backwards: times that a workgroup has all of its waves' positions
     float *marks;  // [N][rounds][Cp]: states before them
@@ -154,9 +155,9 @@ inline int64_t seq_scan_waves(const SeqScanArgs &a, bool sums) { return (int64_t
 inline int64_t seq_join_groups(const SeqScanArgs &a) { return a.N * (((int64_t)a.S * a.Cp + 63) / 64); }
 inline int seq_join_waves(int chunks) { return chunks <= 16 * kSeqJoinWaves ? (chunks + 15) / 16 : kSeqJoinWaves; }
 
-// The recurrence's waves have one block of channels where a block's positions follow one another, and 64 channels where a position's blocks do; the lanes
+// The recurrence's waves have one block of channels where a block's positions follow one another, and 128 bytes of them where a position's blocks do; the lanes
 // that have the same four channels take some positions side by side each at a time.
-inline int seq_rec_cols(bool rows, int vlen) { return rows ? 64 : vlen; }
+inline int seq_rec_cols(bool rows, int vlen) { return rows ? 8 * vlen : vlen; }
 inline int64_t seq_rec_groups(int64_t Cp, bool rows, int vlen) { return (Cp + seq_rec_cols(rows, vlen) - 1) / seq_rec_cols(rows, vlen); }
 inline int seq_rec_lanes(bool rows, int vlen) { return 64 / (seq_rec_cols(rows, vlen) / 4); }
 constexpr int seq_rec_positions(bool rows) { return rows ? 4 : 2; }

@@ -12,18 +12,17 @@ namespace {
 
 constexpr int kRecE = 4;  // channels of a lane
 
-// Which channels and positions a lane has.  Where a block's positions follow one another a wave has one block, else 128 bytes (bf16) or 256 of
-// channels side by side, so that a wave's accesses are whole lines in both.
+// Which channels and positions a lane has.  Where a block's positions follow one another a wave has one block, else 128 bytes of channels side by side, so that
+// a wave's accesses are whole lines in both.
 template <typename T, bool ROWS>
 struct RecLanes {
     static constexpr int V = SeqElem<T>::V;
-    static constexpr int UNITS = ROWS ? 16 : V / kRecE;  // fours of channels of a wave
+    static constexpr int UNITS = ROWS ? 2 * V : V / kRecE;  // fours of channels of a wave
     static constexpr int LANES = 64 / UNITS;             // that have the same ones
     static constexpr int COLS = UNITS * kRecE;
-    static __device__ __forceinline__ int unit(int lane) { return ROWS ? lane % 16 : lane / LANES; }
-    static __device__ __forceinline__ int at(int lane) { return ROWS ? lane / 16 : lane % LANES; }
-    static __device__ __forceinline__ int first(int lane) { return ROWS ? lane % 16 : lane / LANES * LANES; }  // of those that have its channels
-    static constexpr int STEP = ROWS ? 16 : 1;  // from one to the next
+    static __device__ __forceinline__ int unit(int lane) { return ROWS ? lane % UNITS : lane / LANES; }
+    static __device__ __forceinline__ int at(int lane) { return ROWS ? lane / UNITS : lane % LANES; }
+    static constexpr int STEP = ROWS ? UNITS : 1;  // from one to the next
 };
 
 // Four channels.

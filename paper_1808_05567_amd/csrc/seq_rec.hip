@@ -7,8 +7,9 @@ namespace convmi {
 namespace {
 
 // A workgroup takes a wave's channels of one sequence through all of its positions, waves * LANES * P of them at a time.
-// GATE: there is a z.
-template <typename T, bool ROWS, int P, bool GATE, bool PAST>
+// GATE: there is a z.  AHEAD: what the next round needs is asked for when this one's has come (where a compute unit has one workgroup: 1 x 8192 x 2048 bf16 45 -> 43 us,
+// ragged rows 26 -> 21; where its registers cost a third workgroup it does not pay: 8 x 2048 x 2048 72 -> 77).
+template <typename T, bool ROWS, int P, bool GATE, bool PAST, bool AHEAD>
 __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const SeqRecArgs a)
 {
     typedef RecLanes<T, ROWS> L;
@@ -35,9 +36,19 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     float state = a.state_in && kept ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
     const int each = waves * L::LANES * P;
     int turn = 0;
-    for (long long base = 0; base < a.L; base += each, turn ^= 1) {
-        const long long w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
-        Four bx[P], bf[P], bi[P], bz[P];
+    Four bx[P], bf[P], bi[P], bz[P], kz[P];
+    const auto load = [&](long long w0) {
+        const long long l0 = w0 + at * P;
+        if (w0 + L::LANES * P <= len) {
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                bf[j] = f.load(w0 + j);
+                bi[j] = i.load(w0 + j);
+                bx[j] = x.load(w0 + j);
+                if (GATE) bz[j] = z.load(w0 + j);
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             bx[j] = bf[j] = bi[j] = bz[j] = Four{};
@@ -48,6 +59,11 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
                 if (GATE) bz[j] = z.load(w0 + j);
             }
         }
+    };
+    if constexpr (AHEAD) load(wave * L::LANES * P);
+    for (long long base = 0; base < a.L; base += each, turn ^= 1) {
+        const long long w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
+        if constexpr (!AHEAD) load(w0);
         float A[E], H[E], pa[P][E], ph[P][E];
 #pragma unroll
         for (int j = 0; j < P; ++j) {
@@ -65,6 +81,9 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }
         }
+#pragma unroll
+        for (int j = 0; j < P; ++j) kz[j] = bz[j];
+        if (AHEAD && base + each < a.L) load(w0 + each);
         rec_join<T, ROWS, false>(A, H, lane);
         if (at == L::LANES - 1)
 #pragma unroll
@@ -85,7 +104,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             float o[E], fz[E];
-            rec_unpack(bz[j], fz);
+            rec_unpack(kz[j], fz);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
                 h[k] = fmaf(pa[j][k], h[k], ph[j][k]);
@@ -133,16 +152,25 @@ __global__ __launch_bounds__(64) void seq_rec_step_kernel(const SeqRecArgs a)
     *reinterpret_cast<seq_f32x4 *>(to) = seq_f32x4{h[0], h[1], h[2], h[3]};
 }
 
-template <typename T, bool ROWS, bool GATE>
-hipError_t launch_gate(const SeqRecArgs &a, hipStream_t s)
+template <typename T, bool ROWS, bool GATE, bool AHEAD>
+hipError_t launch_ahead(const SeqRecArgs &a, hipStream_t s)
 {
     constexpr int P = seq_rec_positions(ROWS);
     const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.past)
-        seq_rec_fwd_kernel<T, ROWS, P, GATE, true><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, GATE, true, AHEAD><<<grid, 64 * a.waves, 0, s>>>(a);
     else
-        seq_rec_fwd_kernel<T, ROWS, P, GATE, false><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_fwd_kernel<T, ROWS, P, GATE, false, AHEAD><<<grid, 64 * a.waves, 0, s>>>(a);
     return hipGetLastError();
+}
+template <typename T, bool ROWS, bool GATE>
+hipError_t launch_gate(const SeqRecArgs &a, hipStream_t s)
+{
+    constexpr bool REGISTERS = sizeof(T) == 2 || !ROWS || !GATE;  // (there are enough of)
+    if constexpr (REGISTERS) {
+        if (a.few) return launch_ahead<T, ROWS, GATE, true>(a, s);
+    }
+    return launch_ahead<T, ROWS, GATE, false>(a, s);
 }
 template <typename T, bool ROWS>
 hipError_t launch_rows(const SeqRecArgs &a, hipStream_t s)

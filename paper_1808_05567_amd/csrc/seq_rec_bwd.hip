@@ -104,11 +104,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         load(dy, w0, bdy);
         if constexpr (GATE) load(z, w0, bz);
     };
-    load_all(0);
+    // (but where registers do not do for it)
+    constexpr bool AHEAD = sizeof(T) == 2 || !ROWS || !GATE;
+    if constexpr (AHEAD) load_all(0);
     for (int round = 0; round < a.rounds; ++round, turn ^= 1) {
         back = round < a.rounds - 1 ? marks[(long long)round * a.Cp] : 0.0f;
         const long long w0 = (long long)round * each + first, l0 = w0 + at * P;
         Four kx[P], kz[P], kdy[P];
+        if constexpr (!AHEAD) load_all(round);
         float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
         float A[E], H[E], Ab[E], B[E];
 #pragma unroll
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             kz[j] = bz[j];
             kdy[j] = bdy[j];
         }
-        if (round < a.rounds - 1) load_all(round + 1);
+        if (AHEAD && round < a.rounds - 1) load_all(round + 1);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
 #pragma unroll
