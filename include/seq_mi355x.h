@@ -165,10 +165,11 @@ typedef struct {
     seq_view_t dy, dx, df, di, dz;
 } seq_rec_desc_t;
 conv_status_t seq_rec_create(const seq_rec_desc_t *desc, seq_handle_t *out);
+/* ws: workspace_bytes of scratch; CONV_EWORKSPACE if ws_bytes is less than the pass needs. */
 conv_status_t seq_rec_fwd(seq_handle_t h, const void *x, const void *f, const void *i,
                           const float *A, const void *z, const float *f_bias, const float *i_bias,
                           const float *state_in, void *y, float *state_out, const int32_t *slots,
-                          const int32_t *lengths, void *stream);
+                          const int32_t *lengths, void *ws, size_t ws_bytes, void *stream);
 /* One new position of each sequence, the state moved on in place: a plan of L = 1 with slots. */
 conv_status_t seq_rec_step(seq_handle_t h, const void *x, const void *f, const void *i,
                            const float *A, const void *z, const float *f_bias, const float *i_bias,

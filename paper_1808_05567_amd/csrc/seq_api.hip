@@ -411,15 +411,32 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
         while (w < most && (int64_t)w * each < a.L) w *= 2;
         return w;
     };
-    a.waves = waves(seq_rec_lanes(a.rows, v) * seq_rec_positions(a.rows), a.few ? kSeqRecWaves : kSeqRecWaves / 2);
+    // Where there are less than `most` workgroups, of `each` positions at a time, they share a sequence in runs, of which another launch finds out first what they make
+    // of a state.
+    const auto runs = [&](SeqRecArgs &q, int64_t each, int64_t most) {
+        const int64_t want = std::min<int64_t>({(most + columns - 1) / columns, (q.L + each - 1) / each, 64});
+        q.run = (int)(std::min<int64_t>(((q.L + want - 1) / want + each - 1) / each * each, 1 << 30));
+        q.runs = (int)((q.L + (int64_t)q.run - 1) / q.run);
+    };
+    const int lanes = seq_rec_lanes(a.rows, v);
+    a.waves = waves(lanes * seq_rec_positions(a.rows), a.few ? kSeqRecWaves : kSeqRecWaves / 2);
+    const int shared = lanes * seq_rec_positions(a.rows) * kSeqRecTotalsWaves;
+    runs(a, a.L, 1);
+    if (columns < 128 && a.L > 2 * shared) {
+        a.waves = kSeqRecTotalsWaves;
+        runs(a, shared, 512);
+    }
     p->rec_bwd = a;
     SeqRecArgs &b = p->rec_bwd;
-    const int each = seq_rec_lanes(a.rows, v) * kSeqRecBwdPositions;
+    const int each = lanes * kSeqRecBwdPositions;
     b.waves = waves(each, kSeqRecBwdWaves);
-    b.rounds = (int)((a.L + (int64_t)b.waves * each - 1) / ((int64_t)b.waves * each));
+    runs(b, b.L, 1);
+    if (columns < 256 && b.L > 2 * each * b.waves) runs(b, each * b.waves, 768);
+    b.rounds = (int)((std::min(b.L, b.run) + (int64_t)b.waves * each - 1) / ((int64_t)b.waves * each));
     p->info.state_bytes = (size_t)a.Cp * 4;
-    p->bwd_ws = up((size_t)a.N * 3 * a.Cp * 4) + (b.rounds > 1 ? up((size_t)a.N * b.rounds * a.Cp * 4) : 0);
-    const bool fits = columns * 64 * std::max(a.waves, b.waves) <= kMaxItems;
+    p->fwd_ws = a.runs > 1 ? up((size_t)a.N * a.runs * 2 * a.Cp * 4) : 0;
+    p->bwd_ws = up((size_t)a.N * b.runs * 3 * a.Cp * 4) * (b.runs > 1 ? 2 : 1) + up((size_t)a.N * b.runs * b.rounds * a.Cp * 4);
+    const bool fits = columns * 64 * std::max(a.runs * a.waves, b.runs * b.waves) <= kMaxItems;
     return finish(p, fits ? CONV_OK : CONV_EUNSUPPORTED, out);
 }
 
@@ -435,11 +452,13 @@ static void rec_inputs(SeqRecArgs &a, const void *x, const void *f, const void *
 }
 
 conv_status_t seq_rec_fwd(seq_handle_t h, const void *x, const void *f, const void *i, const float *A, const void *z, const float *f_bias,
-                          const float *i_bias, const float *state_in, void *y, float *state_out, const int32_t *slots, const int32_t *lengths, void *stream)
+                          const float *i_bias, const float *state_in, void *y, float *state_out, const int32_t *slots, const int32_t *lengths, void *ws,
+                          size_t ws_bytes, void *stream)
 {
-    if (!h || h->kind != kRec || !given(x, f, i, A, y) || !fine(z, f_bias, i_bias, state_in, state_out) || !aligned(slots, 4) || !aligned(lengths, 4) ||
+    if (!h || h->kind != kRec || !given(x, f, i, A, y) || !fine(z, f_bias, i_bias, state_in, state_out, ws) || !aligned(slots, 4) || !aligned(lengths, 4) ||
         ((state_in || state_out) && h->rec.n_slots == 0))
         return CONV_EINVAL;
+    if (h->fwd_ws && (!ws || ws_bytes < h->fwd_ws)) return CONV_EWORKSPACE;
     SeqRecArgs a = h->rec;
     rec_inputs(a, x, f, i, A, z, f_bias, i_bias);
     a.state_in = state_in;
@@ -447,6 +466,7 @@ conv_status_t seq_rec_fwd(seq_handle_t h, const void *x, const void *f, const vo
     a.state_out = state_out;
     a.slots = slots;
     a.lengths = lengths;
+    a.totals = static_cast<float *>(ws);
     return done(launch_seq_rec_fwd(h->dtype, a, (hipStream_t)stream));
 }
 
@@ -481,8 +501,11 @@ conv_status_t seq_rec_bwd(seq_handle_t h, const void *x, const void *f, const vo
     a.df_bias = df_bias;
     a.di_bias = di_bias;
     a.lengths = lengths;
-    a.part = static_cast<float *>(ws);
-    a.marks = reinterpret_cast<float *>(static_cast<char *>(ws) + up((size_t)a.N * 3 * a.Cp * 4));
+    char *at = static_cast<char *>(ws);
+    const size_t part = up((size_t)a.N * a.runs * 3 * a.Cp * 4);
+    a.part = reinterpret_cast<float *>(at);
+    if (a.runs > 1) a.totals = reinterpret_cast<float *>(at += part);
+    a.marks = reinterpret_cast<float *>(at + part);
     return done(launch_seq_rec_bwd(h->dtype, a, (hipStream_t)stream));
 }
 
@@ -749,8 +772,9 @@ conv_status_t seq_describe(seq_handle_t h, char *buf, size_t buflen)
                      h->scan_bwd.chunks, (long long)h->scan_bwd.N * h->scan_bwd.G * h->scan_bwd.btiles * h->scan_bwd.chunks);
             break;
         case kRec:
-            snprintf(buf, buflen, "seq_rec dt=%d rows=%d workgroups=%lld waves=%d bwd: rounds=%d", h->dtype, h->rec.rows,
-                     (long long)(h->rec.N * seq_rec_groups(h->rec.Cp, h->rec.rows, h->info.vlen)), h->rec.waves, h->rec_bwd.rounds);
+            snprintf(buf, buflen, "seq_rec dt=%d rows=%d columns=%lld fwd: runs=%d waves=%d bwd: runs=%d waves=%d rounds=%d", h->dtype, h->rec.rows,
+                     (long long)(h->rec.N * seq_rec_groups(h->rec.Cp, h->rec.rows, h->info.vlen)), h->rec.runs, h->rec.waves, h->rec_bwd.runs, h->rec_bwd.waves,
+                     h->rec_bwd.rounds);
             break;
         case kNorm: snprintf(buf, buflen, "seq_norm dt=%d parts=%d", h->dtype, h->norm.parts); break;
         case kLnorm: snprintf(buf, buflen, "seq_lnorm dt=%d parts=%d", h->dtype, h->norm.parts); break;

@@ -68,9 +68,12 @@ struct SeqRecArgs {
     int rows;                // a position's blocks follow one another
     int few;                 // workgroups: fewer than two a compute unit
     int waves;               // of a workgroup
+    int runs, run;           // runs of positions that workgroups share a sequence in, and their length
     int rounds;              // backwards: times that a workgroup has all of its waves' positions
-    float *marks;  // [N][rounds][Cp]: states before them
-    float *part;   // [N][3][Cp]: sums of dA, df_bias and di_bias over a sequence
+    float *totals;  // where there are several runs, forwards [N][runs][2][Cp]: 0 and the state before the first run, then what runs make of a state; backwards
+                    // [N][runs][3][Cp]: what they make of a state, from the front and from the back
+    float *marks;   // [N][runs][rounds][Cp]: what reaches the last position of each from behind it
+    float *part;    // [N][runs][3][Cp]: sums of dA, df_bias and di_bias over a run
 };
 
 struct SeqNormArgs {
@@ -132,6 +135,7 @@ hipError_t launch_seq_scan_ends(int dtype, const SeqScanArgs &a, hipStream_t s);
 hipError_t launch_seq_scan_bwd(int dtype, const SeqScanArgs &a, hipStream_t s);
 hipError_t launch_seq_rec_fwd(int dtype, const SeqRecArgs &a, hipStream_t s);
 hipError_t launch_seq_rec_step(int dtype, const SeqRecArgs &a, hipStream_t s);
+hipError_t launch_seq_rec_totals(int dtype, bool back, const SeqRecArgs &a, hipStream_t s);
 hipError_t launch_seq_rec_bwd(int dtype, const SeqRecArgs &a, hipStream_t s);
 hipError_t launch_seq_norm_fwd(int dtype, const SeqNormArgs &a, hipStream_t s);
 hipError_t launch_seq_norm_bwd(int dtype, const SeqNormArgs &a, hipStream_t s);
@@ -161,7 +165,7 @@ inline int seq_rec_cols(bool rows, int vlen) { return rows ? 8 * vlen : vlen; }
 inline int64_t seq_rec_groups(int64_t Cp, bool rows, int vlen) { return (Cp + seq_rec_cols(rows, vlen) - 1) / seq_rec_cols(rows, vlen); }
 inline int seq_rec_lanes(bool rows, int vlen) { return 64 / (seq_rec_cols(rows, vlen) / 4); }
 constexpr int seq_rec_positions(bool rows) { return rows ? 4 : 2; }
-constexpr int kSeqRecBwdPositions = 2, kSeqRecWaves = 16, kSeqRecBwdWaves = 4;  // of a lane; of a workgroup at most
+constexpr int kSeqRecBwdPositions = 2, kSeqRecWaves = 16, kSeqRecBwdWaves = 4, kSeqRecTotalsWaves = 8;  // of a lane; of a workgroup at most
 
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;

@@ -76,15 +76,15 @@ struct RecTensor {
     // l: position of the wave's first lane, the same for all lanes.  (An address in scalar registers and a lane's distance are one instruction; the compiler,
     // left alone, adds the distance to `base` once and to that, in vector registers, the rest.)
     template <typename B>
-    __device__ __forceinline__ __attribute__((address_space(1))) B *at(long long l, unsigned distance) const
+    __device__ __forceinline__ __attribute__((address_space(1))) B *at(int l, unsigned distance) const
     {
         auto *p = (__attribute__((address_space(1))) char *)(base + l * pitch);
         asm("" : "+s"(p), "+v"(distance));
         return (__attribute__((address_space(1))) B *)(p + distance);
     }
-    __device__ __forceinline__ Four load(long long l) const { return *at<Four>(l, lane); }
+    __device__ __forceinline__ Four load(int l) const { return *at<Four>(l, lane); }
     template <bool PAST, typename B>
-    __device__ __forceinline__ void store(long long l, unsigned distance, const B &b) const
+    __device__ __forceinline__ void store(int l, unsigned distance, const B &b) const
     {
         if constexpr (PAST)
             __builtin_nontemporal_store(b, at<B>(l, distance));
@@ -103,7 +103,7 @@ struct RecOut {
     static constexpr int SLOTS = ROWS ? 1 : L::LANES * P;
     seq_u32x4 *lds;  // of the wave
     RecTensor<T> to;
-    __device__ __forceinline__ void put(long long w0, int j, bool ok, int lane, const Four &b) const
+    __device__ __forceinline__ void put(int w0, int j, bool ok, int lane, const Four &b) const
     {
         if constexpr (ROWS) {
             if (ok) to.template store<PAST>(w0 + j, to.lane, b);
@@ -111,7 +111,7 @@ struct RecOut {
             *reinterpret_cast<Four *>(reinterpret_cast<T *>(lds + L::LANES * j + L::at(lane)) + L::unit(lane) * kRecE) = b;
     }
     // ends: behind the last position that there is
-    __device__ __forceinline__ void out(long long w0, long long ends, int lane) const
+    __device__ __forceinline__ void out(int w0, int ends, int lane) const
     {
         if constexpr (!ROWS) {
 #pragma unroll

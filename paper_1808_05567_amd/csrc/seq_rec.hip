@@ -6,7 +6,7 @@
 namespace convmi {
 namespace {
 
-// A workgroup takes a wave's channels of one sequence through all of its positions, waves * LANES * P of them at a time.
+// A workgroup takes a wave's channels of one sequence through all of its positions, or of a run of them, waves * LANES * P at a time.
 // GATE: there is a z.  AHEAD: what the next round needs is asked for when this one's has come (where a compute unit has one workgroup: 1 x 8192 x 2048 bf16 45 -> 43 us,
 // ragged rows 26 -> 21; where its registers cost a third workgroup it does not pay: 8 x 2048 x 2048 72 -> 77).
 template <typename T, bool ROWS, int P, bool GATE, bool PAST, bool AHEAD>
@@ -20,7 +20,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     typedef RecOut<T, ROWS, P, PAST> Out;
     __shared__ seq_u32x4 results[kSeqRecWaves][Out::SLOTS];
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
-    const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
+    const int groups = (a.Cp + L::COLS - 1) / L::COLS, run = blockIdx.x / groups % a.runs, n = blockIdx.x / groups / a.runs, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
     const int c = live ? c0 + unit * E : c0;
     const int len = seq_length(a.lengths, n, a.L);
@@ -33,12 +33,20 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     // between waves each lane has one channel
     const int col = lane % L::COLS;
     const bool kept = has_slot && c0 + col < a.Cp;
-    float state = a.state_in && kept ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
+    float state = 0;
+    if (a.runs == 1)
+        state = a.state_in && kept ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
+    else if (c0 + col < a.Cp)
+        for (int r = 0; r <= run; ++r) {
+            const float *t = a.totals + ((long long)n * a.runs + r) * 2 * a.Cp + c0 + col;
+            state = fmaf(t[0], state, t[a.Cp]);
+        }
+    const int from = run * a.run, to = min(a.L, from + a.run);  // (a.L is at most 2^30)
     const int each = waves * L::LANES * P;
     int turn = 0;
     Four bx[P], bf[P], bi[P], bz[P], kz[P];
-    const auto load = [&](long long w0) {
-        const long long l0 = w0 + at * P;
+    const auto load = [&](int w0) {
+        const int l0 = w0 + at * P;
         if (w0 + L::LANES * P <= len) {
 #pragma unroll
             for (int j = 0; j < P; ++j) {
@@ -60,9 +68,9 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
             }
         }
     };
-    if constexpr (AHEAD) load(wave * L::LANES * P);
-    for (long long base = 0; base < a.L; base += each, turn ^= 1) {
-        const long long w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
+    if constexpr (AHEAD) load(from + wave * L::LANES * P);
+    for (int base = from; base < to; base += each, turn ^= 1) {
+        const int w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
         if constexpr (!AHEAD) load(w0);
         float A[E], H[E], pa[P][E], ph[P][E];
 #pragma unroll
@@ -83,7 +91,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) kz[j] = bz[j];
-        if (AHEAD && base + each < a.L) load(w0 + each);
+        if (AHEAD && base + each < to) load(w0 + each);
         rec_join<T, ROWS, false>(A, H, lane);
         if (at == L::LANES - 1)
 #pragma unroll
@@ -116,7 +124,103 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
         y.out(w0, a.L, lane);
         seq_wave_sync();
     }
-    if (a.state_out && kept && threadIdx.x < L::COLS) a.state_out[(long long)slot * a.Cp + c0 + col] = state;
+    if (a.state_out && kept && run == a.runs - 1 && threadIdx.x < L::COLS) a.state_out[(long long)slot * a.Cp + c0 + col] = state;
+}
+
+// What the runs of a sequence make of a state, for those that come after them: forwards of all but the last, and the state before the first.  BACK: of all, from the
+// front and from the back.
+template <typename T, bool ROWS, int P, bool BACK>
+__global__ __launch_bounds__(64 * kSeqRecTotalsWaves) void seq_rec_totals_kernel(const SeqRecArgs a)
+{
+    typedef RecLanes<T, ROWS> L;
+    typedef typename RecFour<T>::type Four;
+    constexpr int E = kRecE;
+    __shared__ __align__(16) float runs[2][kSeqRecTotalsWaves][L::COLS][4];
+    const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
+    const int groups = (a.Cp + L::COLS - 1) / L::COLS, here = BACK ? a.runs : a.runs - 1;
+    const int run = blockIdx.x / groups % here, n = blockIdx.x / groups / here, c0 = blockIdx.x % groups * L::COLS;
+    const int c = c0 + unit * E < a.Cp ? c0 + unit * E : c0;
+    const int len = seq_length(a.lengths, n, a.L);
+    const auto tensor = [&](const void *p, const SeqView &v) { return RecTensor<T>::template of<L, P>(p, v, n, c0, c, at); };
+    const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
+    const RecParams par(a, c);
+    const int col = lane % L::COLS;
+    const bool mine = c0 + col < a.Cp;
+    const int from = run * a.run, to = min(len, from + a.run);
+    const int each = waves * L::LANES * P;
+    float sumA = 1, sumH = 0, sumB = 0;
+    int turn = 0;
+    // (behind a sequence's end nothing changes)
+    for (int base = from; base < to; base += each, turn ^= 1) {
+        const int w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
+        Four bx[P], bf[P], bi[P], bz[P], bdy[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            bx[j] = bf[j] = bi[j] = bz[j] = bdy[j] = Four{};
+            if (l0 + j < len) {
+                bx[j] = x.load(w0 + j);
+                bf[j] = f.load(w0 + j);
+                bi[j] = i.load(w0 + j);
+                if (BACK) bdy[j] = dy.load(w0 + j);
+                if (BACK && a.z) bz[j] = z.load(w0 + j);
+            }
+        }
+        float A[E], H[E], Ab[E], B[E], pa[P][E], up[P][E];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            float fx[E], ff[E], fi[E], fz[E];
+            rec_unpack(bx[j], fx);
+            rec_unpack(bf[j], ff);
+            rec_unpack(bi[j], fi);
+            rec_unpack(bz[j], fz);
+            rec_unpack(bdy[j], up[j]);
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
+                pa[j][k] = l0 + j < len ? p : 1.0f;
+                const float u = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
+                H[k] = j == 0 ? u : fmaf(pa[j][k], H[k], u);
+                A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
+            }
+            if (BACK && a.z)
+#pragma unroll
+                for (int k = 0; k < E; ++k) up[j][k] *= fz[k] * seq_sigmoid(fz[k]);
+        }
+        if constexpr (BACK) {
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+#pragma unroll
+                for (int j = P - 1; j >= 0; --j) B[k] = pa[j][k] * (j == P - 1 ? up[j][k] : up[j][k] + B[k]);
+                Ab[k] = A[k];
+            }
+            rec_join<T, ROWS, true>(Ab, B, lane);
+            if (at == 0)
+#pragma unroll
+                for (int k = 0; k < E; ++k) runs[turn][wave][unit * E + k][2] = B[k];
+        }
+        rec_join<T, ROWS, false>(A, H, lane);
+        if (at == L::LANES - 1)
+#pragma unroll
+            for (int k = 0; k < E; ++k) *reinterpret_cast<seq_f32x2 *>(&runs[turn][wave][unit * E + k][0]) = seq_f32x2{A[k], H[k]};
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) {
+            const float *r = runs[turn][w][col];
+            if (BACK) sumB = fmaf(sumA, r[2], sumB);
+            sumH = fmaf(r[0], sumH, r[1]);
+            sumA *= r[0];
+        }
+    }
+    if (threadIdx.x >= L::COLS || !mine) return;
+    float *t = a.totals + ((long long)n * a.runs + run + (BACK ? 0 : 1)) * (BACK ? 3 : 2) * a.Cp + c0 + col;
+    t[0] = sumA;
+    t[a.Cp] = sumH;
+    if (BACK) t[2 * a.Cp] = sumB;
+    if (!BACK && run == 0) {
+        const int slot = a.slots ? a.slots[n] : n;
+        t -= 2 * a.Cp;
+        t[0] = 0;
+        t[a.Cp] = a.state_in && slot >= 0 && slot < a.n_slots ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
+    }
 }
 
 template <typename T>
@@ -156,7 +260,7 @@ template <typename T, bool ROWS, bool GATE, bool AHEAD>
 hipError_t launch_ahead(const SeqRecArgs &a, hipStream_t s)
 {
     constexpr int P = seq_rec_positions(ROWS);
-    const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    const unsigned grid = (unsigned)(a.N * a.runs * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.past)
         seq_rec_fwd_kernel<T, ROWS, P, GATE, true, AHEAD><<<grid, 64 * a.waves, 0, s>>>(a);
     else
@@ -177,9 +281,28 @@ hipError_t launch_rows(const SeqRecArgs &a, hipStream_t s)
 {
     return a.z ? launch_gate<T, ROWS, true>(a, s) : launch_gate<T, ROWS, false>(a, s);
 }
+template <typename T, bool ROWS>
+hipError_t launch_totals(bool back, const SeqRecArgs &a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(a.N * (a.runs - !back) * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    if (back)
+        seq_rec_totals_kernel<T, ROWS, kSeqRecBwdPositions, true><<<grid, 64 * a.waves, 0, s>>>(a);
+    else
+        seq_rec_totals_kernel<T, ROWS, seq_rec_positions(ROWS), false><<<grid, 64 * a.waves, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_totals_t(bool back, const SeqRecArgs &a, hipStream_t s)
+{
+    return a.rows ? launch_totals<T, true>(back, a, s) : launch_totals<T, false>(back, a, s);
+}
 template <typename T>
 hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)
 {
+    if (a.runs > 1) {
+        const hipError_t e = launch_totals_t<T>(false, a, s);
+        if (e != hipSuccess) return e;
+    }
     return a.rows ? launch_rows<T, true>(a, s) : launch_rows<T, false>(a, s);
 }
 template <typename T>
@@ -191,6 +314,10 @@ hipError_t launch_step(const SeqRecArgs &a, hipStream_t s)
 }  // namespace
 
 hipError_t launch_seq_rec_fwd(int dtype, const SeqRecArgs &a, hipStream_t s) { return dtype == SEQ_BF16 ? launch_t<unsigned short>(a, s) : launch_t<float>(a, s); }
+hipError_t launch_seq_rec_totals(int dtype, bool back, const SeqRecArgs &a, hipStream_t s)
+{
+    return dtype == SEQ_BF16 ? launch_totals_t<unsigned short>(back, a, s) : launch_totals_t<float>(back, a, s);
+}
 hipError_t launch_seq_rec_step(int dtype, const SeqRecArgs &a, hipStream_t s) { return dtype == SEQ_BF16 ? launch_step<unsigned short>(a, s) : launch_step<float>(a, s); }
 
 }  // namespace convmi

@@ -8,7 +8,7 @@
 namespace convmi {
 namespace {
 
-// A workgroup takes a wave's channels of one sequence through all of its positions: where they are more than its waves have at a time, first from the back for what
+// A workgroup takes a wave's channels of one sequence through all of its positions, or of a run of them: where they are more than its waves have at a time, first from the back for what
 // reaches the last position of each round from behind it (which takes f, dy and z; the states before the rounds would take x, f and i and half as much again), then from
 // the front.
 template <typename T, bool ROWS, int P, bool GATE, int WAVES>
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     static_assert(ROWS || Out::SLOTS == 64 * P || (Out::SLOTS <= 64 && P > 1), "results in the place of what was kept");
     constexpr int RESULTS = ROWS || Out::SLOTS == 64 * P ? 0 : 64 * (P - 1);
     const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, unit = L::unit(lane), at = L::at(lane);
-    const int groups = (a.Cp + L::COLS - 1) / L::COLS, n = blockIdx.x / groups, c0 = blockIdx.x % groups * L::COLS;
+    const int groups = (a.Cp + L::COLS - 1) / L::COLS, run = blockIdx.x / groups % a.runs, n = blockIdx.x / groups / a.runs, c0 = blockIdx.x % groups * L::COLS;
     const bool live = c0 + unit * E < a.Cp;
     const int c = live ? c0 + unit * E : c0;
     const int len = seq_length(a.lengths, n, a.L);
@@ -40,11 +40,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     // between waves each lane has one channel
     const int col = lane % L::COLS;
     const bool mine = c0 + col < a.Cp;
-    float *marks = a.marks + (long long)n * a.rounds * a.Cp + (mine ? c0 + col : 0);
+    float *marks = a.marks + ((long long)n * a.runs + run) * a.rounds * a.Cp + (mine ? c0 + col : 0);
     const int each = waves * L::LANES * P;
     // What is behind a sequence's end is loaded as zeros: nothing comes from there.
-    const auto load = [&](const RecTensor<T> &t, long long w0, Four (&b)[P]) {
-        const long long l0 = w0 + at * P;
+    const auto load = [&](const RecTensor<T> &t, int w0, Four (&b)[P]) {
+        const int l0 = w0 + at * P;
         if (w0 + L::LANES * P <= len) {
 #pragma unroll
             for (int j = 0; j < P; ++j) b[j] = t.load(w0 + j);
@@ -56,13 +56,19 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             }
         }
     };
-    const long long first = wave * L::LANES * P;
+    const int from = run * a.run, first = from + wave * L::LANES * P, to = min(a.L, from + a.run);  // (a.L is at most 2^30)
     int turn = 0;
-    float back = 0;  // a dh of the position behind a round
+    float state = 0, back = 0;  // before the run, and a dh of the position behind it, then behind its rounds
+    if (a.runs > 1) {
+        const float *t = a.totals + (long long)n * a.runs * 3 * a.Cp + (mine ? c0 + col : 0);
+        for (int r = 0; r < run; ++r) state = fmaf(t[(long long)r * 3 * a.Cp], state, t[((long long)r * 3 + 1) * a.Cp]);
+        for (int r = a.runs - 1; r > run; --r) back = fmaf(t[(long long)r * 3 * a.Cp], back, t[((long long)r * 3 + 2) * a.Cp]);
+    }
+    if (mine && threadIdx.x < L::COLS) marks[(a.rounds - 1) * (long long)a.Cp] = back;
     // (what the next round needs is asked for when this one's has come)
     Four bx[P], bf[P], bi[P], bz[P], bdy[P];
     const auto load_back = [&](int round) {
-        const long long w0 = (long long)round * each + first;
+        const int w0 = round * each + first;
         load(f, w0, bf);
         load(dy, w0, bdy);
         if constexpr (GATE) load(z, w0, bz);
@@ -93,11 +99,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         for (int w = waves - 1; w >= 0; --w) back = fmaf(runs[turn][w][col][0], back, runs[turn][w][col][1]);
         if (mine && threadIdx.x < L::COLS) marks[(long long)(round - 1) * a.Cp] = back;
     }
-    if (a.rounds > 1) __syncthreads();  // (the marks are there for all waves)
-    float state = 0;
+    __syncthreads();  // (the marks are there for all waves)
     float sums[3][E] = {};
     const auto load_all = [&](int round) {
-        const long long w0 = (long long)round * each + first;
+        const int w0 = round * each + first;
         load(f, w0, bf);
         load(i, w0, bi);
         load(x, w0, bx);
@@ -108,8 +113,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     constexpr bool AHEAD = sizeof(T) == 2 || !ROWS || !GATE;
     if constexpr (AHEAD) load_all(0);
     for (int round = 0; round < a.rounds; ++round, turn ^= 1) {
-        back = round < a.rounds - 1 ? marks[(long long)round * a.Cp] : 0.0f;
-        const long long w0 = (long long)round * each + first, l0 = w0 + at * P;
+        back = marks[(long long)round * a.Cp];
+        const int w0 = round * each + first, l0 = w0 + at * P;
         Four kx[P], kz[P], kdy[P];
         if constexpr (!AHEAD) load_all(round);
         float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
@@ -218,20 +223,20 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
                 sums[1][k] += ff[k];
                 sums[2][k] += fi[k];
             }
-            const bool ok = live && l0 + j < a.L;
+            const bool ok = live && l0 + j < to;
             dx.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fx) : Four{});
             df.put(w0, j, ok, lane, inside ? RecFour<T>::pack(ff) : Four{});
             di.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fi) : Four{});
             if constexpr (GATE) dz.put(w0, j, ok, lane, inside ? RecFour<T>::pack(fz) : Four{});
         }
         seq_wave_sync();
-        dx.out(w0, a.L, lane);
-        df.out(w0, a.L, lane);
-        di.out(w0, a.L, lane);
-        if constexpr (GATE) dz.out(w0, a.L, lane);
+        dx.out(w0, to, lane);
+        df.out(w0, to, lane);
+        di.out(w0, to, lane);
+        if constexpr (GATE) dz.out(w0, to, lane);
         seq_wave_sync();
     }
-    // the sums of a sequence: over the lanes that have a channel, then over the waves in order
+    // the sums of a run: over the lanes that have a channel, then over the waves in order
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 3; ++q)
@@ -248,15 +253,15 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         for (int q = 0; q < 3; ++q) {
             float s = 0;
             for (int w = 0; w < waves; ++w) s += runs[0][w][col][q];
-            a.part[((long long)n * 3 + q) * a.Cp + c0 + col] = s;
+            a.part[(((long long)n * a.runs + run) * 3 + q) * a.Cp + c0 + col] = s;
         }
 }
 
-// dA, df_bias and di_bias: the sequences' sums in order.
-__global__ __launch_bounds__(1024) void seq_rec_reduce_kernel(const float *part, float *dA, float *df_bias, float *di_bias, int N, int Cp)
+// dA, df_bias and di_bias: the runs' sums in order.
+__global__ __launch_bounds__(1024) void seq_rec_reduce_kernel(const float *part, float *dA, float *df_bias, float *di_bias, int parts, int Cp)
 {
     const int col = blockIdx.x * kSumColumns + threadIdx.x % kSumColumns, q = blockIdx.y;
-    const float s = seq_sum_parts(part + (long long)q * Cp + col, 3LL * Cp, N, col < Cp);
+    const float s = seq_sum_parts(part + (long long)q * Cp + col, 3LL * Cp, parts, col < Cp);
     float *to = q == 0 ? dA : q == 1 ? df_bias : di_bias;
     if (threadIdx.x < kSumColumns && col < Cp && to) to[col] = s;
 }
@@ -264,24 +269,28 @@ __global__ __launch_bounds__(1024) void seq_rec_reduce_kernel(const float *part,
 template <typename T, bool ROWS>
 void launch_rows(const SeqRecArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(a.N * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    const unsigned grid = (unsigned)(a.N * a.runs * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.z)
         seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, true, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
     else
         seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, false, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
 }
 template <typename T>
-hipError_t launch_t(const SeqRecArgs &a, hipStream_t s)
+hipError_t launch_t(int dtype, const SeqRecArgs &a, hipStream_t s)
 {
+    if (a.runs > 1) {
+        const hipError_t e = launch_seq_rec_totals(dtype, true, a, s);
+        if (e != hipSuccess) return e;
+    }
     if (a.rows)
         launch_rows<T, true>(a, s);
     else
         launch_rows<T, false>(a, s);
-    seq_rec_reduce_kernel<<<dim3((a.Cp + kSumColumns - 1) / kSumColumns, 3), 1024, 0, s>>>(a.part, a.dA, a.df_bias, a.di_bias, a.N, a.Cp);
+    seq_rec_reduce_kernel<<<dim3((a.Cp + kSumColumns - 1) / kSumColumns, 3), 1024, 0, s>>>(a.part, a.dA, a.df_bias, a.di_bias, a.N * a.runs, a.Cp);
     return hipGetLastError();
 }
 }  // namespace
 
-hipError_t launch_seq_rec_bwd(int dtype, const SeqRecArgs &a, hipStream_t s) { return dtype == SEQ_BF16 ? launch_t<unsigned short>(a, s) : launch_t<float>(a, s); }
+hipError_t launch_seq_rec_bwd(int dtype, const SeqRecArgs &a, hipStream_t s) { return dtype == SEQ_BF16 ? launch_t<unsigned short>(dtype, a, s) : launch_t<float>(dtype, a, s); }
 
 }  // namespace convmi

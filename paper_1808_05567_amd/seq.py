@@ -72,7 +72,7 @@ def load():
         args = {"seq_destroy": [vp], "seq_query": [vp, vp], "seq_describe": [vp, ctypes.c_char_p, sz],
                 "seq_conv_fwd": [vp] * 10, "seq_conv_step": [vp] * 8, "seq_conv_bwd": [vp] * 10 + [sz, vp],
                 "seq_scan_fwd": [vp] * 15 + [sz, vp], "seq_scan_step": [vp] * 13, "seq_scan_bwd": [vp] * 20 + [sz, vp],
-                "seq_rec_fwd": [vp] * 14, "seq_rec_step": [vp] * 12, "seq_rec_bwd": [vp] * 18 + [sz, vp],
+                "seq_rec_fwd": [vp] * 14 + [sz, vp], "seq_rec_step": [vp] * 12, "seq_rec_bwd": [vp] * 18 + [sz, vp],
                 "seq_lnorm_fwd": [vp] * 9, "seq_lnorm_fwd_q8": [vp] * 10, "seq_lnorm_bwd": [vp] * 10 + [sz, vp], "seq_adamw": [vp] * 10,
                 "seq_norm_fwd": [vp] * 7, "seq_norm_fwd_q8": [vp] * 8, "seq_norm_bwd": [vp] * 8 + [sz, vp],
                 "seq_mv4": [vp] * 8, "seq_mv4_quant": [vp] * 5, "seq_mv4_unquant": [vp] * 5}
@@ -317,12 +317,11 @@ def _rec_inputs(h, x, f, i, A, z, f_bias, i_bias):
 
 
 def seq_rec_fwd(h, x, f, i, A, y, ws=None, z=None, f_bias=None, i_bias=None, state_in=None, state_out=None, slots=None, lengths=None, stream=None):
-    """ws: not used (no pass but seq_rec_bwd has a workspace)."""
-    _here(x, f, i, A, y, z, f_bias, i_bias, state_in, state_out, slots, lengths)
+    _here(x, f, i, A, y, ws, z, f_bias, i_bias, state_in, state_out, slots, lengths)
     conv._check(load().seq_rec_fwd(
         _of(h, "seq_rec"), *_rec_inputs(h, x, f, i, A, z, f_bias, i_bias), _o(state_in, h.f32, h.state, "state_in"), _s(h, "y", y),
-        _o(state_out, h.f32, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"), conv._stream(stream)),
-        "seq_rec_fwd")
+        _o(state_out, h.f32, h.state, "state_out"), _o(slots, h.i32, h.N, "slots"), _o(lengths, h.i32, h.N, "lengths"), *_ws(ws),
+        conv._stream(stream)), "seq_rec_fwd")
 
 
 def seq_rec_step(h, x, f, i, A, state, y, z=None, f_bias=None, i_bias=None, slots=None, stream=None):

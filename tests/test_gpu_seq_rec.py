@@ -24,10 +24,18 @@ CASES = [  # N, C, L, z, biases, lengths, state, layout
     (1, 64, 1, True, True, "none", True, "dense"), (2, 5, 7, False, False, "none", True, "slice"), (3, 40, 33, True, True, "ragged", True, "rows"),
     (1, 130, 65, True, True, "none", False, "dense"), (2, 144, 129, False, True, "ragged", True, "slice"), (4, 32, 64, True, False, "clamped", True, "dense"),
     (1, 72, 200, True, True, "none", True, "rows"), (2, 16, 31, True, True, "ragged", False, "dense"), (5, 200, 12, False, True, "ragged", True, "dense"),
-    # several rounds of a workgroup's positions: of 512 with 16 lanes a block, of 128 with 4, of 32 where sequences are many
+    # several rounds of a workgroup's positions, and sequences shared by several workgroups
     (2, 24, 1537, True, True, "ragged", True, "dense"), (1, 40, 512, False, True, "none", True, "dense"), (1, 9, 513, True, True, "none", True, "slice"),
     (2, 72, 300, True, True, "ragged", True, "rows"), (4100, 8, 70, True, False, "ragged", True, "dense"), (4100, 4, 37, True, True, "ragged", True, "rows"),
+    (2, 12, 5000, True, True, "ragged", True, "dense"), (3, 100, 1300, True, True, "ragged", True, "rows"), (1, 8, 9001, False, False, "none", True, "slice"),
+    (40, 136, 600, True, True, "ragged", True, "dense"),
 ]
+
+
+def scratch(h):
+    """A workspace of whatever, which no result may show."""
+    ws = seq.seq_workspace(h)
+    return None if ws is None else ws.fill_(0xFF)
 
 
 def tensors(p, N, C, L, gate, biases, lengths, layout, dtype):
@@ -49,7 +57,7 @@ def test_forward(N, C, L, gate, biases, kind, with_state, layout, dtype):
     old = rng.standard_normal((slots, C)).astype(np.float32)
     st = vector(old, vlen(dtype)) if with_state else None
     h = seq.seq_rec_create(N, C, L, dtype, slots=slots, views={k: q.t for k, q in t.items()} | {"y": Y.t})
-    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, z=t["z"].t if gate else None, state_in=st, state_out=st, slots=ints(where),
+    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, scratch(h), z=t["z"].t if gate else None, state_in=st, state_out=st, slots=ints(where),
                     lengths=ints(lengths), **opt)
     torch.cuda.synchronize()
     (y, after), (ey, ea) = oracle.rec(p["x"], p["f"], p["i"], p["A"], state=old[where] if with_state else None, **ref)
@@ -102,7 +110,7 @@ def test_sequences_without_a_slot(dtype):
     Y = Seq(N, C, L, dtype)
     for plan, part in ((h, slice(0, first)), (rest, slice(first, L))):
         a = {k: q.t[:, :, part] for k, q in t.items()}
-        seq.seq_rec_fwd(plan, a["x"], a["f"], a["i"], A, Y.t[:, :, part], z=a["z"], state_in=st, state_out=st, slots=ints(where), **opt)
+        seq.seq_rec_fwd(plan, a["x"], a["f"], a["i"], A, Y.t[:, :, part], scratch(plan), z=a["z"], state_in=st, state_out=st, slots=ints(where), **opt)
     begin = np.zeros((N, C))
     begin[0] = old[2]
     (y, after), (ey, ea) = oracle.rec(p["x"], p["f"], p["i"], p["A"], state=begin, **ref)
@@ -162,7 +170,7 @@ def test_the_ends_of_what_parameters_may_be(dtype):
     st = vector(old, vlen(dtype))
     h = seq.seq_rec_create(N, C, L, dtype, slots=N)
     dA = nans(h.info.Cp)
-    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, z=t["z"].t, state_in=st, state_out=st)
+    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, scratch(h), z=t["z"].t, state_in=st, state_out=st)
     (y, after), (ey, ea) = oracle.rec(p["x"], p["f"], p["i"], p["A"], state=old, **ref)
     close(Y.get(), y, ey, dtype == seq.SEQ_BF16, "y")
     close(st.double().cpu().numpy()[:, :C], after, ea, False, "state")
@@ -181,7 +189,7 @@ def test_an_infinity_stays_in_its_sequence_and_channel():
     t, opt, A, ref = tensors(p, N, C, L, True, True, None, "dense", dtype)
     Y = Seq(N, C, L, dtype)
     h = seq.seq_rec_create(N, C, L, dtype)
-    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, z=t["z"].t, **opt)
+    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, scratch(h), z=t["z"].t, **opt)
     got = Y.get()
     assert np.isfinite(got[0, :20]).all() and not np.isfinite(got[0, 20, 3]) and not np.isfinite(got[1, 30:, 5]).any()
     got[0, 20:, 3] = got[1, 30:, 5] = 0
@@ -191,11 +199,11 @@ def test_an_infinity_stays_in_its_sequence_and_channel():
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_captured_and_replayed_beside_another_graph(dtype):
     """Forward and backward on a side stream, two graphs with workspaces of their own, replayed in turn with eager work between."""
-    N, C, L = 2, 40, 600
+    N, C, L = 2, 40, 2100
     runs = []
     for seed in (1, 2):
         _, p = data(N, C, L, dtype, seed)
-        lengths = np.array([L, 333])
+        lengths = np.array([L, 1333])
         t, opt, A, ref = tensors(p, N, C, L, True, True, lengths, "dense", dtype)
         Y, DY = Seq(N, C, L, dtype), Seq(N, C, L, dtype, "dense", spoil(p["dy"], lengths))
         out = {k: Seq(N, C, L, dtype) for k in ("dx", "df", "di", "dz")}
@@ -204,7 +212,7 @@ def test_captured_and_replayed_beside_another_graph(dtype):
         ws, n, st = seq.seq_workspace(h), ints(lengths), torch.zeros(N, h.info.Cp, device="cuda")
 
         def call(h=h, t=t, A=A, Y=Y, DY=DY, out=out, g=g, ws=ws, n=n, st=st, opt=opt):
-            seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, z=t["z"].t, state_out=st, lengths=n, **opt)
+            seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, ws, z=t["z"].t, state_out=st, lengths=n, **opt)
             seq.seq_rec_bwd(h, t["x"].t, t["f"].t, t["i"].t, A, DY.t, out["dx"].t, out["df"].t, out["di"].t, g["dA"], ws, z=t["z"].t, dz=out["dz"].t,
                             df_bias=g["df_bias"], di_bias=g["di_bias"], lengths=n, **opt)
         results = [Y.t, st] + [q.t for q in out.values()] + list(g.values())

@@ -46,13 +46,15 @@ def test_pointers_are_checked_before_any_launch():
     lib, E, WS = seq.load(), conv.CONV_EINVAL, conv.CONV_EWORKSPACE
     r, n, rms = seq.seq_rec_create(1, 8, 4, slots=1), seq.seq_lnorm_create(1, 8, 4), seq.seq_norm_create(1, 8, 4)
     no, p, odd = None, 16, 24
-    fwd = [p, p, p, p, no, no, no, no, p, no, no, no, no]
+    fwd = [p, p, p, p, no, no, no, no, p, no, no, no, no, 0, no]
     assert lib.seq_rec_fwd(no, *fwd) == E and lib.seq_rec_fwd(n._h, *fwd) == E
     for k in (0, 1, 2, 3, 8):
         assert lib.seq_rec_fwd(r._h, *fwd[:k], no, *fwd[k + 1:]) == E
     for k in (0, 1, 2, 3, 4, 5, 6, 7, 8, 9):
         assert lib.seq_rec_fwd(r._h, *fwd[:k], odd, *fwd[k + 1:]) == E
-    assert lib.seq_rec_fwd(r._h, *fwd[:10], 18, no, no) == E and lib.seq_rec_fwd(r._h, *fwd[:11], 18, no) == E
+    assert lib.seq_rec_fwd(r._h, *fwd[:10], 18, *fwd[11:]) == E and lib.seq_rec_fwd(r._h, *fwd[:11], 18, *fwd[12:]) == E
+    long = seq.seq_rec_create(1, 8, 1 << 14)  # (runs of a sequence: what they make of a state)
+    assert lib.seq_rec_fwd(long._h, *fwd) == WS and lib.seq_rec_fwd(long._h, *fwd[:12], p, 16, no) == WS and lib.seq_rec_fwd(long._h, *fwd[:12], odd, 1 << 30, no) == E
     none = seq.seq_rec_create(1, 8, 4)
     assert lib.seq_rec_fwd(none._h, *fwd[:7], p, *fwd[8:]) == E and lib.seq_rec_fwd(none._h, *fwd[:9], p, *fwd[10:]) == E
     assert lib.seq_rec_step(r._h, p, p, p, p, no, no, no, p, p, no, no) == E  # (a plan of four positions)
