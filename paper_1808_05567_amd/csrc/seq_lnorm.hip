@@ -482,7 +482,7 @@ template <typename T, int LT, int NV, bool ALONE>
 hipError_t launch_bwd(const SeqNormArgs &a, int threads, hipStream_t s)
 {
     // parts of dw and db: as many as there are workgroups at a time
-    const long long tiles = (a.rows + LT - 1) / LT, most = threads > 512 ? 256 : 512;
+    const long long each = ALONE ? kAloneWaves : LT, tiles = (a.rows + each - 1) / each, most = threads > 512 ? 256 : 512;
     const unsigned parts = (unsigned)std::min<long long>(std::min<long long>(most, a.parts), tiles);
     if (a.past)
         seq_lnorm_bwd_kernel<T, LT, NV, ALONE, true><<<parts, threads, 0, s>>>(a);
@@ -527,10 +527,14 @@ hipError_t launch_t(const SeqNormArgs &a, hipStream_t s)
     constexpr int V = SeqElem<T>::V;
     const SeqView &v = BWD ? a.vr : a.vx;
     if (v.c == V || a.L == 1) {
-        // a wave each where that leaves every workgroup two for each of its waves
+        // a wave each where that leaves every workgroup two for each of its waves and 16 channels a lane do (8 x 1024 x 1024 fp32, workgroups of one position:
+        // 35 us, this 27; 999 x 1000 take 13 either way)
         if constexpr (BWD) {
-            if (a.rows >= 2LL * kAloneWaves * a.parts && a.Cb <= 2 * 64)
-                return a.Cb <= 64 ? launch_bwd<T, 1, 1, true>(a, 64 * kAloneWaves, s) : launch_bwd<T, 1, 2, true>(a, 64 * kAloneWaves, s);
+            if (a.rows >= 2LL * kAloneWaves * a.parts && a.Cb <= 64 * 16 / V) {
+                if (a.Cb <= 64) return launch_bwd<T, 1, 1, true>(a, 64 * kAloneWaves, s);
+                if (a.Cb <= 2 * 64) return launch_bwd<T, 1, 2, true>(a, 64 * kAloneWaves, s);
+                if constexpr (V == 4) return launch_bwd<T, 1, 4, true>(a, 64 * kAloneWaves, s);
+            }
         }
         return launch_lt<T, 1, BWD>(a, s);
     }

@@ -146,18 +146,28 @@ def _o(x, dtype, least, name):
     return None if x is None else _t(x, dtype, least, name)
 
 
+_device = None  # the current device's number, once a tensor on one is there
+
+
 def _here(*tensors):
     """Refuses tensors of different devices, or of another one than the current one, on which the library's calls run."""
+    global _device
     at = None
     for x in tensors:
         if x is not None:
+            d = x.get_device()
             if at is None:
-                at = x.get_device()
-            elif x.get_device() != at:
-                raise ValueError("tensors on one device are wanted, not on %s and %s" % (at, x.device))
-    import torch
-    if at is not None and at >= 0 and at != torch.cuda.current_device():
-        raise ValueError("tensors on the current device (%d) are wanted, not on %d" % (torch.cuda.current_device(), at))
+                at = d
+            elif d != at:
+                raise ValueError("tensors on one device are wanted, not on %s and %s" % (at, d))
+    if at is None or at < 0:
+        return
+    if _device is None:
+        import torch
+        torch.cuda.current_device()  # (initialises the runtime if need be)
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if at != _device():
+        raise ValueError("tensors on the current device (%d) are wanted, not on %d" % (_device(), at))
 
 
 def _of(h, kind):
