@@ -10,8 +10,8 @@ its 1x1 convolutions, served over single tokens with 4-bit weights.
     out = W_out s        Ci -> C          conv 1x1
 
 Sp is S rounded up to the blocks' channels, so that B and C are whole blocks.  Every step reads parts of the tensors of the one before
-it in place, by their strides, and backwards writes them there.  All computation is the library's; torch holds memory, and
-clears what lies behind the ends of sequences.
+it in place, by their strides, and backwards writes them there.  ``SeqBlockAdamW`` moves its parameters by their gradients.  All computation is the library's; torch
+holds memory, and clears what lies behind the ends of sequences.
 """
 from __future__ import annotations
 
@@ -142,6 +142,11 @@ class SeqBlock:
                 raise ValueError("%s: a tensor of %s is wanted, not one of %s" % (k, tuple(t.shape), tuple(params[k].shape)))
         for k, t in self.params.items():
             t.copy_(params[k])
+        self.lay_out()
+
+    @torch.no_grad()
+    def lay_out(self):
+        """The block's own numbers, ``params``, into the layouts of the operators and of its steps, as ``load`` does with others."""
         p, Ci, Cip, Sp = self.params, self.dims[3], self.Cip, self.Sp
         self.w_in.set(_rows((Cip, p["w_in"][:Ci]), (Cip, p["w_in"][Ci:])))
         mid = _rows((Cip, p["w_dt"]), (Sp, p["w_B"]), (Sp, p["w_C"]))
@@ -276,6 +281,24 @@ class SeqBlockStep:
         return self.out, self.r
 
 
+class SeqBlockAdamW:
+    """AdamW over a block's parameters, its states in 32 bits or 8.  The projections decay, the other parameters do not."""
+
+    def __init__(self, block: SeqBlock, bits=32, betas=(0.9, 0.95), eps=1e-8, decay=0.1):
+        self.block, self.t = block, 0
+        self.plan = seq.seq_adamw_create([t.numel() for t in block.params.values()], seq.SEQ_F32, bits, betas, eps,
+                                         [decay if k.startswith("w_") else 0.0 for k in block.params])
+        self.m, self.v, self.scales = seq.seq_adamw_states(self.plan, block.device)
+
+    def step(self, grads, rate, factor=1.0):
+        """grads: the dict that ``SeqBlock.backward`` returns, times `factor`; the block has the new parameters, in its projections and its steps too."""
+        p = self.block.params
+        tensors = seq.seq_adamw_tensors(self.plan, list(p.values()), [grads[k].contiguous() for k in p])
+        self.t += 1
+        seq.seq_adamw(self.plan, tensors, self.m, self.v, (rate, self.t, factor), scales=self.scales)
+        self.block.lay_out()
+
+
 def main():
     """Times a training step of a block and single tokens of a batch: python -m paper_1808_05567_amd.seq_block"""
     N, L, C, Ci, S, W, M = 2, 2048, 1024, 2048, 16, 4, 16
@@ -294,6 +317,8 @@ def main():
     x, res, dout, dr = (torch.randn(N, C // 8, L, 8, device="cuda").to(torch.bfloat16) for _ in range(4))
     print("block %d -> %d, %d states, bf16: forward of %d x %d positions %.0f us" % (C, Ci, S, N, L, timed(lambda: block.forward(x, res))))
     print("forward and backward %.0f us" % timed(lambda: (block.forward(x, res), block.backward(dout, dr))))
+    adamw, (_, grads) = SeqBlockAdamW(block), block.backward(dout, dr)
+    print("AdamW over its %.1f M parameters, laid out again %.0f us" % (sum(t.numel() for t in block.params.values()) / 1e6, timed(lambda: adamw.step(grads, 1e-6))))
     step, states = SeqBlockStep(block, M), block.states()
     x1, r1 = (torch.randn(M, C // 8, 1, 8, device="cuda").to(torch.bfloat16) for _ in range(2))
     each = timed(lambda: step(x1, r1, states), 200)
