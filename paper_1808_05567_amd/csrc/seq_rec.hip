@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * kSeqRecTotalsWaves) void seq_rec_totals_kernel
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             bx[j] = bf[j] = bi[j] = bz[j] = bdy[j] = Four{};
-            if (l0 + j < len) {
+            if (l0 + j < to) {
                 bx[j] = x.load(w0 + j);
                 bf[j] = f.load(w0 + j);
                 bi[j] = i.load(w0 + j);
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * kSeqRecTotalsWaves) void seq_rec_totals_kernel
 #pragma unroll
             for (int k = 0; k < E; ++k) {
                 const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
-                pa[j][k] = l0 + j < len ? p : 1.0f;
+                pa[j][k] = l0 + j < to ? p : 1.0f;
                 const float u = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
                 H[k] = j == 0 ? u : fmaf(pa[j][k], H[k], u);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
@@ -285,10 +285,11 @@ template <typename T, bool ROWS>
 hipError_t launch_totals(bool back, const SeqRecArgs &a, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.N * (a.runs - !back) * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    constexpr int P = seq_rec_positions(ROWS);
     if (back)
-        seq_rec_totals_kernel<T, ROWS, kSeqRecBwdPositions, true><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_totals_kernel<T, ROWS, P, true><<<grid, 64 * kSeqRecTotalsWaves, 0, s>>>(a);
     else
-        seq_rec_totals_kernel<T, ROWS, seq_rec_positions(ROWS), false><<<grid, 64 * a.waves, 0, s>>>(a);
+        seq_rec_totals_kernel<T, ROWS, P, false><<<grid, 64 * kSeqRecTotalsWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T>
