@@ -220,23 +220,19 @@ static __device__ __forceinline__ void rec_join(float (&A)[kRecE], float (&H)[kR
         if constexpr (L::LANES == 64) across(32, !(lane & 32));
     }
 }
-// What all lanes before (BACK: behind) it make of x, from the joined runs.
+// What all lanes before (BACK: behind) it make of x, from the joined runs: what the nearest of them, with the others, does.
 template <typename T, bool ROWS, bool BACK>
 static __device__ __forceinline__ float rec_until(float A, float H, float x, int lane)
 {
     typedef RecLanes<T, ROWS> L;
-    float a, h;
-    if constexpr (ROWS) {
-        const int from = BACK ? lane + L::STEP : lane - L::STEP;
-        a = rec_lane(A, from & 63);
-        h = rec_lane(H, from & 63);
-    } else {
-        constexpr int SHIFT = BACK ? 0x130 : 0x138;  // by a lane, over the whole wave
-        a = rec_dpp<SHIFT>(1.0f, A);
-        h = rec_dpp<SHIFT>(0.0f, H);
-    }
-    const int at = L::at(lane);
-    return at == (BACK ? L::LANES - 1 : 0) ? x : fmaf(a, x, h);
+    const float own = fmaf(A, x, H);
+    float near;
+    if constexpr (ROWS)
+        near = rec_lane(own, (BACK ? lane + L::STEP : lane - L::STEP) & 63);
+    else
+        near = rec_dpp<BACK ? 0x130 : 0x138>(x, own);  // by a lane, over the whole wave
+    if constexpr (L::LANES == 64) return near;
+    return L::at(lane) == (BACK ? L::LANES - 1 : 0) ? x : near;
 }
 
 }  // namespace
