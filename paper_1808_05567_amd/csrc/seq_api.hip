@@ -398,12 +398,13 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
     for (const auto &w : views)
         if (!view_of(w.v, a.N, a.Cb, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
     a.rows = a.Cb > 1 && a.vx.c < a.vx.l;
-    // (a wave's elements are reached from its first one by 32 bits: 256 positions, 16 blocks)
+    // (a wave's elements are reached from its first one by 32 bits: 128 positions, 8 blocks)
     for (const auto &w : views)
         if (w.to.l > kMaxWaveStride || (a.rows && w.to.c > kMaxTileStride)) return finish(p, CONV_EUNSUPPORTED, out);
     a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
     // Waves of a workgroup: as many as find positions.  Forwards up to 8 where workgroups are two or more a compute unit (8 x 2048 x 2048 bf16: 73 us, with 4 of them 77,
-    // with 16 95), else up to 16 (1 x 8192 x 2048: 46 and 51); backwards 4, whose registers and LDS are three workgroups' a compute unit (2: 227 us, 4: 177).
+    // with 16 95), else up to 16 (1 x 8192 x 2048: 46 and 51); backwards 4, whose registers and LDS are three workgroups' a compute unit (2: 227 us, 4: 177), but 8 where
+    // workgroups are about as many as compute units (1 x 8192 x 2048 bf16 138 -> 103 us, rows of 8 x 2048 x 2048 297 -> 224; at 375 of them 41 -> 45).
     const int64_t columns = a.N * seq_rec_groups(a.Cp, a.rows, v);
     a.few = columns < 512;
     const auto waves = [&](int each, int most) {
@@ -429,9 +430,9 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
     p->rec_bwd = a;
     SeqRecArgs &b = p->rec_bwd;
     const int each = lanes * kSeqRecBwdPositions;
-    b.waves = waves(each, kSeqRecBwdWaves);
+    b.waves = waves(each, columns >= 192 && columns <= 256 ? kSeqRecBwdWaves : kSeqRecBwdWaves / 2);
     runs(b, b.L, 1);
-    if (columns < 256 && b.L > 2 * each * b.waves) runs(b, each * b.waves, 768);
+    if (columns < 192 && b.L > 2 * each * b.waves) runs(b, each * b.waves, 768);
     b.rounds = (int)((std::min(b.L, b.run) + (int64_t)b.waves * each - 1) / ((int64_t)b.waves * each));
     p->info.state_bytes = (size_t)a.Cp * 4;
     p->fwd_ws = a.runs > 1 ? up((size_t)a.N * a.runs * 2 * a.Cp * 4) : 0;

@@ -165,7 +165,7 @@ inline int seq_rec_cols(bool rows, int vlen) { return rows ? 8 * vlen : vlen; }
 inline int64_t seq_rec_groups(int64_t Cp, bool rows, int vlen) { return (Cp + seq_rec_cols(rows, vlen) - 1) / seq_rec_cols(rows, vlen); }
 inline int seq_rec_lanes(bool rows, int vlen) { return 64 / (seq_rec_cols(rows, vlen) / 4); }
 constexpr int seq_rec_positions(bool rows) { return rows ? 4 : 2; }
-constexpr int kSeqRecBwdPositions = 2, kSeqRecWaves = 16, kSeqRecBwdWaves = 4, kSeqRecTotalsWaves = 8;  // of a lane; of a workgroup at most
+constexpr int kSeqRecBwdPositions = 2, kSeqRecWaves = 16, kSeqRecBwdWaves = 8, kSeqRecTotalsWaves = 8;  // of a lane; of a workgroup at most
 
 // Results of more bytes than this go past the caches (the L2s hold 32 MB together).
 constexpr long long kSeqPastBytes = 16LL << 20;

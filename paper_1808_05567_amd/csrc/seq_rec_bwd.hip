@@ -266,14 +266,23 @@ __global__ __launch_bounds__(1024) void seq_rec_reduce_kernel(const float *part,
     if (threadIdx.x < kSumColumns && col < Cp && to) to[col] = s;
 }
 
+template <typename T, bool ROWS, bool GATE>
+void launch_gate(const SeqRecArgs &a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(a.N * a.runs * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
+    constexpr int P = kSeqRecBwdPositions;
+    if (a.waves > kSeqRecBwdWaves / 2)
+        seq_rec_bwd_kernel<T, ROWS, P, GATE, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+    else
+        seq_rec_bwd_kernel<T, ROWS, P, GATE, kSeqRecBwdWaves / 2><<<grid, 64 * a.waves, 0, s>>>(a);
+}
 template <typename T, bool ROWS>
 void launch_rows(const SeqRecArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(a.N * a.runs * seq_rec_groups(a.Cp, a.rows, SeqElem<T>::V));
     if (a.z)
-        seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, true, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+        launch_gate<T, ROWS, true>(a, s);
     else
-        seq_rec_bwd_kernel<T, ROWS, kSeqRecBwdPositions, false, kSeqRecBwdWaves><<<grid, 64 * a.waves, 0, s>>>(a);
+        launch_gate<T, ROWS, false>(a, s);
 }
 template <typename T>
 hipError_t launch_t(int dtype, const SeqRecArgs &a, hipStream_t s)

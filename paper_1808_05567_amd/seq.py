@@ -438,7 +438,7 @@ def seq_adamw_states(h, device="cuda"):
 
 
 class SeqAdamwTensors:
-    """Parameters, their gradients and copies for a plan's calls, checked once.  Holds the tensors."""
+    """Parameters, their gradients and copies for a plan's calls, checked once.  Holds the memory that they have then."""
 
     def __init__(self, h, p, g, copies=None):
         _of(h, "seq_adamw")
@@ -457,8 +457,9 @@ class SeqAdamwTensors:
         if len(set(at)) != len(at):
             raise ValueError("p, copies: a tensor stands there twice")
         _here(*(x for t in lists for x in t if x is not None and x.numel()))
-        self.plan, self.lists, self.tables = h, lists, tables
-        self.first = next((x for x in lists[0] if x.numel()), None)
+        self.plan, self.tables = h, tables
+        self.held = [x.detach() for t in lists for x in t if x is not None]  # (a tensor may get other memory later)
+        self.first = next((x for x in self.held if x.numel()), None)
 
 
 def seq_adamw_tensors(h, p, g, copies=None) -> SeqAdamwTensors:

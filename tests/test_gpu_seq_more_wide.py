@@ -51,6 +51,19 @@ def test_recurrence_of_more_than_16_megabytes(layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("layout,N,blocks,L", [("dense", 24, 8, 1100), ("dense", 256, 1, 700), ("dense", 257, 1, 150), ("rows", 200, 6, 300), ("rows", 191, 8, 100)])
+def test_recurrence_of_about_as_many_workgroups_as_compute_units(layout, N, blocks, L, dtype):
+    """Backwards in workgroups of more waves, and one workgroup beside where that ends."""
+    C = blocks * vlen(dtype) - 1
+    rng, p = data(N, C, L, dtype, N)
+    lengths = rng.integers(0, L + 1, N)
+    lengths[:3] = L, 0, 1
+    t, opt, A, ref = tensors(p, N, C, L, True, True, lengths, layout, dtype)
+    Y, DY = Seq(N, C, L, dtype, layout), Seq(N, C, L, dtype, layout, spoil(p["dy"], lengths))
+    run_rec(p, t, Y, DY, {k: Seq(N, C, L, dtype, layout) for k in GRADS}, N, C, L, dtype, lengths, np.arange(C), opt, A, ref)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("first", ["dense", "rows", "slice"])
 def test_recurrence_of_tensors_in_different_layouts(first, dtype):
     """x decides how lanes are laid out; the others lie as they may."""
@@ -190,3 +203,38 @@ def test_calls_at_once_on_other_streams():
         call(s)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for (_, results), w in zip(jobs, want) for a, b in zip(results, w))
+
+
+def test_a_gradient_that_is_not_finite():
+    """In 32 bits it spoils its own number; in 8 the states of the 256 numbers that share its scale, from the next step on."""
+    n, at = 700, 300
+    for bits in (32, 8):
+        for what in (float("inf"), float("-inf"), float("nan")):
+            h = seq.seq_adamw_create([n], seq.SEQ_F32, bits, decay=0.1)
+            gen = torch.Generator("cuda").manual_seed(1)
+            p, g = torch.randn(n, device="cuda", generator=gen), torch.randn(n, device="cuda", generator=gen)
+            runs = []
+            for spoilt in (False, True):
+                q, d = p.clone(), g.clone()
+                if spoilt:
+                    d[at] = what
+                m, v, scales = seq.seq_adamw_states(h)
+                seq.seq_adamw(h, seq.seq_adamw_tensors(h, [q], [d]), m, v, (1e-2, 1), scales=scales)
+                first = q.clone()
+                seq.seq_adamw(h, seq.seq_adamw_tensors(h, [q], [g]), m, v, (1e-2, 2), scales=scales)
+                runs.append((first, q))
+            (a, b), (c, d) = runs
+            others = torch.arange(n, device="cuda") != at
+            assert torch.equal(a[others], c[others]) and not c[at].isfinite() and not d[at].isfinite()
+            far = others if bits == 32 else (torch.arange(n, device="cuda") < 256) | (torch.arange(n, device="cuda") >= 512)
+            assert torch.equal(b[far], d[far]) and (bits == 32 or bool(d[256:512].isnan().all()))
+
+
+def test_tensors_whose_memory_is_replaced_stay_where_they_were():
+    h = seq.seq_adamw_create([300], seq.SEQ_F32)
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    tensors, (m, v, _) = seq.seq_adamw_tensors(h, [p], [g]), seq.seq_adamw_states(h)
+    old = p.detach()
+    p.data = torch.zeros(300, device="cuda")
+    seq.seq_adamw(h, tensors, m, v, (1e-2, 1))
+    assert not p.any() and bool((old < 1).all())
