@@ -113,12 +113,24 @@ struct RecOut {
     // ends: behind the last position that there is
     __device__ __forceinline__ void out(int w0, int ends, int lane) const
     {
-        if constexpr (!ROWS) {
+        if constexpr (!ROWS) blocks(w0, ends, lane, [&](int q) { return lds[L::LANES * (lane % P) + (64 * q + lane) / P]; });
+    }
+    // zeros at all positions
+    __device__ __forceinline__ void clear(int w0, int ends, bool live, int lane) const
+    {
+        if constexpr (ROWS) {
 #pragma unroll
-            for (int q = 0; q < SLOTS / 64; ++q)
-                if (w0 + 64 * q + lane < ends)
-                    to.template store<PAST>(w0 + 64 * q, (unsigned)lane * (unsigned)to.pitch, lds[L::LANES * (lane % P) + (64 * q + lane) / P]);
-        }
+            for (int j = 0; j < P; ++j)
+                if (live && w0 + L::at(lane) * P + j < ends) to.template store<PAST>(w0 + j, to.lane, Four{});
+        } else
+            blocks(w0, ends, lane, [](int) { return seq_u32x4{}; });
+    }
+    template <typename F>
+    __device__ __forceinline__ void blocks(int w0, int ends, int lane, F &&block) const
+    {
+#pragma unroll
+        for (int q = 0; q < SLOTS / 64; ++q)
+            if (w0 + 64 * q + lane < ends) to.template store<PAST>(w0 + 64 * q, (unsigned)lane * (unsigned)to.pitch, block(q));
     }
 };
 

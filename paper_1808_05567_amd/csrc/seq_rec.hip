@@ -69,7 +69,8 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
         }
     };
     if constexpr (AHEAD) load(from + wave * L::LANES * P);
-    for (int base = from; base < to; base += each, turn ^= 1) {
+    int base = from;
+    for (; base < min(to, len); base += each, turn ^= 1) {
         const int w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
         if constexpr (!AHEAD) load(w0);
         float A[E], H[E], pa[P][E], ph[P][E];
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) kz[j] = bz[j];
-        if (AHEAD && base + each < to) load(w0 + each);
+        if (AHEAD && base + each < min(to, len)) load(w0 + each);
         rec_join<T, ROWS, false>(A, H, lane);
         if (at == L::LANES - 1)
 #pragma unroll
@@ -124,6 +125,7 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
         y.out(w0, a.L, lane);
         seq_wave_sync();
     }
+    for (; base < to; base += each) y.clear(base + wave * L::LANES * P, a.L, live, lane);
     if (a.state_out && kept && run == a.runs - 1 && threadIdx.x < L::COLS) a.state_out[(long long)slot * a.Cp + c0 + col] = state;
 }
 

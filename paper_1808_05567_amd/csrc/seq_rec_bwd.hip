@@ -57,6 +57,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         }
     };
     const int from = run * a.run, first = from + wave * L::LANES * P, to = min(a.L, from + a.run);  // (a.L is at most 2^30)
+    const int rounds = min(a.rounds, (max(len - from, 0) + each - 1) / each);  // that the sequence reaches
     int turn = 0;
     float state = 0, back = 0;  // before the run, and a dh of the position behind it, then behind its rounds
     if (a.runs > 1) {
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         for (int r = 0; r < run; ++r) state = fmaf(t[(long long)r * 3 * a.Cp], state, t[((long long)r * 3 + 1) * a.Cp]);
         for (int r = a.runs - 1; r > run; --r) back = fmaf(t[(long long)r * 3 * a.Cp], back, t[((long long)r * 3 + 2) * a.Cp]);
     }
-    if (mine && threadIdx.x < L::COLS) marks[(a.rounds - 1) * (long long)a.Cp] = back;
+    if (mine && threadIdx.x < L::COLS) marks[max(rounds - 1, 0) * (long long)a.Cp] = back;
     // (what the next round needs is asked for when this one's has come)
     Four bx[P], bf[P], bi[P], bz[P], bdy[P];
     const auto load_back = [&](int round) {
@@ -73,8 +74,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         load(dy, w0, bdy);
         if constexpr (GATE) load(z, w0, bz);
     };
-    if (a.rounds > 1) load_back(a.rounds - 1);
-    for (int round = a.rounds - 1; round > 0; --round, turn ^= 1) {
+    if (rounds > 1) load_back(rounds - 1);
+    for (int round = rounds - 1; round > 0; --round, turn ^= 1) {
         float A[E], B[E];
 #pragma unroll
         for (int j = P - 1; j >= 0; --j) {
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     // (but in fp32 with gates, where registers do not do for it: 4 x 2048 x 2048 149 us so, 147 to 151 ahead with 1 to 6 of them spilled)
     constexpr bool AHEAD = sizeof(T) == 2 || !GATE;
     if constexpr (AHEAD) load_all(0);
-    for (int round = 0; round < a.rounds; ++round, turn ^= 1) {
+    for (int round = 0; round < rounds; ++round, turn ^= 1) {
         back = marks[(long long)round * a.Cp];
         const int w0 = round * each + first, l0 = w0 + at * P;
         Four kx[P], kz[P], kdy[P];
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             kz[j] = bz[j];
             kdy[j] = bdy[j];
         }
-        if (AHEAD && round < a.rounds - 1) load_all(round + 1);
+        if (AHEAD && round < rounds - 1) load_all(round + 1);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
 #pragma unroll
@@ -235,6 +236,13 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         di.out(w0, to, lane);
         if constexpr (GATE) dz.out(w0, to, lane);
         seq_wave_sync();
+    }
+    for (int round = rounds; round < a.rounds; ++round) {
+        const int w0 = round * each + first;
+        dx.clear(w0, to, live, lane);
+        df.clear(w0, to, live, lane);
+        di.clear(w0, to, live, lane);
+        if constexpr (GATE) dz.clear(w0, to, live, lane);
     }
     // the sums of a run: over the lanes that have a channel, then over the waves in order
     __syncthreads();
