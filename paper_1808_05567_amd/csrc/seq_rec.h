@@ -247,5 +247,24 @@ static __device__ __forceinline__ float rec_until(float A, float H, float x, int
     return L::at(lane) == (BACK ? L::LANES - 1 : 0) ? x : near;
 }
 
+// x after n runs, `step` numbers apart, with their A and H: eight at a time, so that one trip to memory brings them.
+static __device__ __forceinline__ float rec_through(const float *A, const float *H, long long step, int n, float x)
+{
+    constexpr int TOGETHER = 8;
+    for (int r = 0; r < n; r += TOGETHER) {
+        float a[TOGETHER], h[TOGETHER];
+#pragma unroll
+        for (int i = 0; i < TOGETHER; ++i) {
+            const long long at = min(r + i, n - 1) * step;
+            a[i] = A[at];
+            h[i] = H[at];
+        }
+#pragma unroll
+        for (int i = 0; i < TOGETHER; ++i)
+            if (r + i < n) x = fmaf(a[i], x, h[i]);
+    }
+    return x;
+}
+
 }  // namespace
 }  // namespace convmi

@@ -43,11 +43,10 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     float state = 0;
     if (a.runs == 1)
         state = a.state_in && kept ? a.state_in[(long long)slot * a.Cp + c0 + col] : 0.0f;
-    else if (c0 + col < a.Cp)
-        for (int r = 0; r <= run; ++r) {
-            const float *t = a.totals + ((long long)n * a.runs + r) * 2 * a.Cp + c0 + col;
-            state = fmaf(t[0], state, t[a.Cp]);
-        }
+    else if (c0 + col < a.Cp) {
+        const float *t = a.totals + (long long)n * a.runs * 2 * a.Cp + c0 + col;
+        state = rec_through(t, t + a.Cp, 2LL * a.Cp, run + 1, state);
+    }
     const int from = run * a.run, to = min(a.L, from + a.run);  // (a.L is at most 2^30)
     const int each = waves * L::LANES * P;
     int turn = 0;

@@ -66,9 +66,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     int turn = 0;
     float state = 0, back = 0;  // before the run, and a dh of the position behind it, then behind its rounds
     if (a.runs > 1) {
-        const float *t = a.totals + (long long)n * a.runs * 3 * a.Cp + (mine ? c0 + col : 0);
-        for (int r = 0; r < run; ++r) state = fmaf(t[(long long)r * 3 * a.Cp], state, t[((long long)r * 3 + 1) * a.Cp]);
-        for (int r = a.runs - 1; r > run; --r) back = fmaf(t[(long long)r * 3 * a.Cp], back, t[((long long)r * 3 + 2) * a.Cp]);
+        const long long step = 3LL * a.Cp;
+        const float *t = a.totals + n * a.runs * step + (mine ? c0 + col : 0), *last = t + (a.runs - 1) * step;
+        state = rec_through(t, t + a.Cp, step, run, state);
+        back = rec_through(last, last + 2 * a.Cp, -step, a.runs - 1 - run, back);
     }
     if (mine && threadIdx.x < L::COLS) marks[max(rounds - 1, 0) * (long long)a.Cp] = back;
     // (what the next round needs is asked for when this one's has come)
