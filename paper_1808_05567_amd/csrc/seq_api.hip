@@ -536,8 +536,8 @@ static conv_status_t norm_create(Kind kind, const seq_norm_desc_t *d, seq_handle
     for (const auto &w : views)
         if (!view_of(w.v, a.N, a.Cb, a.L, v, w.out, w.to)) return finish(p, CONV_EINVAL, out);
     if (!view_of(d->q, a.N, (a.C + 15) / 16, a.L, 16, true, a.vq)) return finish(p, CONV_EINVAL, out);
-    // backward: two workgroups a compute unit, each with a part of dw (and db)
-    a.parts = (int)std::min<int64_t>(512, a.rows);
+    // backward: two workgroups a compute unit, each with a part of dw (and db); of the layer norm up to four
+    a.parts = (int)std::min<int64_t>(kind == kLnorm && a.rows >= 8192 ? 1024 : 512, a.rows);
     p->bwd_ws = up((size_t)a.parts * a.Cp * 4 * (kind == kLnorm ? 2 : 1));
     return finish(p, CONV_OK, out);
 }

@@ -19,7 +19,11 @@
 namespace convmi {
 namespace {
 
-constexpr int kMaxThreads = 1024, kAloneWaves = 4;
+constexpr int kMaxThreads = 1024, kAloneWaves = 4, kParts = 512;
+// Forwards, inputs of more bytes than this are read past the caches, as results are written: with their results they are more than the last one of 256 MB holds (positions of 2048 bf16
+// channels, three sets of tensors in turn: 67 MB 61.5 -> 58.5 us, 50 MB 48.4 -> 46.8, but 42 MB 36.5 -> 41.9).  Backwards they are wherever results are (67 MB 73 -> 70.6, 42 MB 49.5 -> 46.9,
+// 33 MB 37.0 -> 36.7).
+constexpr long long kOnceBytes = 48LL << 20;
 
 // Sums (MAX: largest unsigned) of K numbers over the lanes of a wave with the same place in a tile of LT positions, in all of them.
 template <int LT, bool MAX, int K>
@@ -84,6 +88,14 @@ static __device__ __forceinline__ void join_waves(const SeqNormArgs &a, seq_f32x
     sums = seq_f32x4{mean, u[0], BWD ? t[1] : 0.0f, BWD ? u[1] : 0.0f};
 }
 
+// ONCE: what no one reads again does not stay in the caches.
+template <bool ONCE, typename T>
+static __device__ __forceinline__ seq_u32x4 load_once(const T *p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const seq_u32x4 *>(p));
+    return seq_load(p);
+}
+
 // What is unpacked from b behind this is unpacked again, rather than kept in registers from before, where it takes twice as many.
 static __device__ __forceinline__ void again_from(seq_u32x4 &b) { asm volatile("" : "+v"(b)); }
 
@@ -112,7 +124,7 @@ static __device__ __forceinline__ void clear_beyond(const SeqNormArgs &a, int b,
 }
 
 // LT positions at a time, 64 / LT blocks a wave side by side, as in the root-mean-square norm.  NV: blocks a thread holds; 0: more than fit, read again.
-template <typename T, int LT, int NV, bool Q8, bool PAST>
+template <typename T, int LT, int NV, bool Q8, bool PAST, bool ONCE>
 __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNormArgs a)
 {
     constexpr int V = SeqElem<T>::V;
@@ -167,8 +179,8 @@ __global__ __launch_bounds__(kMaxThreads) void seq_lnorm_fwd_kernel(const SeqNor
             over([&](int j, int b) {
                 keep[j] = more[j] = seq_u32x4{};
                 if (!at.inside) return;
-                keep[j] = seq_load(x + b * a.vx.c);
-                if (res) more[j] = seq_load(res + b * a.vres.c);
+                keep[j] = load_once<ONCE>(x + b * a.vx.c);
+                if (res) more[j] = load_once<ONCE>(res + b * a.vres.c);
             });
             over([&](int j, int b) {
                 if (res) keep[j] = added(keep[j], more[j]);
@@ -310,8 +322,8 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
         for (int j = 0; j < NV; ++j) {
             k.r[j] = k.dy[j] = seq_u32x4{};
             if (!at.inside || first + j * step >= a.Cb) continue;
-            k.r[j] = seq_load(r + j * (step * a.vr.c));
-            k.dy[j] = seq_load(dy + j * (step * a.vdy.c));
+            k.r[j] = load_once<PAST>(r + j * (step * a.vr.c));
+            k.dy[j] = load_once<PAST>(dy + j * (step * a.vdy.c));
         }
     };
     // (dr is needed last: it is asked for when these positions' sums begin)
@@ -320,7 +332,7 @@ __global__ __launch_bounds__(ALONE ? 64 * kAloneWaves : kMaxThreads) void seq_ln
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             now_dr[j] = seq_u32x4{};
-            if (dr && at.inside && first + j * step < a.Cb) now_dr[j] = seq_load(dr + j * (step * a.vdr.c));
+            if (dr && at.inside && first + j * step < a.Cb) now_dr[j] = load_once<PAST>(dr + j * (step * a.vdr.c));
         }
     };
     if constexpr (NV > 0) load_all(place(blockIdx.x), next);
@@ -474,18 +486,22 @@ hipError_t launch_fwd(const SeqNormArgs &a, int threads, hipStream_t s)
     const long long tiles = (a.rows + LT - 1) / LT;
     const unsigned grid = (unsigned)(tiles < 1 << 22 ? tiles : 1 << 22);
     if (a.q)
-        seq_lnorm_fwd_kernel<T, LT, NV, true, false><<<grid, threads, 0, s>>>(a);
+        seq_lnorm_fwd_kernel<T, LT, NV, true, false, false><<<grid, threads, 0, s>>>(a);
+    else if (a.rows * a.Cb * 16 > kOnceBytes)
+        seq_lnorm_fwd_kernel<T, LT, NV, false, true, true><<<grid, threads, 0, s>>>(a);
     else if (a.past)
-        seq_lnorm_fwd_kernel<T, LT, NV, false, true><<<grid, threads, 0, s>>>(a);
+        seq_lnorm_fwd_kernel<T, LT, NV, false, true, false><<<grid, threads, 0, s>>>(a);
     else
-        seq_lnorm_fwd_kernel<T, LT, NV, false, false><<<grid, threads, 0, s>>>(a);
+        seq_lnorm_fwd_kernel<T, LT, NV, false, false, false><<<grid, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T, int LT, int NV, bool ALONE>
 hipError_t launch_bwd(const SeqNormArgs &a, int threads, hipStream_t s)
 {
-    // parts of dw and db: as many as there are workgroups at a time
-    const long long each = ALONE ? kAloneWaves : LT, tiles = (a.rows + each - 1) / each, most = threads > 512 ? 256 : 512;
+    // parts of dw and db: as many as there are workgroups at a time, but 512 where each of 1024 would have less than 8 tiles (8 x 2048 positions of 2048 bf16 channels side by
+    // side: 512 of them 85 us, 1024 71; 3 x 333 of 1000 fp32: 11.3 and 14.0)
+    const long long each = ALONE ? kAloneWaves : LT, tiles = (a.rows + each - 1) / each;
+    const long long most = threads > 512 ? kParts / 2 : !ALONE && threads <= 256 && tiles >= 16LL * kParts ? 2 * kParts : kParts;
     const unsigned parts = (unsigned)std::min<long long>(std::min<long long>(most, a.parts), tiles);
     if (a.past)
         seq_lnorm_bwd_kernel<T, LT, NV, ALONE, true><<<parts, threads, 0, s>>>(a);
@@ -533,7 +549,7 @@ hipError_t launch_t(const SeqNormArgs &a, hipStream_t s)
         // a wave each where that leaves every workgroup two for each of its waves and 16 channels a lane do (8 x 1024 x 1024 fp32, workgroups of one position:
         // 35 us, this 27; 999 x 1000 take 13 either way)
         if constexpr (BWD) {
-            if (a.rows >= 2LL * kAloneWaves * a.parts && a.Cb <= 64 * 16 / V) {
+            if (a.rows >= 2LL * kAloneWaves * kParts && a.Cb <= 64 * 16 / V) {
                 if (a.Cb <= 64) return launch_bwd<T, 1, 1, true>(a, 64 * kAloneWaves, s);
                 if (a.Cb <= 2 * 64) return launch_bwd<T, 1, 2, true>(a, 64 * kAloneWaves, s);
                 if constexpr (V == 4) return launch_bwd<T, 1, 4, true>(a, 64 * kAloneWaves, s);
