@@ -499,9 +499,9 @@ template <typename T, int LT, int NV, bool ALONE>
 hipError_t launch_bwd(const SeqNormArgs &a, int threads, hipStream_t s)
 {
     // parts of dw and db: as many as there are workgroups at a time, but 512 where each of 1024 would have less than 8 tiles (8 x 2048 positions of 2048 bf16 channels side by
-    // side: 512 of them 85 us, 1024 71; 3 x 333 of 1000 fp32: 11.3 and 14.0)
+    // side: 512 of them 85 us, 1024 71; 8 x 8000 of 300 fp32, a wave each, 92 and 72; 3 x 333 of 1000 fp32 11.3 and 14.0)
     const long long each = ALONE ? kAloneWaves : LT, tiles = (a.rows + each - 1) / each;
-    const long long most = threads > 512 ? kParts / 2 : !ALONE && threads <= 256 && tiles >= 16LL * kParts ? 2 * kParts : kParts;
+    const long long most = threads > 512 ? kParts / 2 : threads <= 256 && tiles >= 16LL * kParts ? 2 * kParts : kParts;
     const unsigned parts = (unsigned)std::min<long long>(std::min<long long>(most, a.parts), tiles);
     if (a.past)
         seq_lnorm_bwd_kernel<T, LT, NV, ALONE, true><<<parts, threads, 0, s>>>(a);

@@ -238,3 +238,27 @@ def test_tensors_whose_memory_is_replaced_stay_where_they_were():
     p.data = torch.zeros(300, device="cuda")
     seq.seq_adamw(h, tensors, m, v, (1e-2, 1))
     assert not p.any() and bool((old < 1).all())
+
+
+@pytest.mark.parametrize("N,C,L,layout,dtype", [
+    (9, 1100, 1000, "rows", seq.SEQ_BF16), (9, 700, 1000, "rows", seq.SEQ_F32), (33, 20, 1000, "rows", seq.SEQ_BF16), (33, 300, 1000, "slice", seq.SEQ_F32),
+    (9, 2900, 1001, "rows", seq.SEQ_BF16), (4, 1500, 2200, "dense", seq.SEQ_F32), (40, 4, 900, "dense", seq.SEQ_F32)])
+def test_layer_norm_of_many_positions(N, C, L, layout, dtype):
+    """Gradients in more workgroups, inputs past the caches."""
+    bf16, v = dtype == seq.SEQ_BF16, vlen(dtype)
+    rng = np.random.default_rng(N + C)
+    x, dy = rounded(rng.standard_normal((N, L, C)), dtype), rounded(rng.standard_normal((N, L, C)), dtype)
+    w, b = (np.float32(rng.standard_normal(C)).astype(np.float64) for _ in range(2))
+    lengths = rng.integers(0, L + 1, N)
+    inside = (np.arange(L) < lengths[:, None])[..., None]
+    X, DY, Y, DX = Seq(N, C, L, dtype, layout, spoil(x, lengths)), Seq(N, C, L, dtype, layout, spoil(dy, lengths)), Seq(N, C, L, dtype, layout), Seq(N, C, L, dtype, layout)
+    h = seq.seq_lnorm_create(N, C, L, dtype, EPS, views={"x": X.t, "y": Y.t, "r": X.t, "dy": DY.t, "dx": DX.t})
+    dw, db, n, ws = nans(h.info.Cp), nans(h.info.Cp), ints(lengths), scratch(h)
+    seq.seq_lnorm_fwd(h, X.t, None, vector(w, v), vector(b, v), None, Y.t, lengths=n)
+    seq.seq_lnorm_bwd(h, X.t, vector(w, v), DY.t, None, DX.t, dw, db, ws, lengths=n)
+    y, ey = oracle.lnorm(x, w, b, EPS)
+    close(Y.get(), y * inside, ey * inside, bf16, "y")
+    (dx, *want), (edx, *err) = oracle.lnorm_bwd(x, w, dy * inside, None, EPS)
+    close(DX.get(), dx * inside, edx * inside, bf16, "dx")
+    for name, got, a, e in zip(("dw", "db"), (dw, db), want, err):
+        close(got.double().cpu().numpy()[:C], a, e, False, name)
