@@ -407,9 +407,13 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
     // workgroups are about as many as compute units (1 x 8192 x 2048 bf16 138 -> 103 us, rows of 8 x 2048 x 2048 297 -> 224; at 375 of them 41 -> 45).
     const int64_t columns = a.N * seq_rec_groups(a.Cp, a.rows, v);
     a.few = columns < 512;
-    const auto waves = [&](int each, int most) {
+    // (of the same number of rounds the one with the fewest waves: 16 x 300 x 2048 bf16 35 -> 31 us, gradients 101 -> 86; but a workgroup alone on a compute unit takes powers of
+    // two: 2 x 530 x 1000 11.6 us, 15.2 with the fewest)
+    const auto waves = [&](int each, int most, bool fewest) {
+        const int64_t all = (a.L + (int64_t)each - 1) / each, rounds = (all + most - 1) / most;
+        if (fewest) return (int)((all + rounds - 1) / rounds);
         int w = 1;
-        while (w < most && (int64_t)w * each < a.L) w *= 2;
+        while (w < most && w < all) w *= 2;
         return w;
     };
     // Where there are less than `most` workgroups, of `each` positions at a time, they share a sequence in runs, of which another launch finds out first what they make
@@ -421,7 +425,7 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
         q.runs = (int)((q.L + (int64_t)q.run - 1) / q.run);
     };
     const int lanes = seq_rec_lanes(a.rows, v);
-    a.waves = waves(lanes * seq_rec_positions(a.rows), a.few ? kSeqRecWaves : kSeqRecWaves / 2);
+    a.waves = waves(lanes * seq_rec_positions(a.rows), a.few ? kSeqRecWaves : kSeqRecWaves / 2, !a.few);
     const int shared = lanes * seq_rec_positions(a.rows) * kSeqRecTotalsWaves;
     runs(a, a.L, 1);
     if (columns < 128 && a.L > 2 * shared) {
@@ -431,7 +435,7 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
     p->rec_bwd = a;
     SeqRecArgs &b = p->rec_bwd;
     const int each = lanes * kSeqRecBwdPositions;
-    b.waves = waves(each, columns >= 192 && columns <= 256 ? kSeqRecBwdWaves : kSeqRecBwdWaves / 2);
+    b.waves = waves(each, columns >= 192 && columns <= 256 ? kSeqRecBwdWaves : kSeqRecBwdWaves / 2, true);
     runs(b, b.L, 1);
     if (columns < 192 && b.L > 2 * each * b.waves) runs(b, each * b.waves, 768);
     b.rounds = (int)((std::min(b.L, b.run) + (int64_t)b.waves * each - 1) / ((int64_t)b.waves * each));
