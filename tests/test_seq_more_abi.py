@@ -1,6 +1,7 @@
 """Host-side checks of the recurrence, the layer norm and AdamW: sizes, refusals before anything is launched, and the oracle's gradients against
 differences of its forward passes."""
 import ctypes
+import functools
 
 import numpy as np
 import pytest
@@ -158,6 +159,21 @@ def test_views_and_extents_of_the_recurrence(calls):  # noqa: F811
     with pytest.raises(ValueError):
         seq.seq_rec_fwd(h, *parts[:3], w[:8], y, stream=0)
     assert calls == ["seq_rec_fwd"]
+
+
+def test_distances_that_the_recurrence_refuses():
+    """Positions more than 2^20 elements apart and, where x has its blocks nearer than its positions, blocks more than 2^24."""
+    def at(c, l):
+        return torch.empty_strided((2, 3, 5, 8), (1 << 40, c, l, 1), dtype=torch.bfloat16, device="meta")
+    far, near = 1 << 20, 64
+    plan = functools.partial(seq.seq_rec_create, 2, 24, 5, seq.SEQ_BF16)
+    for name in ("x", "f", "i", "z", "y", "dy", "dx", "df", "di", "dz"):
+        rows = {"x": at(8, near)}
+        for views in ({name: at(8, far)}, rows | {name: at(1 << 24, near)}, {name: at(1 << 36, near)}):
+            plan(views=views)
+        for views in ({name: at(8, far + 8)}, rows | {name: at((1 << 24) + 8, near)}):
+            if name != "x" or views["x"].stride(1) == 8:  # (with its blocks further apart x is not such a tensor)
+                assert status(plan, views=views) == conv.CONV_EUNSUPPORTED
 
 
 # ---------------------------------------------------------------------------- the oracle
