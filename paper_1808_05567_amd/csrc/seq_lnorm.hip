@@ -8,8 +8,8 @@
 //   q_w = sum (r - m_w)^2,  and backwards  G_w = sum w dy,  p_w = sum w dy (r - m_w),
 // which the workgroup joins in one exchange:  mean = sum n_w m_w / C,  sum (r - mean)^2 = sum q_w + n_w (m_w - mean)^2,
 //   sum w dy (r - mean) = sum p_w + G_w (m_w - mean).
-// A few operations an element: bound by memory.  Measured, 8 x 2048 positions of 2048 channels in bf16, 268 MB: forward 58 us (4.6 TB/s; 52 where half of it is still in the
-// caches; positions side by side 51), backward 70 (3.8 TB/s; 71), of which 5 are the sums of dw and db over the workgroups; 3 x 333 positions of 1000 fp32 channels side by side, 12 MB: backward 9 and 3;
+// A few operations an element: bound by memory.  Measured, 8 x 2048 positions of 2048 channels in bf16, 268 MB: forward 58 us (4.6 TB/s; positions side by side 51),
+// backward 70 (3.8 TB/s; 71), of which 5 are the sums of dw and db over the workgroups; 3 x 333 positions of 1000 fp32 channels side by side, 12 MB: backward 9 and 4;
 // 16 x 4096 to 8 bits 5.4.
 #include <algorithm>
 #include <type_traits>
