@@ -24,7 +24,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     constexpr int E = kRecE;
     __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, from the back, B
     __shared__ __align__(16) float begin[2][WAVES][L::COLS];
-    // of each lane, from the gates to the gradients: s, g, k and sigmoid(z), in LDS rather than computed again (20 operations of some 110) or in registers, of which four waves
+    // of each lane, from the gates to the gradients: s, g, k and what h is multiplied by in dz, in LDS rather than computed again (20 operations of some 110) or in registers, of which four waves
     // a SIMD have 128
     constexpr int KEPT = GATE ? 4 : 3;
     __shared__ seq_u32x4 kept[WAVES][KEPT][P * 64];
@@ -41,7 +41,15 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     const RecTensor<T> x = tensor(a.x, a.vx), f = tensor(a.f, a.vf), i = tensor(a.i, a.vi), z = tensor(a.z, a.vz), dy = tensor(a.dy, a.vdy);
     const Out dx = {kept[wave][0] + RESULTS, tensor(a.dx, a.vdx)}, df = {kept[wave][1] + RESULTS, tensor(a.df, a.vdf)},
               di = {kept[wave][2] + RESULTS, tensor(a.di, a.vdi)}, dz = {kept[wave][KEPT - 1] + RESULTS, tensor(a.dz, a.vdz)};
-    const RecParams par(a, c);
+    // A and the biases, in LDS rather than in 12 registers between their uses (8 x 2048 x 2048 bf16 without z: 141 -> 131 us)
+    __shared__ seq_f32x4 params[3][L::UNITS];
+    if (wave == 0 && at == 0) {
+        const RecParams p(a, c);
+        params[0][unit] = RecFour<float>::pack(p.A);
+        params[1][unit] = RecFour<float>::pack(p.f);
+        params[2][unit] = RecFour<float>::pack(p.i);
+    }
+    __syncthreads();
     // between waves each lane has one channel
     const int col = lane % L::COLS;
     const bool mine = c0 + col < a.Cp;
@@ -82,7 +90,9 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     };
     if (rounds > 1) load_back(rounds - 1);
     for (int round = rounds - 1; round > 0; --round, turn ^= 1) {
-        float A[E], B[E];
+        float A[E], B[E], pA[E], pf[E];
+        rec_unpack(params[0][unit], pA);
+        rec_unpack(params[1][unit], pf);
 #pragma unroll
         for (int j = P - 1; j >= 0; --j) {
             float ff[E], fz[E], up[E];
@@ -91,7 +101,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             if constexpr (GATE) rec_unpack(bz[j], fz);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float p = seq_exp2(par.A[k] * rec_gate(ff[k], par.f[k]));
+                const float p = seq_exp2(pA[k] * rec_gate(ff[k], pf[k]));
                 if constexpr (GATE) up[k] *= fz[k] * seq_sigmoid(fz[k]);
                 B[k] = p * (j == P - 1 ? up[k] : up[k] + B[k]);
                 A[k] = j == P - 1 ? p : A[k] * p;
@@ -108,24 +118,32 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     }
     __syncthreads();  // (the marks are there for all waves)
     float sums[3][E] = {};
-    const auto load_all = [&](int round) {
+    // What a round needs is asked for when the one before has come: all of it, or f and i, which it needs first, where that leaves registers for a fourth workgroup a compute unit
+    // (8 x 2048 x 2048 bf16: all 171 us, those 164; but rows of 8 x 2048 x 2048, one workgroup a compute unit, 207 and 226).
+    constexpr bool ALL = ROWS || WAVES > kSeqRecBwdWaves / 2;
+    const auto load_rest = [&](int round) {
         const int w0 = round * each + first;
-        load(f, w0, bf);
-        load(i, w0, bi);
         load(x, w0, bx);
         load(dy, w0, bdy);
         if constexpr (GATE) load(z, w0, bz);
     };
-    // (but in fp32 with gates, where registers do not do for it: 4 x 2048 x 2048 149 us so, 147 to 151 ahead with 1 to 6 of them spilled)
-    constexpr bool AHEAD = sizeof(T) == 2 || !GATE;
-    if constexpr (AHEAD) load_all(0);
+    const auto load_ahead = [&](int round) {
+        const int w0 = round * each + first;
+        load(f, w0, bf);
+        load(i, w0, bi);
+        if constexpr (ALL) load_rest(round);
+    };
+    load_ahead(0);
     for (int round = 0; round < rounds; ++round, turn ^= 1) {
         back = marks[(long long)round * a.Cp];
         const int w0 = round * each + first, l0 = w0 + at * P;
-        Four kx[P], kz[P], kdy[P];
-        if constexpr (!AHEAD) load_all(round);
+        Four kx[P];
+        if constexpr (!ALL) load_rest(round);
         float pa[P][E], ph[P][E], up[P][E];  // a; k g x, then the state before; what reaches h from y
-        float A[E], H[E], Ab[E], B[E];
+        float A[E], H[E], Ab[E], B[E], pA[E], pf[E], pi[E];
+        rec_unpack(params[0][unit], pA);
+        rec_unpack(params[1][unit], pf);
+        rec_unpack(params[2][unit], pi);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             float fx[E], ff[E], fi[E], fz[E], root[E];
@@ -136,16 +154,16 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
             if constexpr (GATE) rec_unpack(bz[j], fz);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                ff[k] = rec_gate(ff[k], par.f[k]);
-                fi[k] = rec_gate(fi[k], par.i[k]);
-                const float t = par.A[k] * ff[k];
+                ff[k] = rec_gate(ff[k], pf[k]);
+                fi[k] = rec_gate(fi[k], pi[k]);
+                const float t = pA[k] * ff[k];
                 pa[j][k] = seq_exp2(t);
                 root[k] = __builtin_amdgcn_sqrtf(rec_rest(t, pa[j][k]));
                 ph[j][k] = root[k] * fi[k] * fx[k];
                 if constexpr (GATE) {
-                    const float p = seq_sigmoid(fz[k]);
+                    const float p = seq_sigmoid(fz[k]), y = up[j][k];
                     up[j][k] *= fz[k] * p;
-                    fz[k] = p;
+                    fz[k] = y * p * fmaf(fz[k], 1.0f - p, 1.0f);
                 }
                 H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
@@ -158,10 +176,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             kx[j] = bx[j];
-            kz[j] = bz[j];
-            kdy[j] = bdy[j];
         }
-        if (AHEAD && round < rounds - 1) load_all(round + 1);
+        if (round < rounds - 1) load_ahead(round + 1);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
 #pragma unroll
@@ -187,6 +203,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         begin[1][wave][col] = back;
         seq_wave_sync();
         float h[E], d[E];
+        rec_unpack(params[0][unit], pA);
         rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[0][wave][unit * E]), h);
         rec_unpack(*reinterpret_cast<const seq_f32x4 *>(&begin[1][wave][unit * E]), d);
 #pragma unroll
@@ -202,14 +219,12 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
         }
 #pragma unroll
         for (int j = P - 1; j >= 0; --j) {
-            float fx[E], ff[E], fi[E], fz[E], fdy[E], s[E], g[E], root[E], p[E];
+            float fx[E], ff[E], fi[E], fz[E], s[E], g[E], root[E], p[E];
             rec_unpack(kx[j], fx);
             SeqElem<float>::unpack(kept[wave][0][j * 64 + lane], s);
             SeqElem<float>::unpack(kept[wave][1][j * 64 + lane], g);
             SeqElem<float>::unpack(kept[wave][2][j * 64 + lane], root);
             if constexpr (GATE) {
-                rec_unpack(kz[j], fz);
-                rec_unpack(kdy[j], fdy);
                 SeqElem<float>::unpack(kept[wave][3][j * 64 + lane], p);
             }
             seq_wave_sync();
@@ -220,11 +235,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
                 // (a pays for what k lets in; k of zero lets nothing in)
                 const float inv = root[k] > 0 ? __builtin_amdgcn_rcpf(root[k]) : 0.0f;
                 const float dt = back * fmaf(-gx * pa[j][k], inv, ph[j][k]);
-                if constexpr (GATE) fz[k] = fdy[k] * fmaf(pa[j][k], ph[j][k], root[k] * gx) * p[k] * fmaf(fz[k], 1.0f - p[k], 1.0f);
+                if constexpr (GATE) fz[k] = p[k] * fmaf(pa[j][k], ph[j][k], root[k] * gx);
                 fi[k] = dhk * gx * (1.0f - g[k]);
                 fx[k] = dhk * g[k];
                 const float dts = dt * s[k];
-                ff[k] = dts * (par.A[k] * kLn2) * (1.0f - s[k]);
+                ff[k] = dts * (pA[k] * kLn2) * (1.0f - s[k]);
                 d[k] = back;
                 sums[0][k] += dts;
                 sums[1][k] += ff[k];
