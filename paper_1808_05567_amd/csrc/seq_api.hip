@@ -403,7 +403,7 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
         if (w.to.l > kMaxWaveStride || (a.rows && w.to.c > kMaxTileStride)) return finish(p, CONV_EUNSUPPORTED, out);
     a.past = (long long)a.N * a.Cb * a.L * 16 > kSeqPastBytes;
     // Waves of a workgroup: as many as find positions.  Forwards up to 8 where workgroups are two or more a compute unit (8 x 2048 x 2048 bf16: 73 us, with 4 of them 77,
-    // with 16 95), else up to 16 (1 x 8192 x 2048: 46 and 51); backwards 4, whose registers and LDS are three workgroups' a compute unit (2: 227 us, 4: 177), but 8 where
+    // with 16 95), else up to 16 (1 x 8192 x 2048: 46 and 51); backwards 4, whose registers and LDS are three or four workgroups' a compute unit (2: 227 us, 4: 177), but 8 where
     // workgroups are about as many as compute units (1 x 8192 x 2048 bf16 138 -> 103 us, rows of 8 x 2048 x 2048 297 -> 224; at 375 of them 41 -> 45).
     const int64_t columns = a.N * seq_rec_groups(a.Cp, a.rows, v);
     a.few = columns < 512;

@@ -16,8 +16,10 @@ namespace {
 // not, since moves between lanes go through LDS there (5 ragged fp32 sequences: two 25.6 us, four 21.3).
 // GATE: there is a z.  AHEAD: what the next round needs is asked for when this one's has come (where a compute unit has one workgroup: 1 x 8192 x 2048 bf16 45 -> 43 us,
 // ragged rows 26 -> 21; where its registers cost a third workgroup it does not pay: 8 x 2048 x 2048 72 -> 77).
+// Without that, and but for fp32 with z, 64 registers do, so that four workgroups of 8 waves share a compute unit (8 x 2048 x 2048 bf16 75.0 -> 74.1 us, without z 77.6 -> 72.6;
+// 16 x 300 x 2048 30.5 -> 27.9; 4 x 2048 x 2048 fp32, 5 registers spilled, 64.9 -> 71.4).
 template <typename T, bool ROWS, int P, bool GATE, bool PAST, bool AHEAD>
-__global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const SeqRecArgs a)
+__global__ __launch_bounds__(64 * kSeqRecWaves, AHEAD || ROWS || (GATE && sizeof(T) == 4) ? 4 : 8) void seq_rec_fwd_kernel(const SeqRecArgs a)
 {
     typedef RecLanes<T, ROWS> L;
     typedef typename RecFour<T>::type Four;
@@ -36,7 +38,14 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     const Out y = {results[wave], tensor(a.y, a.vy)};
     const int slot = a.slots ? a.slots[n] : n;
     const bool has_slot = slot >= 0 && slot < a.n_slots;
-    const RecParams par(a, c);
+    __shared__ seq_f32x4 params[3][L::UNITS];  // A and the biases: not in registers between their uses
+    if (wave == 0 && at == 0) {
+        const RecParams p(a, c);
+        params[0][unit] = RecFour<float>::pack(p.A);
+        params[1][unit] = RecFour<float>::pack(p.f);
+        params[2][unit] = RecFour<float>::pack(p.i);
+    }
+    __syncthreads();
     // between waves each lane has one channel
     const int col = lane % L::COLS;
     const bool kept = has_slot && c0 + col < a.Cp;
@@ -79,7 +88,10 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
     for (; base < min(to, len); base += each, turn ^= 1) {
         const int w0 = base + wave * L::LANES * P, l0 = w0 + at * P;
         if constexpr (!AHEAD) load(w0);
-        float A[E], H[E], pa[P][E], ph[P][E];
+        float A[E], H[E], pa[P][E], ph[P][E], pA[E], pf[E], pi[E];
+        rec_unpack(params[0][unit], pA);
+        rec_unpack(params[1][unit], pf);
+        rec_unpack(params[2][unit], pi);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             float fx[E], ff[E], fi[E];
@@ -88,10 +100,10 @@ __global__ __launch_bounds__(64 * kSeqRecWaves) void seq_rec_fwd_kernel(const Se
             rec_unpack(bi[j], fi);
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float t = par.A[k] * rec_gate(ff[k], par.f[k]), p = seq_exp2(t);
+                const float t = pA[k] * rec_gate(ff[k], pf[k]), p = seq_exp2(t);
                 pa[j][k] = l0 + j < len ? p : 1.0f;
                 // (what is behind the end was loaded as zero)
-                ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], par.i[k]) * fx[k];
+                ph[j][k] = __builtin_amdgcn_sqrtf(rec_rest(t, p)) * rec_gate(fi[k], pi[k]) * fx[k];
                 H[k] = j == 0 ? ph[j][k] : fmaf(pa[j][k], H[k], ph[j][k]);
                 A[k] = j == 0 ? pa[j][k] : A[k] * pa[j][k];
             }

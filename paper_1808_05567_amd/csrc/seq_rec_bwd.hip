@@ -6,8 +6,8 @@
 //
 // States go forwards and their gradients backwards, so that what a run of positions makes of either is found before both are known.  Some 120 operations an element, 14 of them
 // exponentials, reciprocals or roots, and f, dy and z are read a second time where a sequence is longer than a workgroup takes at a time.  Measured, bf16 with z: 8 x 2048 positions
-// of 2048 channels, 604 MB and 201 of them again, 170 us (4.7 TB/s with those, vector units 0.7 busy; positions side by side, 256 workgroups, 224), of which 5 are the sums over the
-// workgroups; 1 x 8192 103 us.
+// of 2048 channels, 604 MB and 201 of them again, 164 us (4.9 TB/s with those, vector units 0.7 busy; positions side by side, 256 workgroups, 207), of which 5 are the sums over the
+// workgroups; 1 x 8192 104 us.
 #include "seq_rec.h"
 
 namespace convmi {
@@ -24,8 +24,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     constexpr int E = kRecE;
     __shared__ __align__(16) float runs[2][WAVES][L::COLS][4];  // A, H and, from the back, B
     __shared__ __align__(16) float begin[2][WAVES][L::COLS];
-    // of each lane, from the gates to the gradients: s, g, k and what h is multiplied by in dz, in LDS rather than computed again (20 operations of some 110) or in registers, of which four waves
-    // a SIMD have 128
+    // of each lane, from the gates to the gradients: s, g, k and what h is multiplied by in dz, in LDS rather than computed again (20 operations of some 110) or in registers,
+    // of which four waves a SIMD have 128
     constexpr int KEPT = GATE ? 4 : 3;
     __shared__ seq_u32x4 kept[WAVES][KEPT][P * 64];
     typedef RecOut<T, ROWS, P, false> Out;
