@@ -102,8 +102,12 @@ __global__ __launch_bounds__(256) void seq_adamw_kernel(const SeqAdamwArgs a)
         for (int i = 0; i < kEach; ++i) {
             if (e + i >= t.size) m[i] = v[i] = 0;
             const float s = g[i] * factor;
-            m[i] = fmaf(a.rest1, s, a.beta1 * m[i]);
-            v[i] = fmaf(a.rest2 * s, s, a.beta2 * v[i]);
+            {
+                // (each product rounded by itself, as the formula's operations one after the other are: in 8 bits a root next to a half is rounded as theirs is)
+#pragma clang fp contract(off)
+                m[i] = a.rest1 * s + a.beta1 * m[i];
+                v[i] = a.rest2 * (s * s) + a.beta2 * v[i];
+            }
             root[i] = sqrtf(v[i]);
             p[i] = p[i] - keep * p[i] - by_m * m[i] / fmaf(root[i], by_v, a.eps);
         }
@@ -122,13 +126,20 @@ __global__ __launch_bounds__(256) void seq_adamw_kernel(const SeqAdamwArgs a)
                 xm = __uint_as_float(max(__float_as_uint(xm), __float_as_uint(fabsf(m[i]))));
                 xv = __uint_as_float(max(__float_as_uint(xv), __float_as_uint(root[i])));
             }
-            const float sm = wave_max(xm) / 127.0f, sv = wave_max(xv) / 255.0f;
+            const float sm = wave_max(xm) * (1 / 127.0f), sv = wave_max(xv) * (1 / 255.0f);
             const float im = sm == 0 ? 0 : 1.0f / sm, iv = sv == 0 ? 0 : 1.0f / sv;
+            // a root over the scale, with what its product with the rounded reciprocal is off by, so that what is next to a half goes to the side that the quotient does
+            // (scales that are not finite: their reciprocal is 0, and stays)
+            const float tm = im > 0 ? sm : 0.0f, tv = iv > 0 ? sv : 0.0f;
+            const auto over = [](float x, float scale, float inverse) {
+                const float q = x * inverse;
+                return fmaf(fmaf(-q, scale, x), inverse, q);
+            };
             unsigned bm = 0, bv = 0;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int qm = (int)rintf(fminf(fmaxf(m[i] * im, -127.0f), 127.0f));
-                const int qv = (int)rintf(fminf(root[i] * iv, 255.0f));
+                const int qm = (int)rintf(fminf(fmaxf(over(m[i], tm, im), -127.0f), 127.0f));
+                const int qv = (int)rintf(fminf(over(root[i], tv, iv), 255.0f));
                 bm |= (unsigned)(qm & 255) << 8 * i;
                 bv |= (unsigned)(root[i] > 0 && qv == 0 ? 1 : qv) << 8 * i;
             }

@@ -262,3 +262,29 @@ def test_layer_norm_of_many_positions(N, C, L, layout, dtype):
     close(DX.get(), dx * inside, edx * inside, bf16, "dx")
     for name, got, a, e in zip(("dw", "db"), (dw, db), want, err):
         close(got.double().cpu().numpy()[:C], a, e, False, name)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_eight_bits_hold_what_the_operations_one_after_the_other_give(dtype):
+    """The states' codes and scales after each of several steps, in every bit: fp32 operations rounded one by one, the nearest whole number of the rounded quotient.
+    (A code that goes to the other side of a half moves the number by a step, and with it the scale of the steps behind.)"""
+    f = np.float32
+    n, beta1, beta2, rate, factor = 3000 * 256, 0.9, 0.95, 1e-3, 0.7
+    h = seq.seq_adamw_create([n], dtype, 8, betas=(beta1, beta2))
+    rng = np.random.default_rng(1)
+    p, m, v = torch.zeros(n, device="cuda"), np.zeros(n, f), np.zeros(n, f)
+    gm, gv, scales = seq.seq_adamw_states(h)
+    for step in range(1, 5):
+        g = torch.from_numpy((rng.standard_normal(n) * np.exp(rng.standard_normal((n // 256, 1)) - 6).repeat(256, 1).reshape(-1)).astype(f)).to(TORCH[dtype])
+        seq.seq_adamw(h, seq.seq_adamw_tensors(h, [p], [g.cuda()]), gm, gv, (rate, step, factor), scales=scales)
+        s = g.float().numpy() * f(factor)
+        m, v = m * f(beta1) + s * f(1 - beta1), v * f(beta2) + s * s * f(1 - beta2)
+        a, b = np.sqrt(np.abs(m)).reshape(-1, 256), np.sqrt(np.sqrt(v)).reshape(-1, 256)
+        sa, sb = a.max(1, keepdims=True) * (f(1) / f(127)), b.max(1, keepdims=True) * (f(1) / f(255))
+        qa, qb = np.rint(a / sa) * np.sign(m).reshape(a.shape), np.maximum(np.rint(b / sb), b > 0)
+        assert a.dtype == b.dtype == sa.dtype == f
+        got = scales.cpu().numpy().reshape(2, -1)
+        assert np.array_equal(got[0], sa[:, 0]) and np.array_equal(got[1], sb[:, 0])
+        assert np.array_equal(gm.cpu().numpy().reshape(a.shape), qa) and np.array_equal(gv.cpu().numpy().reshape(a.shape), qb)
+        a, b = qa * sa, qb * sb
+        m, v = (a * np.abs(a)).reshape(-1).astype(f), np.square(b * b).reshape(-1).astype(f)
