@@ -3,7 +3,7 @@
 //   s = sigmoid(f + f_bias), g = sigmoid(i + i_bias), a = exp(A s), h[l] = a h[l-1] + sqrt(1 - a^2) g x[l], y = h z sigmoid(z)
 //
 // Each tensor is read once: what positions make of a state is kept in registers until the state before them is known.  Some 50 operations an element,
-// four of them exponentials, three reciprocals, one a root, so that memory and the vector units are both near their rates.  Measured, bf16 with z: 8 x 2048 positions of 2048 channels, 336 MB, 74 us
+// four of them exponentials, three reciprocals, one a root, so that memory and the vector units are both near their rates.  Measured, bf16 with z: 8 x 2048 positions of 2048 channels, 336 MB, 73.5 us
 // (4.5 TB/s, vector units 0.8 busy; positions side by side 79), 1 x 8192, 168 MB, 40 us (4.2 TB/s); fp32 without z, 5 sequences of up to 777, 1000 channels side by side, 62 MB: 20 us;
 // one position of 32 sequences, 4096 channels: 3.6 us, a trip to memory and the launch.
 #include "seq_rec.h"
