@@ -126,11 +126,11 @@ __global__ __launch_bounds__(256) void seq_adamw_kernel(const SeqAdamwArgs a)
                 xm = __uint_as_float(max(__float_as_uint(xm), __float_as_uint(fabsf(m[i]))));
                 xv = __uint_as_float(max(__float_as_uint(xv), __float_as_uint(root[i])));
             }
-            const float sm = wave_max(xm) * (1 / 127.0f), sv = wave_max(xv) * (1 / 255.0f);
+            // (not infinite: what is not zero would stand for infinity, an infinite v, which stops a parameter and does not show)
+            const auto scale_of = [](float largest, float by) { return largest < INFINITY ? largest * by : NAN; };
+            const float sm = scale_of(wave_max(xm), 1 / 127.0f), sv = scale_of(wave_max(xv), 1 / 255.0f);
             const float im = sm == 0 ? 0 : 1.0f / sm, iv = sv == 0 ? 0 : 1.0f / sv;
             // a root over the scale, with what its product with the rounded reciprocal is off by, so that what is next to a half goes to the side that the quotient does
-            // (scales that are not finite: their reciprocal is 0, and stays)
-            const float tm = im > 0 ? sm : 0.0f, tv = iv > 0 ? sv : 0.0f;
             const auto over = [](float x, float scale, float inverse) {
                 const float q = x * inverse;
                 return fmaf(fmaf(-q, scale, x), inverse, q);
@@ -138,8 +138,8 @@ __global__ __launch_bounds__(256) void seq_adamw_kernel(const SeqAdamwArgs a)
             unsigned bm = 0, bv = 0;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int qm = (int)rintf(fminf(fmaxf(over(m[i], tm, im), -127.0f), 127.0f));
-                const int qv = (int)rintf(fminf(over(root[i], tv, iv), 255.0f));
+                const int qm = (int)rintf(fminf(fmaxf(over(m[i], sm, im), -127.0f), 127.0f));
+                const int qv = (int)rintf(fminf(over(root[i], sv, iv), 255.0f));
                 bm |= (unsigned)(qm & 255) << 8 * i;
                 bv |= (unsigned)(root[i] > 0 && qv == 0 ? 1 : qv) << 8 * i;
             }
