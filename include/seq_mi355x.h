@@ -176,7 +176,7 @@ conv_status_t seq_rec_step(seq_handle_t h, const void *x, const void *f, const v
                            float *state, void *y, const int32_t *slots, void *stream);
 /* Gradients of seq_rec_fwd without states.  dx, df, di: sequence tensors; dz: one where there is a
  * z; dA, df_bias, di_bias: fp32 vectors, the last two or NULL.  Where 1 - a^2 is zero, the square
- * root's slope is left out of dA and df. */
+ * root's slope is left out of dA and df; dA of an A above zero is zero. */
 conv_status_t seq_rec_bwd(seq_handle_t h, const void *x, const void *f, const void *i,
                           const float *A, const void *z, const float *f_bias, const float *i_bias,
                           const void *dy, void *dx, void *df, void *di, float *dA, void *dz,
