@@ -1,8 +1,13 @@
-"""AdamW where a state leaves what its type holds."""
+"""AdamW where a state leaves what its type holds; the recurrence's forward builds for many workgroups whose results go past the caches."""
+import re
+
+import numpy as np
 import pytest
 import torch
 
-from seq_util import DTYPES, TORCH
+import seq_rec_oracle as oracle
+from seq_util import DTYPES, TORCH, Seq, close, ints, vector, vlen
+from test_gpu_seq_rec import data, scratch, tensors
 from paper_1808_05567_amd import seq
 
 pytestmark = pytest.mark.gpu
@@ -45,3 +50,25 @@ def test_a_state_that_is_not_finite(what, dtype):
         assert bool(v[block].isnan().all()) and bool(m[block].isfinite().all() if finite else m[block].isnan().all())
         beside = (torch.arange(n, device="cuda") < block.start) | (torch.arange(n, device="cuda") >= block.stop)
         assert torch.equal(b[beside], d[beside]) and bool(d[block].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("layout,N,C,L", [("dense", 5, 1044, 1700), ("rows", 33, 1044, 260)])
+def test_recurrence_of_more_than_16_megabytes_in_many_workgroups(layout, N, C, L, gate, dtype):
+    """At least 512 workgroups, which ask for nothing ahead, each result past the caches; compared at every 61st channel and the last two."""
+    rng, p = data(N, C, L, dtype, 6)
+    lengths = rng.integers(0, L + 1, N)
+    lengths[:3] = L, 0, 1
+    t, opt, A, _ = tensors(p, N, C, L, gate, True, lengths, layout, dtype)
+    Y, old = Seq(N, C, L, dtype, layout), rng.standard_normal((N, C)).astype(np.float32)
+    st = vector(old, vlen(dtype))
+    h = seq.seq_rec_create(N, C, L, dtype, slots=N, views={k: q.t for k, q in t.items()} | {"y": Y.t})
+    assert int(re.search(r"columns=(\d+)", seq.seq_describe(h)).group(1)) >= 512 and N * h.info.Cb * L * 16 > 16 << 20
+    seq.seq_rec_fwd(h, t["x"].t, t["f"].t, t["i"].t, A, Y.t, scratch(h), z=t["z"].t if gate else None, state_in=st, state_out=st, lengths=ints(lengths), **opt)
+    some = np.append(np.arange(0, C, 61), [C - 2, C - 1])
+    pick = {k: q[..., some] for k, q in p.items()}
+    (y, after), (ey, ea) = oracle.rec(*(pick[k] for k in ("x", "f", "i", "A")), z=pick["z"] if gate else None, f_bias=pick["f_bias"], i_bias=pick["i_bias"],
+                                      state=old[:, some], lengths=lengths)
+    close(Y.get()[..., some], y, ey, dtype == seq.SEQ_BF16, "y")
+    close(st.double().cpu().numpy()[:, some], after, ea, False, "state")
