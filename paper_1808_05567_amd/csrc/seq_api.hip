@@ -28,7 +28,6 @@ struct seq_plan {
     SeqAdamwArgs adamw;        // without its tensors
     SeqAdamwTensor *tensors;   // their sizes, places and decays
     int count, bits;
-    double beta1, beta2;
     ~seq_plan() { delete[] tensors; }
 };
 
@@ -699,8 +698,6 @@ conv_status_t seq_adamw_create(const seq_adamw_desc_t *d, seq_handle_t *out)
     if (!p->tensors) return finish(p, CONV_EUNSUPPORTED, out);
     p->count = d->count;
     p->bits = d->bits;
-    p->beta1 = d->beta1;
-    p->beta2 = d->beta2;
     int64_t blocks = 0;
     for (int k = 0; k < d->count; ++k) {
         if (d->sizes[k] > kMaxNumbers - blocks * kSeqAdamwBlock) return finish(p, CONV_EUNSUPPORTED, out);

@@ -51,9 +51,6 @@ struct RecFour<unsigned short> {
     typedef seq_u32x2 type;
     static __device__ __forceinline__ type pack(const float (&f)[kRecE]) { return type{seq_pack_bf16(f[0], f[1]), seq_pack_bf16(f[2], f[3])}; }
 };
-// What is computed from b behind this is computed again, rather than kept in registers from before.
-static __device__ __forceinline__ void rec_again(seq_u32x2 &b) { asm volatile("" : "+v"(b)); }
-static __device__ __forceinline__ void rec_again(seq_f32x4 &b) { asm volatile("" : "+v"(b)); }
 
 // A tensor as a wave takes it: where its first block and a sequence begin, the same for all lanes, and the bytes from there to a lane's channels and
 // first position, which 32 bits hold (a plan's views see to that).
