@@ -265,9 +265,10 @@ conv_status_t seq_mv4_unquant(seq_handle_t h, const void *wt, const float *scale
  * the one before; what lies between is written as zero.  Zeros are a fresh state.
  * bits = 32: m and v in fp32.  bits = 8: of m its signed square root, of v its fourth root, in int8
  * and uint8 times a scale for each 256 numbers: scales [2][numbers / 256], m's first.  The scale is
- * the largest's over 127 (m) and 255 (v); the others are rounded to nearest even, of v never down
- * to zero.  p moves by m and v before that rounding.  An m or v that is not finite makes those of
- * its 256 numbers NaN.
+ * the largest's times 1/127 (m) and 1/255 (v), factor and product rounded to fp32; a root over it is
+ * rounded to the nearest whole number, halves to even, of v never down to zero.  p moves by m and v
+ * before that rounding.  An m or v that is not finite (v from scaled gradients of 1.85e19 on, whose
+ * square fp32 does not hold) makes those of its 256 numbers NaN.
  * The step's rate, t and factor are doubles in host memory (now), or, so that a recorded step may
  * run with new ones, fp32 in device memory (now_device); the other is NULL.
  * sizes: numbers of each tensor, >= 0; decays: decay of each.  Both are copied.
