@@ -4,7 +4,7 @@
 //
 // Bound by memory: every number is read and written once, in a launch for 80 tensors, whose pointers are kernel arguments (nothing is kept on the GPU for a plan, and a recorded
 // step has them with it).  A workgroup has 4096 numbers of one tensor, a wave 256 at a time, so that the scales' largest are a wave's own.  Measured: 10.6 M numbers, fp32 states,
-// gradients and a bf16 copy, 317 MB: 66 us (4.8 TB/s); 58.7 M with 8-bit states, bf16 gradients and copies, 940 MB: 200 us (4.7 TB/s, the vector units full too: 130 operations a number); 64 vectors, 0.1 M: 4.
+// gradients and a bf16 copy, 317 MB: 66 us (4.8 TB/s); 58.7 M with 8-bit states, bf16 gradients and copies, 940 MB: 200 us (4.7 TB/s; 135 operations a number, which keep the vector units busy for at least 0.6 of that); 64 vectors, 0.1 M: 4.
 //
 // Roots in 8 bits: m's is signed and v's is the fourth, for sqrt(v) is what p is divided by.  With steps of 1/127 of the largest root an m below 1.6e-5 of its block's largest becomes
 // zero (without roots 4e-3 would); with steps of 1/255 a sqrt(v) below 1.5e-5 of the largest stays at one step, rather than at zero, which would divide by eps alone.

@@ -416,8 +416,9 @@ conv_status_t seq_rec_create(const seq_rec_desc_t *d, seq_handle_t *out)
         return w;
     };
     // Where there are less than `most` workgroups, of `each` positions at a time, they share a sequence in runs, of which another launch finds out first what they make
-    // of a state, for which it reads most of the tensors: forwards below 128 workgroups (1 x 8192 x 512 bf16 33 -> 21 us, 1 x 16384 x 64 61 -> 14), backwards below 192
-    // (128 of them, rows of 4 x 2048 x 2048 bf16: 172 us with eight waves each, 141 in runs; 192, rows of 6 x 2048 x 2048: 197 and 207).
+    // of a state, for which it reads most of the tensors: forwards below 128 workgroups (1 x 8192 x 512 bf16 33 -> 21 us, 1 x 16384 x 64 61 -> 14; 160 of them, ragged
+    // fp32 rows of 5 x 777 x 1000: 21 -> 26 in four runs and 31 in two), backwards below 192 (128 of them, rows of 4 x 2048 x 2048 bf16: 172 us with eight waves each,
+    // 141 in runs; 192, rows of 6 x 2048 x 2048: 197 and 207).
     const auto runs = [&](SeqRecArgs &q, int64_t each, int64_t most) {
         const int64_t want = std::min<int64_t>({(most + columns - 1) / columns, (q.L + each - 1) / each, 64});
         q.run = (int)(std::min<int64_t>(((q.L + want - 1) / want + each - 1) / each * each, 1 << 30));

@@ -3,9 +3,10 @@
 //   s = sigmoid(f + f_bias), g = sigmoid(i + i_bias), a = exp(A s), h[l] = a h[l-1] + sqrt(1 - a^2) g x[l], y = h z sigmoid(z)
 //
 // Each tensor is read once: what positions make of a state is kept in registers until the state before them is known.  Some 50 operations an element,
-// four of them exponentials, three reciprocals, one a root, so that memory and the vector units are both near their rates.  Measured, bf16 with z: 8 x 2048 positions of 2048 channels, 336 MB, 73.5 us
-// (4.5 TB/s, vector units 0.8 busy; positions side by side 79), 1 x 8192, 168 MB, 40 us (4.2 TB/s); fp32 without z, 5 sequences of up to 777, 1000 channels side by side, 62 MB: 20 us;
-// one position of 32 sequences, 4096 channels: 3.6 us, a trip to memory and the launch.
+// four of them exponentials, three reciprocals, one a root: bound by memory, the vector units 0.4 to 0.7 busy (counters do not tell operations of 2 clocks from those of 4).
+// Measured, bf16 with z: 8 x 2048 positions of 2048 channels, 336 MB, 73.5 us (4.5 TB/s; positions side by side 79; without z, 268 MB, 71.5; fp32, 1024 channels, 65.7 and
+// without z 66.4), 1 x 8192, 168 MB, 40 us (4.2 TB/s); fp32 without z, 5 sequences of up to 777, 1000 channels side by side, 62 MB: 20.7 us;
+// one position of 32 sequences, 4096 channels: 3.7 us, a trip to memory and the launch.
 #include "seq_rec.h"
 
 namespace convmi {
@@ -16,8 +17,10 @@ namespace {
 // not, since moves between lanes go through LDS there (5 ragged fp32 sequences: two 25.6 us, four 21.3).
 // GATE: there is a z.  AHEAD: what the next round needs is asked for when this one's has come (where a compute unit has one workgroup: 1 x 8192 x 2048 bf16 45 -> 43 us,
 // ragged rows 26 -> 21; where its registers cost a third workgroup it does not pay: 8 x 2048 x 2048 72 -> 77).
-// Without that, and but for fp32 with z, 64 registers do, so that four workgroups of 8 waves share a compute unit (8 x 2048 x 2048 bf16 75.0 -> 74.1 us, without z 77.6 -> 72.6;
-// 16 x 300 x 2048 30.5 -> 27.9; 4 x 2048 x 2048 fp32, 5 registers spilled, 64.9 -> 71.4).
+// Without that, dense blocks have 64 registers but in fp32 with z, so that four workgroups of 8 waves share a compute unit (8 x 2048 x 2048 bf16, one register spilled, 75.0 -> 74.1 us,
+// without z 77.6 -> 72.6; 16 x 300 x 2048 30.5 -> 27.9; 4 x 2048 x 2048 fp32, 5 registers spilled, 64.9 -> 71.4).  Positions side by side take 79 to 110, with AHEAD up to 128, all there
+// are (fp32 without z: one spilled).  All builds without z keep some of what they have loaded in scratch memory, 24 bytes a lane in bf16 and 48 in fp32: they move a fifth less
+// than those with z and take as long.
 template <typename T, bool ROWS, int P, bool GATE, bool PAST, bool AHEAD>
 __global__ __launch_bounds__(64 * kSeqRecWaves, AHEAD || ROWS || (GATE && sizeof(T) == 4) ? 4 : 8) void seq_rec_fwd_kernel(const SeqRecArgs a)
 {

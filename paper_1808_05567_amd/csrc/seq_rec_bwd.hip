@@ -5,9 +5,9 @@
 //   dz = dy h sigmoid(z) (1 + z (1 - sigmoid(z))),   df_bias = sum df,   di_bias = sum di
 //
 // States go forwards and their gradients backwards, so that what a run of positions makes of either is found before both are known.  Some 120 operations an element, 14 of them
-// exponentials, reciprocals or roots, and f, dy and z are read a second time where a sequence is longer than a workgroup takes at a time.  Measured, bf16 with z: 8 x 2048 positions
-// of 2048 channels, 604 MB and 201 of them again, 164 us (4.9 TB/s with those, vector units 0.7 busy; positions side by side, 256 workgroups, 207), of which 5 are the sums over the
-// workgroups; 1 x 8192 104 us.
+// exponentials, reciprocals or roots, and f, dy and z are read a second time, but for the first round, where a sequence is longer than a workgroup takes at a time.  Measured, bf16 with z:
+// 8 x 2048 positions of 2048 channels, 604 MB and 176 of them again, of which the last cache may hold a part, 162 us (3.7 TB/s without those; vector units 0.4 to 0.7 busy; without z 128;
+// positions side by side, 256 workgroups, 207), of which 5 are the sums over the workgroups; 1 x 8192 104 us; fp32, 1024 channels, 141 and without z 105.
 #include "seq_rec.h"
 
 namespace convmi {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void seq_rec_bwd_kernel(const SeqRec
     __syncthreads();  // (the marks are there for all waves)
     float sums[3][E] = {};
     // What a round needs is asked for when the one before has come: all of it, or f and i, which it needs first, where that leaves registers for a fourth workgroup a compute unit
-    // (8 x 2048 x 2048 bf16: all 171 us, those 164; but rows of 8 x 2048 x 2048, one workgroup a compute unit, 207 and 226).
+    // (8 x 2048 x 2048 bf16: all 171 us, those 164; but rows of 8 x 2048 x 2048, one workgroup a compute unit, 207 and 226, of 16 x 1024 x 2048, two, 214 and 216, without z 182 and 203).
     constexpr bool ALL = ROWS || WAVES > kSeqRecBwdWaves / 2;
     const auto load_rest = [&](int round) {
         const int w0 = round * each + first;
